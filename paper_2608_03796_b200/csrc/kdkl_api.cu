@@ -15,27 +15,9 @@
 #include "aux_kernels.cuh"
 #include "feature_kernels.cuh"
 #include "gemm_tcgen05.cuh"
+#include "host_common.cuh"
 
 namespace kdkl {
-
-static thread_local char g_err[512] = "";
-static thread_local int64_t g_launches = 0;
-
-static int cuda_fail(const char* what, cudaError_t e) {
-  snprintf(g_err, sizeof(g_err), "%s: %s", what, cudaGetErrorString(e));
-  return KDKL_ERR_CUDA;
-}
-#define KDKL_CUDA(call)                                   \
-  do {                                                    \
-    cudaError_t e__ = (call);                             \
-    if (e__ != cudaSuccess) return cuda_fail(#call, e__); \
-  } while (0)
-#define KDKL_LAUNCHED(name)                               \
-  do {                                                    \
-    cudaError_t e__ = cudaGetLastError();                 \
-    if (e__ != cudaSuccess) return cuda_fail(name, e__);  \
-    ++g_launches;                                         \
-  } while (0)
 
 // ------------------------------------------------------------------ per-stage event timing
 // Off unless kdkl_profile_stages() is running on this thread. When on, every launch site first
@@ -93,58 +75,6 @@ struct HostPipe {
 };
 static thread_local HostPipe* g_pipe = nullptr;
 
-// ------------------------------------------------------------------ tensor maps
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-static EncodeTiledFn get_encode_fn() {
-  static EncodeTiledFn fn = nullptr;
-  if (fn) return fn;
-  void* p = nullptr;
-  cudaDriverEntryPointQueryResult qres;
-  if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &qres) != cudaSuccess ||
-      qres != cudaDriverEntryPointSuccess)
-    return nullptr;
-  fn = reinterpret_cast<EncodeTiledFn>(p);
-  return fn;
-}
-
-// 2-D bf16 tensor, `inner` contiguous elements per row, `outer` rows of `pitch_bytes`;
-// boxes of box_inner x box_outer written to shared memory with the 128-byte swizzle;
-// out-of-bounds elements read as zero.
-static int make_tmap(CUtensorMap* m, CUtensorMapDataType dtype, const void* base, uint64_t inner, uint64_t outer,
-                     uint64_t pitch_bytes, uint32_t box_inner, uint32_t box_outer) {
-  EncodeTiledFn fn = get_encode_fn();
-  if (!fn) { snprintf(g_err, sizeof(g_err), "cuTensorMapEncodeTiled entry point not found"); return KDKL_ERR_CUDA; }
-  cuuint64_t dims[2] = {inner, outer};
-  cuuint64_t strides[1] = {pitch_bytes};
-  cuuint32_t box[2] = {box_inner, box_outer};
-  cuuint32_t estr[2] = {1, 1};
-  CUresult r = fn(m, dtype, 2, const_cast<void*>(base), dims, strides, box, estr,
-                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  if (r != CUDA_SUCCESS) {
-    snprintf(g_err, sizeof(g_err), "cuTensorMapEncodeTiled failed (%d): inner=%llu outer=%llu pitch=%llu box=%ux%u",
-             (int)r, (unsigned long long)inner, (unsigned long long)outer, (unsigned long long)pitch_bytes, box_inner,
-             box_outer);
-    return KDKL_ERR_CUDA;
-  }
-  return KDKL_OK;
-}
-
-static int make_tmap_bf16(CUtensorMap* m, const void* base, uint64_t inner, uint64_t outer, uint64_t pitch_bytes,
-                          uint32_t box_inner, uint32_t box_outer) {
-  return make_tmap(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, base, inner, outer, pitch_bytes, box_inner, box_outer);
-}
-// Output maps: the epilogue stores boxes of 32 rows x 128 bytes (32 fp32 or 64 bf16 columns).
-static int make_tmap_out_f32(CUtensorMap* m, void* base, uint64_t cols, uint64_t rows, uint64_t ld_elems) {
-  return make_tmap(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, base, cols, rows, ld_elems * 4, 32, 32);
-}
-static int make_tmap_out_bf16(CUtensorMap* m, void* base, uint64_t cols, uint64_t rows, uint64_t ld_elems) {
-  return make_tmap(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, base, cols, rows, ld_elems * 2, 64, 32);
-}
-
 // ------------------------------------------------------------------ device / launch helpers
 // All GEMMs of the loss run as CTA pairs (256 x 256 tile per pair, see GemmCfg).
 constexpr int kNCTA = 2;
@@ -163,27 +93,6 @@ static int m_group_for(long long H) {
 }
 static bool use_wide(long long N) { return ((N + kWideN - 1) / kWideN) * kWideN * 10 <= N * 11; }
 static long long n_tiles_for(long long N, bool wide) { return wide ? (N + kWideN - 1) / kWideN : (N + BN - 1) / BN; }
-// What the library has learnt about each device, asked once per device and process (a benign race: two
-// threads asking at the same time store the same values).
-constexpr int kMaxDevices = 64;
-struct DeviceInfo { int dev; int sm_count; int cc_major; };
-struct DeviceCache { bool known; int sm_count; int cc_major; };
-static DeviceCache g_devices[kMaxDevices];
-static int device_info(DeviceInfo* di) {
-  int dev = 0;
-  KDKL_CUDA(cudaGetDevice(&dev));
-  di->dev = dev;
-  if (dev >= 0 && dev < kMaxDevices && g_devices[dev].known) {
-    di->sm_count = g_devices[dev].sm_count; di->cc_major = g_devices[dev].cc_major;
-    return KDKL_OK;
-  }
-  KDKL_CUDA(cudaDeviceGetAttribute(&di->sm_count, cudaDevAttrMultiProcessorCount, dev));
-  KDKL_CUDA(cudaDeviceGetAttribute(&di->cc_major, cudaDevAttrComputeCapabilityMajor, dev));
-  if (dev >= 0 && dev < kMaxDevices) {
-    g_devices[dev].sm_count = di->sm_count; g_devices[dev].cc_major = di->cc_major; g_devices[dev].known = true;
-  }
-  return KDKL_OK;
-}
 // SM count of the current device for sizing decisions that are also taken where there may be no device
 // (kdkl_workspace_bytes on a build machine): a B200's 148 then.
 static int sm_count_or_default() {
@@ -234,7 +143,6 @@ static int launch_gemm(const CUtensorMap& ta, const CUtensorMap& tb, const CUten
 }
 
 // ------------------------------------------------------------------ workspace
-static inline size_t up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 // How many work units to cut each output tile's contraction into so that the units fill whole
 // waves of SMs: the smallest count (<= 4, each unit keeping >= 32 k-blocks) that reaches 95 %
@@ -371,8 +279,6 @@ static int check_common(const void* hidden, const void* weight, long long T, lon
   return KDKL_OK;
 }
 
-template <typename Tp>
-static Tp* at(void* ws, size_t off) { return reinterpret_cast<Tp*>(reinterpret_cast<uint8_t*>(ws) + off); }
 
 static int next_pow2(int x) { int p = 2; while (p < x) p <<= 1; return p; }
 
