@@ -358,6 +358,119 @@ int kdkl_teacher_topk_stored(const void* hidden_bf16, const void* weight_bf16, i
                              int32_t K, float temperature, void* workspace, size_t workspace_bytes,
                              int32_t* topk_idx, float* topk_val, float* lse, void* cuda_stream);
 
+/* ------------------------------------------------------------------ operators of the student's body
+ * The loss above never holds the T x V logits; what then grows with T in a distillation step is what the student's
+ * body keeps for its backward pass. These operators keep it in 8 bits, and compute the layers that read it: the
+ * weight gradient of a linear layer, the gated activation of a feed-forward block, and the join between two blocks
+ * (norm after a block, gate, residual sum, norm before the next). (No counterpart in the paper.)
+ * Conventions as above, except: T = 0 is allowed (nothing to do: outputs summed over tokens become 0), rows may lie
+ * further apart than their width (`ld`, in elements), and any width is accepted; rows that start on 16 bytes with
+ * a width that is a multiple of 8 are read and written in 16-byte words, others element by element.
+ * `type` arguments: */
+#define KDKL_TYPE_BF16 0
+#define KDKL_TYPE_F32 1
+#define KDKL_TYPE_F16 2
+
+/* The 8-bit record of activations x [T, H]: for every 32 consecutive values of a row one power of two 2^e and 32
+ * one-byte codes, x ~ code 2^e.
+ *   e    = smallest integer with max |x| <= Q 2^e over the 32 values (Q = 127 or 448), at least -126
+ *   code = x 2^-e rounded to nearest even, as an integer of 8 bits (INT8) or as an e4m3 value (E4M3)
+ * A group that holds an infinity or a NaN reads back as NaN in all its 32 places. Error of a value: at most half a
+ * step, |x - x~| <= max |x| / 127 (INT8), or |x| / 16 + max |x| 2^-17 (E4M3); finite values read back as finite ones.
+ * Decoded values are exact in bf16.
+ * `record`: device, 256-byte aligned, kdkl_act8_bytes(T, H) bytes (H + H / 32 bytes a token, both rounded up): codes
+ * [T, Hp], Hp = H rounded up to 32, padding codes 0; at the next multiple of 256 bytes the scale bytes e + 127
+ * (255: not finite) [T, Sp], Sp = Hp / 32 rounded up to 16. `format` and T, H must be those the record was written with.
+ * store: x [T, H] of `type`, rows ld >= H apart, is read once. load: out [T, H] of `type`, rows ld apart. */
+#define KDKL_ACT8_NONE (-1)
+#define KDKL_ACT8_INT8 0
+#define KDKL_ACT8_E4M3 1
+size_t kdkl_act8_bytes(int64_t T, int64_t H);
+int kdkl_act8_store(const void* x, int32_t type, int64_t ld, int64_t T, int64_t H, int32_t format, void* record,
+                    size_t record_bytes, void* cuda_stream);
+int kdkl_act8_load(const void* record, size_t record_bytes, int64_t T, int64_t H, int32_t format, void* out,
+                   int32_t type, int64_t ld, void* cuda_stream);
+
+/* Gated activation h = act(gate) up, [T, F], act = x sigmoid(x) or the tanh form of gelu, computed in fp32 and
+ * rounded once. With a format, the same pass leaves records of gate and up (both required) and, if h_record is not
+ * NULL, of h as it was returned (for the weight gradient of the layer that reads h); with KDKL_ACT8_NONE nothing is
+ * kept and the record arguments are ignored. gate and up: rows ld apart (the two halves of one projection:
+ * ld = 2 F, up = gate + F). type BF16 or F16, also of h.
+ * backward: dgate = dh up act'(gate), dup = dh act(gate) at the values the two records stand for; rows ld apart. */
+#define KDKL_GATED_SILU 0
+#define KDKL_GATED_GELU 1
+int kdkl_gated_act_forward(const void* gate, const void* up, int64_t ld, int32_t type, int64_t T, int64_t F,
+                           int32_t act, int32_t format, void* h, int64_t ld_h, void* gate_record, void* up_record,
+                           void* h_record, size_t record_bytes, void* cuda_stream);
+int kdkl_gated_act_backward(const void* gate_record, const void* up_record, size_t record_bytes, int32_t format,
+                            const void* dh, int64_t ld_dh, int32_t type, int64_t T, int64_t F, int32_t act,
+                            void* dgate, void* dup, int64_t ld, void* cuda_stream);
+
+/* Weight gradient of a linear layer from the record of its input: dweight [N, H] (= or, with accumulate = 1, +=)
+ * dY^T x~, dY [T, N] bf16 with rows ld_dy apart, x~ [T, H] what the record stands for; sums in fp32, rounded once to
+ * `type` (F32 or BF16). T = 0 writes zeros (nothing when accumulating).
+ * workspace: device, 256-byte aligned, kdkl_act8_dweight_workspace_bytes(); its first words are a status block readable
+ * with kdkl_status (KDKL_ERR_TIMEOUT). Bitwise reproducible. */
+size_t kdkl_act8_dweight_workspace_bytes(int64_t T, int64_t N, int64_t H, int32_t type);
+int kdkl_act8_dweight(const void* dy_bf16, int64_t ld_dy, const void* record, size_t record_bytes, int64_t T, int64_t N,
+                      int64_t H, int32_t format, void* dweight, int32_t type, int32_t accumulate, void* workspace,
+                      size_t workspace_bytes, void* cuda_stream);
+
+/* The join between two blocks:
+ *   n = branch rho_post (post_weight + weight_offset),  rho_post = 1 / sqrt(mean(branch^2) + eps)
+ *   x = residual_scale residual + branch_scale gate n
+ *   y = x rho_pre (pre_weight + weight_offset),         rho_pre = 1 / sqrt(mean(x^2) + eps)
+ * per token over the H columns. post_weight NULL: n = branch. pre_weight NULL: no y. gate: none, one per channel [H] or
+ * one per token [T]. Everything is computed in fp32 (the pre norm from the unrounded x) and rounded once.
+ * Backward, from dy and the gradient `dsum` that reaches x along the residual stream (NULL: none), evaluates the
+ * gradient at what was kept of branch and x - the tensors themselves, or their records - with the forward pass's
+ * rho_post and rho_pre: dresidual, dbranch, dpost_weight, dpre_weight (sums over the tokens) and dgate. The sums over
+ * tokens are taken in a fixed order: bitwise reproducible. H <= 32768.
+ * One struct serves both calls; a call reads the fields it needs. Outputs [T, H] are contiguous. */
+#define KDKL_GATE_NONE 0
+#define KDKL_GATE_CHANNEL 1
+#define KDKL_GATE_TOKEN 2
+typedef struct kdkl_block_norm_args {
+  int32_t struct_size;        /* sizeof(kdkl_block_norm_args) */
+  int32_t type;               /* BF16 or F16: branch, y and their gradients */
+  int32_t residual_type;      /* `type` or F32: residual, sum and their gradients */
+  int32_t weight_type;        /* BF16, F32 or F16: the two norm weights and their gradients */
+  int32_t gate_type;          /* BF16, F32 or F16: gate and dgate */
+  int32_t gate_kind;          /* KDKL_GATE_* */
+  int32_t format;             /* KDKL_ACT8_*: the format of the records; NONE: tensors are kept instead */
+  float eps, weight_offset, branch_scale, residual_scale;
+  int64_t T, H;
+  const void* residual;       /* forward [T, H], rows ld_residual apart */
+  int64_t ld_residual;
+  const void* branch;         /* forward, and backward without records; rows ld_branch apart */
+  int64_t ld_branch;
+  const void* post_weight;    /* [H] or NULL */
+  const void* pre_weight;     /* [H] or NULL */
+  const void* gate;           /* [H] or [T]; NULL with KDKL_GATE_NONE */
+  void* y;                    /* forward out; required with pre_weight */
+  void* sum;                  /* forward out x; backward without records reads it (with pre_weight) */
+  float* rho_post;            /* [T]; forward out (optional), backward in (required with post_weight) */
+  float* rho_pre;             /* [T]; the same with pre_weight */
+  void* branch_record;        /* forward out (optional), backward in, with a format */
+  void* sum_record;           /* the same; backward needs it with pre_weight */
+  void* y_record;             /* forward out (optional): for the weight gradient of the layer that reads y */
+  size_t record_bytes;        /* size of each record: at least kdkl_act8_bytes(T, H) */
+  const void* dy;             /* backward in, with pre_weight; rows ld_dy apart */
+  int64_t ld_dy;
+  const void* dsum;           /* backward in, or NULL; rows ld_dsum apart */
+  int64_t ld_dsum;
+  void* dresidual;            /* backward out */
+  void* dbranch;
+  void* dpost_weight;         /* required with post_weight */
+  void* dpre_weight;          /* required with pre_weight */
+  void* dgate;                /* required with a gate */
+  void* workspace;            /* backward; 256-byte aligned, kdkl_block_norm_workspace_bytes(T, H) */
+  size_t workspace_bytes;
+} kdkl_block_norm_args;
+size_t kdkl_block_norm_workspace_bytes(int64_t T, int64_t H);
+int kdkl_block_norm_forward(const kdkl_block_norm_args* args, void* cuda_stream);
+int kdkl_block_norm_backward(const kdkl_block_norm_args* args, void* cuda_stream);
+
 /* Exercises the bounded wait every kernel of this library uses on its mbarriers: one thread waits on
  * a barrier that nothing completes, gives up after limit_ns (1 .. 1e9) and the kernel returns normally.
  * status: device int32[2], zeroed by the caller; afterwards {KDKL_ERR_TIMEOUT, 99}. The context stays

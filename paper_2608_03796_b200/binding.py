@@ -31,7 +31,9 @@ EXPORTS = [
     "kdkl_feature_loss", "kdkl_feature_loss_device_grad", "kdkl_feature_loss_workspace_bytes", "kdkl_step_host_record", "kdkl_record_staging_bytes",
     "kdkl_forward_backward", "kdkl_profile_single_pass", "kdkl_teacher_topk_stored",
     "kdkl_teacher_topk_stored_workspace_bytes", "kdkl_workspace_layout", "kdkl_count_tokens",
-    "kdkl_debug_guard_bytes",
+    "kdkl_debug_guard_bytes", "kdkl_act8_bytes", "kdkl_act8_store", "kdkl_act8_load", "kdkl_gated_act_forward",
+    "kdkl_gated_act_backward", "kdkl_act8_dweight_workspace_bytes", "kdkl_act8_dweight",
+    "kdkl_block_norm_workspace_bytes", "kdkl_block_norm_forward", "kdkl_block_norm_backward",
 ]
 
 FEATURE_MSE, FEATURE_COSINE = 0, 1
@@ -123,6 +125,26 @@ def lib() -> ctypes.CDLL:
     L.kdkl_feature_loss.argtypes = [vp, vp, vp, i64, i64, i32, f32, f32, f32, i32, vp, sz, vp, vp, vp, vp]
     L.kdkl_feature_loss_device_grad.restype = ctypes.c_int
     L.kdkl_feature_loss_device_grad.argtypes = [vp, vp, vp, i64, i64, i32, f32, vp, f32, i32, vp, sz, vp, vp, vp, vp]
+    L.kdkl_act8_bytes.restype = sz
+    L.kdkl_act8_bytes.argtypes = [i64, i64]
+    L.kdkl_act8_store.restype = ctypes.c_int
+    L.kdkl_act8_store.argtypes = [vp, i32, i64, i64, i64, i32, vp, sz, vp]
+    L.kdkl_act8_load.restype = ctypes.c_int
+    L.kdkl_act8_load.argtypes = [vp, sz, i64, i64, i32, vp, i32, i64, vp]
+    L.kdkl_gated_act_forward.restype = ctypes.c_int
+    L.kdkl_gated_act_forward.argtypes = [vp, vp, i64, i32, i64, i64, i32, i32, vp, i64, vp, vp, vp, sz, vp]
+    L.kdkl_gated_act_backward.restype = ctypes.c_int
+    L.kdkl_gated_act_backward.argtypes = [vp, vp, sz, i32, vp, i64, i32, i64, i64, i32, vp, vp, i64, vp]
+    L.kdkl_act8_dweight_workspace_bytes.restype = sz
+    L.kdkl_act8_dweight_workspace_bytes.argtypes = [i64, i64, i64, i32]
+    L.kdkl_act8_dweight.restype = ctypes.c_int
+    L.kdkl_act8_dweight.argtypes = [vp, i64, vp, sz, i64, i64, i64, i32, vp, i32, i32, vp, sz, vp]
+    L.kdkl_block_norm_workspace_bytes.restype = sz
+    L.kdkl_block_norm_workspace_bytes.argtypes = [i64, i64]
+    L.kdkl_block_norm_forward.restype = ctypes.c_int
+    L.kdkl_block_norm_forward.argtypes = [vp, vp]
+    L.kdkl_block_norm_backward.restype = ctypes.c_int
+    L.kdkl_block_norm_backward.argtypes = [vp, vp]
     L.kdkl_wait_selftest.restype = ctypes.c_int
     L.kdkl_wait_selftest.argtypes = [vp, i64, vp]
     L.kdkl_last_error.restype = ctypes.c_char_p

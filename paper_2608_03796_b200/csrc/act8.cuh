@@ -1,0 +1,277 @@
+// The 8-bit activation record and the vector loads and stores that the kernels on activations share.
+//
+// A record of x [T, H] holds one byte per value and one power of two per 32 consecutive values of a row:
+//   x[t, h] ~ code[t, h] * 2^e[t, h / 32],   code = int8 (-127 .. 127) or e4m3 (|code| <= 448)
+//   e = the smallest integer with max |x| <= Q 2^e over the 32 values, Q = 127 or 448, at least kActMinExp
+//   code = x 2^-e rounded to nearest even (exact scaling: nothing saturates); stored scale byte = e + 127
+//   (where rounding up would pass the largest finite fp32 number, the code below it is taken)
+// A group that holds an infinity or a NaN stores byte 255 and reads back as NaN in all its 32 places.
+// Why a power of two per 32 and not one fp32 factor per row or per 128: 7 or 4 significant bits times a power of two
+// are exact in bf16, so a record is a bf16 operand of the tensor cores without a second rounding, and scaling by it
+// is exact everywhere. What the coarser factor loses (a factor of at most 2 in the int8 step) the shorter group gains
+// back: the largest of 32 normal values is about 2.1 deviations, of 128 about 2.8.
+//
+// Layout in one buffer: codes [T, Hp] with Hp = H rounded up to 32 (padding codes are 0), then at the next multiple of
+// 256 bytes the scale bytes [T, Sp] with Sp = Hp / 32 rounded up to 16: both are tensor-map pitches.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+namespace kdkl {
+
+constexpr int kActGroup = 32;
+constexpr int kActMinExp = -126;        // 2^e and 2^-e are then normal fp32 numbers
+constexpr int kFmtInt8 = 0, kFmtE4M3 = 1;
+
+struct ActRecord {                      // a record in device memory
+  uint8_t* codes;
+  uint8_t* scales;
+};
+__host__ __device__ inline long long act_codes_pitch(long long H) { return (H + 31) / 32 * 32; }
+__host__ __device__ inline long long act_scale_pitch(long long H) { return (act_codes_pitch(H) / 32 + 15) / 16 * 16; }
+__host__ __device__ inline long long act_scales_at(long long T, long long H) {
+  return (T * act_codes_pitch(H) + 255) / 256 * 256;
+}
+
+// ------------------------------------------------------------------ eight values of a row
+// VEC: rows start on 16 bytes and H % 8 == 0, so that eight values are whole 16-byte words. Otherwise element by
+// element, and what lies past the row's end reads as 0 and is not written.
+__device__ __forceinline__ float to_f32(float x) { return x; }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ float to_f32(__half x) { return __half2float(x); }
+template <typename T> __device__ __forceinline__ T from_f32(float x);
+template <> __device__ __forceinline__ float from_f32<float>(float x) { return x; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+template <> __device__ __forceinline__ __half from_f32<__half>(float x) { return __float2half_rn(x); }
+
+template <typename T> struct Raw8 { uint4 v; };            // eight 16-bit values as they were loaded
+template <> struct Raw8<float> { uint4 v, w; };
+
+__device__ __forceinline__ void words_to_f32(const uint4& v, float (&f)[8], __nv_bfloat16) {
+  const __nv_bfloat162* p = reinterpret_cast<const __nv_bfloat162*>(&v);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { const float2 x = __bfloat1622float2(p[i]); f[2 * i] = x.x; f[2 * i + 1] = x.y; }
+}
+__device__ __forceinline__ void words_to_f32(const uint4& v, float (&f)[8], __half) {
+  const __half2* p = reinterpret_cast<const __half2*>(&v);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { const float2 x = __half22float2(p[i]); f[2 * i] = x.x; f[2 * i + 1] = x.y; }
+}
+template <typename T> __device__ __forceinline__ void raw_to_f32(const Raw8<T>& r, float (&f)[8]) {
+  words_to_f32(r.v, f, T());
+}
+template <> __device__ __forceinline__ void raw_to_f32<float>(const Raw8<float>& r, float (&f)[8]) {
+  f[0] = __uint_as_float(r.v.x); f[1] = __uint_as_float(r.v.y); f[2] = __uint_as_float(r.v.z); f[3] = __uint_as_float(r.v.w);
+  f[4] = __uint_as_float(r.w.x); f[5] = __uint_as_float(r.w.y); f[6] = __uint_as_float(r.w.z); f[7] = __uint_as_float(r.w.w);
+}
+__device__ __forceinline__ void f32_to_words(const float (&f)[8], uint4& v, __nv_bfloat16) {
+  __nv_bfloat162* p = reinterpret_cast<__nv_bfloat162*>(&v);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) p[i] = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+}
+__device__ __forceinline__ void f32_to_words(const float (&f)[8], uint4& v, __half) {
+  __half2* p = reinterpret_cast<__half2*>(&v);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) p[i] = __floats2half2_rn(f[2 * i], f[2 * i + 1]);
+}
+template <typename T> __device__ __forceinline__ Raw8<T> f32_to_raw(const float (&f)[8]) {
+  Raw8<T> r;
+  f32_to_words(f, r.v, T());
+  return r;
+}
+template <> __device__ __forceinline__ Raw8<float> f32_to_raw<float>(const float (&f)[8]) {
+  Raw8<float> r;
+  r.v = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+  r.w = make_uint4(__float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7]));
+  return r;
+}
+
+// columns [c, c + 8) of a row of `width` values; c is a multiple of 8
+template <typename T, bool VEC>
+__device__ __forceinline__ Raw8<T> load_raw8(const T* __restrict__ row, int c, int width) {
+  Raw8<T> r;
+  if (VEC) {
+    const uint4* p = reinterpret_cast<const uint4*>(row + c);
+    if (c < width) {
+      r.v = __ldg(p);
+      if constexpr (sizeof(T) == 4) r.w = __ldg(p + 1);
+    } else {
+      r.v = make_uint4(0u, 0u, 0u, 0u);
+      if constexpr (sizeof(T) == 4) r.w = r.v;
+    }
+  } else {
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = c + i < width ? to_f32(row[c + i]) : 0.f;
+    r = f32_to_raw<T>(f);                 // back to the type it came from: exact
+  }
+  return r;
+}
+template <typename T, bool VEC>
+__device__ __forceinline__ void load8(const T* __restrict__ row, int c, int width, float (&f)[8]) {
+  raw_to_f32(load_raw8<T, VEC>(row, c, width), f);
+}
+template <typename T, bool VEC>
+__device__ __forceinline__ void store_raw8(T* __restrict__ row, int c, int width, const Raw8<T>& r) {
+  if (VEC) {
+    if (c < width) {
+      uint4* p = reinterpret_cast<uint4*>(row + c);
+      p[0] = r.v;
+      if constexpr (sizeof(T) == 4) p[1] = r.w;
+    }
+  } else {
+    float f[8];
+    raw_to_f32(r, f);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (c + i < width) row[c + i] = from_f32<T>(f[i]);
+  }
+}
+
+// ------------------------------------------------------------------ codes
+// Scale byte of a group from the largest |x| of it, taken as an unsigned integer of the fp32 bits (which orders
+// magnitudes, infinities above all numbers and NaNs above those).
+template <int FMT>
+__device__ __forceinline__ uint32_t act_scale_byte(uint32_t amax_bits) {
+  if (amax_bits >= 0x7f800000u) return 255u;
+  // max|x| = (1 + m / 2^23) 2^(E - 127); Q = 1.984375 * 2^6 or 1.75 * 2^8
+  constexpr uint32_t kFrac = FMT == kFmtInt8 ? 0x7e0000u : 0x600000u;
+  constexpr int kShift = FMT == kFmtInt8 ? 6 : 8;
+  int e = (int)(amax_bits >> 23) - 127 - kShift + ((amax_bits & 0x7fffffu) > kFrac ? 1 : 0);
+  if (e < kActMinExp) e = kActMinExp;     // zeros and subnormal maxima too
+  return (uint32_t)(e + 127);
+}
+__device__ __forceinline__ float act_scale(uint32_t byte) {          // 2^e, NaN for byte 255
+  return byte == 255u ? __uint_as_float(0x7fffffffu) : __uint_as_float(byte << 23);
+}
+__device__ __forceinline__ float act_inverse(uint32_t byte) {        // 2^-e; 0 for byte 255 (codes 0)
+  return byte == 255u ? 0.f : __uint_as_float((254u - byte) << 23);
+}
+__device__ __forceinline__ uint32_t abs_max_bits(const float (&f)[8]) {
+  uint32_t m = 0u;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(f[i]) & 0x7fffffffu);
+  return m;
+}
+// the largest of the four neighbouring lanes that share a group (all four take part)
+__device__ __forceinline__ uint32_t group_max(uint32_t m) {
+  m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+  return max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+}
+template <int FMT>
+__device__ __forceinline__ uint2 act_codes(const float (&x)[8], uint32_t byte) {
+  const float inv = act_inverse(byte);
+  const bool bad = byte == 255u;
+  float f[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f[i] = x[i];
+  // the one exponent at which a code rounded up would stand for 2^128
+  constexpr uint32_t kTopByte = FMT == kFmtInt8 ? 122 + 127 : 120 + 127;
+  constexpr float kTopCode = FMT == kFmtInt8 ? 63.f : 240.f;
+  if (byte == kTopByte) {
+    const float lim = kTopCode * act_scale(byte);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = fminf(fmaxf(f[i], -lim), lim);
+  }
+  uint32_t w[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    if (FMT == kFmtInt8) {
+      uint32_t v = 0u;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v |= (uint32_t)(__float2int_rn(f[4 * k + i] * inv) & 0xff) << (8 * i);
+      w[k] = bad ? 0u : v;
+    } else {
+      const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(f[4 * k] * inv, f[4 * k + 1] * inv), __NV_SATFINITE, __NV_E4M3);
+      const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(f[4 * k + 2] * inv, f[4 * k + 3] * inv), __NV_SATFINITE, __NV_E4M3);
+      w[k] = bad ? 0u : (lo & 0xffffu) | (hi << 16);
+    }
+  }
+  return make_uint2(w[0], w[1]);
+}
+template <int FMT>
+__device__ __forceinline__ void act_values(const uint2& codes, uint32_t byte, float (&f)[8]) {
+  const float s = act_scale(byte);
+  const uint32_t w[2] = {codes.x, codes.y};
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    if (FMT == kFmtInt8) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) f[4 * k + i] = (float)(int8_t)(w[k] >> (8 * i)) * s;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[k] >> (16 * i)), __NV_E4M3);
+        const float2 v = __half22float2(__half2(h));
+        f[4 * k + 2 * i] = v.x * s;
+        f[4 * k + 2 * i + 1] = v.y * s;
+      }
+    }
+  }
+}
+
+// Write eight values (columns [c, c + 8) of row t; the four lanes of a group call together) into a record; c < Hp.
+// Values past the row's end are 0.
+template <int FMT>
+__device__ __forceinline__ void record_write8(const ActRecord& r, long long t, long long cpitch, long long spitch, int c,
+                                              const float (&f)[8], bool write) {
+  const uint32_t byte = act_scale_byte<FMT>(group_max(abs_max_bits(f)));
+  if (!write) return;
+  *reinterpret_cast<uint2*>(r.codes + t * cpitch + c) = act_codes<FMT>(f, byte);
+  if ((c & 31) == 0) r.scales[t * spitch + (c >> 5)] = (uint8_t)byte;
+}
+template <int FMT>
+__device__ __forceinline__ void record_read8(const ActRecord& r, long long t, long long cpitch, long long spitch, int c,
+                                             float (&f)[8]) {
+  const uint2 codes = __ldg(reinterpret_cast<const uint2*>(r.codes + t * cpitch + c));
+  act_values<FMT>(codes, __ldg(r.scales + t * spitch + (c >> 5)), f);
+}
+
+// The same with a format that is known at run time, uniform over a launch.
+__device__ __forceinline__ void record_write8(int fmt, const ActRecord& r, long long t, long long cpitch, long long spitch,
+                                              int c, const float (&f)[8], bool write) {
+  if (fmt == kFmtInt8) record_write8<kFmtInt8>(r, t, cpitch, spitch, c, f, write);
+  else record_write8<kFmtE4M3>(r, t, cpitch, spitch, c, f, write);
+}
+__device__ __forceinline__ void record_read8(int fmt, const ActRecord& r, long long t, long long cpitch, long long spitch,
+                                             int c, float (&f)[8]) {
+  if (fmt == kFmtInt8) record_read8<kFmtInt8>(r, t, cpitch, spitch, c, f);
+  else record_read8<kFmtE4M3>(r, t, cpitch, spitch, c, f);
+}
+
+// ------------------------------------------------------------------ store and load
+// One thread per eight values; a block covers 2048 columns of the rows blockIdx.y, blockIdx.y + gridDim.y, ...
+template <typename T, int FMT, bool VEC>
+__global__ void __launch_bounds__(256)
+act8_store_kernel(const T* __restrict__ x, long long ld, long long rows, int H, ActRecord rec) {
+  const long long cpitch = act_codes_pitch(H), spitch = act_scale_pitch(H);
+  const int c = (blockIdx.x * 256 + threadIdx.x) * 8;
+  for (long long t = blockIdx.y; t < rows; t += gridDim.y) {
+    float f[8];
+    load8<T, VEC>(x + t * ld, c, H, f);
+    record_write8<FMT>(rec, t, cpitch, spitch, c, f, c < cpitch);
+  }
+}
+template <typename T, int FMT, bool VEC>
+__global__ void __launch_bounds__(256)
+act8_load_kernel(ActRecord rec, long long rows, int H, T* __restrict__ out, long long ld) {
+  const long long cpitch = act_codes_pitch(H), spitch = act_scale_pitch(H);
+  const int c = (blockIdx.x * 256 + threadIdx.x) * 8;
+  if (c >= H) return;
+  for (long long t = blockIdx.y; t < rows; t += gridDim.y) {
+    float f[8];
+    record_read8<FMT>(rec, t, cpitch, spitch, c, f);
+    if constexpr (std::is_same<T, __half>::value) {   // a code rounded up past the largest fp16 value
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[i] = f[i] > 65504.f ? 65504.f : f[i] < -65504.f ? -65504.f : f[i];
+    }
+    store_raw8<T, VEC>(out + t * ld, c, H, f32_to_raw<T>(f));
+  }
+}
+
+}  // namespace kdkl

@@ -1,0 +1,338 @@
+// The join between two blocks of a student: norm of a block's output, gate, residual sum, norm for the next block.
+//
+//   n = b rho1 (w1 + o),  rho1 = 1 / sqrt(mean b^2 + eps)         post norm (absent: n = b)
+//   x = beta r + alpha gate n                                     gate: none, per channel or per token
+//   y = x rho2 (w2 + o),  rho2 = 1 / sqrt(mean x^2 + eps)         pre norm of the next block (absent: no y)
+//
+// Backward, from dy and the residual stream's gradient dx, with b^ = b rho1 and x^ = x rho2 of what was kept:
+//   d  = dx + rho2 (gy - x^ c2),   gy = dy (w2 + o),   c2 = mean(gy x^)
+//   dr = beta d,   dw2 = sum_t dy x^
+//   db = rho1 (k d - b^ c1),       k = alpha gate (w1 + o),   c1 = mean(k d b^);       dw1 = sum_t alpha gate d b^
+//   dgate = sum alpha d b^ (w1 + o), over the tokens (channel gate) or over the row (token gate)
+// c1 needs d and so c2, but mean(k d b^) = mean(k b^ (dx + rho2 gy)) - c2 rho2 mean(k b^ x^): all sums of a row come
+// from one reduction over its values, and nothing is read twice.
+//
+// Bound by memory: forward 8 bytes a value (+ 33/32 per record), backward 12 (10.06 from records). One block per row
+// and a stride over the rows; a thread keeps the same columns throughout, so the column sums dw1, dw2 and dgate stay
+// in its registers until the end, leave as one partial row per block, and a second kernel adds the partial rows in a
+// fixed order: bitwise reproducible.
+#pragma once
+#include "act8.cuh"
+
+namespace kdkl {
+
+constexpr int kGateNone = 0, kGateChannel = 1, kGateToken = 2;
+
+// Weights and gates come in one of three types; the type is uniform over a launch.
+struct AnyVec { const void* p; int type; };              // type: 0 bf16, 1 fp32, 2 fp16
+__device__ __forceinline__ float any_at(const AnyVec& v, long long i) {
+  if (v.type == 1) return reinterpret_cast<const float*>(v.p)[i];
+  if (v.type == 0) return __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(v.p)[i]);
+  return __half2float(reinterpret_cast<const __half*>(v.p)[i]);
+}
+template <bool VEC>
+__device__ __forceinline__ void any_load8(const AnyVec& v, int c, int width, float (&f)[8]) {
+  if (VEC) {
+    if (v.type == 1) load8<float, true>(reinterpret_cast<const float*>(v.p), c, width, f);
+    else if (v.type == 0) load8<__nv_bfloat16, true>(reinterpret_cast<const __nv_bfloat16*>(v.p), c, width, f);
+    else load8<__half, true>(reinterpret_cast<const __half*>(v.p), c, width, f);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = c + i < width ? any_at(v, c + i) : 0.f;
+  }
+}
+__device__ __forceinline__ void any_store(void* p, int type, long long i, float x) {
+  if (type == 1) reinterpret_cast<float*>(p)[i] = x;
+  else if (type == 0) reinterpret_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(x);
+  else reinterpret_cast<__half*>(p)[i] = __float2half_rn(x);
+}
+
+// Sums of N values over the block, the same in every thread. `sm` holds N * 32 floats. One barrier a call is enough as
+// long as no two calls in a row use the same buffer: a warp cannot write a buffer again before it has passed the
+// barrier of the call in between, which every warp reaches only after it has read that buffer.
+template <int N, int THREADS>
+__device__ __forceinline__ void block_sums(float (&x)[N], float* sm) {
+  constexpr int WARPS = THREADS / 32;
+#pragma unroll
+  for (int k = 0; k < N; ++k)
+#pragma unroll
+    for (int o = 16; o; o >>= 1) x[k] += __shfl_xor_sync(0xffffffffu, x[k], o);
+  if (WARPS == 1) return;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (lane == 0)
+#pragma unroll
+    for (int k = 0; k < N; ++k) sm[k * 32 + warp] = x[k];
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    float s = lane < WARPS ? sm[k * 32 + lane] : 0.f;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    x[k] = s;
+  }
+}
+
+struct NormForward {
+  const void* residual; long long ld_residual;
+  const void* branch; long long ld_branch;
+  AnyVec post, pre, gate;               // p == nullptr: absent
+  void* y; void* sum;                   // [T, H]; y only with a pre norm
+  float* rho_post; float* rho_pre;      // [T] each, or nullptr
+  ActRecord rec_branch, rec_sum, rec_y; // REC; codes == nullptr: not kept
+  int format;
+  long long T; int H;
+  int gate_kind;
+  float eps, offset, alpha, beta;
+};
+
+template <typename A, typename R, bool REC, int THREADS, int NV, bool VEC>
+__global__ void __launch_bounds__(THREADS)
+block_norm_forward_kernel(const NormForward p) {
+  __shared__ float sm[4][32];           // post and pre, alternating by row (see block_sums)
+  int parity = 0;
+  const int H = p.H;
+  const long long cpitch = act_codes_pitch(H), spitch = act_scale_pitch(H);
+  const float inv_h = 1.f / (float)H;
+  for (long long t = blockIdx.x; t < p.T; t += gridDim.x, parity ^= 2) {
+    const A* brow = reinterpret_cast<const A*>(p.branch) + t * p.ld_branch;
+    const R* rrow = reinterpret_cast<const R*>(p.residual) + t * p.ld_residual;
+    float b[NV][8], x[NV][8];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (threadIdx.x + i * THREADS) * 8;
+      load8<A, VEC>(brow, c, H, b[i]);
+      load8<R, VEC>(rrow, c, H, x[i]);
+      if constexpr (REC) {
+        if (p.rec_branch.codes != nullptr) record_write8(p.format, p.rec_branch, t, cpitch, spitch, c, b[i], c < cpitch);
+      }
+    }
+    float rho1 = 1.f;
+    if (p.post.p != nullptr) {
+      float s[1] = {0.f};
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[0] = fmaf(b[i][j], b[i][j], s[0]);
+      block_sums<1, THREADS>(s, sm[parity]);
+      rho1 = 1.f / sqrtf(fmaf(s[0], inv_h, p.eps));
+    }
+    float scale = p.alpha * rho1;
+    if (p.gate_kind == kGateToken) scale *= any_at(p.gate, t);
+    float s[1] = {0.f};
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (threadIdx.x + i * THREADS) * 8;
+      float w[8], g[8];
+      if (p.post.p != nullptr) any_load8<VEC>(p.post, c, H, w);
+      if (p.gate_kind == kGateChannel) any_load8<VEC>(p.gate, c, H, g);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        float k = scale;
+        if (p.post.p != nullptr) k *= w[j] + p.offset;
+        if (p.gate_kind == kGateChannel) k *= g[j];
+        x[i][j] = fmaf(k, b[i][j], p.beta * x[i][j]);
+        s[0] = fmaf(x[i][j], x[i][j], s[0]);
+      }
+    }
+    float rho2 = 1.f;
+    if (p.pre.p != nullptr) {
+      block_sums<1, THREADS>(s, sm[parity + 1]);
+      rho2 = 1.f / sqrtf(fmaf(s[0], inv_h, p.eps));
+    }
+    if (threadIdx.x == 0) {
+      if (p.rho_post != nullptr) p.rho_post[t] = rho1;
+      if (p.rho_pre != nullptr) p.rho_pre[t] = rho2;
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (threadIdx.x + i * THREADS) * 8;
+      const Raw8<R> raw = f32_to_raw<R>(x[i]);
+      store_raw8<R, VEC>(reinterpret_cast<R*>(p.sum) + t * H, c, H, raw);
+      if constexpr (REC) {
+        if (p.rec_sum.codes != nullptr) {             // what a record of the returned sum would hold
+          float v[8];
+          raw_to_f32(raw, v);
+          record_write8(p.format, p.rec_sum, t, cpitch, spitch, c, v, c < cpitch);
+        }
+      }
+      if (p.pre.p != nullptr) {
+        float w[8];
+        any_load8<VEC>(p.pre, c, H, w);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[i][j] *= rho2 * (w[j] + p.offset);
+        const Raw8<A> yr = f32_to_raw<A>(x[i]);
+        store_raw8<A, VEC>(reinterpret_cast<A*>(p.y) + t * H, c, H, yr);
+        if constexpr (REC) {
+          if (p.rec_y.codes != nullptr) {
+            float v[8];
+            raw_to_f32(yr, v);
+            record_write8(p.format, p.rec_y, t, cpitch, spitch, c, v, c < cpitch);
+          }
+        }
+      }
+    }
+  }
+}
+
+struct NormBackward {
+  const void* dsum; long long ld_dsum;  // gradient of x from the residual stream, or nullptr (0)
+  const void* dy; long long ld_dy;      // gradient of y, or nullptr (no pre norm)
+  const void* sum; long long ld_sum;    // what was kept of x ...
+  const void* branch; long long ld_branch;   // ... and of b, where it is not in a record
+  ActRecord rec_sum, rec_branch;        // REC
+  int format;
+  AnyVec post, pre, gate;
+  const float* rho_post; const float* rho_pre;
+  void* dresidual; void* dbranch;       // [T, H]
+  void* dgate_token; int gate_type;     // token gate: [T]
+  float* partial;                       // [gridDim.x, 3, Hp]: dw1, dw2, dgate (channel)
+  long long T; int H;
+  int gate_kind;
+  float offset, alpha, beta;
+};
+
+template <typename A, typename R, bool REC, int THREADS, int NV, bool VEC>
+__global__ void __launch_bounds__(THREADS)
+block_norm_backward_kernel(const NormBackward p) {
+  __shared__ float sm[2][4 * 32];
+  const int H = p.H;
+  const long long cpitch = act_codes_pitch(H), spitch = act_scale_pitch(H);
+  const float inv_h = 1.f / (float)H;
+  float dw1[NV][8], dw2[NV][8], dgt[NV][8];
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) dw1[i][j] = dw2[i][j] = dgt[i][j] = 0.f;
+  const bool has_post = p.post.p != nullptr, has_pre = p.pre.p != nullptr;
+  const bool channel = p.gate_kind == kGateChannel, token = p.gate_kind == kGateToken;
+  int parity = 0;
+  for (long long t = blockIdx.x; t < p.T; t += gridDim.x, parity ^= 1) {
+    const float rho1 = has_post ? p.rho_post[t] : 1.f, rho2 = has_pre ? p.rho_pre[t] : 1.f;
+    const float scale = token ? p.alpha * any_at(p.gate, t) : p.alpha;
+    float d[NV][8], gy[NV][8], bh[NV][8], xh[NV][8];
+    float s[4] = {0.f, 0.f, 0.f, 0.f};   // gy x^;  q b^ (dx + rho2 gy);  q b^ x^   with q = alpha gate_c (w1 + o)
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (threadIdx.x + i * THREADS) * 8;
+      if constexpr (REC) {
+        if (c < cpitch) {
+          record_read8(p.format, p.rec_branch, t, cpitch, spitch, c, bh[i]);
+          if (has_pre) record_read8(p.format, p.rec_sum, t, cpitch, spitch, c, xh[i]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) bh[i][j] = xh[i][j] = 0.f;
+        }
+      } else {
+        load8<A, VEC>(reinterpret_cast<const A*>(p.branch) + t * p.ld_branch, c, H, bh[i]);
+        if (has_pre) load8<R, VEC>(reinterpret_cast<const R*>(p.sum) + t * p.ld_sum, c, H, xh[i]);
+      }
+      if (p.dsum != nullptr) {
+        load8<R, VEC>(reinterpret_cast<const R*>(p.dsum) + t * p.ld_dsum, c, H, d[i]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) d[i][j] = 0.f;
+      }
+      float q[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) q[j] = p.alpha;
+      if (has_post) {
+        float w[8];
+        any_load8<VEC>(p.post, c, H, w);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) q[j] *= w[j] + p.offset;
+      }
+      if (channel) {
+        float g[8];
+        any_load8<VEC>(p.gate, c, H, g);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) q[j] *= g[j];
+      }
+      if (has_pre) {
+        float w[8], dy[8];
+        any_load8<VEC>(p.pre, c, H, w);
+        load8<A, VEC>(reinterpret_cast<const A*>(p.dy) + t * p.ld_dy, c, H, dy);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          xh[i][j] *= rho2;
+          dw2[i][j] = fmaf(dy[j], xh[i][j], dw2[i][j]);
+          gy[i][j] = dy[j] * (w[j] + p.offset);
+          s[0] = fmaf(gy[i][j], xh[i][j], s[0]);
+          d[i][j] = fmaf(rho2, gy[i][j], d[i][j]);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        bh[i][j] *= rho1;
+        const float qb = q[j] * bh[i][j];
+        s[1] = fmaf(qb, d[i][j], s[1]);
+        if (has_pre) s[2] = fmaf(qb, xh[i][j], s[2]);
+      }
+    }
+    block_sums<4, THREADS>(s, sm[parity]);
+    const float c2 = s[0] * inv_h;
+    const float dot = s[1] - c2 * rho2 * s[2];         // sum_h q b^ d
+    const float c1 = has_post ? dot * (token ? any_at(p.gate, t) : 1.f) * inv_h : 0.f;
+    if (token && threadIdx.x == 0) any_store(p.dgate_token, p.gate_type, t, dot);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (threadIdx.x + i * THREADS) * 8;
+      float k[8], o[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) k[j] = scale;
+      if (channel) {
+        float g[8];
+        any_load8<VEC>(p.gate, c, H, g);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) k[j] *= g[j];
+      }
+      float w[8];
+      if (has_post) any_load8<VEC>(p.post, c, H, w);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float wj = has_post ? w[j] + p.offset : 1.f;
+        const float dj = has_pre ? fmaf(-c2 * rho2, xh[i][j], d[i][j]) : d[i][j];
+        const float dn = k[j] * dj;
+        if (has_post) dw1[i][j] = fmaf(dn, bh[i][j], dw1[i][j]);
+        if (channel) dgt[i][j] = fmaf(p.alpha * dj * wj, bh[i][j], dgt[i][j]);
+        d[i][j] = p.beta * dj;
+        o[j] = rho1 * fmaf(-c1, bh[i][j], dn * wj);
+      }
+      store_raw8<R, VEC>(reinterpret_cast<R*>(p.dresidual) + t * H, c, H, f32_to_raw<R>(d[i]));
+      store_raw8<A, VEC>(reinterpret_cast<A*>(p.dbranch) + t * H, c, H, f32_to_raw<A>(o));
+    }
+  }
+  float* out = p.partial + (long long)blockIdx.x * 3 * cpitch;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = (threadIdx.x + i * THREADS) * 8;
+    if (c >= cpitch) continue;
+    if (has_post) store_raw8<float, true>(out, c, (int)cpitch, f32_to_raw<float>(dw1[i]));
+    if (has_pre) store_raw8<float, true>(out + cpitch, c, (int)cpitch, f32_to_raw<float>(dw2[i]));
+    if (channel) store_raw8<float, true>(out + 2 * cpitch, c, (int)cpitch, f32_to_raw<float>(dgt[i]));
+  }
+}
+
+// Column sums of the partial rows, in a fixed order: thread y of a block adds the rows y, y + 8, ...; then the eight
+// partial sums are added in order.
+struct NormColumns { void* out[3]; int type[3]; };
+__global__ void __launch_bounds__(256)
+block_norm_columns_kernel(const float* __restrict__ partial, int parts, int H, long long cpitch, const NormColumns p) {
+  __shared__ float sm[8][33];
+  const int which = blockIdx.y, c = blockIdx.x * 32 + threadIdx.x;
+  if (p.out[which] == nullptr) return;
+  float s = 0.f;
+  if (c < H) {
+    const float* src = partial + which * cpitch + c;
+#pragma unroll 8
+    for (int i = threadIdx.y; i < parts; i += 8) s += src[(long long)i * 3 * cpitch];
+  }
+  sm[threadIdx.y][threadIdx.x] = s;
+  __syncthreads();
+  if (threadIdx.y == 0 && c < H) {
+#pragma unroll
+    for (int i = 1; i < 8; ++i) s += sm[i][threadIdx.x];
+    any_store(p.out[which], p.type[which], c, s);
+  }
+}
+
+}  // namespace kdkl

@@ -1,0 +1,67 @@
+// Argument checks and dispatch that the host sides of the student-body operators share.
+#pragma once
+#include "act8.cuh"
+#include "host_common.cuh"
+
+namespace kdkl {
+
+inline bool is_type(int type) { return type >= KDKL_TYPE_BF16 && type <= KDKL_TYPE_F16; }
+inline bool is_format(int f) { return f == KDKL_ACT8_INT8 || f == KDKL_ACT8_E4M3; }
+inline int type_bytes(int type) { return type == KDKL_TYPE_F32 ? 4 : 2; }
+inline size_t record_need(long long T, long long H) {
+  return (size_t)(act_scales_at(T, H) + T * act_scale_pitch(H));
+}
+inline ActRecord record_at(const void* record, long long T, long long H) {
+  ActRecord r;
+  r.codes = reinterpret_cast<uint8_t*>(const_cast<void*>(record));
+  r.scales = record == nullptr ? nullptr : r.codes + act_scales_at(T, H);
+  return r;
+}
+// Rows that can be read and written in 16-byte words: start, distance and width.
+inline bool words(const void* p, long long ld, long long T, long long H, int type) {
+  return ((uintptr_t)p & 15) == 0 && (T <= 1 || (ld * type_bytes(type)) % 16 == 0) && H % 8 == 0;
+}
+inline bool shape_ok(long long T, long long H) {
+  return T >= 0 && T < (1ll << 31) && H >= 1 && H < (1ll << 30);
+}
+inline int need_b200(DeviceInfo* di) {
+  int rc = device_info(di);
+  if (rc) return rc;
+  return di->cc_major == 10 ? KDKL_OK : KDKL_ERR_ARCH;
+}
+// Grid of the element-wise kernels: 2048 columns a block in x; in y as many rows at a time as fill the device.
+inline dim3 rows_grid(long long T, long long H, const DeviceInfo& di) {
+  const long long gx = (act_codes_pitch(H) + 2047) / 2048;
+  long long gy = ((long long)di.sm_count * 16 + gx - 1) / gx;
+  if (gy > T) gy = T;
+  if (gy > 65535) gy = 65535;
+  return dim3((unsigned)gx, (unsigned)gy, 1);
+}
+
+#define KDKL_BY_BOOL(cond, NAME, ...)                                  \
+  do {                                                                 \
+    if (cond) { constexpr bool NAME = true; __VA_ARGS__; }             \
+    else { constexpr bool NAME = false; __VA_ARGS__; }                 \
+  } while (0)
+#define KDKL_BY_FORMAT(fmt, NAME, ...)                                              \
+  do {                                                                              \
+    if ((fmt) == KDKL_ACT8_INT8) { constexpr int NAME = kFmtInt8; __VA_ARGS__; }    \
+    else { constexpr int NAME = kFmtE4M3; __VA_ARGS__; }                            \
+  } while (0)
+#define KDKL_BY_FORMAT_OR_NONE(fmt, NAME, ...)                           \
+  do {                                                                   \
+    if ((fmt) == KDKL_ACT8_NONE) { constexpr int NAME = -1; __VA_ARGS__; } \
+    else KDKL_BY_FORMAT(fmt, NAME, __VA_ARGS__);                         \
+  } while (0)
+#define KDKL_BY_TYPE16(type, NAME, ...)                                          \
+  do {                                                                           \
+    if ((type) == KDKL_TYPE_BF16) { using NAME = __nv_bfloat16; __VA_ARGS__; }   \
+    else { using NAME = __half; __VA_ARGS__; }                                   \
+  } while (0)
+#define KDKL_BY_TYPE(type, NAME, ...)                              \
+  do {                                                             \
+    if ((type) == KDKL_TYPE_F32) { using NAME = float; __VA_ARGS__; } \
+    else KDKL_BY_TYPE16(type, NAME, __VA_ARGS__);                  \
+  } while (0)
+
+}  // namespace kdkl

@@ -1,0 +1,177 @@
+// Host side of the block norm: argument checks and launches; enqueue-only.
+#include <math.h>
+#include <string.h>
+
+#include <type_traits>
+
+#include "block_norm_kernels.cuh"
+#include "body_host.cuh"
+
+using namespace kdkl;
+
+// ------------------------------------------------------------------ block norm
+static constexpr long long kNormMaxH = 32768;
+// Blocks of the backward kernel, each of which leaves one partial row: two per SM, or one per token.
+static long long norm_parts(long long T) {
+  const long long most = 2 * 148;
+  return T < most ? T : most;
+}
+
+extern "C" size_t kdkl_block_norm_workspace_bytes(int64_t T, int64_t H) {
+  if (!shape_ok(T, H) || H > kNormMaxH) return 0;
+  return up((size_t)norm_parts(T) * 3 * act_codes_pitch(H) * 4, 256) + 256;
+}
+
+static int check_norm(const kdkl_block_norm_args* a, bool backward) {
+  if (!a) return KDKL_ERR_NULL;
+  if (a->struct_size != (int32_t)sizeof(kdkl_block_norm_args)) return KDKL_ERR_ARG;
+  if (!shape_ok(a->T, a->H) || a->H > kNormMaxH) return KDKL_ERR_SHAPE;
+  if (a->type != KDKL_TYPE_BF16 && a->type != KDKL_TYPE_F16) return KDKL_ERR_ARG;
+  if (a->residual_type != a->type && a->residual_type != KDKL_TYPE_F32) return KDKL_ERR_ARG;
+  if (!is_type(a->weight_type) || !is_type(a->gate_type)) return KDKL_ERR_ARG;
+  if (a->gate_kind < KDKL_GATE_NONE || a->gate_kind > KDKL_GATE_TOKEN) return KDKL_ERR_ARG;
+  if (a->format != KDKL_ACT8_NONE && !is_format(a->format)) return KDKL_ERR_ARG;
+  if (!isfinite(a->eps) || a->eps < 0.f || !isfinite(a->weight_offset) || !isfinite(a->branch_scale) ||
+      !isfinite(a->residual_scale))
+    return KDKL_ERR_ARG;
+  if (a->gate_kind != KDKL_GATE_NONE && !a->gate && (a->T != 0 || a->gate_kind == KDKL_GATE_CHANNEL)) return KDKL_ERR_NULL;
+  const int tb = type_bytes(a->type), rb = type_bytes(a->residual_type), wb = type_bytes(a->weight_type);
+  if ((uintptr_t)a->post_weight % wb || (uintptr_t)a->pre_weight % wb || (uintptr_t)a->gate % type_bytes(a->gate_type))
+    return KDKL_ERR_ALIGN;
+  if (a->format != KDKL_ACT8_NONE) {
+    if ((((uintptr_t)a->branch_record) | ((uintptr_t)a->sum_record) | ((uintptr_t)a->y_record)) & 255) return KDKL_ERR_ALIGN;
+    if ((a->branch_record || a->sum_record || a->y_record) && a->record_bytes < record_need(a->T, a->H)) return KDKL_ERR_WORKSPACE;
+  }
+  if (((uintptr_t)a->rho_post | (uintptr_t)a->rho_pre) & 3) return KDKL_ERR_ALIGN;
+  if (!backward) {
+    if (a->T == 0) return KDKL_OK;
+    if (!a->residual || !a->branch || !a->sum || (a->pre_weight && !a->y)) return KDKL_ERR_NULL;
+    if (a->T > 1 && (a->ld_residual < a->H || a->ld_branch < a->H)) return KDKL_ERR_SHAPE;
+    if ((uintptr_t)a->residual % rb || (uintptr_t)a->branch % tb || (uintptr_t)a->sum % rb || (uintptr_t)a->y % tb)
+      return KDKL_ERR_ALIGN;
+    return KDKL_OK;
+  }
+  const bool has_post = a->post_weight != nullptr, has_pre = a->pre_weight != nullptr;
+  if ((has_post && !a->dpost_weight) || (has_pre && !a->dpre_weight) || !a->workspace) return KDKL_ERR_NULL;
+  if (a->gate_kind == KDKL_GATE_CHANNEL && !a->dgate) return KDKL_ERR_NULL;
+  if ((uintptr_t)a->workspace & 255) return KDKL_ERR_ALIGN;
+  if ((uintptr_t)a->dpost_weight % wb || (uintptr_t)a->dpre_weight % wb || (uintptr_t)a->dgate % type_bytes(a->gate_type))
+    return KDKL_ERR_ALIGN;
+  if (a->workspace_bytes < kdkl_block_norm_workspace_bytes(a->T, a->H)) return KDKL_ERR_WORKSPACE;
+  if (a->T == 0) return KDKL_OK;
+  if (!a->dresidual || !a->dbranch || (has_pre && !a->dy) || (a->gate_kind == KDKL_GATE_TOKEN && !a->dgate)) return KDKL_ERR_NULL;
+  if ((has_post && !a->rho_post) || (has_pre && !a->rho_pre)) return KDKL_ERR_NULL;
+  if (a->format != KDKL_ACT8_NONE) {
+    if (!a->branch_record || (has_pre && !a->sum_record)) return KDKL_ERR_NULL;
+  } else {
+    if (!a->branch || (has_pre && !a->sum)) return KDKL_ERR_NULL;
+    if (a->T > 1 && a->ld_branch < a->H) return KDKL_ERR_SHAPE;
+    if ((uintptr_t)a->branch % tb || (uintptr_t)a->sum % rb) return KDKL_ERR_ALIGN;
+  }
+  if (a->T > 1 && ((has_pre && a->ld_dy < a->H) || (a->dsum && a->ld_dsum < a->H))) return KDKL_ERR_SHAPE;
+  if ((uintptr_t)a->dy % tb || (uintptr_t)a->dsum % rb || (uintptr_t)a->dresidual % rb || (uintptr_t)a->dbranch % tb)
+    return KDKL_ERR_ALIGN;
+  return KDKL_OK;
+}
+
+static bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+// Threads a row and groups of eight columns a thread.
+// (rows that are not whole 16-byte words: fewer shapes)
+#define KDKL_NORM_SHAPE(H, vec, VEC, THREADS, NV, ...)                                                     \
+  do {                                                                                                     \
+    const long long nv__ = act_codes_pitch(H) / 8;                                                         \
+    if (!(vec)) {                                                                                          \
+      if (nv__ <= 512) { constexpr bool VEC = false; constexpr int THREADS = 512, NV = 1; __VA_ARGS__; }   \
+      else { constexpr bool VEC = false; constexpr int THREADS = 1024, NV = 4; __VA_ARGS__; }              \
+    } else if (nv__ <= 128) { constexpr bool VEC = true; constexpr int THREADS = 128, NV = 1; __VA_ARGS__; } \
+    else if (nv__ <= 256) { constexpr bool VEC = true; constexpr int THREADS = 256, NV = 1; __VA_ARGS__; } \
+    else if (nv__ <= 512) { constexpr bool VEC = true; constexpr int THREADS = 512, NV = 1; __VA_ARGS__; } \
+    else if (nv__ <= 1024) { constexpr bool VEC = true; constexpr int THREADS = 512, NV = 2; __VA_ARGS__; } \
+    else { constexpr bool VEC = true; constexpr int THREADS = 1024, NV = 4; __VA_ARGS__; }                 \
+  } while (0)
+
+extern "C" {
+
+int kdkl_block_norm_forward(const kdkl_block_norm_args* a, void* cuda_stream) {
+  g_launches = 0;
+  int rc = check_norm(a, false);
+  if (rc || a->T == 0) return rc;
+  DeviceInfo di;
+  if ((rc = need_b200(&di))) return rc;
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
+  NormForward p;
+  p.residual = a->residual; p.ld_residual = a->ld_residual;
+  p.branch = a->branch; p.ld_branch = a->ld_branch;
+  p.post = AnyVec{a->post_weight, a->weight_type}; p.pre = AnyVec{a->pre_weight, a->weight_type};
+  p.gate = AnyVec{a->gate, a->gate_type};
+  p.y = a->y; p.sum = a->sum; p.rho_post = a->rho_post; p.rho_pre = a->rho_pre;
+  p.rec_branch = record_at(a->branch_record, a->T, a->H);
+  p.rec_sum = record_at(a->sum_record, a->T, a->H);
+  p.rec_y = record_at(a->pre_weight ? a->y_record : nullptr, a->T, a->H);
+  p.format = a->format;
+  p.T = a->T; p.H = (int)a->H; p.gate_kind = a->gate_kind;
+  p.eps = a->eps; p.offset = a->weight_offset; p.alpha = a->branch_scale; p.beta = a->residual_scale;
+  const bool vec = words(a->residual, a->ld_residual, a->T, a->H, a->residual_type) &&
+                   words(a->branch, a->ld_branch, a->T, a->H, a->type) && aligned16(a->sum) && aligned16(a->y) &&
+                   aligned16(a->post_weight) && aligned16(a->pre_weight) &&
+                   (a->gate_kind != KDKL_GATE_CHANNEL || aligned16(a->gate));
+  const bool any_record = a->format != KDKL_ACT8_NONE && (a->branch_record || a->sum_record || p.rec_y.codes);
+  const long long most = (long long)di.sm_count * 8;
+  const unsigned grid = (unsigned)(a->T < most ? a->T : most);
+  KDKL_BY_TYPE16(a->type, A, KDKL_BY_BOOL(a->residual_type == KDKL_TYPE_F32, WIDE,
+    KDKL_BY_BOOL(any_record, REC, KDKL_NORM_SHAPE(a->H, vec, VEC, THREADS, NV,
+      (block_norm_forward_kernel<A, std::conditional_t<WIDE, float, A>, REC, THREADS, NV, VEC><<<grid, THREADS, 0, st>>>(p))))));
+  KDKL_LAUNCHED("block_norm_forward_kernel");
+  return KDKL_OK;
+}
+
+int kdkl_block_norm_backward(const kdkl_block_norm_args* a, void* cuda_stream) {
+  g_launches = 0;
+  int rc = check_norm(a, true);
+  if (rc) return rc;
+  DeviceInfo di;
+  if ((rc = need_b200(&di))) return rc;
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
+  const bool has_post = a->post_weight != nullptr, has_pre = a->pre_weight != nullptr;
+  const bool channel = a->gate_kind == KDKL_GATE_CHANNEL;
+  const long long parts = norm_parts(a->T);
+  if (a->T > 0) {
+    NormBackward p;
+    p.dsum = a->dsum; p.ld_dsum = a->ld_dsum; p.dy = a->dy; p.ld_dy = a->ld_dy;
+    p.sum = a->sum; p.ld_sum = a->H; p.branch = a->branch; p.ld_branch = a->ld_branch;
+    p.rec_sum = record_at(a->sum_record, a->T, a->H); p.rec_branch = record_at(a->branch_record, a->T, a->H);
+    p.format = a->format;
+    p.post = AnyVec{a->post_weight, a->weight_type}; p.pre = AnyVec{a->pre_weight, a->weight_type};
+    p.gate = AnyVec{a->gate, a->gate_type};
+    p.rho_post = a->rho_post; p.rho_pre = a->rho_pre;
+    p.dresidual = a->dresidual; p.dbranch = a->dbranch; p.dgate_token = a->dgate; p.gate_type = a->gate_type;
+    p.partial = at<float>(a->workspace, 0);
+    p.T = a->T; p.H = (int)a->H; p.gate_kind = a->gate_kind;
+    p.offset = a->weight_offset; p.alpha = a->branch_scale; p.beta = a->residual_scale;
+    const bool kept = a->format != KDKL_ACT8_NONE ||
+                      (words(a->branch, a->ld_branch, a->T, a->H, a->type) && (!has_pre || aligned16(a->sum)));
+    const bool vec = kept && a->H % 8 == 0 && (!has_pre || words(a->dy, a->ld_dy, a->T, a->H, a->type)) &&
+                     (!a->dsum || words(a->dsum, a->ld_dsum, a->T, a->H, a->residual_type)) && aligned16(a->dresidual) &&
+                     aligned16(a->dbranch) && aligned16(a->post_weight) && aligned16(a->pre_weight) &&
+                     (!channel || aligned16(a->gate));
+    KDKL_BY_TYPE16(a->type, A, KDKL_BY_BOOL(a->residual_type == KDKL_TYPE_F32, WIDE,
+      KDKL_BY_BOOL(a->format != KDKL_ACT8_NONE, REC, KDKL_NORM_SHAPE(a->H, vec, VEC, THREADS, NV,
+        (block_norm_backward_kernel<A, std::conditional_t<WIDE, float, A>, REC, THREADS, NV, VEC><<<(unsigned)parts, THREADS, 0, st>>>(p))))));
+    KDKL_LAUNCHED("block_norm_backward_kernel");
+  }
+  if (has_post || has_pre || channel) {
+    NormColumns c;
+    memset(&c, 0, sizeof(c));
+    c.out[0] = has_post ? a->dpost_weight : nullptr; c.type[0] = a->weight_type;
+    c.out[1] = has_pre ? a->dpre_weight : nullptr; c.type[1] = a->weight_type;
+    c.out[2] = channel ? a->dgate : nullptr; c.type[2] = a->gate_type;
+    const dim3 grid((unsigned)((a->H + 31) / 32), 3, 1);
+    block_norm_columns_kernel<<<grid, dim3(32, 8, 1), 0, st>>>(at<float>(a->workspace, 0), (int)parts, (int)a->H,
+                                                             act_codes_pitch(a->H), c);
+    KDKL_LAUNCHED("block_norm_columns_kernel");
+  }
+  return KDKL_OK;
+}
+
+}  // extern "C"
