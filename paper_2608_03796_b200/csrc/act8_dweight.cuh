@@ -1,7 +1,27 @@
 // Weight gradient of a linear layer whose input was kept in an 8-bit record:
 //   dW[n, h] (= or +=) sum_t dY[t, n] x~[t, h],  x~ = what the record stands for.
+//
+// A matrix product of 2 T N H flops over operands that fit the L2 in slices: bound by the tensor pipe from a few
+// thousand tokens on. act8_dweight_kernel keeps it there by reading the record inside the product: the codes come
+// through TMA (half the bytes of bf16), are turned into bf16 by eight warps - exactly, 7 or 4 significant bits times a
+// power of two - and written as the swizzled operand tile that tcgen05.mma reads, while the products of earlier blocks
+// run. No bf16 copy of the activations ever exists in memory.
+//
+//   tile 256 (n) x 256 (h) per CTA pair (cta_group::2); a block of the contraction is 64 tokens
+//   warp 0       TMA of dY (bf16, contiguous along n: MN-major operand), STAGES deep
+//   warp 2       TMA of codes (64 x 128 a CTA) and scale bytes, RAW deep
+//   warp 1       tensor memory; the pair leader's lane 0 issues the MMAs
+//   warps 4-11   codes -> bf16 operand tile of this CTA's 128 columns
+//   warps 12-19  running sums in registers (128 rows x 256 columns a CTA, 128 values a thread)
+//
+// Why sums in registers: an accumulator in tensor memory truncates at each addition, measured as a relative error of
+// 1.1e-9 per token contracted (4.4e-6 at 4096, 3.8e-5 at 32768). It therefore only runs over RUN blocks; then
+// the eight warps add it, rounding to nearest, to the sums they hold, while the second accumulator fills.
+// Work units are (tile, part of the contraction); parts beyond one leave fp32 slabs that act8_dweight_join_kernel adds
+// in order, so results are reproducible bit for bit.
 #pragma once
 #include "act8.cuh"
+#include "sm100_prims.cuh"
 
 namespace kdkl {
 
@@ -10,7 +30,14 @@ struct DweightParams {
   ActRecord rec;
   long long T; int N, H;
   void* out; int type; int accumulate;
+  int* status;              // 256 bytes, set to zero by the first block
 };
+__device__ __forceinline__ void clear_status(int* status) {
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < 64) status[threadIdx.x] = 0;
+}
+
+// Any alignment and width: rows of dY or of the result that tensor maps cannot describe (not 16 bytes apart).
+// 64 x 64 tiles of fp32 FMAs.
 
 template <int FMT>
 __global__ void __launch_bounds__(256)
@@ -19,6 +46,7 @@ act8_dweight_simple_kernel(const DweightParams p) {
   const long long cpitch = act_codes_pitch(p.H), spitch = act_scale_pitch(p.H);
   const int n0 = blockIdx.y * 64, h0 = blockIdx.x * 64;
   const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
+  clear_status(p.status);
   float acc[4][4] = {};
   for (long long t0 = 0; t0 < p.T; t0 += 16) {
     for (int i = threadIdx.x; i < 16 * 64; i += 256) {
@@ -58,6 +86,353 @@ act8_dweight_simple_kernel(const DweightParams p) {
         o[at] = __float2bfloat16_rn(p.accumulate ? __bfloat162float(o[at]) + acc[i][j] : acc[i][j]);
       }
     }
+}
+
+struct DwCfg {
+  static constexpr int TILE = 256, BK = 64, STAGES = 4, RAW = 5, RUN = 12;
+  static constexpr int A_BYTES = 128 * BK * 2, B_BYTES = 128 * BK * 2, STAGE_BYTES = A_BYTES + B_BYTES;
+  static constexpr int CODE_BYTES = 128 * BK, SCALE_BYTES = 16 * BK, RAW_BYTES = CODE_BYTES + SCALE_BYTES;
+  static constexpr int CONVERT_WARPS = 8, SUM_WARPS = 8;
+  static constexpr int CONVERT_TEAM = 2, TEAMS = CONVERT_WARPS / CONVERT_TEAM;   // warps a block; blocks in work at once
+  static constexpr int THREADS = 128 + 32 * (CONVERT_WARPS + SUM_WARPS);
+  static constexpr int BOX_BYTES = 4096;      // 32 rows x 128 bytes of output per summing warp
+  static constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + RAW * RAW_BYTES + SUM_WARPS * BOX_BYTES + 1024 + 256;
+  // registers a thread of each warpgroup: launched with 96, 32 + 2 * 48 + 2 * 176 <= 5 * 96
+  static constexpr int REGS_FEED = 32, REGS_CONVERT = 48, REGS_SUM = 176;
+};
+
+struct DwParams {
+  long long T;
+  int N, H;
+  int n_tiles, h_tiles, parts;     // units = n_tiles * h_tiles * parts
+  int part_rows;                   // output row distance between the slabs of two parts
+  int reduce;                      // fp32 output: += instead of =
+  int* status;
+};
+
+// Two bf16 values from two codes in the low bytes of `p`'s halves, times `scale` (a power of two in both halves). Exact.
+template <int FMT>
+__device__ __forceinline__ uint32_t codes_to_bf16x2(uint32_t p, uint32_t scale) {
+  uint32_t v;
+  if (FMT == kFmtInt8) {
+    // 0x43cc: the low 7 bits of a code as the fraction of 128 + low; minus 128, or minus 256 where the sign bit is set
+    const uint32_t a = p & 0xff7fff7fu, b = p & 0xff80ff80u;
+    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(v) : "r"(a), "r"(b));
+  } else {
+    // 0xcc00: sign, then exponent and fraction four places down: the value times 2^-120 (subnormals included)
+    const uint32_t m = (p & 0x7f007f00u) >> 4;
+    const uint32_t w = m | (p & 0x80008000u);
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(v) : "r"(w), "r"(0x7b807b80u));
+  }
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(v) : "r"(v), "r"(scale));
+  return v;
+}
+template <int FMT>
+__device__ __forceinline__ void codes_to_bf16x8(const uint2& c, uint32_t byte, uint32_t (&o)[4]) {
+  const uint32_t scale = (byte << 7) * 0x00010001u;         // 2^e; byte 255 (codes 0): 0 * infinity = NaN
+  const uint32_t w[2] = {c.x, c.y};
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    if (FMT == kFmtInt8) {
+      o[2 * k] = codes_to_bf16x2<FMT>(__byte_perm(w[k], 0x43434343u, 0x4140), scale);
+      o[2 * k + 1] = codes_to_bf16x2<FMT>(__byte_perm(w[k], 0x43434343u, 0x4342), scale);
+    } else {
+      o[2 * k] = codes_to_bf16x2<FMT>(__byte_perm(w[k], 0u, 0x1404), scale);
+      o[2 * k + 1] = codes_to_bf16x2<FMT>(__byte_perm(w[k], 0u, 0x3424), scale);
+    }
+  }
+}
+
+template <int FMT, bool F32_OUT>
+__global__ void __launch_bounds__(DwCfg::THREADS, 1) __cluster_dims__(2, 1, 1)
+act8_dweight_kernel(const __grid_constant__ CUtensorMap tmY, const __grid_constant__ CUtensorMap tmCodes,
+                    const __grid_constant__ CUtensorMap tmScales, const __grid_constant__ CUtensorMap tmOut,
+                    const DwParams p) {
+  using C = DwCfg;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* base_ptr = smem_raw + (base - smem_u32(smem_raw));
+  const uint32_t raw0 = base + C::STAGES * C::STAGE_BYTES;
+  const uint32_t box0 = raw0 + C::RAW * C::RAW_BYTES;
+  const uint32_t bar0 = box0 + C::SUM_WARPS * C::BOX_BYTES;
+  // Barriers. In the leader: yfull (bytes of both CTAs' dY), bfull (both CTAs' converting warps), tempty (both CTAs'
+  // summing warps). In each CTA: empty and tfull (committed to both by the leader's MMAs), rfull, rempty.
+  auto yfull = [&](uint32_t s) { return bar0 + 8u * s; };
+  auto bfull = [&](uint32_t s) { return bar0 + 8u * (C::STAGES + s); };
+  auto empty = [&](uint32_t s) { return bar0 + 8u * (2 * C::STAGES + s); };
+  auto rfull = [&](uint32_t s) { return bar0 + 8u * (3 * C::STAGES + s); };
+  auto rempty = [&](uint32_t s) { return bar0 + 8u * (3 * C::STAGES + C::RAW + s); };
+  auto tfull = [&](uint32_t a) { return bar0 + 8u * (3 * C::STAGES + 2 * C::RAW + a); };
+  auto tempty = [&](uint32_t a) { return bar0 + 8u * (3 * C::STAGES + 2 * C::RAW + 2 + a); };
+  constexpr int kBars = 3 * C::STAGES + 2 * C::RAW + 4;
+  static_assert(8 * kBars + 8 <= 256, "barrier block");
+  uint8_t* bar_ptr = base_ptr + (bar0 - base);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar_ptr + 8 * kBars);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_ctarank();
+  const bool leader = rank == 0u;
+  clear_status(p.status);
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < C::STAGES; ++s) {
+      mbar_init(yfull(s), 1);
+      mbar_init(bfull(s), 2 * C::CONVERT_TEAM);
+      mbar_init(empty(s), 1);
+    }
+    for (int s = 0; s < C::RAW; ++s) { mbar_init(rfull(s), 1); mbar_init(rempty(s), C::CONVERT_TEAM); }
+    for (int a = 0; a < 2; ++a) { mbar_init(tfull(a), 1); mbar_init(tempty(a), 2 * C::SUM_WARPS); }
+    *abort_flag = 0;
+    mbar_fence_init();
+    tma_prefetch_desc(&tmY); tma_prefetch_desc(&tmCodes); tma_prefetch_desc(&tmScales); tma_prefetch_desc(&tmOut);
+  }
+  if (warp == 1) { tmem_alloc_pair(smem_u32(tmem_slot), 512); tmem_relinquish_pair(); }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+
+  const int worker = blockIdx.x >> 1, workers = gridDim.x >> 1;
+  const int tiles = p.n_tiles * p.h_tiles, units = tiles * p.parts;
+  const int kblocks = (int)((p.T + C::BK - 1) / C::BK), per_part = (kblocks + p.parts - 1) / p.parts;
+  struct Unit { int n0, h0, part, kb0, kb1; };
+  auto unit_at = [&](int u) {
+    Unit r;
+    r.part = u / tiles;
+    const int tile = u - r.part * tiles;
+    r.n0 = (tile / p.h_tiles) * C::TILE;
+    r.h0 = (tile % p.h_tiles) * C::TILE;
+    r.kb0 = r.part * per_part;
+    r.kb1 = r.kb0 + per_part < kblocks ? r.kb0 + per_part : kblocks;
+    return r;
+  };
+  bool ok = true;
+
+  if (warp < 4) {
+    regs_dec<C::REGS_FEED>();
+    if (warp == 0 && lane == 0) {
+      // -------------------------------------------------- dY
+      uint32_t it = 0;
+      for (int u = worker; u < units && ok; u += workers) {
+        const Unit w = unit_at(u);
+        for (int kb = w.kb0; kb < w.kb1; ++kb, ++it) {
+          const uint32_t s = it % C::STAGES, ph = (it / C::STAGES) & 1u;
+          if (!mbar_wait(empty(s), ph ^ 1u, abort_flag, p.status, 1)) { ok = false; break; }
+          const uint32_t fb = map_to_cta(yfull(s), 0u);
+          if (leader) mbar_arrive_expect_tx(yfull(s), 2 * C::A_BYTES);
+          const uint32_t dst = base + s * C::STAGE_BYTES;
+          const int n = w.n0 + (int)rank * 128;
+          tma_load_2d_pair(dst, &tmY, n, kb * C::BK, fb);
+          tma_load_2d_pair(dst + C::BK * 128, &tmY, n + 64, kb * C::BK, fb);
+        }
+      }
+    } else if (warp == 2 && lane == 0) {
+      // -------------------------------------------------- codes and scales
+      uint32_t it = 0;
+      for (int u = worker; u < units && ok; u += workers) {
+        const Unit w = unit_at(u);
+        const int h = w.h0 + (int)rank * 128;
+        for (int kb = w.kb0; kb < w.kb1; ++kb, ++it) {
+          const uint32_t s = it % C::RAW, ph = (it / C::RAW) & 1u;
+          if (!mbar_wait(rempty(s), ph ^ 1u, abort_flag, p.status, 2)) { ok = false; break; }
+          mbar_arrive_expect_tx(rfull(s), C::RAW_BYTES);
+          const uint32_t dst = raw0 + s * C::RAW_BYTES;
+          tma_load_2d(dst, &tmCodes, h, kb * C::BK, rfull(s));
+          tma_load_2d(dst + C::CODE_BYTES, &tmScales, (h / 32) & ~15, kb * C::BK, rfull(s));
+        }
+      }
+    } else if (warp == 1 && lane == 0 && leader) {
+      // -------------------------------------------------- products
+      const uint32_t idesc = make_idesc_bf16(C::TILE, C::TILE, 1u, 1u);
+      constexpr uint32_t STEP = (16 * 128) >> 4;               // 16 tokens further in an MN-major tile
+      const uint64_t a_proto = make_smem_desc(base, C::BK * 128, 1024);
+      const uint64_t b_proto = make_smem_desc(base + C::A_BYTES, C::BK * 128, 1024);
+      const uint32_t a_hi = (uint32_t)(a_proto >> 32), a_lo0 = (uint32_t)a_proto;
+      const uint32_t b_hi = (uint32_t)(b_proto >> 32), b_lo0 = (uint32_t)b_proto;
+      auto desc = [](uint32_t lo, uint32_t hi) { return (static_cast<uint64_t>(hi) << 32) | lo; };
+      uint32_t it = 0, run = 0;
+      for (int u = worker; u < units && ok; u += workers) {
+        const Unit w = unit_at(u);
+        for (int k0 = w.kb0; k0 < w.kb1 && ok; k0 += C::RUN, ++run) {
+          const uint32_t acc = run & 1u, aph = (run >> 1) & 1u;
+          if (!mbar_wait(tempty(acc), aph ^ 1u, abort_flag, p.status, 3)) { ok = false; break; }
+          tc_fence_after();
+          const int k1 = k0 + C::RUN < w.kb1 ? k0 + C::RUN : w.kb1;
+          uint32_t add = 0u;
+          for (int kb = k0; kb < k1; ++kb, ++it) {
+            const uint32_t s = it % C::STAGES, ph = (it / C::STAGES) & 1u;
+            if (!mbar_wait(yfull(s), ph, abort_flag, p.status, 4) ||
+                !mbar_wait_cluster(bfull(s), ph, abort_flag, p.status, 5)) { ok = false; break; }
+            tc_fence_after();
+            const uint32_t alo = a_lo0 + s * (C::STAGE_BYTES >> 4), blo = b_lo0 + s * (C::STAGE_BYTES >> 4);
+#pragma unroll
+            for (int j = 0; j < C::BK / 16; ++j) {
+              umma_bf16_pair(tmem + acc * C::TILE, desc(alo + j * STEP, a_hi), desc(blo + j * STEP, b_hi), idesc, add);
+              add = 1u;
+            }
+            umma_commit_pair(empty(s));
+          }
+          if (ok) umma_commit_pair(tfull(acc));
+        }
+      }
+    }
+    if ((warp == 0 || warp == 2) && lane == 0 && !ok) {        // aborted: copies in flight get a bounded time to land
+      const uint64_t t0 = globaltimer_ns();
+      while (globaltimer_ns() - t0 < 2000000ull) {}
+    }
+  } else if (warp < 4 + C::CONVERT_WARPS) {
+    regs_dec<C::REGS_CONVERT>();
+    // ---------------------------------------------------- codes -> bf16
+    // A block is converted by a team of warps, successive blocks by successive teams, so that their waits overlap.
+    // A thread takes eight columns of a token at a time: 16 lanes read 128 consecutive code bytes, eight lanes write
+    // one 128-byte line of the operand tile (chunk c of line t sits at c ^ (t & 7)): no bank conflicts either way.
+    const int team = (warp - 4) / C::CONVERT_TEAM, member = (warp - 4) % C::CONVERT_TEAM;
+    const int c = lane & 15, t_first = member * 2 + (lane >> 4);
+    constexpr int T_STEP = 2 * C::CONVERT_TEAM, ITEMS = C::BK / T_STEP, BATCH = 4;
+    const uint32_t blk = (uint32_t)(c >> 3) * (C::BK * 128);
+    uint32_t it = 0;
+    for (int u = worker; u < units && ok; u += workers) {
+      const Unit w = unit_at(u);
+      const int scale_at = (((w.h0 + (int)rank * 128) / 32) & 15) + (c >> 2);
+      for (int kb = w.kb0; kb < w.kb1; ++kb, ++it) {
+        if ((int)(it % C::TEAMS) != team) continue;
+        const uint32_t s = it % C::STAGES, ph = (it / C::STAGES) & 1u;
+        const uint32_t r = it % C::RAW, rph = (it / C::RAW) & 1u;
+        bool here = mbar_wait(rfull(r), rph, abort_flag, p.status, 6);
+        here = here && mbar_wait(empty(s), ph ^ 1u, abort_flag, p.status, 7);
+        if (!__all_sync(0xffffffffu, here)) { ok = false; break; }
+        const uint8_t* raw = base_ptr + (raw0 - base) + r * C::RAW_BYTES;
+        const uint32_t tile = base + s * C::STAGE_BYTES + C::A_BYTES + blk;
+#pragma unroll
+        for (int i0 = 0; i0 < ITEMS; i0 += BATCH) {
+          uint2 codes[BATCH];
+          uint32_t bytes[BATCH];
+#pragma unroll
+          for (int j = 0; j < BATCH; ++j) {
+            const int t = t_first + T_STEP * (i0 + j);
+            codes[j] = *reinterpret_cast<const uint2*>(raw + t * 128 + c * 8);
+            bytes[j] = raw[C::CODE_BYTES + t * 16 + scale_at];
+          }
+#pragma unroll
+          for (int j = 0; j < BATCH; ++j) {
+            const int t = t_first + T_STEP * (i0 + j);
+            uint32_t o[4];
+            codes_to_bf16x8<FMT>(codes[j], bytes[j], o);
+            st_shared_v4(tile + t * 128 + (((c & 7) ^ (t & 7)) << 4), o[0], o[1], o[2], o[3]);
+          }
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(rempty(r));
+          mbar_arrive_release_cluster(map_to_cta(bfull(s), 0u));
+        }
+      }
+    }
+  } else {
+    regs_inc<C::REGS_SUM>();
+    // ---------------------------------------------------- sums and output
+    const int sw = warp - 4 - C::CONVERT_WARPS;
+    const int lg = warp & 3;                                   // tensor memory lanes this warp may read
+    const int col_half = (sw >> 2) * 128;
+    const uint32_t box = box0 + sw * C::BOX_BYTES;
+    float sum[128];
+    uint32_t run = 0;
+    for (int u = worker; u < units && ok; u += workers) {
+      const Unit w = unit_at(u);
+#pragma unroll
+      for (int j = 0; j < 128; ++j) sum[j] = 0.f;              // (a part may be empty)
+      for (int k0 = w.kb0; k0 < w.kb1; k0 += C::RUN, ++run) {
+        const uint32_t acc = run & 1u, aph = (run >> 1) & 1u;
+        const bool here = mbar_wait(tfull(acc), aph, abort_flag, p.status, 8);
+        if (!__all_sync(0xffffffffu, here)) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t taddr = tmem + (uint32_t(lg * 32) << 16) + acc * C::TILE + col_half;
+#pragma unroll
+        for (int v = 0; v < 8; ++v) {
+          uint32_t r[16];
+          tmem_ld16(taddr + v * 16, r);
+          tmem_ld_wait();
+#pragma unroll
+          for (int j = 0; j < 16; ++j) sum[v * 16 + j] += __uint_as_float(r[j]);
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(map_to_cta(tempty(acc), 0u));
+      }
+      if (!ok) break;
+      const int row0 = w.n0 + (int)rank * 128 + lg * 32, col0 = w.h0 + col_half;
+      constexpr int BOX_COLS = F32_OUT ? 32 : 64;
+#pragma unroll
+      for (int b = 0; b < 128 / BOX_COLS; ++b) {
+        if (row0 < p.N && col0 + b * BOX_COLS < p.H) {         // uniform over the warp
+          if (lane == 0) bulk_wait_read<0>();
+          __syncwarp();
+#pragma unroll
+          for (int ch = 0; ch < 8; ++ch) {
+            uint32_t v[4];                                     // volatile: copies made here do not pile up in registers
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              if constexpr (F32_OUT) {
+                asm volatile("mov.b32 %0, %1;" : "=r"(v[j]) : "f"(sum[b * 32 + ch * 4 + j]));
+              } else {
+                asm volatile("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v[j])
+                             : "f"(sum[b * 64 + ch * 8 + 2 * j + 1]), "f"(sum[b * 64 + ch * 8 + 2 * j]));
+              }
+            }
+            st_shared_v4(box + lane * 128 + ((ch ^ (lane & 7)) << 4), v[0], v[1], v[2], v[3]);
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            const int y = row0 + w.part * p.part_rows, x = col0 + b * BOX_COLS;
+            if (F32_OUT && p.reduce) tma_reduce_add_2d(&tmOut, box, x, y);
+            else tma_store_2d(&tmOut, box, x, y);
+            bulk_commit();
+          }
+        }
+      }
+    }
+    if (lane == 0) bulk_wait_all();
+  }
+
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();                                          // neither CTA leaves while the other may reach its barriers
+  tc_fence_after();
+  if (warp == 1) tmem_dealloc_pair(tmem, 512);
+}
+
+// out (= or +=) slab 0 + slab 1 + ... in that order, one rounding. H % 8 == 0.
+__global__ void __launch_bounds__(256)
+act8_dweight_join_kernel(const float* __restrict__ slabs, long long slab, int parts, long long n8, void* __restrict__ out,
+                         int type, int accumulate) {
+  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n8) return;
+  float f[8], g[8];
+  raw_to_f32(load_raw8<float, true>(slabs + i * 8, 0, 8), f);
+  for (int q = 1; q < parts; ++q) {
+    raw_to_f32(load_raw8<float, true>(slabs + q * slab + i * 8, 0, 8), g);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] += g[j];
+  }
+  if (type == 1) {
+    float* o = reinterpret_cast<float*>(out) + i * 8;
+    if (accumulate) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[j] += o[j];
+    }
+    store_raw8<float, true>(o, 0, 8, f32_to_raw<float>(f));
+  } else {
+    __nv_bfloat16* o = reinterpret_cast<__nv_bfloat16*>(out) + i * 8;
+    if (accumulate) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[j] += __bfloat162float(o[j]);
+    }
+    store_raw8<__nv_bfloat16, true>(o, 0, 8, f32_to_raw<__nv_bfloat16>(f));
+  }
 }
 
 }  // namespace kdkl

@@ -122,10 +122,59 @@ int kdkl_gated_act_backward(const void* gate_record, const void* up_record, size
 }
 
 // ------------------------------------------------------------------ weight gradient from a record
+// Rows that tensor maps can describe (16 bytes apart): the tensor-core kernel. Others: the FMA kernel.
+static bool dw_mapped(const void* dy, long long ld_dy, long long T, long long N, long long H, const void* out) {
+  return words(dy, ld_dy, T, N, KDKL_TYPE_BF16) && H % 8 == 0 && ((uintptr_t)out & 15) == 0;
+}
+// Parts of the contraction: the count with the least estimated cycles. A block of 64 tokens takes a unit 512 cycles of
+// the tensor pipe; starting a unit and draining its tile about five blocks; the slabs of two or more parts one more
+// launch, and being written and read once at about 2600 bytes a cycle.
+static int dw_parts(long long T, long long N, long long H) {
+  const long long tiles = ((N + 255) / 256) * ((H + 255) / 256), kb = (T + 63) / 64, pairs = 74;
+  int best = 1;
+  double least = 0.0;
+  for (int parts = 1; parts <= 8; ++parts) {
+    if (parts > 1 && kb / parts < 8) break;
+    const long long waves = (tiles * parts + pairs - 1) / pairs;
+    double cost = (double)waves * ((kb + parts - 1) / parts + 5) * 512.0;
+    if (parts > 1) cost += 6000.0 + (double)N * H * (8.0 * parts + 4.0) / 2600.0;
+    if (parts == 1 || cost < least) { least = cost; best = parts; }
+  }
+  return best;
+}
+// Rows of a slab: output boxes are 32 rows high, and what lies past N must not reach the next slab.
+static long long dw_slab_rows(long long N) { return (N + 31) / 32 * 32; }
+// With more than one part, and for += in bf16, fp32 slabs go through the workspace.
+static size_t dw_slab_bytes(long long T, long long N, long long H, int type, bool accumulate, int* parts) {
+  *parts = dw_parts(T, N, H);
+  const bool slabs = *parts > 1 || (accumulate && type == KDKL_TYPE_BF16);
+  return slabs ? (size_t)*parts * dw_slab_rows(N) * H * 4 : 0;
+}
+
 size_t kdkl_act8_dweight_workspace_bytes(int64_t T, int64_t N, int64_t H, int32_t type) {
   if (!shape_ok(T, H) || !shape_ok(T, N) || (type != KDKL_TYPE_BF16 && type != KDKL_TYPE_F32)) return 0;
-  return 256;
+  int parts;
+  return 256 + up(dw_slab_bytes(T, N, H, type, true, &parts), 256);
 }
+
+}  // extern "C"
+
+template <int FMT, bool F32_OUT>
+static int launch_dweight(const CUtensorMap& ty, const CUtensorMap& tc, const CUtensorMap& ts, const CUtensorMap& to,
+                          const DwParams& p, const DeviceInfo& di, cudaStream_t st) {
+  auto kern = act8_dweight_kernel<FMT, F32_OUT>;
+  static bool attr_set[kMaxDevices];
+  if (di.dev < 0 || di.dev >= kMaxDevices || !attr_set[di.dev]) {
+    KDKL_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, DwCfg::SMEM_BYTES));
+    if (di.dev >= 0 && di.dev < kMaxDevices) attr_set[di.dev] = true;
+  }
+  const int units = p.n_tiles * p.h_tiles * p.parts, most = di.sm_count / 2;
+  kern<<<2 * (units < most ? units : most), DwCfg::THREADS, DwCfg::SMEM_BYTES, st>>>(ty, tc, ts, to, p);
+  KDKL_LAUNCHED("act8_dweight_kernel");
+  return KDKL_OK;
+}
+
+extern "C" {
 
 int kdkl_act8_dweight(const void* dy, int64_t ld_dy, const void* record, size_t record_bytes, int64_t T, int64_t N,
                       int64_t H, int32_t format, void* dweight, int32_t type, int32_t accumulate, void* workspace,
@@ -143,16 +192,49 @@ int kdkl_act8_dweight(const void* dy, int64_t ld_dy, const void* record, size_t 
   DeviceInfo di;
   if ((rc = need_b200(&di))) return rc;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
-  KDKL_CUDA(cudaMemsetAsync(workspace, 0, 256, st));
-  DweightParams p;
-  p.dy = reinterpret_cast<const __nv_bfloat16*>(dy); p.ld_dy = ld_dy;
-  p.rec = record_at(record, T, H);
+  const ActRecord rec = record_at(record, T, H);
+  int* status = at<int>(workspace, 0);
+  if (T == 0 || !dw_mapped(dy, ld_dy, T, N, H, dweight)) {
+    DweightParams p;
+    p.dy = reinterpret_cast<const __nv_bfloat16*>(dy); p.ld_dy = ld_dy;
+    p.rec = rec;
+    p.T = T; p.N = (int)N; p.H = (int)H;
+    p.out = dweight; p.type = type; p.accumulate = accumulate;
+    p.status = status;
+    const dim3 grid((unsigned)((H + 63) / 64), (unsigned)((N + 63) / 64), 1);
+    if (grid.y > 65535) return KDKL_ERR_SHAPE;
+    KDKL_BY_FORMAT(format, FMT, (act8_dweight_simple_kernel<FMT><<<grid, 256, 0, st>>>(p)));
+    KDKL_LAUNCHED("act8_dweight_simple_kernel");
+    return KDKL_OK;
+  }
+  int parts;
+  const bool slabs = dw_slab_bytes(T, N, H, type, accumulate != 0, &parts) != 0;
+  float* slab = at<float>(workspace, 256);
+  const bool f32_out = slabs || type == KDKL_TYPE_F32;
+  CUtensorMap ty, tc, ts, to;
+  const long long ld = T > 1 ? ld_dy : N;
+  if ((rc = make_tmap_bf16(&ty, dy, (uint64_t)N, (uint64_t)T, (uint64_t)ld * 2, 64, DwCfg::BK))) return rc;
+  if ((rc = make_tmap(&tc, CU_TENSOR_MAP_DATA_TYPE_UINT8, rec.codes, (uint64_t)act_codes_pitch(H), (uint64_t)T,
+                      (uint64_t)act_codes_pitch(H), 128, DwCfg::BK, CU_TENSOR_MAP_SWIZZLE_NONE)))
+    return rc;
+  if ((rc = make_tmap(&ts, CU_TENSOR_MAP_DATA_TYPE_UINT8, rec.scales, (uint64_t)act_scale_pitch(H), (uint64_t)T,
+                      (uint64_t)act_scale_pitch(H), 16, DwCfg::BK, CU_TENSOR_MAP_SWIZZLE_NONE)))
+    return rc;
+  DwParams p;
   p.T = T; p.N = (int)N; p.H = (int)H;
-  p.out = dweight; p.type = type; p.accumulate = accumulate;
-  const dim3 grid((unsigned)((H + 63) / 64), (unsigned)((N + 63) / 64), 1);
-  if (grid.y > 65535) return KDKL_ERR_SHAPE;
-  KDKL_BY_FORMAT(format, FMT, (act8_dweight_simple_kernel<FMT><<<grid, 256, 0, st>>>(p)));
-  KDKL_LAUNCHED("act8_dweight_simple_kernel");
+  p.n_tiles = (int)((N + 255) / 256); p.h_tiles = (int)((H + 255) / 256); p.parts = parts;
+  p.part_rows = (int)dw_slab_rows(N);
+  p.reduce = !slabs && accumulate;
+  p.status = status;
+  if (slabs) rc = make_tmap_out_f32(&to, slab, (uint64_t)H, (uint64_t)parts * dw_slab_rows(N), (uint64_t)H);
+  else if (f32_out) rc = make_tmap_out_f32(&to, dweight, (uint64_t)H, (uint64_t)N, (uint64_t)H);
+  else rc = make_tmap_out_bf16(&to, dweight, (uint64_t)H, (uint64_t)N, (uint64_t)H);
+  if (rc) return rc;
+  KDKL_BY_FORMAT(format, FMT, KDKL_BY_BOOL(f32_out, F32_OUT, rc = (launch_dweight<FMT, F32_OUT>(ty, tc, ts, to, p, di, st))));
+  if (rc || !slabs) return rc;
+  const long long n8 = N * H / 8;
+  act8_dweight_join_kernel<<<(unsigned)((n8 + 255) / 256), 256, 0, st>>>(slab, dw_slab_rows(N) * H, parts, n8, dweight, type, accumulate);
+  KDKL_LAUNCHED("act8_dweight_join_kernel");
   return KDKL_OK;
 }
 

@@ -51,10 +51,11 @@ inline EncodeTiledFn get_encode_fn() {
 }
 
 // 2-D bf16 tensor, `inner` contiguous elements per row, `outer` rows of `pitch_bytes`;
-// boxes of box_inner x box_outer written to shared memory with the 128-byte swizzle;
+// boxes of box_inner x box_outer written to shared memory with the 128-byte swizzle unless another is given;
 // out-of-bounds elements read as zero.
 inline int make_tmap(CUtensorMap* m, CUtensorMapDataType dtype, const void* base, uint64_t inner, uint64_t outer,
-                     uint64_t pitch_bytes, uint32_t box_inner, uint32_t box_outer) {
+                     uint64_t pitch_bytes, uint32_t box_inner, uint32_t box_outer,
+                     CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B) {
   EncodeTiledFn fn = get_encode_fn();
   if (!fn) { snprintf(g_err, sizeof(g_err), "cuTensorMapEncodeTiled entry point not found"); return KDKL_ERR_CUDA; }
   cuuint64_t dims[2] = {inner, outer};
@@ -62,7 +63,7 @@ inline int make_tmap(CUtensorMap* m, CUtensorMapDataType dtype, const void* base
   cuuint32_t box[2] = {box_inner, box_outer};
   cuuint32_t estr[2] = {1, 1};
   CUresult r = fn(m, dtype, 2, const_cast<void*>(base), dims, strides, box, estr,
-                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) {
     snprintf(g_err, sizeof(g_err), "cuTensorMapEncodeTiled failed (%d): inner=%llu outer=%llu pitch=%llu box=%ux%u",

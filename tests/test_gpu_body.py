@@ -216,6 +216,25 @@ def test_dweight_matches_oracle(fmt, dtype, how):
         assert op.status()[0] == 0
 
 
+@pytest.mark.parametrize("T,N,H,dtype", [(6000, 264, 520, F32), (6000, 264, 520, BF16), (20000, 64, 96, F32),
+                                         (2500, 1000, 1544, BF16), (1536, 2048, 2560, F32)])
+def test_dweight_over_long_batches(T, N, H, dtype):
+    """Many runs of an accumulator, contractions in several parts, parts and runs of uneven length, several tiles a CTA
+    pair. Against float64 on the GPU, with the bound of the tests above."""
+    dy, x = _randn(1, T, N).to(_dev()), _randn(2, T, H, outliers=True).to(_dev())
+    rec = body.Act8Record(T, H).store(x)
+    xk = rec.load(dtype=F32).double()
+    op = body.Act8WeightGrad(T, N, H, dtype=dtype)
+    op.dweight.fill_(NAN)
+    op.workspace.fill_(0xFF)
+    got = op.run(dy, rec)
+    terms = _np(dy.double().abs().t() @ xk.abs())
+    _close(got, _np(dy.double().t() @ xk), dtype, (T * 2.0 ** -24 + 2.0 ** -22) / ABS * terms)
+    want = got.clone()
+    op.workspace.fill_(0xFF)
+    assert torch.equal(op.run(dy, rec), want) and op.status()[0] == 0
+
+
 def test_dweight_of_records_that_are_not_finite_and_of_nothing():
     T, N, H = 100, 64, 256
     x = _randn(1, T, H); x[50, 70] = float("inf")
