@@ -89,7 +89,7 @@ act8_dweight_simple_kernel(const DweightParams p) {
 }
 
 struct DwCfg {
-  static constexpr int TILE = 256, BK = 64, STAGES = 4, RAW = 5, RUN = 12;
+  static constexpr int TILE = 256, BK = 64, STAGES = 4, RAW = 4, RUN = 12;
   static constexpr int A_BYTES = 128 * BK * 2, B_BYTES = 128 * BK * 2, STAGE_BYTES = A_BYTES + B_BYTES;
   static constexpr int CODE_BYTES = 128 * BK, SCALE_BYTES = 16 * BK, RAW_BYTES = CODE_BYTES + SCALE_BYTES;
   static constexpr int CONVERT_WARPS = 8, SUM_WARPS = 8;
@@ -97,6 +97,9 @@ struct DwCfg {
   static constexpr int THREADS = 128 + 32 * (CONVERT_WARPS + SUM_WARPS);
   static constexpr int BOX_BYTES = 4096;      // 32 rows x 128 bytes of output per summing warp
   static constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + RAW * RAW_BYTES + SUM_WARPS * BOX_BYTES + 1024 + 256;
+  // A wait knows a barrier's phase by one bit, so each slot of a ring has to be waited for by one team, in order: a team
+  // that came to a slot of another could take the phase before the last for the one it needs.
+  static_assert(STAGES % TEAMS == 0 && RAW % TEAMS == 0, "a ring slot belongs to one team");
   // registers a thread of each warpgroup: launched with 96, 32 + 2 * 48 + 2 * 176 <= 5 * 96
   static constexpr int REGS_FEED = 32, REGS_CONVERT = 48, REGS_SUM = 176;
 };
@@ -263,7 +266,7 @@ act8_dweight_kernel(const __grid_constant__ CUtensorMap tmY, const __grid_consta
           for (int kb = k0; kb < k1; ++kb, ++it) {
             const uint32_t s = it % C::STAGES, ph = (it / C::STAGES) & 1u;
             if (!mbar_wait(yfull(s), ph, abort_flag, p.status, 4) ||
-                !mbar_wait_cluster(bfull(s), ph, abort_flag, p.status, 5)) { ok = false; break; }
+                !mbar_wait(bfull(s), ph, abort_flag, p.status, 5)) { ok = false; break; }
             tc_fence_after();
             const uint32_t alo = a_lo0 + s * (C::STAGE_BYTES >> 4), blo = b_lo0 + s * (C::STAGE_BYTES >> 4);
 #pragma unroll
@@ -326,7 +329,7 @@ act8_dweight_kernel(const __grid_constant__ CUtensorMap tmY, const __grid_consta
         __syncwarp();
         if (lane == 0) {
           mbar_arrive(rempty(r));
-          mbar_arrive_release_cluster(map_to_cta(bfull(s), 0u));
+          mbar_arrive_cluster(map_to_cta(bfull(s), 0u));
         }
       }
     }

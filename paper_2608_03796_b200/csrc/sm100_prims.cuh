@@ -53,14 +53,13 @@ template <int N> __device__ __forceinline__ void regs_dec() { asm volatile("setm
 
 // Bounded wait. Returns false when the CTA has aborted (flag set by any role) or the
 // limit expired (then it sets the flag itself and records `where` in the status word).
-template <typename Try>
-__device__ __forceinline__ bool bounded_wait(Try try_wait, volatile int* abort_flag, int* status_word, int where,
-                                             uint64_t limit_ns) {
-  if (try_wait()) return true;
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag,
+                                          int* status_word, int where, uint64_t limit_ns = kWaitLimitNs) {
+  if (mbar_try_wait(bar, parity)) return true;
   const uint64_t t0 = globaltimer_ns();
   uint32_t spins = 0;
   while (true) {
-    if (try_wait()) return true;
+    if (mbar_try_wait(bar, parity)) return true;
     if ((++spins & 63u) == 0u) {
       if (*abort_flag) return false;
       if (globaltimer_ns() - t0 > limit_ns) {
@@ -73,11 +72,6 @@ __device__ __forceinline__ bool bounded_wait(Try try_wait, volatile int* abort_f
       }
     }
   }
-}
-
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag,
-                                          int* status_word, int where, uint64_t limit_ns = kWaitLimitNs) {
-  return bounded_wait([&] { return mbar_try_wait(bar, parity); }, abort_flag, status_word, where, limit_ns);
 }
 
 // ---------------------------------------------------------------- TMA
@@ -198,27 +192,6 @@ __device__ __forceinline__ uint32_t map_to_cta(uint32_t smem_addr, uint32_t rank
 }
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_bar) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
-}
-// The same arrival with release semantics for the whole cluster, and the wait that acquires it: for data that this
-// thread's warp wrote into its own CTA's shared memory and the pair's leader hands to an MMA.
-__device__ __forceinline__ void mbar_arrive_release_cluster(uint32_t cluster_bar) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
-}
-__device__ __forceinline__ bool mbar_try_wait_acquire_cluster(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
-__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity, volatile int* abort_flag,
-                                                  int* status_word, int where) {
-  return bounded_wait([&] { return mbar_try_wait_acquire_cluster(bar, parity); }, abort_flag, status_word, where,
-                      kWaitLimitNs);
 }
 // TMA load into this CTA's shared memory whose completion is signalled on a barrier that may
 // belong to the other CTA of the pair (no multicast: every CTA fetches its own boxes).
