@@ -17,8 +17,9 @@
 // Why sums in registers: an accumulator in tensor memory truncates at each addition, measured as a relative error of
 // 1.1e-9 per token contracted (4.4e-6 at 4096, 3.8e-5 at 32768). It therefore only runs over RUN blocks; then
 // the eight warps add it, rounding to nearest, to the sums they hold, while the second accumulator fills.
-// Work units are (tile, part of the contraction); parts beyond one leave fp32 slabs that act8_dweight_join_kernel adds
-// in order, so results are reproducible bit for bit.
+// Work units: whole tiles as far as they fill whole waves of CTA pairs, then the remaining tiles cut into parts of the
+// contraction, so that the last wave is as short as it can be. Parts leave fp32 slabs that act8_dweight_join_kernel adds
+// in order: results are reproducible bit for bit.
 #pragma once
 #include "act8.cuh"
 #include "sm100_prims.cuh"
@@ -107,9 +108,11 @@ struct DwCfg {
 struct DwParams {
   long long T;
   int N, H;
-  int n_tiles, h_tiles, parts;     // units = n_tiles * h_tiles * parts
-  int part_rows;                   // output row distance between the slabs of two parts
-  int reduce;                      // fp32 output: += instead of =
+  int h_tiles;
+  int whole;                       // tiles that are one unit each; the first ones
+  int rest, parts;                 // tiles that are cut into `parts` units each: [rest, parts] slabs of 256 x 256 fp32
+  int accumulate;
+  const __nv_bfloat16* out;        // bf16 output: what += adds to
   int* status;
 };
 
@@ -150,7 +153,7 @@ template <int FMT, bool F32_OUT>
 __global__ void __launch_bounds__(DwCfg::THREADS, 1) __cluster_dims__(2, 1, 1)
 act8_dweight_kernel(const __grid_constant__ CUtensorMap tmY, const __grid_constant__ CUtensorMap tmCodes,
                     const __grid_constant__ CUtensorMap tmScales, const __grid_constant__ CUtensorMap tmOut,
-                    const DwParams p) {
+                    const __grid_constant__ CUtensorMap tmSlab, const DwParams p) {
   using C = DwCfg;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -188,6 +191,7 @@ act8_dweight_kernel(const __grid_constant__ CUtensorMap tmY, const __grid_consta
     *abort_flag = 0;
     mbar_fence_init();
     tma_prefetch_desc(&tmY); tma_prefetch_desc(&tmCodes); tma_prefetch_desc(&tmScales); tma_prefetch_desc(&tmOut);
+    if (p.rest > 0) tma_prefetch_desc(&tmSlab);
   }
   if (warp == 1) { tmem_alloc_pair(smem_u32(tmem_slot), 512); tmem_relinquish_pair(); }
   tc_fence_before();
@@ -197,17 +201,22 @@ act8_dweight_kernel(const __grid_constant__ CUtensorMap tmY, const __grid_consta
   const uint32_t tmem = *tmem_slot;
 
   const int worker = blockIdx.x >> 1, workers = gridDim.x >> 1;
-  const int tiles = p.n_tiles * p.h_tiles, units = tiles * p.parts;
+  const int units = p.whole + p.rest * p.parts;
   const int kblocks = (int)((p.T + C::BK - 1) / C::BK), per_part = (kblocks + p.parts - 1) / p.parts;
-  struct Unit { int n0, h0, part, kb0, kb1; };
+  struct Unit { int n0, h0, slab, kb0, kb1; };
   auto unit_at = [&](int u) {
     Unit r;
-    r.part = u / tiles;
-    const int tile = u - r.part * tiles;
+    int tile = u;
+    r.slab = -1; r.kb0 = 0; r.kb1 = kblocks;
+    if (u >= p.whole) {
+      const int part = (u - p.whole) / p.rest, i = (u - p.whole) % p.rest;
+      tile = p.whole + i;
+      r.slab = i * p.parts + part;
+      r.kb0 = part * per_part;
+      if (r.kb0 + per_part < kblocks) r.kb1 = r.kb0 + per_part;
+    }
     r.n0 = (tile / p.h_tiles) * C::TILE;
     r.h0 = (tile % p.h_tiles) * C::TILE;
-    r.kb0 = r.part * per_part;
-    r.kb1 = r.kb0 + per_part < kblocks ? r.kb0 + per_part : kblocks;
     return r;
   };
   bool ok = true;
@@ -365,34 +374,59 @@ act8_dweight_kernel(const __grid_constant__ CUtensorMap tmY, const __grid_consta
         if (lane == 0) mbar_arrive_cluster(map_to_cta(tempty(acc), 0u));
       }
       if (!ok) break;
+      // Boxes of 32 rows x 128 bytes, to the result or to the unit's slab.
       const int row0 = w.n0 + (int)rank * 128 + lg * 32, col0 = w.h0 + col_half;
-      constexpr int BOX_COLS = F32_OUT ? 32 : 64;
+      auto send = [&](const CUtensorMap* map, int x, int y, bool add) {
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          if (add) tma_reduce_add_2d(map, box, x, y); else tma_store_2d(map, box, x, y);
+          bulk_commit();
+        }
+      };
+      const bool to_slab = w.slab >= 0;
+      if (F32_OUT || to_slab) {
 #pragma unroll
-      for (int b = 0; b < 128 / BOX_COLS; ++b) {
-        if (row0 < p.N && col0 + b * BOX_COLS < p.H) {         // uniform over the warp
-          if (lane == 0) bulk_wait_read<0>();
-          __syncwarp();
+        for (int b = 0; b < 4; ++b) {
+          if (row0 < p.N && col0 + b * 32 < p.H) {             // uniform over the warp
+            if (lane == 0) bulk_wait_read<0>();
+            __syncwarp();
 #pragma unroll
-          for (int ch = 0; ch < 8; ++ch) {
-            uint32_t v[4];                                     // volatile: copies made here do not pile up in registers
+            for (int ch = 0; ch < 8; ++ch) {
+              uint32_t v[4];                                   // volatile: copies made here do not pile up in registers
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              if constexpr (F32_OUT) {
-                asm volatile("mov.b32 %0, %1;" : "=r"(v[j]) : "f"(sum[b * 32 + ch * 4 + j]));
-              } else {
+              for (int j = 0; j < 4; ++j) asm volatile("mov.b32 %0, %1;" : "=r"(v[j]) : "f"(sum[b * 32 + ch * 4 + j]));
+              st_shared_v4(box + lane * 128 + ((ch ^ (lane & 7)) << 4), v[0], v[1], v[2], v[3]);
+            }
+            if (to_slab) send(&tmSlab, col_half + b * 32, w.slab * C::TILE + (int)rank * 128 + lg * 32, false);
+            else send(&tmOut, col0 + b * 32, row0, p.accumulate != 0);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          if (row0 < p.N && col0 + b * 64 < p.H) {
+            if (lane == 0) bulk_wait_read<0>();
+            __syncwarp();
+#pragma unroll
+            for (int ch = 0; ch < 8; ++ch) {
+              if (p.accumulate) {                              // += in bf16: the old values first, rounded once after
+                const int col = col0 + b * 64 + ch * 8;
+                float old[8];
+                if (row0 + lane < p.N && col < p.H) {          // H % 8 == 0
+                  load8<__nv_bfloat16, true>(p.out + (long long)(row0 + lane) * p.H, col, p.H, old);
+#pragma unroll
+                  for (int j = 0; j < 8; ++j) sum[b * 64 + ch * 8 + j] += old[j];
+                }
+              }
+              uint32_t v[4];
+#pragma unroll
+              for (int j = 0; j < 4; ++j)
                 asm volatile("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v[j])
                              : "f"(sum[b * 64 + ch * 8 + 2 * j + 1]), "f"(sum[b * 64 + ch * 8 + 2 * j]));
-              }
+              st_shared_v4(box + lane * 128 + ((ch ^ (lane & 7)) << 4), v[0], v[1], v[2], v[3]);
             }
-            st_shared_v4(box + lane * 128 + ((ch ^ (lane & 7)) << 4), v[0], v[1], v[2], v[3]);
-          }
-          fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0) {
-            const int y = row0 + w.part * p.part_rows, x = col0 + b * BOX_COLS;
-            if (F32_OUT && p.reduce) tma_reduce_add_2d(&tmOut, box, x, y);
-            else tma_store_2d(&tmOut, box, x, y);
-            bulk_commit();
+            send(&tmOut, col0 + b * 64, row0, false);
           }
         }
       }
@@ -408,28 +442,32 @@ act8_dweight_kernel(const __grid_constant__ CUtensorMap tmY, const __grid_consta
   if (warp == 1) tmem_dealloc_pair(tmem, 512);
 }
 
-// out (= or +=) slab 0 + slab 1 + ... in that order, one rounding. H % 8 == 0.
+// The tiles that were cut: out (= or +=) slab 0 + slab 1 + ... in that order, rounded once. One block per 8 rows of a
+// tile, 32 threads a row. H % 8 == 0.
 __global__ void __launch_bounds__(256)
-act8_dweight_join_kernel(const float* __restrict__ slabs, long long slab, int parts, long long n8, void* __restrict__ out,
-                         int type, int accumulate) {
-  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-  if (i >= n8) return;
+act8_dweight_join_kernel(const float* __restrict__ slabs, int whole, int parts, int h_tiles, int N, int H,
+                         void* __restrict__ out, int type, int accumulate) {
+  const int i = blockIdx.x >> 5, r = (blockIdx.x & 31) * 8 + (threadIdx.x >> 5), c = (threadIdx.x & 31) * 8;
+  const int tile = whole + i, row = (tile / h_tiles) * 256 + r, col = (tile % h_tiles) * 256 + c;
+  if (row >= N || col >= H) return;
+  const float* src = slabs + ((long long)i * parts * 256 + r) * 256 + c;
   float f[8], g[8];
-  raw_to_f32(load_raw8<float, true>(slabs + i * 8, 0, 8), f);
+  raw_to_f32(load_raw8<float, true>(src, 0, 8), f);
   for (int q = 1; q < parts; ++q) {
-    raw_to_f32(load_raw8<float, true>(slabs + q * slab + i * 8, 0, 8), g);
+    raw_to_f32(load_raw8<float, true>(src + (long long)q * 65536, 0, 8), g);
 #pragma unroll
     for (int j = 0; j < 8; ++j) f[j] += g[j];
   }
+  const long long at = (long long)row * H + col;
   if (type == 1) {
-    float* o = reinterpret_cast<float*>(out) + i * 8;
+    float* o = reinterpret_cast<float*>(out) + at;
     if (accumulate) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) f[j] += o[j];
     }
     store_raw8<float, true>(o, 0, 8, f32_to_raw<float>(f));
   } else {
-    __nv_bfloat16* o = reinterpret_cast<__nv_bfloat16*>(out) + i * 8;
+    __nv_bfloat16* o = reinterpret_cast<__nv_bfloat16*>(out) + at;
     if (accumulate) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) f[j] += __bfloat162float(o[j]);

@@ -126,50 +126,44 @@ int kdkl_gated_act_backward(const void* gate_record, const void* up_record, size
 static bool dw_mapped(const void* dy, long long ld_dy, long long T, long long N, long long H, const void* out) {
   return words(dy, ld_dy, T, N, KDKL_TYPE_BF16) && H % 8 == 0 && ((uintptr_t)out & 15) == 0;
 }
-// Parts of the contraction: the count with the least estimated cycles. A block of 64 tokens takes a unit 512 cycles of
-// the tensor pipe; starting a unit and draining its tile about five blocks; the slabs of two or more parts one more
-// launch, and being written and read once at about 2600 bytes a cycle.
-static int dw_parts(long long T, long long N, long long H) {
-  const long long tiles = ((N + 255) / 256) * ((H + 255) / 256), kb = (T + 63) / 64, pairs = 74;
-  int best = 1;
-  double least = 0.0;
-  for (int parts = 1; parts <= 8; ++parts) {
-    if (parts > 1 && kb / parts < 8) break;
-    const long long waves = (tiles * parts + pairs - 1) / pairs;
-    double cost = (double)waves * ((kb + parts - 1) / parts + 5) * 512.0;
-    if (parts > 1) cost += 6000.0 + (double)N * H * (8.0 * parts + 4.0) / 2600.0;
-    if (parts == 1 || cost < least) { least = cost; best = parts; }
+// Which tiles are cut, and into how many parts of the contraction: the choice with the least estimated cycles. A block
+// of 64 tokens takes a unit 600 cycles, starting a unit and draining its tile about five blocks; the slabs of cut tiles
+// one more launch, and being written and read once at about 2600 bytes a cycle.
+struct DwPlan { int whole, rest, parts; };
+static DwPlan dw_plan(long long T, long long N, long long H) {
+  const long long tiles = ((N + 255) / 256) * ((H + 255) / 256), kb = (T + 63) / 64;
+  const long long pairs = sm_count_or_default() / 2;
+  DwPlan best = {(int)tiles, 0, 1};
+  double least = (double)((tiles + pairs - 1) / pairs) * (kb + 5) * 600.0;
+  const long long rest = tiles % pairs;                    // what whole waves leave over
+  for (int parts = 2; rest != 0 && parts <= 16 && kb / parts >= 8; ++parts) {
+    const long long waves = (rest * parts + pairs - 1) / pairs;
+    const double cost = (double)((tiles / pairs) * (kb + 5) + waves * ((kb + parts - 1) / parts + 5)) * 600.0 + 6000.0 +
+                        (double)rest * 65536.0 * (8.0 * parts + 4.0) / 2600.0;
+    if (cost < least) { least = cost; best = DwPlan{(int)(tiles - rest), (int)rest, parts}; }
   }
   return best;
-}
-// Rows of a slab: output boxes are 32 rows high, and what lies past N must not reach the next slab.
-static long long dw_slab_rows(long long N) { return (N + 31) / 32 * 32; }
-// With more than one part, and for += in bf16, fp32 slabs go through the workspace.
-static size_t dw_slab_bytes(long long T, long long N, long long H, int type, bool accumulate, int* parts) {
-  *parts = dw_parts(T, N, H);
-  const bool slabs = *parts > 1 || (accumulate && type == KDKL_TYPE_BF16);
-  return slabs ? (size_t)*parts * dw_slab_rows(N) * H * 4 : 0;
 }
 
 size_t kdkl_act8_dweight_workspace_bytes(int64_t T, int64_t N, int64_t H, int32_t type) {
   if (!shape_ok(T, H) || !shape_ok(T, N) || (type != KDKL_TYPE_BF16 && type != KDKL_TYPE_F32)) return 0;
-  int parts;
-  return 256 + up(dw_slab_bytes(T, N, H, type, true, &parts), 256);
+  const DwPlan plan = dw_plan(T, N, H);
+  return 256 + (size_t)plan.rest * plan.parts * 65536 * 4;
 }
 
 }  // extern "C"
 
 template <int FMT, bool F32_OUT>
 static int launch_dweight(const CUtensorMap& ty, const CUtensorMap& tc, const CUtensorMap& ts, const CUtensorMap& to,
-                          const DwParams& p, const DeviceInfo& di, cudaStream_t st) {
+                          const CUtensorMap& tslab, const DwParams& p, const DeviceInfo& di, cudaStream_t st) {
   auto kern = act8_dweight_kernel<FMT, F32_OUT>;
   static bool attr_set[kMaxDevices];
   if (di.dev < 0 || di.dev >= kMaxDevices || !attr_set[di.dev]) {
     KDKL_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, DwCfg::SMEM_BYTES));
     if (di.dev >= 0 && di.dev < kMaxDevices) attr_set[di.dev] = true;
   }
-  const int units = p.n_tiles * p.h_tiles * p.parts, most = di.sm_count / 2;
-  kern<<<2 * (units < most ? units : most), DwCfg::THREADS, DwCfg::SMEM_BYTES, st>>>(ty, tc, ts, to, p);
+  const int units = p.whole + p.rest * p.parts, most = di.sm_count / 2;
+  kern<<<2 * (units < most ? units : most), DwCfg::THREADS, DwCfg::SMEM_BYTES, st>>>(ty, tc, ts, to, tslab, p);
   KDKL_LAUNCHED("act8_dweight_kernel");
   return KDKL_OK;
 }
@@ -207,11 +201,9 @@ int kdkl_act8_dweight(const void* dy, int64_t ld_dy, const void* record, size_t 
     KDKL_LAUNCHED("act8_dweight_simple_kernel");
     return KDKL_OK;
   }
-  int parts;
-  const bool slabs = dw_slab_bytes(T, N, H, type, accumulate != 0, &parts) != 0;
+  const DwPlan plan = dw_plan(T, N, H);
   float* slab = at<float>(workspace, 256);
-  const bool f32_out = slabs || type == KDKL_TYPE_F32;
-  CUtensorMap ty, tc, ts, to;
+  CUtensorMap ty, tc, ts, to, tslab;
   const long long ld = T > 1 ? ld_dy : N;
   if ((rc = make_tmap_bf16(&ty, dy, (uint64_t)N, (uint64_t)T, (uint64_t)ld * 2, 64, DwCfg::BK))) return rc;
   if ((rc = make_tmap(&tc, CU_TENSOR_MAP_DATA_TYPE_UINT8, rec.codes, (uint64_t)act_codes_pitch(H), (uint64_t)T,
@@ -220,20 +212,23 @@ int kdkl_act8_dweight(const void* dy, int64_t ld_dy, const void* record, size_t 
   if ((rc = make_tmap(&ts, CU_TENSOR_MAP_DATA_TYPE_UINT8, rec.scales, (uint64_t)act_scale_pitch(H), (uint64_t)T,
                       (uint64_t)act_scale_pitch(H), 16, DwCfg::BK, CU_TENSOR_MAP_SWIZZLE_NONE)))
     return rc;
-  DwParams p;
-  p.T = T; p.N = (int)N; p.H = (int)H;
-  p.n_tiles = (int)((N + 255) / 256); p.h_tiles = (int)((H + 255) / 256); p.parts = parts;
-  p.part_rows = (int)dw_slab_rows(N);
-  p.reduce = !slabs && accumulate;
-  p.status = status;
-  if (slabs) rc = make_tmap_out_f32(&to, slab, (uint64_t)H, (uint64_t)parts * dw_slab_rows(N), (uint64_t)H);
-  else if (f32_out) rc = make_tmap_out_f32(&to, dweight, (uint64_t)H, (uint64_t)N, (uint64_t)H);
+  if (type == KDKL_TYPE_F32) rc = make_tmap_out_f32(&to, dweight, (uint64_t)H, (uint64_t)N, (uint64_t)H);
   else rc = make_tmap_out_bf16(&to, dweight, (uint64_t)H, (uint64_t)N, (uint64_t)H);
   if (rc) return rc;
-  KDKL_BY_FORMAT(format, FMT, KDKL_BY_BOOL(f32_out, F32_OUT, rc = (launch_dweight<FMT, F32_OUT>(ty, tc, ts, to, p, di, st))));
-  if (rc || !slabs) return rc;
-  const long long n8 = N * H / 8;
-  act8_dweight_join_kernel<<<(unsigned)((n8 + 255) / 256), 256, 0, st>>>(slab, dw_slab_rows(N) * H, parts, n8, dweight, type, accumulate);
+  tslab = to;
+  if (plan.rest > 0 && (rc = make_tmap_out_f32(&tslab, slab, 256, (uint64_t)plan.rest * plan.parts * 256, 256))) return rc;
+  DwParams p;
+  p.T = T; p.N = (int)N; p.H = (int)H;
+  p.h_tiles = (int)((H + 255) / 256);
+  p.whole = plan.whole; p.rest = plan.rest; p.parts = plan.parts;
+  p.accumulate = accumulate;
+  p.out = reinterpret_cast<const __nv_bfloat16*>(dweight);
+  p.status = status;
+  KDKL_BY_FORMAT(format, FMT, KDKL_BY_BOOL(type == KDKL_TYPE_F32, F32_OUT,
+    rc = (launch_dweight<FMT, F32_OUT>(ty, tc, ts, to, tslab, p, di, st))));
+  if (rc || plan.rest == 0) return rc;
+  act8_dweight_join_kernel<<<(unsigned)plan.rest * 32, 256, 0, st>>>(slab, plan.whole, plan.parts, p.h_tiles, (int)N, (int)H,
+                                                                     dweight, type, accumulate);
   KDKL_LAUNCHED("act8_dweight_join_kernel");
   return KDKL_OK;
 }

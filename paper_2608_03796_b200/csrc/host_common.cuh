@@ -108,4 +108,15 @@ inline int device_info(DeviceInfo* di) {
   return KDKL_OK;
 }
 
+// SM count of the current device for sizing decisions that are also taken where there may be no device
+// (kdkl_workspace_bytes on a build machine): a B200's 148 then.
+inline int sm_count_or_default() {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return 148; }
+  if (dev >= 0 && dev < kMaxDevices && g_devices[dev].known) return g_devices[dev].sm_count;
+  DeviceInfo di;
+  if (device_info(&di) != KDKL_OK || di.sm_count < 2) { cudaGetLastError(); return 148; }
+  return di.sm_count;
+}
+
 }  // namespace kdkl

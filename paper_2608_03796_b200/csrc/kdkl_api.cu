@@ -93,17 +93,6 @@ static int m_group_for(long long H) {
 }
 static bool use_wide(long long N) { return ((N + kWideN - 1) / kWideN) * kWideN * 10 <= N * 11; }
 static long long n_tiles_for(long long N, bool wide) { return wide ? (N + kWideN - 1) / kWideN : (N + BN - 1) / BN; }
-// SM count of the current device for sizing decisions that are also taken where there may be no device
-// (kdkl_workspace_bytes on a build machine): a B200's 148 then.
-static int sm_count_or_default() {
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return 148; }
-  if (dev >= 0 && dev < kMaxDevices && g_devices[dev].known) return g_devices[dev].sm_count;
-  DeviceInfo di;
-  if (device_info(&di) != KDKL_OK || di.sm_count < 2) { cudaGetLastError(); return 148; }
-  return di.sm_count;
-}
-
 template <int EPI, bool A_MN, bool B_MN, bool WIDE = false>
 static int launch_gemm(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& tc, const GemmParams& p,
                        const DeviceInfo& di, cudaStream_t st) {
