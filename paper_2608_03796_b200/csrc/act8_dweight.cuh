@@ -9,7 +9,7 @@
 //
 //   tile 256 (n) x 256 (h) per CTA pair (cta_group::2); a block of the contraction is 64 tokens
 //   warp 0       TMA of dY (bf16, contiguous along n: MN-major operand), STAGES deep
-//   warp 2       TMA of codes (64 x 128 a CTA) and scale bytes, RAW deep
+//   warps 2, 3   TMA of codes and scale bytes, 32 tokens x 128 columns each, RAW / 2 deep
 //   warp 1       tensor memory; the pair leader's lane 0 issues the MMAs
 //   warps 4-11   codes -> bf16 operand tile of this CTA's 128 columns
 //   warps 12-19  running sums in registers (128 rows x 256 columns a CTA, 128 values a thread)
@@ -90,9 +90,10 @@ act8_dweight_simple_kernel(const DweightParams p) {
 }
 
 struct DwCfg {
-  static constexpr int TILE = 256, BK = 64, STAGES = 4, RAW = 4, RUN = 12;
+  static constexpr int TILE = 256, BK = 64, STAGES = 4, RUN = 12;
   static constexpr int A_BYTES = 128 * BK * 2, B_BYTES = 128 * BK * 2, STAGE_BYTES = A_BYTES + B_BYTES;
-  static constexpr int CODE_BYTES = 128 * BK, SCALE_BYTES = 16 * BK, RAW_BYTES = CODE_BYTES + SCALE_BYTES;
+  // codes and scale bytes wait in slots of half a block, each free again as soon as it is in registers
+  static constexpr int RAW = 8, RAW_T = BK / 2, CODE_BYTES = 128 * RAW_T, RAW_BYTES = CODE_BYTES + 16 * RAW_T;
   static constexpr int CONVERT_WARPS = 8, SUM_WARPS = 8;
   static constexpr int CONVERT_TEAM = 2, TEAMS = CONVERT_WARPS / CONVERT_TEAM;   // warps a block; blocks in work at once
   static constexpr int THREADS = 128 + 32 * (CONVERT_WARPS + SUM_WARPS);
@@ -100,7 +101,7 @@ struct DwCfg {
   static constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + RAW * RAW_BYTES + SUM_WARPS * BOX_BYTES + 1024 + 256;
   // A wait knows a barrier's phase by one bit, so each slot of a ring has to be waited for by one team, in order: a team
   // that came to a slot of another could take the phase before the last for the one it needs.
-  static_assert(STAGES % TEAMS == 0 && RAW % TEAMS == 0, "a ring slot belongs to one team");
+  static_assert(STAGES % TEAMS == 0 && RAW % (2 * TEAMS) == 0, "a ring slot belongs to one team");
   // registers a thread of each warpgroup: launched with 96, 32 + 2 * 48 + 2 * 176 <= 5 * 96
   static constexpr int REGS_FEED = 32, REGS_CONVERT = 48, REGS_SUM = 176;
 };
@@ -116,36 +117,42 @@ struct DwParams {
   int* status;
 };
 
-// Two bf16 values from two codes in the low bytes of `p`'s halves, times `scale` (a power of two in both halves). Exact.
+// Four bf16 values from four codes, times `scale` (a power of two in both halves). Exact. e4m3 codes arrive as their
+// value times 2^-120, so their scale carries 2^120.
 template <int FMT>
-__device__ __forceinline__ uint32_t codes_to_bf16x2(uint32_t p, uint32_t scale) {
-  uint32_t v;
-  if (FMT == kFmtInt8) {
-    // 0x43cc: the low 7 bits of a code as the fraction of 128 + low; minus 128, or minus 256 where the sign bit is set
-    const uint32_t a = p & 0xff7fff7fu, b = p & 0xff80ff80u;
-    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(v) : "r"(a), "r"(b));
-  } else {
-    // 0xcc00: sign, then exponent and fraction four places down: the value times 2^-120 (subnormals included)
-    const uint32_t m = (p & 0x7f007f00u) >> 4;
-    const uint32_t w = m | (p & 0x80008000u);
-    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(v) : "r"(w), "r"(0x7b807b80u));
-  }
-  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(v) : "r"(v), "r"(scale));
-  return v;
-}
-template <int FMT>
-__device__ __forceinline__ void codes_to_bf16x8(const uint2& c, uint32_t byte, uint32_t (&o)[4]) {
-  const uint32_t scale = (byte << 7) * 0x00010001u;         // 2^e; byte 255 (codes 0): 0 * infinity = NaN
-  const uint32_t w[2] = {c.x, c.y};
+__device__ __forceinline__ void codes_to_bf16x4(uint32_t codes, uint32_t scale, uint32_t (&o)[2]) {
 #pragma unroll
-  for (int k = 0; k < 2; ++k) {
+  for (int i = 0; i < 2; ++i) {
+    uint32_t v;
     if (FMT == kFmtInt8) {
-      o[2 * k] = codes_to_bf16x2<FMT>(__byte_perm(w[k], 0x43434343u, 0x4140), scale);
-      o[2 * k + 1] = codes_to_bf16x2<FMT>(__byte_perm(w[k], 0x43434343u, 0x4342), scale);
+      // 0x43cc: the low 7 bits of a code as the fraction of 128 + low; minus 128, or minus 256 where the sign bit is set
+      const uint32_t p = __byte_perm(codes, 0x43434343u, i == 0 ? 0x4140 : 0x4342);
+      const uint32_t a = p & 0xff7fff7fu, b = p & 0xff80ff80u;
+      asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(v) : "r"(a), "r"(b));
     } else {
-      o[2 * k] = codes_to_bf16x2<FMT>(__byte_perm(w[k], 0u, 0x1404), scale);
-      o[2 * k + 1] = codes_to_bf16x2<FMT>(__byte_perm(w[k], 0u, 0x3424), scale);
+      // 0xcc00: sign, then exponent and fraction four places down: the value times 2^-120 (subnormals included)
+      const uint32_t p = __byte_perm(codes, 0u, i == 0 ? 0x1404 : 0x3424);
+      v = ((p & 0x7f007f00u) >> 4) | (p & 0x80008000u);
     }
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(o[i]) : "r"(v), "r"(scale));
+  }
+}
+// Sixteen codes of one group. Byte 255 (codes 0) becomes an infinite scale: 0 * infinity = NaN.
+template <int FMT>
+__device__ __forceinline__ void codes_to_bf16x16(const uint4& c, uint32_t byte, uint32_t (&o)[8]) {
+  // e4m3: 2^e 2^120 passes the largest bf16 from byte 135 on (values beyond 57344): the factor 2^120 is then split off
+  const bool split = FMT == kFmtE4M3 && byte > 134u;
+  const uint32_t scale = ((FMT == kFmtE4M3 && !split ? byte + 120u : byte) << 7) * 0x00010001u;
+  const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    uint32_t v[2];
+    codes_to_bf16x4<FMT>(w[k], split ? 0x7b807b80u : scale, v);
+    o[2 * k] = v[0]; o[2 * k + 1] = v[1];
+  }
+  if (split) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(o[k]) : "r"(o[k]), "r"(scale));
   }
 }
 
@@ -161,16 +168,16 @@ act8_dweight_kernel(const __grid_constant__ CUtensorMap tmY, const __grid_consta
   const uint32_t raw0 = base + C::STAGES * C::STAGE_BYTES;
   const uint32_t box0 = raw0 + C::RAW * C::RAW_BYTES;
   const uint32_t bar0 = box0 + C::SUM_WARPS * C::BOX_BYTES;
-  // Barriers. In the leader: yfull (bytes of both CTAs' dY), bfull (both CTAs' converting warps), tempty (both CTAs'
-  // summing warps). In each CTA: empty and tfull (committed to both by the leader's MMAs), rfull, rempty.
-  auto yfull = [&](uint32_t s) { return bar0 + 8u * s; };
-  auto bfull = [&](uint32_t s) { return bar0 + 8u * (C::STAGES + s); };
-  auto empty = [&](uint32_t s) { return bar0 + 8u * (2 * C::STAGES + s); };
-  auto rfull = [&](uint32_t s) { return bar0 + 8u * (3 * C::STAGES + s); };
-  auto rempty = [&](uint32_t s) { return bar0 + 8u * (3 * C::STAGES + C::RAW + s); };
-  auto tfull = [&](uint32_t a) { return bar0 + 8u * (3 * C::STAGES + 2 * C::RAW + a); };
-  auto tempty = [&](uint32_t a) { return bar0 + 8u * (3 * C::STAGES + 2 * C::RAW + 2 + a); };
-  constexpr int kBars = 3 * C::STAGES + 2 * C::RAW + 4;
+  // Barriers. In the leader: full (the bytes of both CTAs' dY and both CTAs' converting warps: one wait for the thread that
+  // issues the products), tempty (both CTAs' summing warps). In each CTA: empty and tfull (committed to both by the
+  // leader's MMAs), rfull, rempty.
+  auto full = [&](uint32_t s) { return bar0 + 8u * s; };
+  auto empty = [&](uint32_t s) { return bar0 + 8u * (C::STAGES + s); };
+  auto rfull = [&](uint32_t s) { return bar0 + 8u * (2 * C::STAGES + s); };
+  auto rempty = [&](uint32_t s) { return bar0 + 8u * (2 * C::STAGES + C::RAW + s); };
+  auto tfull = [&](uint32_t a) { return bar0 + 8u * (2 * C::STAGES + 2 * C::RAW + a); };
+  auto tempty = [&](uint32_t a) { return bar0 + 8u * (2 * C::STAGES + 2 * C::RAW + 2 + a); };
+  constexpr int kBars = 2 * C::STAGES + 2 * C::RAW + 4;
   static_assert(8 * kBars + 8 <= 256, "barrier block");
   uint8_t* bar_ptr = base_ptr + (bar0 - base);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar_ptr + 8 * kBars);
@@ -182,8 +189,7 @@ act8_dweight_kernel(const __grid_constant__ CUtensorMap tmY, const __grid_consta
   clear_status(p.status);
   if (threadIdx.x == 0) {
     for (int s = 0; s < C::STAGES; ++s) {
-      mbar_init(yfull(s), 1);
-      mbar_init(bfull(s), 2 * C::CONVERT_TEAM);
+      mbar_init(full(s), 1 + 2 * C::CONVERT_TEAM);
       mbar_init(empty(s), 1);
     }
     for (int s = 0; s < C::RAW; ++s) { mbar_init(rfull(s), 1); mbar_init(rempty(s), C::CONVERT_TEAM); }
@@ -223,38 +229,46 @@ act8_dweight_kernel(const __grid_constant__ CUtensorMap tmY, const __grid_consta
 
   if (warp < 4) {
     regs_dec<C::REGS_FEED>();
-    if (warp == 0 && lane == 0) {
+    // Each of these warps has 512 cycles for a block, and every instruction of its loop counts: all lanes walk the loop,
+    // so that addresses and descriptors stay in uniform registers, and one of them issues.
+    if (warp == 0) {
       // -------------------------------------------------- dY
+      const bool one = elect_one();
       uint32_t it = 0;
-      for (int u = worker; u < units && ok; u += workers) {
+      for (int u = worker; u < units; u += workers) {
         const Unit w = unit_at(u);
+        const int n = w.n0 + (int)rank * 128;
         for (int kb = w.kb0; kb < w.kb1; ++kb, ++it) {
           const uint32_t s = it % C::STAGES, ph = (it / C::STAGES) & 1u;
-          if (!mbar_wait(empty(s), ph ^ 1u, abort_flag, p.status, 1)) { ok = false; break; }
-          const uint32_t fb = map_to_cta(yfull(s), 0u);
-          if (leader) mbar_arrive_expect_tx(yfull(s), 2 * C::A_BYTES);
-          const uint32_t dst = base + s * C::STAGE_BYTES;
-          const int n = w.n0 + (int)rank * 128;
-          tma_load_2d_pair(dst, &tmY, n, kb * C::BK, fb);
-          tma_load_2d_pair(dst + C::BK * 128, &tmY, n + 64, kb * C::BK, fb);
+          if (!__all_sync(0xffffffffu, mbar_wait(empty(s), ph ^ 1u, abort_flag, p.status, 1))) { ok = false; goto fed; }
+          if (one) {
+            if (leader) mbar_arrive_expect_tx(full(s), 2 * C::A_BYTES);
+            const uint32_t fb = map_to_cta(full(s), 0u), dst = base + s * C::STAGE_BYTES;
+            tma_load_2d_pair(dst, &tmY, n, kb * C::BK, fb);
+            tma_load_2d_pair(dst + C::BK * 128, &tmY, n + 64, kb * C::BK, fb);
+          }
         }
       }
-    } else if (warp == 2 && lane == 0) {
-      // -------------------------------------------------- codes and scales
+    } else if (warp >= 2) {
+      // -------------------------------------------------- codes and scales: one warp for each half of the blocks
+      const bool one = elect_one();
       uint32_t it = 0;
-      for (int u = worker; u < units && ok; u += workers) {
+      for (int u = worker; u < units; u += workers) {
         const Unit w = unit_at(u);
         const int h = w.h0 + (int)rank * 128;
         for (int kb = w.kb0; kb < w.kb1; ++kb, ++it) {
-          const uint32_t s = it % C::RAW, ph = (it / C::RAW) & 1u;
-          if (!mbar_wait(rempty(s), ph ^ 1u, abort_flag, p.status, 2)) { ok = false; break; }
-          mbar_arrive_expect_tx(rfull(s), C::RAW_BYTES);
-          const uint32_t dst = raw0 + s * C::RAW_BYTES;
-          tma_load_2d(dst, &tmCodes, h, kb * C::BK, rfull(s));
-          tma_load_2d(dst + C::CODE_BYTES, &tmScales, (h / 32) & ~15, kb * C::BK, rfull(s));
+          const uint32_t s = (2 * it + warp - 2) % C::RAW, ph = (2 * it / C::RAW) & 1u;
+          if (!__all_sync(0xffffffffu, mbar_wait(rempty(s), ph ^ 1u, abort_flag, p.status, 2))) { ok = false; goto fed; }
+          if (one) {
+            mbar_arrive_expect_tx(rfull(s), C::RAW_BYTES);
+            const uint32_t dst = raw0 + s * C::RAW_BYTES;
+            const int t = kb * C::BK + (warp - 2) * C::RAW_T;
+            tma_load_2d(dst, &tmCodes, h, t, rfull(s));
+            tma_load_2d(dst + C::CODE_BYTES, &tmScales, (h / 32) & ~15, t, rfull(s));
+          }
         }
       }
-    } else if (warp == 1 && lane == 0 && leader) {
+    } else if (warp == 1 && leader) {
       // -------------------------------------------------- products
       const uint32_t idesc = make_idesc_bf16(C::TILE, C::TILE, 1u, 1u);
       constexpr uint32_t STEP = (16 * 128) >> 4;               // 16 tokens further in an MN-major tile
@@ -263,33 +277,37 @@ act8_dweight_kernel(const __grid_constant__ CUtensorMap tmY, const __grid_consta
       const uint32_t a_hi = (uint32_t)(a_proto >> 32), a_lo0 = (uint32_t)a_proto;
       const uint32_t b_hi = (uint32_t)(b_proto >> 32), b_lo0 = (uint32_t)b_proto;
       auto desc = [](uint32_t lo, uint32_t hi) { return (static_cast<uint64_t>(hi) << 32) | lo; };
-      uint32_t it = 0, run = 0;
-      for (int u = worker; u < units && ok; u += workers) {
+      uint32_t s = 0, ph = 0, run = 0;
+      const bool one = elect_one();
+      for (int u = worker; u < units; u += workers) {
         const Unit w = unit_at(u);
-        for (int k0 = w.kb0; k0 < w.kb1 && ok; k0 += C::RUN, ++run) {
+        for (int k0 = w.kb0; k0 < w.kb1; k0 += C::RUN, ++run) {
           const uint32_t acc = run & 1u, aph = (run >> 1) & 1u;
-          if (!mbar_wait(tempty(acc), aph ^ 1u, abort_flag, p.status, 3)) { ok = false; break; }
-          tc_fence_after();
-          const int k1 = k0 + C::RUN < w.kb1 ? k0 + C::RUN : w.kb1;
+          if (!__all_sync(0xffffffffu, mbar_wait(tempty(acc), aph ^ 1u, abort_flag, p.status, 3))) goto fed;
+          const uint32_t d = tmem + acc * C::TILE;
           uint32_t add = 0u;
-          for (int kb = k0; kb < k1; ++kb, ++it) {
-            const uint32_t s = it % C::STAGES, ph = (it / C::STAGES) & 1u;
-            if (!mbar_wait(yfull(s), ph, abort_flag, p.status, 4) ||
-                !mbar_wait(bfull(s), ph, abort_flag, p.status, 5)) { ok = false; break; }
+          for (int n = (w.kb1 - k0 < C::RUN ? w.kb1 - k0 : C::RUN); n > 0; --n) {
+            if (!__all_sync(0xffffffffu, mbar_wait(full(s), ph, abort_flag, p.status, 4))) goto fed;
             tc_fence_after();
-            const uint32_t alo = a_lo0 + s * (C::STAGE_BYTES >> 4), blo = b_lo0 + s * (C::STAGE_BYTES >> 4);
+            const uint32_t at = s * (C::STAGE_BYTES >> 4);
+            if (one) {
 #pragma unroll
-            for (int j = 0; j < C::BK / 16; ++j) {
-              umma_bf16_pair(tmem + acc * C::TILE, desc(alo + j * STEP, a_hi), desc(blo + j * STEP, b_hi), idesc, add);
-              add = 1u;
+              for (int j = 0; j < C::BK / 16; ++j) {
+                umma_bf16_pair(d, desc(a_lo0 + at + j * STEP, a_hi), desc(b_lo0 + at + j * STEP, b_hi), idesc, add);
+                add = 1u;
+              }
+              umma_commit_pair(empty(s));
             }
-            umma_commit_pair(empty(s));
+            add = 1u;
+            s = s + 1 == C::STAGES ? 0u : s + 1;
+            ph ^= s == 0u ? 1u : 0u;
           }
-          if (ok) umma_commit_pair(tfull(acc));
+          if (one) umma_commit_pair(tfull(acc));
         }
       }
     }
-    if ((warp == 0 || warp == 2) && lane == 0 && !ok) {        // aborted: copies in flight get a bounded time to land
+  fed:
+    if (warp != 1 && lane == 0 && !ok) {        // aborted: copies in flight get a bounded time to land
       const uint64_t t0 = globaltimer_ns();
       while (globaltimer_ns() - t0 < 2000000ull) {}
     }
@@ -297,49 +315,57 @@ act8_dweight_kernel(const __grid_constant__ CUtensorMap tmY, const __grid_consta
     regs_dec<C::REGS_CONVERT>();
     // ---------------------------------------------------- codes -> bf16
     // A block is converted by a team of warps, successive blocks by successive teams, so that their waits overlap.
-    // A thread takes eight columns of a token at a time: 16 lanes read 128 consecutive code bytes, eight lanes write
-    // one 128-byte line of the operand tile (chunk c of line t sits at c ^ (t & 7)): no bank conflicts either way.
+    // A thread takes 16 columns of a token at a time: eight lanes read the 128 code bytes of a token and write two
+    // 128-byte lines of the operand tile, one per 64 columns (chunk c of line t sits at c ^ (t & 7)). The lanes of the
+    // second line write their odd chunk first, so that eight lanes always meet all 32 banks once.
     const int team = (warp - 4) / C::CONVERT_TEAM, member = (warp - 4) % C::CONVERT_TEAM;
-    const int c = lane & 15, t_first = member * 2 + (lane >> 4);
-    constexpr int T_STEP = 2 * C::CONVERT_TEAM, ITEMS = C::BK / T_STEP, BATCH = 4;
-    const uint32_t blk = (uint32_t)(c >> 3) * (C::BK * 128);
+    const int q = lane & 7;                                    // columns 16 q .. 16 q + 15
+    constexpr int T_STEP = 4 * C::CONVERT_TEAM, ITEMS = C::RAW_T / T_STEP;
+    static_assert(T_STEP % 8 == 0, "t & 7 is the same for all items of a thread");
+    const int t0 = member * 4 + (lane >> 3);
+    const uint32_t line = (uint32_t)(q >> 2) * (C::BK * 128) + t0 * 128;
+    const int odd = q >> 2;                                    // which of its two chunks a thread writes first
+    const uint32_t dst0 = line + ((((q & 3) * 2 + odd) ^ (t0 & 7)) << 4), dst1 = line + ((((q & 3) * 2 + 1 - odd) ^ (t0 & 7)) << 4);
     uint32_t it = 0;
     for (int u = worker; u < units && ok; u += workers) {
       const Unit w = unit_at(u);
-      const int scale_at = (((w.h0 + (int)rank * 128) / 32) & 15) + (c >> 2);
+      const uint32_t src = raw0 + t0 * 128 + q * 16;
+      const uint32_t src_scale = raw0 + C::CODE_BYTES + t0 * 16 + (((w.h0 + (int)rank * 128) / 32) & 15) + (q >> 1);
       for (int kb = w.kb0; kb < w.kb1; ++kb, ++it) {
         if ((int)(it % C::TEAMS) != team) continue;
         const uint32_t s = it % C::STAGES, ph = (it / C::STAGES) & 1u;
-        const uint32_t r = it % C::RAW, rph = (it / C::RAW) & 1u;
-        bool here = mbar_wait(rfull(r), rph, abort_flag, p.status, 6);
-        here = here && mbar_wait(empty(s), ph ^ 1u, abort_flag, p.status, 7);
-        if (!__all_sync(0xffffffffu, here)) { ok = false; break; }
-        const uint8_t* raw = base_ptr + (raw0 - base) + r * C::RAW_BYTES;
-        const uint32_t tile = base + s * C::STAGE_BYTES + C::A_BYTES + blk;
 #pragma unroll
-        for (int i0 = 0; i0 < ITEMS; i0 += BATCH) {
-          uint2 codes[BATCH];
-          uint32_t bytes[BATCH];
+        for (int half = 0; half < 2; ++half) {
+          const uint32_t r = (2 * it + half) % C::RAW, rph = ((2 * it + half) / C::RAW) & 1u;
+          bool here = mbar_wait(rfull(r), rph, abort_flag, p.status, 6);
+          uint4 codes[ITEMS];
+          uint32_t bytes[ITEMS];
+          const uint32_t from = src + r * C::RAW_BYTES, from_scale = src_scale + r * C::RAW_BYTES;
 #pragma unroll
-          for (int j = 0; j < BATCH; ++j) {
-            const int t = t_first + T_STEP * (i0 + j);
-            codes[j] = *reinterpret_cast<const uint2*>(raw + t * 128 + c * 8);
-            bytes[j] = raw[C::CODE_BYTES + t * 16 + scale_at];
+          for (int j = 0; j < ITEMS; ++j) {
+            codes[j] = ld_shared_v4(from + T_STEP * 128 * j);
+            bytes[j] = ld_shared_u8(from_scale + T_STEP * 16 * j);
           }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(rempty(r));
+          if (half == 0) here = here && mbar_wait(empty(s), ph ^ 1u, abort_flag, p.status, 7);
+          ok = ok && __all_sync(0xffffffffu, here);
+          if (!ok) break;
+          const uint32_t tile = base + s * C::STAGE_BYTES + C::A_BYTES + half * (C::RAW_T * 128);
 #pragma unroll
-          for (int j = 0; j < BATCH; ++j) {
-            const int t = t_first + T_STEP * (i0 + j);
-            uint32_t o[4];
-            codes_to_bf16x8<FMT>(codes[j], bytes[j], o);
-            st_shared_v4(tile + t * 128 + (((c & 7) ^ (t & 7)) << 4), o[0], o[1], o[2], o[3]);
+          for (int j = 0; j < ITEMS; ++j) {
+            const uint4 c = codes[j];
+            uint32_t o[8];
+            codes_to_bf16x16<FMT>(odd ? make_uint4(c.z, c.w, c.x, c.y) : c, bytes[j], o);
+            const uint32_t at = tile + T_STEP * 128 * j;
+            st_shared_v4(at + dst0, o[0], o[1], o[2], o[3]);
+            st_shared_v4(at + dst1, o[4], o[5], o[6], o[7]);
           }
         }
+        if (!ok) break;
         fence_proxy_async_smem();
         __syncwarp();
-        if (lane == 0) {
-          mbar_arrive(rempty(r));
-          mbar_arrive_cluster(map_to_cta(bfull(s), 0u));
-        }
+        if (lane == 0) mbar_arrive_cluster(map_to_cta(full(s), 0u));
       }
     }
   } else {

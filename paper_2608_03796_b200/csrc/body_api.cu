@@ -207,10 +207,10 @@ int kdkl_act8_dweight(const void* dy, int64_t ld_dy, const void* record, size_t 
   const long long ld = T > 1 ? ld_dy : N;
   if ((rc = make_tmap_bf16(&ty, dy, (uint64_t)N, (uint64_t)T, (uint64_t)ld * 2, 64, DwCfg::BK))) return rc;
   if ((rc = make_tmap(&tc, CU_TENSOR_MAP_DATA_TYPE_UINT8, rec.codes, (uint64_t)act_codes_pitch(H), (uint64_t)T,
-                      (uint64_t)act_codes_pitch(H), 128, DwCfg::BK, CU_TENSOR_MAP_SWIZZLE_NONE)))
+                      (uint64_t)act_codes_pitch(H), 128, DwCfg::RAW_T, CU_TENSOR_MAP_SWIZZLE_NONE)))
     return rc;
   if ((rc = make_tmap(&ts, CU_TENSOR_MAP_DATA_TYPE_UINT8, rec.scales, (uint64_t)act_scale_pitch(H), (uint64_t)T,
-                      (uint64_t)act_scale_pitch(H), 16, DwCfg::BK, CU_TENSOR_MAP_SWIZZLE_NONE)))
+                      (uint64_t)act_scale_pitch(H), 16, DwCfg::RAW_T, CU_TENSOR_MAP_SWIZZLE_NONE)))
     return rc;
   if (type == KDKL_TYPE_F32) rc = make_tmap_out_f32(&to, dweight, (uint64_t)H, (uint64_t)N, (uint64_t)H);
   else rc = make_tmap_out_bf16(&to, dweight, (uint64_t)H, (uint64_t)N, (uint64_t)H);

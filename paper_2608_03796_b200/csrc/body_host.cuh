@@ -22,7 +22,7 @@ inline bool words(const void* p, long long ld, long long T, long long H, int typ
   return ((uintptr_t)p & 15) == 0 && (T <= 1 || (ld * type_bytes(type)) % 16 == 0) && H % 8 == 0;
 }
 inline bool shape_ok(long long T, long long H) {
-  return T >= 0 && T < (1ll << 31) && H >= 1 && H < (1ll << 30);
+  return T >= 0 && T <= 0x7fffff00ll && H >= 1 && H < (1ll << 30);
 }
 inline int need_b200(DeviceInfo* di) {
   int rc = device_info(di);
