@@ -38,6 +38,34 @@ __host__ __device__ inline long long act_scales_at(long long T, long long H) {
   return (T * act_codes_pitch(H) + 255) / 256 * 256;
 }
 
+// ------------------------------------------------------------------ two fp32 values an instruction
+__device__ __forceinline__ uint64_t f2_bits(float2 a) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a.x), "f"(a.y));
+  return r;
+}
+__device__ __forceinline__ float2 f2_of(uint64_t r) {
+  float2 a;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(a.x), "=f"(a.y) : "l"(r));
+  return a;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(f2_bits(a)), "l"(f2_bits(b)), "l"(f2_bits(c)));
+  return f2_of(r);
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(f2_bits(a)), "l"(f2_bits(b)));
+  return f2_of(r);
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(f2_bits(a)), "l"(f2_bits(b)));
+  return f2_of(r);
+}
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+
 // ------------------------------------------------------------------ eight values of a row
 // VEC: rows start on 16 bytes and H % 8 == 0, so that eight values are whole 16-byte words. Otherwise element by
 // element, and what lies past the row's end reads as 0 and is not written.
@@ -182,10 +210,12 @@ __device__ __forceinline__ uint2 act_codes(const float (&x)[8], uint32_t byte) {
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     if (FMT == kFmtInt8) {
-      uint32_t v = 0u;
+      // 1.5 * 2^23 + code: rounded to nearest even by the addition, the code in the low byte in two's complement
+      uint32_t v[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v |= (uint32_t)(__float2int_rn(f[4 * k + i] * inv) & 0xff) << (8 * i);
-      w[k] = bad ? 0u : v;
+      for (int i = 0; i < 4; ++i) v[i] = __float_as_uint(fmaf(f[4 * k + i], inv, 12582912.f));
+      const uint32_t c = __byte_perm(__byte_perm(v[0], v[1], 0x0040), __byte_perm(v[2], v[3], 0x0040), 0x5410);
+      w[k] = bad ? 0u : c;
     } else {
       const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(f[4 * k] * inv, f[4 * k + 1] * inv), __NV_SATFINITE, __NV_E4M3);
       const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(f[4 * k + 2] * inv, f[4 * k + 3] * inv), __NV_SATFINITE, __NV_E4M3);
@@ -201,8 +231,14 @@ __device__ __forceinline__ void act_values(const uint2& codes, uint32_t byte, fl
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     if (FMT == kFmtInt8) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) f[4 * k + i] = (float)(int8_t)(w[k] >> (8 * i)) * s;
+      // 2^23 + (code + 128) as bits, minus 2^23 + 128, times 2^e: every step is exact
+      const uint32_t u = w[k] ^ 0x80808080u;
+      const float2 off = make_float2(-8388736.f, -8388736.f), s2 = make_float2(s, s);
+      const float2 a = mul2(add2(make_float2(__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7540)),
+                                             __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7541))), off), s2);
+      const float2 b = mul2(add2(make_float2(__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7542)),
+                                             __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7543))), off), s2);
+      f[4 * k] = a.x; f[4 * k + 1] = a.y; f[4 * k + 2] = b.x; f[4 * k + 3] = b.y;
     } else {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {

@@ -11,15 +11,22 @@ using namespace kdkl;
 
 // ------------------------------------------------------------------ block norm
 static constexpr long long kNormMaxH = 32768;
-// Blocks of the backward kernel, each of which leaves one partial row: two per SM, or one per token.
-static long long norm_parts(long long T) {
-  const long long most = 2 * 148;
+// Threads of the *_rows kernels and how many blocks of them an SM is given: registers for 512 threads.
+static int rows_threads(long long H) {
+  const long long groups = act_codes_pitch(H) / 8;
+  const long long t = (groups + 31) / 32 * 32;
+  return (int)(t > kRowsThreads ? (t / 2 + 31) / 32 * 32 : t);
+}
+// Blocks of the backward kernels, each of which leaves one partial row.
+static long long norm_parts(long long T, long long H) {
+  const int threads = H <= kRowsMaxH ? rows_threads(H) : kRowsThreads;
+  const long long most = (long long)sm_count_or_default() * (kRowsThreads / threads > 8 ? 8 : kRowsThreads / threads);
   return T < most ? T : most;
 }
 
 extern "C" size_t kdkl_block_norm_workspace_bytes(int64_t T, int64_t H) {
   if (!shape_ok(T, H) || H > kNormMaxH) return 0;
-  return up((size_t)norm_parts(T) * 3 * act_codes_pitch(H) * 4, 256) + 256;
+  return up((size_t)norm_parts(T, H) * 3 * act_codes_pitch(H) * 4, 256) + 256;
 }
 
 static int check_norm(const kdkl_block_norm_args* a, bool backward) {
@@ -74,21 +81,29 @@ static int check_norm(const kdkl_block_norm_args* a, bool backward) {
   return KDKL_OK;
 }
 
+// The shared memory a kernel may use beyond 48 KiB (its static part included) is an attribute of its copy on the device:
+// raised when a launch needs more than any before.
+template <auto KERN, typename P>
+static int launch_rows(unsigned grid, int threads, int smem, const P& p, const char* name, const DeviceInfo& di, cudaStream_t st) {
+  static int allowed[kMaxDevices];
+  const bool known = di.dev >= 0 && di.dev < kMaxDevices;
+  if (smem > 40 * 1024 && (!known || smem > allowed[di.dev])) {
+    KDKL_CUDA(cudaFuncSetAttribute(KERN, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    if (known) allowed[di.dev] = smem;
+  }
+  KERN<<<grid, threads, smem, st>>>(p);
+  KDKL_LAUNCHED(name);
+  return KDKL_OK;
+}
+
 static bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
-// Threads a row and groups of eight columns a thread.
-// (rows that are not whole 16-byte words: fewer shapes)
-#define KDKL_NORM_SHAPE(H, vec, VEC, THREADS, NV, ...)                                                     \
-  do {                                                                                                     \
-    const long long nv__ = act_codes_pitch(H) / 8;                                                         \
-    if (!(vec)) {                                                                                          \
-      if (nv__ <= 512) { constexpr bool VEC = false; constexpr int THREADS = 512, NV = 1; __VA_ARGS__; }   \
-      else { constexpr bool VEC = false; constexpr int THREADS = 1024, NV = 4; __VA_ARGS__; }              \
-    } else if (nv__ <= 128) { constexpr bool VEC = true; constexpr int THREADS = 128, NV = 1; __VA_ARGS__; } \
-    else if (nv__ <= 256) { constexpr bool VEC = true; constexpr int THREADS = 256, NV = 1; __VA_ARGS__; } \
-    else if (nv__ <= 512) { constexpr bool VEC = true; constexpr int THREADS = 512, NV = 1; __VA_ARGS__; } \
-    else if (nv__ <= 1024) { constexpr bool VEC = true; constexpr int THREADS = 512, NV = 2; __VA_ARGS__; } \
-    else { constexpr bool VEC = true; constexpr int THREADS = 1024, NV = 4; __VA_ARGS__; }                 \
+// Threads a row and groups of eight columns a thread of the *_any kernels.
+#define KDKL_NORM_SHAPE(H, vec, VEC, THREADS, NV, ...)                                                       \
+  do {                                                                                                       \
+    if ((vec)) { constexpr bool VEC = true; constexpr int THREADS = 1024, NV = 4; __VA_ARGS__; }             \
+    else if ((H) <= 4096) { constexpr bool VEC = false; constexpr int THREADS = 512, NV = 1; __VA_ARGS__; }  \
+    else { constexpr bool VEC = false; constexpr int THREADS = 1024, NV = 4; __VA_ARGS__; }                  \
   } while (0)
 
 extern "C" {
@@ -119,10 +134,20 @@ int kdkl_block_norm_forward(const kdkl_block_norm_args* a, void* cuda_stream) {
   const bool any_record = a->format != KDKL_ACT8_NONE && (a->branch_record || a->sum_record || p.rec_y.codes);
   const long long most = (long long)di.sm_count * 8;
   const unsigned grid = (unsigned)(a->T < most ? a->T : most);
+  if (vec && a->H <= kRowsMaxH) {
+    const int threads = rows_threads(a->H), nv = act_codes_pitch(a->H) / 8 > threads ? 2 : 1;
+    const int smem = rows_stages(nv) * nv * threads * rows_forward_slot(type_bytes(a->residual_type));
+    const long long rows_most = (long long)di.sm_count * (1024 / threads > 16 ? 16 : 1024 / threads);
+    const unsigned rows_grid = (unsigned)(a->T < rows_most ? a->T : rows_most);
+    KDKL_BY_TYPE16(a->type, A, KDKL_BY_BOOL(a->residual_type == KDKL_TYPE_F32, WIDE, KDKL_BY_BOOL(any_record, REC,
+      KDKL_BY_BOOL(nv == 2, TWO,
+        return (launch_rows<block_norm_forward_rows_kernel<A, std::conditional_t<WIDE, float, A>, REC, TWO ? 2 : 1>>(
+            rows_grid, threads, smem, p, "block_norm_forward_rows_kernel", di, st))))));
+  }
   KDKL_BY_TYPE16(a->type, A, KDKL_BY_BOOL(a->residual_type == KDKL_TYPE_F32, WIDE,
     KDKL_BY_BOOL(any_record, REC, KDKL_NORM_SHAPE(a->H, vec, VEC, THREADS, NV,
-      (block_norm_forward_kernel<A, std::conditional_t<WIDE, float, A>, REC, THREADS, NV, VEC><<<grid, THREADS, 0, st>>>(p))))));
-  KDKL_LAUNCHED("block_norm_forward_kernel");
+      (block_norm_forward_any_kernel<A, std::conditional_t<WIDE, float, A>, REC, THREADS, NV, VEC><<<grid, THREADS, 0, st>>>(p))))));
+  KDKL_LAUNCHED("block_norm_forward_any_kernel");
   return KDKL_OK;
 }
 
@@ -135,7 +160,7 @@ int kdkl_block_norm_backward(const kdkl_block_norm_args* a, void* cuda_stream) {
   cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
   const bool has_post = a->post_weight != nullptr, has_pre = a->pre_weight != nullptr;
   const bool channel = a->gate_kind == KDKL_GATE_CHANNEL;
-  const long long parts = norm_parts(a->T);
+  const long long parts = norm_parts(a->T, a->H);
   if (a->T > 0) {
     NormBackward p;
     p.dsum = a->dsum; p.ld_dsum = a->ld_dsum; p.dy = a->dy; p.ld_dy = a->ld_dy;
@@ -155,10 +180,21 @@ int kdkl_block_norm_backward(const kdkl_block_norm_args* a, void* cuda_stream) {
                      (!a->dsum || words(a->dsum, a->ld_dsum, a->T, a->H, a->residual_type)) && aligned16(a->dresidual) &&
                      aligned16(a->dbranch) && aligned16(a->post_weight) && aligned16(a->pre_weight) &&
                      (!channel || aligned16(a->gate));
-    KDKL_BY_TYPE16(a->type, A, KDKL_BY_BOOL(a->residual_type == KDKL_TYPE_F32, WIDE,
-      KDKL_BY_BOOL(a->format != KDKL_ACT8_NONE, REC, KDKL_NORM_SHAPE(a->H, vec, VEC, THREADS, NV,
-        (block_norm_backward_kernel<A, std::conditional_t<WIDE, float, A>, REC, THREADS, NV, VEC><<<(unsigned)parts, THREADS, 0, st>>>(p))))));
-    KDKL_LAUNCHED("block_norm_backward_kernel");
+    if (vec && a->H <= kRowsMaxH) {
+      const bool rec = a->format != KDKL_ACT8_NONE;
+      const int threads = rows_threads(a->H), nv = act_codes_pitch(a->H) / 8 > threads ? 2 : 1;
+      const int smem = rows_stages(nv) * nv * threads * rows_backward_slot(type_bytes(a->residual_type), rec);
+      KDKL_BY_TYPE16(a->type, A, KDKL_BY_BOOL(a->residual_type == KDKL_TYPE_F32, WIDE, KDKL_BY_BOOL(rec, REC,
+        KDKL_BY_BOOL(nv == 2, TWO,
+          rc = (launch_rows<block_norm_backward_rows_kernel<A, std::conditional_t<WIDE, float, A>, REC, TWO ? 2 : 1>>(
+              (unsigned)parts, threads, smem, p, "block_norm_backward_rows_kernel", di, st))))));
+      if (rc) return rc;
+    } else {
+      KDKL_BY_TYPE16(a->type, A, KDKL_BY_BOOL(a->residual_type == KDKL_TYPE_F32, WIDE,
+        KDKL_BY_BOOL(a->format != KDKL_ACT8_NONE, REC, KDKL_NORM_SHAPE(a->H, vec, VEC, THREADS, NV,
+          (block_norm_backward_any_kernel<A, std::conditional_t<WIDE, float, A>, REC, THREADS, NV, VEC><<<(unsigned)parts, THREADS, 0, st>>>(p))))));
+      KDKL_LAUNCHED("block_norm_backward_any_kernel");
+    }
   }
   if (has_post || has_pre || channel) {
     NormColumns c;
