@@ -180,11 +180,16 @@ __device__ __forceinline__ float act_scale(uint32_t byte) {          // 2^e, NaN
 __device__ __forceinline__ float act_inverse(uint32_t byte) {        // 2^-e; 0 for byte 255 (codes 0)
   return byte == 255u ? 0.f : __uint_as_float((254u - byte) << 23);
 }
+// the largest |x| of eight as fp32 bits; NaN where there is one
+__device__ __forceinline__ float max3_abs(float a, float b, float c) {
+  float r;
+  asm("{\n\t.reg .f32 x, y, z;\n\tabs.f32 x, %1;\n\tabs.f32 y, %2;\n\tabs.f32 z, %3;\n\tmax.NaN.f32 %0, x, y, z;\n\t}"
+      : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
 __device__ __forceinline__ uint32_t abs_max_bits(const float (&f)[8]) {
-  uint32_t m = 0u;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(f[i]) & 0x7fffffffu);
-  return m;
+  const float m = max3_abs(max3_abs(f[0], f[1], f[2]), f[3], f[4]);
+  return __float_as_uint(max3_abs(max3_abs(m, f[5], f[6]), f[7], f[7]));
 }
 // the largest of the four neighbouring lanes that share a group (all four take part)
 __device__ __forceinline__ uint32_t group_max(uint32_t m) {
@@ -211,10 +216,11 @@ __device__ __forceinline__ uint2 act_codes(const float (&x)[8], uint32_t byte) {
   for (int k = 0; k < 2; ++k) {
     if (FMT == kFmtInt8) {
       // 1.5 * 2^23 + code: rounded to nearest even by the addition, the code in the low byte in two's complement
-      uint32_t v[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = __float_as_uint(fmaf(f[4 * k + i], inv, 12582912.f));
-      const uint32_t c = __byte_perm(__byte_perm(v[0], v[1], 0x0040), __byte_perm(v[2], v[3], 0x0040), 0x5410);
+      const float2 magic = both(12582912.f);
+      const float2 u = fma2(make_float2(f[4 * k], f[4 * k + 1]), both(inv), magic);
+      const float2 v = fma2(make_float2(f[4 * k + 2], f[4 * k + 3]), both(inv), magic);
+      const uint32_t c = __byte_perm(__byte_perm(__float_as_uint(u.x), __float_as_uint(u.y), 0x0040),
+                                     __byte_perm(__float_as_uint(v.x), __float_as_uint(v.y), 0x0040), 0x5410);
       w[k] = bad ? 0u : c;
     } else {
       const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(f[4 * k] * inv, f[4 * k + 1] * inv), __NV_SATFINITE, __NV_E4M3);

@@ -93,10 +93,11 @@ __device__ __forceinline__ void block_sums_any(float (&x)[N], float* sm) {
   __syncthreads();
 #pragma unroll
   for (int k = 0; k < N; ++k) {
-    float s = lane < warps ? sm[k * 32 + lane] : 0.f;        // at most 16 warps: the upper half of the lanes adds zeros
+    float s = (lane & 15) < warps ? sm[k * 32 + (lane & 15)] : 0.f;    // at most 16 warps
+    if (warps > 8) s += __shfl_xor_sync(0xffffffffu, s, 8);
 #pragma unroll
-    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    x[k] = s;
+    for (int o = 4; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    x[k] = __shfl_sync(0xffffffffu, s, 0);
   }
 }
 
@@ -341,9 +342,9 @@ block_norm_backward_any_kernel(const NormBackward p) {
 }
 
 // ------------------------------------------------------------------ rows of whole 16-byte words
-constexpr int kRowsThreads = 512, kRowsMaxH = 8192;
-// rows in shared memory or on their way there; two where a thread has twice the columns
-__host__ __device__ constexpr int rows_stages(int nv) { return nv == 1 ? 3 : 2; }
+// A thread has two groups of eight columns: that halves what a row costs per value in sums, factors and addresses
+// (with one group a thread both kernels were bound by instructions, 63 and 54 a value).
+constexpr int kRowsThreads = 512, kRowsMaxH = 2 * 8 * kRowsThreads;
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool live) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
@@ -354,14 +355,11 @@ __device__ __forceinline__ void cp_async8(uint32_t dst, const void* src, bool li
 __device__ __forceinline__ void cp_async4(uint32_t dst, const void* src, bool live) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(live ? 4 : 0) : "memory");
 }
-__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
 // Eight values as pairs.
 struct V8 { float2 p[4]; };
-template <typename T> __device__ __forceinline__ V8 v8_from(const Raw8<T>& r) {
-  float f[8];
-  raw_to_f32(r, f);
+__device__ __forceinline__ V8 v8_of(const float (&f)[8]) {
   V8 v;
 #pragma unroll
   for (int i = 0; i < 4; ++i) v.p[i] = make_float2(f[2 * i], f[2 * i + 1]);
@@ -379,10 +377,7 @@ template <typename T> __device__ __forceinline__ Raw8<T> v8_raw(const V8& v) {
 __device__ __forceinline__ V8 v8_any(const AnyVec& a, int c, int H) {
   float f[8];
   any_load8<true>(a, c, H, f);
-  V8 v;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) v.p[i] = make_float2(f[2 * i], f[2 * i + 1]);
-  return v;
+  return v8_of(f);
 }
 __device__ __forceinline__ V8 v8_all(float x) {
   V8 v;
@@ -390,156 +385,150 @@ __device__ __forceinline__ V8 v8_all(float x) {
   for (int i = 0; i < 4; ++i) v.p[i] = both(x);
   return v;
 }
-__device__ __forceinline__ V8 v8_codes(int fmt, const uint2& c, uint32_t byte) {
-  float f[8];
-  if (fmt == kFmtInt8) act_values<kFmtInt8>(c, byte, f);
-  else act_values<kFmtE4M3>(c, byte, f);
-  V8 v;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) v.p[i] = make_float2(f[2 * i], f[2 * i + 1]);
-  return v;
-}
 __device__ __forceinline__ float sum2(float2 a) { return a.x + a.y; }
+__device__ __forceinline__ void v8_write_record(int fmt, const ActRecord& r, long long t, long long cpitch, long long spitch,
+                                                int c, const V8& v) {
+  float f[8];
+  v8_to(v, f);
+  record_write8(fmt, r, t, cpitch, spitch, c, f, c < cpitch);
+}
 
-// One thread's slots for a tensor: `width` bytes for each of its NV groups of eight columns, in each of the stages.
-// Slots of neighbouring threads are neighbours.
-struct Slots {
-  uint32_t at;
-  int width;
-  __device__ __forceinline__ uint32_t of(int stage, int i, int nv) const {
-    return at + (uint32_t)(((stage * nv + i) * (int)blockDim.x + (int)threadIdx.x) * width);
-  }
+// What the next row brings waits in shared memory, in places that only their own thread touches: per group of eight
+// columns and warp one chunk of 32 lanes' places, field after field, so that every address is one of three lane offsets
+// plus a constant.
+struct Places {
+  uint32_t l16, l8, l4;
+  __device__ __forceinline__ Places(uint32_t chunk, int lane) : l16(chunk + lane * 16), l8(chunk + lane * 8), l4(chunk + lane * 4) {}
 };
-template <typename T> __device__ __forceinline__ void fetch8(uint32_t slot, const T* row, int c, int H) {
-  const bool live = c < H;
-  const T* src = row + (live ? c : 0);
-  cp_async16(slot, src, live);
-  if constexpr (sizeof(T) == 4) cp_async16(slot + 16, src + 4, live);
+// A row's values [c, c + 8) of 2 or 4 bytes; 4-byte values take two places 512 bytes apart.
+template <typename T, int AT> __device__ __forceinline__ void fetch8(const Places& s, const T* row, int c, bool live) {
+  const T* src = row + (uint32_t)(live ? c : 0);
+  cp_async16(s.l16 + AT, src, live);
+  if constexpr (sizeof(T) == 4) cp_async16(s.l16 + AT + 512, src + 4, live);
 }
-template <typename T> __device__ __forceinline__ V8 take8(uint32_t slot) {
+template <typename T, int AT> __device__ __forceinline__ V8 take8(const Places& s) {
   Raw8<T> r;
-  r.v = ld_shared_v4(slot);
-  if constexpr (sizeof(T) == 4) r.w = ld_shared_v4(slot + 16);
-  return v8_from<T>(r);
+  r.v = ld_shared_v4(s.l16 + AT);
+  if constexpr (sizeof(T) == 4) r.w = ld_shared_v4(s.l16 + AT + 512);
+  float f[8];
+  raw_to_f32(r, f);
+  return v8_of(f);
 }
-// codes (8 bytes) and the word that holds the group's scale byte
-__device__ __forceinline__ void fetch_record8(uint32_t codes_slot, uint32_t scale_slot, const ActRecord& r, long long t,
-                                              long long cpitch, long long spitch, int c) {
-  const bool live = c < cpitch;
-  const int k = live ? c : 0;
-  cp_async8(codes_slot, r.codes + t * cpitch + k, live);
-  cp_async4(scale_slot, r.scales + t * spitch + ((k >> 5) & ~3), live);
+// Eight codes and, 256 bytes on, the word that holds the group's scale byte.
+template <int AT> __device__ __forceinline__ void fetch_record8(const Places& s, const uint8_t* codes, const uint8_t* scales,
+                                                                int c, bool live) {
+  const uint32_t k = live ? c : 0;
+  cp_async8(s.l8 + AT, codes + k, live);
+  cp_async4(s.l4 + AT + 256, scales + ((k >> 5) & ~3u), live);
 }
-__device__ __forceinline__ V8 take_record8(uint32_t codes_slot, uint32_t scale_slot, int fmt, int c) {
-  const uint32_t word = ld_shared_u32(scale_slot);
-  return v8_codes(fmt, ld_shared_v2(codes_slot), (word >> (((c >> 5) & 3) * 8)) & 0xffu);
+template <int AT> __device__ __forceinline__ V8 take_record8(const Places& s, int fmt, int shift) {
+  const uint32_t byte = (ld_shared_u32(s.l4 + AT + 256) >> shift) & 0xffu;
+  const uint2 codes = ld_shared_v2(s.l8 + AT);
+  float f[8];
+  if (fmt == kFmtInt8) act_values<kFmtInt8>(codes, byte, f);
+  else act_values<kFmtE4M3>(codes, byte, f);
+  return v8_of(f);
+}
+// Bytes of a chunk: fields for 32 lanes.
+__host__ __device__ constexpr int rows_forward_chunk(int residual_bytes) { return 512 + 256 * residual_bytes; }
+__host__ __device__ constexpr int rows_backward_chunk(int residual_bytes, bool rec) {
+  return 256 * residual_bytes + 512 + (rec ? 2 * 384 : 512 + 256 * residual_bytes);
 }
 
-// Bytes of one thread's slots in one stage, per group of eight columns.
-__host__ __device__ constexpr int rows_forward_slot(int residual_bytes) { return 16 + 8 * residual_bytes; }
-__host__ __device__ constexpr int rows_backward_slot(int residual_bytes, bool rec) {
-  return 8 * residual_bytes + 16 + (rec ? 24 : 16 + 8 * residual_bytes);
-}
-
-template <typename A, typename R, bool REC, int NV>
+template <typename A, typename R, bool REC>
 __global__ void __launch_bounds__(kRowsThreads)
 block_norm_forward_rows_kernel(const NormForward p) {
-  constexpr int S = rows_stages(NV);
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ float sm[4][32];
-  const int H = p.H, threads = blockDim.x;
-  const uint32_t smem0 = smem_u32(smem);
-  const Slots sb = {smem0, 16}, sr = {smem0 + (uint32_t)(S * NV * threads * 16), 8 * (int)sizeof(R)};
+  constexpr int kResidual = 512;        // field offsets: branch, residual
+  const int H = p.H, threads = blockDim.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const long long cpitch = act_codes_pitch(H), spitch = act_scale_pitch(H);
   const float inv_h = 1.f / (float)H;
-  const bool has_post = p.post.p != nullptr, has_pre = p.pre.p != nullptr;
-  V8 k[NV], w2[NV];                     // alpha (w1 + o) gate_c;  w2 + o
+  const bool has_post = p.post.p != nullptr, has_pre = p.pre.p != nullptr, token = p.gate_kind == kGateToken;
+  const int c[2] = {(int)threadIdx.x * 8, (int)(threadIdx.x + threads) * 8};
+  const uint32_t chunk = smem_u32(smem) + warp * rows_forward_chunk(sizeof(R));
+  const Places at[2] = {Places(chunk, lane), Places(chunk + (threads >> 5) * rows_forward_chunk(sizeof(R)), lane)};
+  auto fetch = [&](long long t) {
+    const A* b = reinterpret_cast<const A*>(p.branch) + t * p.ld_branch;
+    const R* r = reinterpret_cast<const R*>(p.residual) + t * p.ld_residual;
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int c = (threadIdx.x + i * threads) * 8;
+    for (int i = 0; i < 2; ++i) {
+      fetch8<A, 0>(at[i], b, c[i], c[i] < H);
+      fetch8<R, kResidual>(at[i], r, c[i], c[i] < H);
+    }
+  };
+  fetch(blockIdx.x);
+  V8 k[2], w2[2];                       // alpha (w1 + o) gate_c;  w2 + o
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
     k[i] = w2[i] = v8_all(0.f);
-    if (c >= H) continue;
+    if (c[i] >= H) continue;
     k[i] = v8_all(p.alpha);
     if (has_post) {
-      const V8 w = v8_any(p.post, c, H);
+      const V8 w = v8_any(p.post, c[i], H);
 #pragma unroll
       for (int j = 0; j < 4; ++j) k[i].p[j] = mul2(k[i].p[j], add2(w.p[j], both(p.offset)));
     }
     if (p.gate_kind == kGateChannel) {
-      const V8 g = v8_any(p.gate, c, H);
+      const V8 g = v8_any(p.gate, c[i], H);
 #pragma unroll
       for (int j = 0; j < 4; ++j) k[i].p[j] = mul2(k[i].p[j], g.p[j]);
     }
     if (has_pre) {
-      const V8 w = v8_any(p.pre, c, H);
+      const V8 w = v8_any(p.pre, c[i], H);
 #pragma unroll
       for (int j = 0; j < 4; ++j) w2[i].p[j] = add2(w.p[j], both(p.offset));
     }
   }
-  auto fetch = [&](long long t, int stage) {
-    if (t < p.T) {
-#pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        const int c = (threadIdx.x + i * threads) * 8;
-        fetch8<A>(sb.of(stage, i, NV), reinterpret_cast<const A*>(p.branch) + t * p.ld_branch, c, H);
-        fetch8<R>(sr.of(stage, i, NV), reinterpret_cast<const R*>(p.residual) + t * p.ld_residual, c, H);
-      }
-    }
-    cp_async_commit();
-  };
-#pragma unroll
-  for (int q = 0; q < S - 1; ++q) fetch(blockIdx.x + (long long)q * gridDim.x, q);
-  int stage = 0, parity = 0;
+  int parity = 0;
+  float gate_next = token ? any_at(p.gate, blockIdx.x) : 1.f;
   for (long long t = blockIdx.x; t < p.T; t += gridDim.x, parity ^= 2) {
-    cp_async_wait<S - 2>();
-    V8 b[NV], x[NV];
+    const float gate_t = gate_next;
+    cp_async_wait_all();
+    V8 b[2], x[2];
     float2 acc = both(0.f);
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      b[i] = take8<A>(sb.of(stage, i, NV));
-      x[i] = take8<R>(sr.of(stage, i, NV));
+    for (int i = 0; i < 2; ++i) {
+      b[i] = take8<A, 0>(at[i]);
+      x[i] = take8<R, kResidual>(at[i]);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) acc = fma2(b[i].p[j], b[i].p[j], acc);
+      for (int j = 0; j < 4; ++j) { acc = fma2(b[i].p[j], b[i].p[j], acc); x[i].p[j] = mul2(x[i].p[j], both(p.beta)); }
     }
-    fetch(t + (long long)(S - 1) * gridDim.x, stage == 0 ? S - 1 : stage - 1);
-    stage = stage + 1 == S ? 0 : stage + 1;
+    if (t + gridDim.x < p.T) {          // the row is in registers: its places take the next one
+      fetch(t + gridDim.x);
+      if (token) gate_next = any_at(p.gate, t + gridDim.x);
+    }
     if constexpr (REC) {
       if (p.rec_branch.codes != nullptr) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-          const int c = (threadIdx.x + i * threads) * 8;
-          float f[8];
-          v8_to(b[i], f);
-          record_write8(p.format, p.rec_branch, t, cpitch, spitch, c, f, c < cpitch);
-        }
+        for (int i = 0; i < 2; ++i) v8_write_record(p.format, p.rec_branch, t, cpitch, spitch, c[i], b[i]);
       }
     }
     float rho1 = 1.f;
     if (has_post) {
       float s[1] = {sum2(acc)};
       block_sums_any<1>(s, sm[parity]);
-      rho1 = 1.f / sqrtf(fmaf(s[0], inv_h, p.eps));
+      rho1 = rsqrtf(fmaf(s[0], inv_h, p.eps));
     }
-    float scale = rho1;
-    if (p.gate_kind == kGateToken) scale *= any_at(p.gate, t);
+    const float2 scale = both(rho1 * gate_t);
     acc = both(0.f);
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        x[i].p[j] = fma2(mul2(k[i].p[j], both(scale)), b[i].p[j], mul2(x[i].p[j], both(p.beta)));
+        x[i].p[j] = fma2(mul2(k[i].p[j], scale), b[i].p[j], x[i].p[j]);
         acc = fma2(x[i].p[j], x[i].p[j], acc);
       }
+    R* sum_row = reinterpret_cast<R*>(p.sum) + t * H;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = (threadIdx.x + i * threads) * 8;
+    for (int i = 0; i < 2; ++i) {
       const Raw8<R> raw = v8_raw<R>(x[i]);
-      store_raw8<R, true>(reinterpret_cast<R*>(p.sum) + t * H, c, H, raw);
+      store_raw8<R, true>(sum_row, c[i], H, raw);
       if constexpr (REC) {
         if (p.rec_sum.codes != nullptr) {              // what a record of the returned sum would hold
           float f[8];
           raw_to_f32(raw, f);
-          record_write8(p.format, p.rec_sum, t, cpitch, spitch, c, f, c < cpitch);
+          record_write8(p.format, p.rec_sum, t, cpitch, spitch, c[i], f, c[i] < cpitch);
         }
       }
     }
@@ -547,19 +536,19 @@ block_norm_forward_rows_kernel(const NormForward p) {
     if (has_pre) {
       float s[1] = {sum2(acc)};
       block_sums_any<1>(s, sm[parity + 1]);
-      rho2 = 1.f / sqrtf(fmaf(s[0], inv_h, p.eps));
+      rho2 = rsqrtf(fmaf(s[0], inv_h, p.eps));
+      A* y_row = reinterpret_cast<A*>(p.y) + t * H;
 #pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        const int c = (threadIdx.x + i * threads) * 8;
+      for (int i = 0; i < 2; ++i) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) x[i].p[j] = mul2(x[i].p[j], mul2(w2[i].p[j], both(rho2)));
         const Raw8<A> raw = v8_raw<A>(x[i]);
-        store_raw8<A, true>(reinterpret_cast<A*>(p.y) + t * H, c, H, raw);
+        store_raw8<A, true>(y_row, c[i], H, raw);
         if constexpr (REC) {
           if (p.rec_y.codes != nullptr) {
             float f[8];
             raw_to_f32(raw, f);
-            record_write8(p.format, p.rec_y, t, cpitch, spitch, c, f, c < cpitch);
+            record_write8(p.format, p.rec_y, t, cpitch, spitch, c[i], f, c[i] < cpitch);
           }
         }
       }
@@ -569,7 +558,6 @@ block_norm_forward_rows_kernel(const NormForward p) {
       if (p.rho_pre != nullptr) p.rho_pre[t] = rho2;
     }
   }
-  cp_async_wait<0>();
 }
 
 // With Q = gate_c (w1 + o), sigma = alpha rho1 gate_t, u = dy rho2 and x, b as kept (not normalised):
@@ -577,81 +565,79 @@ block_norm_forward_rows_kernel(const NormForward p) {
 //   A = sum_t sigma d b     (per column; dw1 = gate_c A, dgate_c = (w1 + o) A),   dw2 = sum_t u x
 //   db = sigma Q d - rho1^2 c1 b
 // so a column needs one sum for the gate and the post weight together.
-template <typename A, typename R, bool REC, int NV>
+template <typename A, typename R, bool REC>
 __global__ void __launch_bounds__(kRowsThreads)
 block_norm_backward_rows_kernel(const NormBackward p) {
-  constexpr int S = rows_stages(NV);
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ float sm[2][3 * 32];
-  const int H = p.H, threads = blockDim.x;
-  const uint32_t smem0 = smem_u32(smem), per = (uint32_t)(S * NV * threads);
-  constexpr int RB = 8 * (int)sizeof(R);
-  const Slots s_dx = {smem0, RB}, s_dy = {smem0 + per * RB, 16}, s_b = {smem0 + per * (RB + 16), REC ? 8 : 16},
-              s_x = {smem0 + per * (RB + 16 + (REC ? 8 : 16)), REC ? 8 : RB},
-              s_bs = {smem0 + per * (RB + 32), 4}, s_xs = {smem0 + per * (RB + 36), 4};   // (scales: with records)
+  constexpr int kRB = 256 * (int)sizeof(R), kDy = kRB, kBranch = kRB + 512, kSum = kBranch + (REC ? 384 : 512);
+  const int H = p.H, threads = blockDim.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const long long cpitch = act_codes_pitch(H), spitch = act_scale_pitch(H);
   const float inv_h = 1.f / (float)H;
   const bool has_post = p.post.p != nullptr, has_pre = p.pre.p != nullptr, token = p.gate_kind == kGateToken;
-  V8 q[NV], w2[NV], sum_a[NV], sum_w[NV];
+  const bool has_dx = p.dsum != nullptr;
+  const int c[2] = {(int)threadIdx.x * 8, (int)(threadIdx.x + threads) * 8};
+  constexpr int kChunk = rows_backward_chunk(sizeof(R), REC);
+  const uint32_t chunk = smem_u32(smem) + warp * kChunk;
+  const Places at[2] = {Places(chunk, lane), Places(chunk + (threads >> 5) * kChunk, lane)};
+  float rho1_next = 1.f, rho2_next = 1.f, gate_next = 1.f;
+  auto fetch = [&](long long t) {
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int c = (threadIdx.x + i * threads) * 8;
+    for (int i = 0; i < 2; ++i) {
+      const bool live = c[i] < H;
+      if (has_dx) fetch8<R, 0>(at[i], reinterpret_cast<const R*>(p.dsum) + t * p.ld_dsum, c[i], live);
+      if (has_pre) fetch8<A, kDy>(at[i], reinterpret_cast<const A*>(p.dy) + t * p.ld_dy, c[i], live);
+      if constexpr (REC) {
+        fetch_record8<kBranch>(at[i], p.rec_branch.codes + t * cpitch, p.rec_branch.scales + t * spitch, c[i], live);
+        if (has_pre) fetch_record8<kSum>(at[i], p.rec_sum.codes + t * cpitch, p.rec_sum.scales + t * spitch, c[i], live);
+      } else {
+        fetch8<A, kBranch>(at[i], reinterpret_cast<const A*>(p.branch) + t * p.ld_branch, c[i], live);
+        if (has_pre) fetch8<R, kSum>(at[i], reinterpret_cast<const R*>(p.sum) + t * p.ld_sum, c[i], live);
+      }
+    }
+    if (has_post) rho1_next = p.rho_post[t];
+    if (has_pre) rho2_next = p.rho_pre[t];
+    if (token) gate_next = any_at(p.gate, t);
+  };
+  if (blockIdx.x < p.T) fetch(blockIdx.x);
+  V8 q[2], w2[2], sum_a[2], sum_w[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
     q[i] = w2[i] = sum_a[i] = sum_w[i] = v8_all(0.f);
-    if (c >= H) continue;
+    if (c[i] >= H) continue;
     q[i] = v8_all(1.f);
     if (has_post) {
-      const V8 w = v8_any(p.post, c, H);
+      const V8 w = v8_any(p.post, c[i], H);
 #pragma unroll
       for (int j = 0; j < 4; ++j) q[i].p[j] = add2(w.p[j], both(p.offset));
     }
     if (p.gate_kind == kGateChannel) {
-      const V8 g = v8_any(p.gate, c, H);
+      const V8 g = v8_any(p.gate, c[i], H);
 #pragma unroll
       for (int j = 0; j < 4; ++j) q[i].p[j] = mul2(q[i].p[j], g.p[j]);
     }
     if (has_pre) {
-      const V8 w = v8_any(p.pre, c, H);
+      const V8 w = v8_any(p.pre, c[i], H);
 #pragma unroll
       for (int j = 0; j < 4; ++j) w2[i].p[j] = add2(w.p[j], both(p.offset));
     }
   }
-  auto fetch = [&](long long t, int stage) {
-    if (t < p.T) {
-#pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        const int c = (threadIdx.x + i * threads) * 8;
-        if (p.dsum != nullptr) fetch8<R>(s_dx.of(stage, i, NV), reinterpret_cast<const R*>(p.dsum) + t * p.ld_dsum, c, H);
-        if (has_pre) fetch8<A>(s_dy.of(stage, i, NV), reinterpret_cast<const A*>(p.dy) + t * p.ld_dy, c, H);
-        if constexpr (REC) {
-          fetch_record8(s_b.of(stage, i, NV), s_bs.of(stage, i, NV), p.rec_branch, t, cpitch, spitch, c);
-          if (has_pre) fetch_record8(s_x.of(stage, i, NV), s_xs.of(stage, i, NV), p.rec_sum, t, cpitch, spitch, c);
-        } else {
-          fetch8<A>(s_b.of(stage, i, NV), reinterpret_cast<const A*>(p.branch) + t * p.ld_branch, c, H);
-          if (has_pre) fetch8<R>(s_x.of(stage, i, NV), reinterpret_cast<const R*>(p.sum) + t * p.ld_sum, c, H);
-        }
-      }
-    }
-    cp_async_commit();
-  };
-#pragma unroll
-  for (int k = 0; k < S - 1; ++k) fetch(blockIdx.x + (long long)k * gridDim.x, k);
-  int stage = 0, parity = 0;
+  const int shift0 = ((c[0] >> 5) & 3) * 8, shift1 = ((c[1] >> 5) & 3) * 8;
+  int parity = 0;
   for (long long t = blockIdx.x; t < p.T; t += gridDim.x, parity ^= 1) {
-    const float rho1 = has_post ? p.rho_post[t] : 1.f, rho2 = has_pre ? p.rho_pre[t] : 1.f;
-    const float gate_t = token ? any_at(p.gate, t) : 1.f;
-    cp_async_wait<S - 2>();
-    V8 e[NV], x[NV], b[NV];
+    const float rho1 = rho1_next, rho2 = rho2_next, gate_t = gate_next;
+    cp_async_wait_all();
+    V8 e[2], x[2], b[2];
     float2 a0 = both(0.f), a1 = both(0.f), a2 = both(0.f);   // u x w2';  Q b e;  Q b x
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = (threadIdx.x + i * threads) * 8;
-      e[i] = p.dsum != nullptr ? take8<R>(s_dx.of(stage, i, NV)) : v8_all(0.f);
-      if constexpr (REC) b[i] = take_record8(s_b.of(stage, i, NV), s_bs.of(stage, i, NV), p.format, c);
-      else b[i] = take8<A>(s_b.of(stage, i, NV));
+    for (int i = 0; i < 2; ++i) {
+      e[i] = has_dx ? take8<R, 0>(at[i]) : v8_all(0.f);
+      if constexpr (REC) b[i] = take_record8<kBranch>(at[i], p.format, i == 0 ? shift0 : shift1);
+      else b[i] = take8<A, kBranch>(at[i]);
       if (has_pre) {
-        if constexpr (REC) x[i] = take_record8(s_x.of(stage, i, NV), s_xs.of(stage, i, NV), p.format, c);
-        else x[i] = take8<R>(s_x.of(stage, i, NV));
-        const V8 dy = take8<A>(s_dy.of(stage, i, NV));
+        if constexpr (REC) x[i] = take_record8<kSum>(at[i], p.format, i == 0 ? shift0 : shift1);
+        else x[i] = take8<R, kSum>(at[i]);
+        const V8 dy = take8<A, kDy>(at[i]);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const float2 u = mul2(dy.p[j], both(rho2)), ux = mul2(u, x[i].p[j]);
@@ -669,8 +655,7 @@ block_norm_backward_rows_kernel(const NormBackward p) {
         a2 = fma2(qb, x[i].p[j], a2);
       }
     }
-    fetch(t + (long long)(S - 1) * gridDim.x, stage == 0 ? S - 1 : stage - 1);
-    stage = stage + 1 == S ? 0 : stage + 1;
+    if (t + gridDim.x < p.T) fetch(t + gridDim.x);           // the row is in registers: its places take the next one
     float s[3] = {sum2(a0), sum2(a1), sum2(a2)};
     block_sums_any<3>(s, sm[parity]);
     const float k2 = rho2 * rho2 * s[0] * inv_h;             // d = e - k2 x
@@ -678,44 +663,43 @@ block_norm_backward_rows_kernel(const NormBackward p) {
     if (token && threadIdx.x == 0) any_store(p.dgate_token, p.gate_type, t, dot);
     const float sigma = p.alpha * rho1 * gate_t;
     const float tau = has_post ? -rho1 * rho1 * dot * gate_t * inv_h : 0.f;
+    R* dr_row = reinterpret_cast<R*>(p.dresidual) + t * H;
+    A* db_row = reinterpret_cast<A*>(p.dbranch) + t * H;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = (threadIdx.x + i * threads) * 8;
+    for (int i = 0; i < 2; ++i) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const float2 d = fma2(x[i].p[j], both(-k2), e[i].p[j]);
-        sum_a[i].p[j] = fma2(d, mul2(b[i].p[j], both(sigma)), sum_a[i].p[j]);
+        const float2 d = fma2(x[i].p[j], both(-k2), e[i].p[j]), sd = mul2(d, both(sigma));
+        sum_a[i].p[j] = fma2(sd, b[i].p[j], sum_a[i].p[j]);
         e[i].p[j] = mul2(d, both(p.beta));
-        b[i].p[j] = fma2(mul2(q[i].p[j], both(sigma)), d, mul2(b[i].p[j], both(tau)));
+        b[i].p[j] = fma2(q[i].p[j], sd, mul2(b[i].p[j], both(tau)));
       }
-      store_raw8<R, true>(reinterpret_cast<R*>(p.dresidual) + t * H, c, H, v8_raw<R>(e[i]));
-      store_raw8<A, true>(reinterpret_cast<A*>(p.dbranch) + t * H, c, H, v8_raw<A>(b[i]));
+      store_raw8<R, true>(dr_row, c[i], H, v8_raw<R>(e[i]));
+      store_raw8<A, true>(db_row, c[i], H, v8_raw<A>(b[i]));
     }
   }
-  cp_async_wait<0>();
   float* out = p.partial + (long long)blockIdx.x * 3 * cpitch;
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int c = (threadIdx.x + i * threads) * 8;
-    if (c >= H) continue;
-    if (has_pre) store_raw8<float, true>(out + cpitch, c, (int)cpitch, v8_raw<float>(sum_w[i]));
+  for (int i = 0; i < 2; ++i) {
+    if (c[i] >= H) continue;
+    if (has_pre) store_raw8<float, true>(out + cpitch, c[i], (int)cpitch, v8_raw<float>(sum_w[i]));
     if (has_post) {
       V8 v = sum_a[i];
       if (p.gate_kind == kGateChannel) {
-        const V8 g = v8_any(p.gate, c, H);
+        const V8 g = v8_any(p.gate, c[i], H);
 #pragma unroll
         for (int j = 0; j < 4; ++j) v.p[j] = mul2(v.p[j], g.p[j]);
       }
-      store_raw8<float, true>(out, c, (int)cpitch, v8_raw<float>(v));
+      store_raw8<float, true>(out, c[i], (int)cpitch, v8_raw<float>(v));
     }
     if (p.gate_kind == kGateChannel) {
       V8 v = sum_a[i];
       if (has_post) {
-        const V8 w = v8_any(p.post, c, H);
+        const V8 w = v8_any(p.post, c[i], H);
 #pragma unroll
         for (int j = 0; j < 4; ++j) v.p[j] = mul2(v.p[j], add2(w.p[j], both(p.offset)));
       }
-      store_raw8<float, true>(out + 2 * cpitch, c, (int)cpitch, v8_raw<float>(v));
+      store_raw8<float, true>(out + 2 * cpitch, c[i], (int)cpitch, v8_raw<float>(v));
     }
   }
 }

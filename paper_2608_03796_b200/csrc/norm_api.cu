@@ -11,12 +11,8 @@ using namespace kdkl;
 
 // ------------------------------------------------------------------ block norm
 static constexpr long long kNormMaxH = 32768;
-// Threads of the *_rows kernels and how many blocks of them an SM is given: registers for 512 threads.
-static int rows_threads(long long H) {
-  const long long groups = act_codes_pitch(H) / 8;
-  const long long t = (groups + 31) / 32 * 32;
-  return (int)(t > kRowsThreads ? (t / 2 + 31) / 32 * 32 : t);
-}
+// Threads of the *_rows kernels: two groups of eight columns each.
+static int rows_threads(long long H) { return (int)((act_codes_pitch(H) / 16 + 31) / 32 * 32); }
 // Blocks of the backward kernels, each of which leaves one partial row.
 static long long norm_parts(long long T, long long H) {
   const int threads = H <= kRowsMaxH ? rows_threads(H) : kRowsThreads;
@@ -135,14 +131,12 @@ int kdkl_block_norm_forward(const kdkl_block_norm_args* a, void* cuda_stream) {
   const long long most = (long long)di.sm_count * 8;
   const unsigned grid = (unsigned)(a->T < most ? a->T : most);
   if (vec && a->H <= kRowsMaxH) {
-    const int threads = rows_threads(a->H), nv = act_codes_pitch(a->H) / 8 > threads ? 2 : 1;
-    const int smem = rows_stages(nv) * nv * threads * rows_forward_slot(type_bytes(a->residual_type));
+    const int threads = rows_threads(a->H), smem = threads / 16 * rows_forward_chunk(type_bytes(a->residual_type));
     const long long rows_most = (long long)di.sm_count * (1024 / threads > 16 ? 16 : 1024 / threads);
     const unsigned rows_grid = (unsigned)(a->T < rows_most ? a->T : rows_most);
     KDKL_BY_TYPE16(a->type, A, KDKL_BY_BOOL(a->residual_type == KDKL_TYPE_F32, WIDE, KDKL_BY_BOOL(any_record, REC,
-      KDKL_BY_BOOL(nv == 2, TWO,
-        return (launch_rows<block_norm_forward_rows_kernel<A, std::conditional_t<WIDE, float, A>, REC, TWO ? 2 : 1>>(
-            rows_grid, threads, smem, p, "block_norm_forward_rows_kernel", di, st))))));
+      return (launch_rows<block_norm_forward_rows_kernel<A, std::conditional_t<WIDE, float, A>, REC>>(
+          rows_grid, threads, smem, p, "block_norm_forward_rows_kernel", di, st)))));
   }
   KDKL_BY_TYPE16(a->type, A, KDKL_BY_BOOL(a->residual_type == KDKL_TYPE_F32, WIDE,
     KDKL_BY_BOOL(any_record, REC, KDKL_NORM_SHAPE(a->H, vec, VEC, THREADS, NV,
@@ -182,12 +176,10 @@ int kdkl_block_norm_backward(const kdkl_block_norm_args* a, void* cuda_stream) {
                      (!channel || aligned16(a->gate));
     if (vec && a->H <= kRowsMaxH) {
       const bool rec = a->format != KDKL_ACT8_NONE;
-      const int threads = rows_threads(a->H), nv = act_codes_pitch(a->H) / 8 > threads ? 2 : 1;
-      const int smem = rows_stages(nv) * nv * threads * rows_backward_slot(type_bytes(a->residual_type), rec);
+      const int threads = rows_threads(a->H), smem = threads / 16 * rows_backward_chunk(type_bytes(a->residual_type), rec);
       KDKL_BY_TYPE16(a->type, A, KDKL_BY_BOOL(a->residual_type == KDKL_TYPE_F32, WIDE, KDKL_BY_BOOL(rec, REC,
-        KDKL_BY_BOOL(nv == 2, TWO,
-          rc = (launch_rows<block_norm_backward_rows_kernel<A, std::conditional_t<WIDE, float, A>, REC, TWO ? 2 : 1>>(
-              (unsigned)parts, threads, smem, p, "block_norm_backward_rows_kernel", di, st))))));
+        rc = (launch_rows<block_norm_backward_rows_kernel<A, std::conditional_t<WIDE, float, A>, REC>>(
+            (unsigned)parts, threads, smem, p, "block_norm_backward_rows_kernel", di, st)))));
       if (rc) return rc;
     } else {
       KDKL_BY_TYPE16(a->type, A, KDKL_BY_BOOL(a->residual_type == KDKL_TYPE_F32, WIDE,
