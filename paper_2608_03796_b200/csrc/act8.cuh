@@ -196,6 +196,7 @@ __device__ __forceinline__ uint32_t group_max(uint32_t m) {
   m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
   return max(m, __shfl_xor_sync(0xffffffffu, m, 2));
 }
+// (the whole warp calls)
 template <int FMT>
 __device__ __forceinline__ uint2 act_codes(const float (&x)[8], uint32_t byte) {
   const float inv = act_inverse(byte);
@@ -206,8 +207,8 @@ __device__ __forceinline__ uint2 act_codes(const float (&x)[8], uint32_t byte) {
   // the one exponent at which a code rounded up would stand for 2^128
   constexpr uint32_t kTopByte = FMT == kFmtInt8 ? 122 + 127 : 120 + 127;
   constexpr float kTopCode = FMT == kFmtInt8 ? 63.f : 240.f;
-  if (byte == kTopByte) {
-    const float lim = kTopCode * act_scale(byte);
+  if (__any_sync(0xffffffffu, byte == kTopByte)) {
+    const float lim = byte == kTopByte ? kTopCode * act_scale(byte) : __uint_as_float(0x7f7fffffu);
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[i] = fminf(fmaxf(f[i], -lim), lim);
   }
@@ -263,9 +264,9 @@ template <int FMT>
 __device__ __forceinline__ void record_write8(const ActRecord& r, long long t, long long cpitch, long long spitch, int c,
                                               const float (&f)[8], bool write) {
   const uint32_t byte = act_scale_byte<FMT>(group_max(abs_max_bits(f)));
-  if (!write) return;
-  *reinterpret_cast<uint2*>(r.codes + t * cpitch + c) = act_codes<FMT>(f, byte);
-  if ((c & 31) == 0) r.scales[t * spitch + (c >> 5)] = (uint8_t)byte;
+  const uint2 codes = act_codes<FMT>(f, byte);
+  if (write) *reinterpret_cast<uint2*>(r.codes + t * cpitch + c) = codes;
+  if (write && (c & 31) == 0) r.scales[t * spitch + (c >> 5)] = (uint8_t)byte;
 }
 template <int FMT>
 __device__ __forceinline__ void record_read8(const ActRecord& r, long long t, long long cpitch, long long spitch, int c,

@@ -36,6 +36,15 @@ __device__ __forceinline__ float any_at(const AnyVec& v, long long i) {
   if (v.type == 0) return __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(v.p)[i]);
   return __half2float(reinterpret_cast<const __half*>(v.p)[i]);
 }
+// one element as bits, and what they stand for: apart, so that nothing waits for the load before its value is used
+__device__ __forceinline__ uint32_t any_bits(const AnyVec& v, long long i) {
+  return v.type == 1 ? __ldg(reinterpret_cast<const uint32_t*>(v.p) + i) : __ldg(reinterpret_cast<const uint16_t*>(v.p) + i);
+}
+__device__ __forceinline__ float any_value(uint32_t bits, int type) {
+  if (type == 1) return __uint_as_float(bits);
+  if (type == 0) return __uint_as_float(bits << 16);
+  return __half2float(__ushort_as_half((unsigned short)bits));
+}
 template <bool VEC>
 __device__ __forceinline__ void any_load8(const AnyVec& v, int c, int width, float (&f)[8]) {
   if (VEC) {
@@ -344,7 +353,7 @@ block_norm_backward_any_kernel(const NormBackward p) {
 // ------------------------------------------------------------------ rows of whole 16-byte words
 // A thread has two groups of eight columns: that halves what a row costs per value in sums, factors and addresses
 // (with one group a thread both kernels were bound by instructions, 63 and 54 a value).
-constexpr int kRowsThreads = 512, kRowsMaxH = 2 * 8 * kRowsThreads;
+constexpr int kRowsThreads = 512, kRowsMaxH = 2 * 8 * kRowsThreads, kRowsStages = 3;
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool live) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
@@ -355,6 +364,8 @@ __device__ __forceinline__ void cp_async8(uint32_t dst, const void* src, bool li
 __device__ __forceinline__ void cp_async4(uint32_t dst, const void* src, bool live) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(live ? 4 : 0) : "memory");
 }
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
 // Eight values as pairs.
@@ -386,11 +397,12 @@ __device__ __forceinline__ V8 v8_all(float x) {
   return v;
 }
 __device__ __forceinline__ float sum2(float2 a) { return a.x + a.y; }
-__device__ __forceinline__ void v8_write_record(int fmt, const ActRecord& r, long long t, long long cpitch, long long spitch,
+template <int FMT>
+__device__ __forceinline__ void v8_write_record(const ActRecord& r, long long t, long long cpitch, long long spitch,
                                                 int c, const V8& v) {
   float f[8];
   v8_to(v, f);
-  record_write8(fmt, r, t, cpitch, spitch, c, f, c < cpitch);
+  record_write8<FMT>(r, t, cpitch, spitch, c, f, c < cpitch);
 }
 
 // What the next row brings waits in shared memory, in places that only their own thread touches: per group of eight
@@ -421,12 +433,11 @@ template <int AT> __device__ __forceinline__ void fetch_record8(const Places& s,
   cp_async8(s.l8 + AT, codes + k, live);
   cp_async4(s.l4 + AT + 256, scales + ((k >> 5) & ~3u), live);
 }
-template <int AT> __device__ __forceinline__ V8 take_record8(const Places& s, int fmt, int shift) {
+template <int FMT, int AT> __device__ __forceinline__ V8 take_record8(const Places& s, int shift) {
   const uint32_t byte = (ld_shared_u32(s.l4 + AT + 256) >> shift) & 0xffu;
   const uint2 codes = ld_shared_v2(s.l8 + AT);
   float f[8];
-  if (fmt == kFmtInt8) act_values<kFmtInt8>(codes, byte, f);
-  else act_values<kFmtE4M3>(codes, byte, f);
+  act_values<FMT>(codes, byte, f);
   return v8_of(f);
 }
 // Bytes of a chunk: fields for 32 lanes.
@@ -435,7 +446,9 @@ __host__ __device__ constexpr int rows_backward_chunk(int residual_bytes, bool r
   return 256 * residual_bytes + 512 + (rec ? 2 * 384 : 512 + 256 * residual_bytes);
 }
 
-template <typename A, typename R, bool REC>
+// FMT -1: no records. FULL: both norms (and, backward, a gradient along the residual stream) are there, which spares the
+// loop its questions.
+template <typename A, typename R, int FMT, bool FULL>
 __global__ void __launch_bounds__(kRowsThreads)
 block_norm_forward_rows_kernel(const NormForward p) {
   extern __shared__ __align__(16) uint8_t smem[];
@@ -444,7 +457,7 @@ block_norm_forward_rows_kernel(const NormForward p) {
   const int H = p.H, threads = blockDim.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const long long cpitch = act_codes_pitch(H), spitch = act_scale_pitch(H);
   const float inv_h = 1.f / (float)H;
-  const bool has_post = p.post.p != nullptr, has_pre = p.pre.p != nullptr, token = p.gate_kind == kGateToken;
+  const bool has_post = FULL || p.post.p != nullptr, has_pre = FULL || p.pre.p != nullptr, token = p.gate_kind == kGateToken;
   const int c[2] = {(int)threadIdx.x * 8, (int)(threadIdx.x + threads) * 8};
   const uint32_t chunk = smem_u32(smem) + warp * rows_forward_chunk(sizeof(R));
   const Places at[2] = {Places(chunk, lane), Places(chunk + (threads >> 5) * rows_forward_chunk(sizeof(R)), lane)};
@@ -481,9 +494,9 @@ block_norm_forward_rows_kernel(const NormForward p) {
     }
   }
   int parity = 0;
-  float gate_next = token ? any_at(p.gate, blockIdx.x) : 1.f;
+  uint32_t gate_next = token ? any_bits(p.gate, blockIdx.x) : 0u;
   for (long long t = blockIdx.x; t < p.T; t += gridDim.x, parity ^= 2) {
-    const float gate_t = gate_next;
+    const float gate_t = token ? any_value(gate_next, p.gate.type) : 1.f;
     cp_async_wait_all();
     V8 b[2], x[2];
     float2 acc = both(0.f);
@@ -496,12 +509,12 @@ block_norm_forward_rows_kernel(const NormForward p) {
     }
     if (t + gridDim.x < p.T) {          // the row is in registers: its places take the next one
       fetch(t + gridDim.x);
-      if (token) gate_next = any_at(p.gate, t + gridDim.x);
+      if (token) gate_next = any_bits(p.gate, t + gridDim.x);
     }
-    if constexpr (REC) {
+    if constexpr (FMT >= 0) {
       if (p.rec_branch.codes != nullptr) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) v8_write_record(p.format, p.rec_branch, t, cpitch, spitch, c[i], b[i]);
+        for (int i = 0; i < 2; ++i) v8_write_record<FMT>(p.rec_branch, t, cpitch, spitch, c[i], b[i]);
       }
     }
     float rho1 = 1.f;
@@ -524,11 +537,11 @@ block_norm_forward_rows_kernel(const NormForward p) {
     for (int i = 0; i < 2; ++i) {
       const Raw8<R> raw = v8_raw<R>(x[i]);
       store_raw8<R, true>(sum_row, c[i], H, raw);
-      if constexpr (REC) {
+      if constexpr (FMT >= 0) {
         if (p.rec_sum.codes != nullptr) {              // what a record of the returned sum would hold
           float f[8];
           raw_to_f32(raw, f);
-          record_write8(p.format, p.rec_sum, t, cpitch, spitch, c[i], f, c[i] < cpitch);
+          record_write8<FMT>(p.rec_sum, t, cpitch, spitch, c[i], f, c[i] < cpitch);
         }
       }
     }
@@ -544,11 +557,11 @@ block_norm_forward_rows_kernel(const NormForward p) {
         for (int j = 0; j < 4; ++j) x[i].p[j] = mul2(x[i].p[j], mul2(w2[i].p[j], both(rho2)));
         const Raw8<A> raw = v8_raw<A>(x[i]);
         store_raw8<A, true>(y_row, c[i], H, raw);
-        if constexpr (REC) {
+        if constexpr (FMT >= 0) {
           if (p.rec_y.codes != nullptr) {
             float f[8];
             raw_to_f32(raw, f);
-            record_write8(p.format, p.rec_y, t, cpitch, spitch, c[i], f, c[i] < cpitch);
+            record_write8<FMT>(p.rec_y, t, cpitch, spitch, c[i], f, c[i] < cpitch);
           }
         }
       }
@@ -565,29 +578,33 @@ block_norm_forward_rows_kernel(const NormForward p) {
 //   A = sum_t sigma d b     (per column; dw1 = gate_c A, dgate_c = (w1 + o) A),   dw2 = sum_t u x
 //   db = sigma Q d - rho1^2 c1 b
 // so a column needs one sum for the gate and the post weight together.
-template <typename A, typename R, bool REC>
+template <typename A, typename R, int FMT, bool FULL>
 __global__ void __launch_bounds__(kRowsThreads)
 block_norm_backward_rows_kernel(const NormBackward p) {
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ float sm[2][3 * 32];
-  constexpr int kRB = 256 * (int)sizeof(R), kDy = kRB, kBranch = kRB + 512, kSum = kBranch + (REC ? 384 : 512);
+  constexpr int kRB = 256 * (int)sizeof(R), kDy = kRB, kBranch = kRB + 512, kSum = kBranch + (FMT >= 0 ? 384 : 512);
   const int H = p.H, threads = blockDim.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const long long cpitch = act_codes_pitch(H), spitch = act_scale_pitch(H);
   const float inv_h = 1.f / (float)H;
-  const bool has_post = p.post.p != nullptr, has_pre = p.pre.p != nullptr, token = p.gate_kind == kGateToken;
-  const bool has_dx = p.dsum != nullptr;
+  const bool has_post = FULL || p.post.p != nullptr, has_pre = FULL || p.pre.p != nullptr, token = p.gate_kind == kGateToken;
+  const bool has_dx = FULL || p.dsum != nullptr;
   const int c[2] = {(int)threadIdx.x * 8, (int)(threadIdx.x + threads) * 8};
-  constexpr int kChunk = rows_backward_chunk(sizeof(R), REC);
+  constexpr int kChunk = rows_backward_chunk(sizeof(R), FMT >= 0);
   const uint32_t chunk = smem_u32(smem) + warp * kChunk;
-  const Places at[2] = {Places(chunk, lane), Places(chunk + (threads >> 5) * kChunk, lane)};
-  float rho1_next = 1.f, rho2_next = 1.f, gate_next = 1.f;
-  auto fetch = [&](long long t) {
+  const uint32_t stage_bytes = (threads >> 4) * kChunk;
+  float rho1_next = 1.f, rho2_next = 1.f;
+  uint32_t gate_next = 0u;
+  auto places = [&](int i, int stage) { return Places(chunk + stage * stage_bytes + i * (stage_bytes / 2), lane); };
+  auto fetch = [&](long long t, int stage) {
+    if (t < p.T) {
+    const Places at[2] = {places(0, stage), places(1, stage)};
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const bool live = c[i] < H;
       if (has_dx) fetch8<R, 0>(at[i], reinterpret_cast<const R*>(p.dsum) + t * p.ld_dsum, c[i], live);
       if (has_pre) fetch8<A, kDy>(at[i], reinterpret_cast<const A*>(p.dy) + t * p.ld_dy, c[i], live);
-      if constexpr (REC) {
+      if constexpr (FMT >= 0) {
         fetch_record8<kBranch>(at[i], p.rec_branch.codes + t * cpitch, p.rec_branch.scales + t * spitch, c[i], live);
         if (has_pre) fetch_record8<kSum>(at[i], p.rec_sum.codes + t * cpitch, p.rec_sum.scales + t * spitch, c[i], live);
       } else {
@@ -595,11 +612,20 @@ block_norm_backward_rows_kernel(const NormBackward p) {
         if (has_pre) fetch8<R, kSum>(at[i], reinterpret_cast<const R*>(p.sum) + t * p.ld_sum, c[i], live);
       }
     }
+    }
+    cp_async_commit();
+  };
+  auto factors = [&](long long t) {
+    if (t >= p.T) return;
     if (has_post) rho1_next = p.rho_post[t];
     if (has_pre) rho2_next = p.rho_pre[t];
-    if (token) gate_next = any_at(p.gate, t);
+    if (token) gate_next = any_bits(p.gate, t);
   };
-  if (blockIdx.x < p.T) fetch(blockIdx.x);
+  constexpr int S = kRowsStages;
+#pragma unroll
+  for (int k = 0; k < S - 1; ++k) fetch(blockIdx.x + (long long)k * gridDim.x, k);
+  factors(blockIdx.x);
+  int stage = 0;
   V8 q[2], w2[2], sum_a[2], sum_w[2];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
@@ -625,17 +651,21 @@ block_norm_backward_rows_kernel(const NormBackward p) {
   const int shift0 = ((c[0] >> 5) & 3) * 8, shift1 = ((c[1] >> 5) & 3) * 8;
   int parity = 0;
   for (long long t = blockIdx.x; t < p.T; t += gridDim.x, parity ^= 1) {
-    const float rho1 = rho1_next, rho2 = rho2_next, gate_t = gate_next;
-    cp_async_wait_all();
+    const float rho1 = rho1_next, rho2 = rho2_next, gate_t = token ? any_value(gate_next, p.gate.type) : 1.f;
+    fetch(t + (long long)(S - 1) * gridDim.x, stage == 0 ? S - 1 : stage - 1);
+    factors(t + gridDim.x);
+    cp_async_wait<S - 1>();
+    const Places at[2] = {places(0, stage), places(1, stage)};
+    stage = stage + 1 == S ? 0 : stage + 1;
     V8 e[2], x[2], b[2];
     float2 a0 = both(0.f), a1 = both(0.f), a2 = both(0.f);   // u x w2';  Q b e;  Q b x
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       e[i] = has_dx ? take8<R, 0>(at[i]) : v8_all(0.f);
-      if constexpr (REC) b[i] = take_record8<kBranch>(at[i], p.format, i == 0 ? shift0 : shift1);
+      if constexpr (FMT >= 0) b[i] = take_record8<FMT, kBranch>(at[i], i == 0 ? shift0 : shift1);
       else b[i] = take8<A, kBranch>(at[i]);
       if (has_pre) {
-        if constexpr (REC) x[i] = take_record8<kSum>(at[i], p.format, i == 0 ? shift0 : shift1);
+        if constexpr (FMT >= 0) x[i] = take_record8<FMT, kSum>(at[i], i == 0 ? shift0 : shift1);
         else x[i] = take8<R, kSum>(at[i]);
         const V8 dy = take8<A, kDy>(at[i]);
 #pragma unroll
@@ -655,7 +685,6 @@ block_norm_backward_rows_kernel(const NormBackward p) {
         a2 = fma2(qb, x[i].p[j], a2);
       }
     }
-    if (t + gridDim.x < p.T) fetch(t + gridDim.x);           // the row is in registers: its places take the next one
     float s[3] = {sum2(a0), sum2(a1), sum2(a2)};
     block_sums_any<3>(s, sm[parity]);
     const float k2 = rho2 * rho2 * s[0] * inv_h;             // d = e - k2 x

@@ -13,10 +13,10 @@ using namespace kdkl;
 static constexpr long long kNormMaxH = 32768;
 // Threads of the *_rows kernels: two groups of eight columns each.
 static int rows_threads(long long H) { return (int)((act_codes_pitch(H) / 16 + 31) / 32 * 32); }
-// Blocks of the backward kernels, each of which leaves one partial row.
+// The most blocks of the backward kernels, each of which leaves one partial row: what 1024 threads an SM amount to.
 static long long norm_parts(long long T, long long H) {
-  const int threads = H <= kRowsMaxH ? rows_threads(H) : kRowsThreads;
-  const long long most = (long long)sm_count_or_default() * (kRowsThreads / threads > 8 ? 8 : kRowsThreads / threads);
+  const int threads = H <= kRowsMaxH ? rows_threads(H) : 2 * kRowsThreads;
+  const long long most = (long long)sm_count_or_default() * (1024 / threads > 16 ? 16 : 1024 / threads);
   return T < most ? T : most;
 }
 
@@ -77,17 +77,30 @@ static int check_norm(const kdkl_block_norm_args* a, bool backward) {
   return KDKL_OK;
 }
 
-// The shared memory a kernel may use beyond 48 KiB (its static part included) is an attribute of its copy on the device:
-// raised when a launch needs more than any before.
+// Launches a *_rows kernel with as many blocks as the device holds at once (at most `most`: one per row, one per partial
+// row). The shared memory a kernel may use beyond 48 KiB, its static part included, is an attribute of its copy on the
+// device, raised when a launch needs more than any before; how many blocks fit an SM is asked once per number of warps.
 template <auto KERN, typename P>
-static int launch_rows(unsigned grid, int threads, int smem, const P& p, const char* name, const DeviceInfo& di, cudaStream_t st) {
-  static int allowed[kMaxDevices];
-  const bool known = di.dev >= 0 && di.dev < kMaxDevices;
-  if (smem > 40 * 1024 && (!known || smem > allowed[di.dev])) {
+static int launch_rows(long long most, int threads, int smem, const P& p, const char* name, const DeviceInfo& di,
+                       cudaStream_t st, int* blocks) {
+  struct Known { int allowed; int fit[kRowsThreads / 32 + 1]; };
+  static Known known[kMaxDevices];
+  Known fresh;
+  memset(&fresh, 0, sizeof(fresh));
+  Known& k = di.dev >= 0 && di.dev < kMaxDevices ? known[di.dev] : fresh;
+  if (smem > 40 * 1024 && smem > k.allowed) {
     KDKL_CUDA(cudaFuncSetAttribute(KERN, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-    if (known) allowed[di.dev] = smem;
+    k.allowed = smem;
   }
-  KERN<<<grid, threads, smem, st>>>(p);
+  int fit = k.fit[threads / 32];
+  if (fit == 0) {
+    KDKL_CUDA(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&fit, KERN, threads, smem));
+    if (fit < 1) fit = 1;
+    k.fit[threads / 32] = fit;
+  }
+  const long long held = (long long)di.sm_count * fit;
+  *blocks = (int)(most < held ? most : held);
+  KERN<<<*blocks, threads, smem, st>>>(p);
   KDKL_LAUNCHED(name);
   return KDKL_OK;
 }
@@ -131,12 +144,13 @@ int kdkl_block_norm_forward(const kdkl_block_norm_args* a, void* cuda_stream) {
   const long long most = (long long)di.sm_count * 8;
   const unsigned grid = (unsigned)(a->T < most ? a->T : most);
   if (vec && a->H <= kRowsMaxH) {
+    const int fmt = any_record ? a->format : KDKL_ACT8_NONE;
+    const bool full = a->post_weight && a->pre_weight;
     const int threads = rows_threads(a->H), smem = threads / 16 * rows_forward_chunk(type_bytes(a->residual_type));
-    const long long rows_most = (long long)di.sm_count * (1024 / threads > 16 ? 16 : 1024 / threads);
-    const unsigned rows_grid = (unsigned)(a->T < rows_most ? a->T : rows_most);
-    KDKL_BY_TYPE16(a->type, A, KDKL_BY_BOOL(a->residual_type == KDKL_TYPE_F32, WIDE, KDKL_BY_BOOL(any_record, REC,
-      return (launch_rows<block_norm_forward_rows_kernel<A, std::conditional_t<WIDE, float, A>, REC>>(
-          rows_grid, threads, smem, p, "block_norm_forward_rows_kernel", di, st)))));
+    int blocks;
+    KDKL_BY_TYPE16(a->type, A, KDKL_BY_BOOL(a->residual_type == KDKL_TYPE_F32, WIDE, KDKL_BY_FORMAT_OR_NONE(fmt, FMT, KDKL_BY_BOOL(full, FULL,
+      return (launch_rows<block_norm_forward_rows_kernel<A, std::conditional_t<WIDE, float, A>, FMT, FULL>>(
+          a->T, threads, smem, p, "block_norm_forward_rows_kernel", di, st, &blocks))))));
   }
   KDKL_BY_TYPE16(a->type, A, KDKL_BY_BOOL(a->residual_type == KDKL_TYPE_F32, WIDE,
     KDKL_BY_BOOL(any_record, REC, KDKL_NORM_SHAPE(a->H, vec, VEC, THREADS, NV,
@@ -154,7 +168,7 @@ int kdkl_block_norm_backward(const kdkl_block_norm_args* a, void* cuda_stream) {
   cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
   const bool has_post = a->post_weight != nullptr, has_pre = a->pre_weight != nullptr;
   const bool channel = a->gate_kind == KDKL_GATE_CHANNEL;
-  const long long parts = norm_parts(a->T, a->H);
+  int parts = (int)norm_parts(a->T, a->H);
   if (a->T > 0) {
     NormBackward p;
     p.dsum = a->dsum; p.ld_dsum = a->ld_dsum; p.dy = a->dy; p.ld_dy = a->ld_dy;
@@ -175,11 +189,11 @@ int kdkl_block_norm_backward(const kdkl_block_norm_args* a, void* cuda_stream) {
                      aligned16(a->dbranch) && aligned16(a->post_weight) && aligned16(a->pre_weight) &&
                      (!channel || aligned16(a->gate));
     if (vec && a->H <= kRowsMaxH) {
-      const bool rec = a->format != KDKL_ACT8_NONE;
-      const int threads = rows_threads(a->H), smem = threads / 16 * rows_backward_chunk(type_bytes(a->residual_type), rec);
-      KDKL_BY_TYPE16(a->type, A, KDKL_BY_BOOL(a->residual_type == KDKL_TYPE_F32, WIDE, KDKL_BY_BOOL(rec, REC,
-        rc = (launch_rows<block_norm_backward_rows_kernel<A, std::conditional_t<WIDE, float, A>, REC>>(
-            (unsigned)parts, threads, smem, p, "block_norm_backward_rows_kernel", di, st)))));
+      const bool rec = a->format != KDKL_ACT8_NONE, full = has_post && has_pre && a->dsum;
+      const int threads = rows_threads(a->H), smem = kRowsStages * (threads / 16) * rows_backward_chunk(type_bytes(a->residual_type), rec);
+      KDKL_BY_TYPE16(a->type, A, KDKL_BY_BOOL(a->residual_type == KDKL_TYPE_F32, WIDE, KDKL_BY_FORMAT_OR_NONE(a->format, FMT, KDKL_BY_BOOL(full, FULL,
+        rc = (launch_rows<block_norm_backward_rows_kernel<A, std::conditional_t<WIDE, float, A>, FMT, FULL>>(
+            parts, threads, smem, p, "block_norm_backward_rows_kernel", di, st, &parts))))));
       if (rc) return rc;
     } else {
       KDKL_BY_TYPE16(a->type, A, KDKL_BY_BOOL(a->residual_type == KDKL_TYPE_F32, WIDE,
@@ -195,7 +209,7 @@ int kdkl_block_norm_backward(const kdkl_block_norm_args* a, void* cuda_stream) {
     c.out[1] = has_pre ? a->dpre_weight : nullptr; c.type[1] = a->weight_type;
     c.out[2] = channel ? a->dgate : nullptr; c.type[2] = a->gate_type;
     const dim3 grid((unsigned)((a->H + 31) / 32), 3, 1);
-    block_norm_columns_kernel<<<grid, dim3(32, 8, 1), 0, st>>>(at<float>(a->workspace, 0), (int)parts, (int)a->H,
+    block_norm_columns_kernel<<<grid, dim3(32, 8, 1), 0, st>>>(at<float>(a->workspace, 0), parts, (int)a->H,
                                                              act_codes_pitch(a->H), c);
     KDKL_LAUNCHED("block_norm_columns_kernel");
   }
