@@ -29,10 +29,10 @@ inline int need_b200(DeviceInfo* di) {
   if (rc) return rc;
   return di->cc_major == 10 ? KDKL_OK : KDKL_ERR_ARCH;
 }
-// Grid of the element-wise kernels: 2048 columns a block in x; in y as many rows at a time as fill the device.
-inline dim3 rows_grid(long long T, long long H, const DeviceInfo& di) {
+// Grid of the element-wise kernels: 2048 columns a block in x; in y as many rows as make `per_sm` blocks an SM.
+inline dim3 rows_grid(long long T, long long H, const DeviceInfo& di, int per_sm) {
   const long long gx = (act_codes_pitch(H) + 2047) / 2048;
-  long long gy = ((long long)di.sm_count * 16 + gx - 1) / gx;
+  long long gy = ((long long)di.sm_count * per_sm + gx - 1) / gx;
   if (gy > T) gy = T;
   if (gy > 65535) gy = 65535;
   return dim3((unsigned)gx, (unsigned)gy, 1);
