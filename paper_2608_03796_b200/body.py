@@ -34,14 +34,17 @@ def _lookup(table, key, name):
     return table[key]
 
 
+_device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+
+
 def _rows(t: torch.Tensor, T: int, H: int, dtype, name: str):
     """(address, distance of rows) of a CUDA tensor [T, H] whose rows are contiguous but may lie apart. Refused here,
     as in binding: another device, type or shape, or columns that are not neighbours."""
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
-        raise TypeError(f"kdkl: {name}: expected a tensor on the current CUDA device, got one on {t.device}")
-    if t.dtype != dtype:
-        raise TypeError(f"kdkl: {name}: expected dtype {dtype}, got {t.dtype}")
-    if t.shape != (T, H):
+    if t.get_device() != _device() or t.dtype is not dtype or t.shape != (T, H):
+        if not t.is_cuda or t.device.index != _device():
+            raise TypeError(f"kdkl: {name}: expected a tensor on the current CUDA device, got one on {t.device}")
+        if t.dtype != dtype:
+            raise TypeError(f"kdkl: {name}: expected dtype {dtype}, got {t.dtype}")
         raise TypeError(f"kdkl: {name}: expected shape {(T, H)}, got {tuple(t.shape)}")
     apart, along = t.stride()
     if (along != 1 and H > 1) or (apart < H and T > 1):
@@ -49,8 +52,16 @@ def _rows(t: torch.Tensor, T: int, H: int, dtype, name: str):
     return t.data_ptr(), (apart if T > 1 else H)
 
 
+def _stream() -> int:
+    return _raw_stream(_device())
+
+
 def _vector(t: Optional[torch.Tensor], n: int, dtype, name: str):
-    return None if t is None else B._dptr(t, dtype, (n,), name).value
+    if t is None:
+        return None
+    if t.get_device() == _device() and t.dtype is dtype and t.shape == (n,) and (n <= 1 or t.stride(0) == 1):
+        return t.data_ptr()
+    return B._dptr(t, dtype, (n,), name).value                          # says what is wrong
 
 
 class Act8Record:
@@ -69,7 +80,7 @@ class Act8Record:
     def store(self, x: torch.Tensor) -> "Act8Record":
         ptr, ld = _rows(x, self.T, self.H, x.dtype, "x")
         B._check(B.lib().kdkl_act8_store(ptr, _lookup(TYPES, x.dtype, "x"), ld, self.T, self.H, self.code, self.ptr,
-                                         self.nbytes, B._stream()))
+                                         self.nbytes, _stream()))
         return self
 
     def load(self, out: Optional[torch.Tensor] = None, dtype=torch.bfloat16) -> torch.Tensor:
@@ -77,7 +88,7 @@ class Act8Record:
             out = torch.empty(self.T, self.H, dtype=dtype, device=self.buffer.device)
         ptr, ld = _rows(out, self.T, self.H, out.dtype, "out")
         B._check(B.lib().kdkl_act8_load(self.ptr, self.nbytes, self.T, self.H, self.code, ptr,
-                                        _lookup(TYPES, out.dtype, "out"), ld, B._stream()))
+                                        _lookup(TYPES, out.dtype, "out"), ld, _stream()))
         return out
 
 
@@ -105,7 +116,7 @@ class Act8WeightGrad:
         B._check(B.lib().kdkl_act8_dweight(
             ptr, ld, record.ptr, record.nbytes, self.T, self.N, self.H, record.code,
             B._dptr(out, self.dtype, (self.N, self.H), "out"), self.type, 1 if accumulate else 0,
-            self.workspace.data_ptr(), self.workspace.numel(), B._stream()))
+            self.workspace.data_ptr(), self.workspace.numel(), _stream()))
         return out
 
     def status(self):
@@ -138,7 +149,7 @@ class GatedAct:
         if ld_u != ld:
             raise TypeError(f"kdkl: gate and up must have their rows equally far apart, got {ld} and {ld_u}")
         B._check(B.lib().kdkl_gated_act_forward(g, u, ld, self.type, self.T, self.F, self.act, self.format,
-                                                self.h.data_ptr(), self.F, *self.records, B._stream()))
+                                                self.h.data_ptr(), self.F, *self.records, _stream()))
         return self.h
 
     def backward(self, dh: torch.Tensor):
@@ -152,7 +163,7 @@ class GatedAct:
         out = self.dgate_up.data_ptr()
         B._check(B.lib().kdkl_gated_act_backward(
             self.records[0], self.records[1], self.records[3], self.format, d, ld, self.type, self.T, self.F, self.act,
-            out, out + self.F * self.dtype.itemsize, 2 * self.F, B._stream()))
+            out, out + self.F * self.dtype.itemsize, 2 * self.F, _stream()))
         return self.halves
 
 
@@ -235,7 +246,7 @@ class BlockNorm:
         a.residual, a.ld_residual = _rows(residual, self.T, self.H, self.residual_dtype, "residual")
         a.branch, a.ld_branch = _rows(branch, self.T, self.H, self.dtype, "branch")
         self._weights(post_weight, pre_weight, gate)
-        B._check(B.lib().kdkl_block_norm_forward(ctypes.byref(a), B._stream()))
+        B._check(B.lib().kdkl_block_norm_forward(ctypes.byref(a), _stream()))
         # what the backward call reads is kept alive here
         self.kept = (branch, post_weight, pre_weight, gate)
         return (self.y if pre_weight is not None else None), self.sum
@@ -283,5 +294,5 @@ class BlockNorm:
         a.dpost_weight = None if d.post_weight is None else d.post_weight.data_ptr()
         a.dpre_weight = None if d.pre_weight is None else d.pre_weight.data_ptr()
         a.dgate = None if d.gate is None else d.gate.data_ptr()
-        B._check(B.lib().kdkl_block_norm_backward(ctypes.byref(a), B._stream()))
+        B._check(B.lib().kdkl_block_norm_backward(ctypes.byref(a), _stream()))
         return d

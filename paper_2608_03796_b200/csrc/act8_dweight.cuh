@@ -15,8 +15,9 @@
 //   warps 12-19  running sums in registers (128 rows x 256 columns a CTA, 128 values a thread)
 //
 // Why sums in registers: an accumulator in tensor memory truncates at each addition, measured as a relative error of
-// 1.1e-9 per token contracted (4.4e-6 at 4096, 3.8e-5 at 32768). It therefore only runs over RUN blocks; then
-// the eight warps add it, rounding to nearest, to the sums they hold, while the second accumulator fills.
+// 1.1e-9 per token contracted with two bf16 operands (3.8e-5 at 32768 tokens) and 2.4e-10 with codes on one side. It
+// therefore only runs over RUN blocks (1024 tokens); then the eight warps add it, rounding to nearest, to the sums they
+// hold, while the second accumulator fills. (Runs of 2048 tokens cost 1 % less.)
 // Work units: whole tiles as far as they fill whole waves of CTA pairs, then the remaining tiles cut into parts of the
 // contraction, so that the last wave is as short as it can be. Parts leave fp32 slabs that act8_dweight_join_kernel adds
 // in order: results are reproducible bit for bit.
@@ -90,7 +91,7 @@ act8_dweight_simple_kernel(const DweightParams p) {
 }
 
 struct DwCfg {
-  static constexpr int TILE = 256, BK = 64, STAGES = 4, RUN = 12;
+  static constexpr int TILE = 256, BK = 64, STAGES = 4, RUN = 16;
   static constexpr int A_BYTES = 128 * BK * 2, B_BYTES = 128 * BK * 2, STAGE_BYTES = A_BYTES + B_BYTES;
   // codes and scale bytes wait in slots of half a block, each free again as soon as it is in registers
   static constexpr int RAW = 8, RAW_T = BK / 2, CODE_BYTES = 128 * RAW_T, RAW_BYTES = CODE_BYTES + 16 * RAW_T;
@@ -469,7 +470,7 @@ act8_dweight_kernel(const __grid_constant__ CUtensorMap tmY, const __grid_consta
 }
 
 // The tiles that were cut: out (= or +=) slab 0 + slab 1 + ... in that order, rounded once. One block per 8 rows of a
-// tile, 32 threads a row. H % 8 == 0.
+// tile, 32 threads a row. H % 8 == 0. Starts while the products drain and waits for them before it reads.
 __global__ void __launch_bounds__(256)
 act8_dweight_join_kernel(const float* __restrict__ slabs, int whole, int parts, int h_tiles, int N, int H,
                          void* __restrict__ out, int type, int accumulate) {
@@ -477,6 +478,7 @@ act8_dweight_join_kernel(const float* __restrict__ slabs, int whole, int parts, 
   const int tile = whole + i, row = (tile / h_tiles) * 256 + r, col = (tile % h_tiles) * 256 + c;
   if (row >= N || col >= H) return;
   const float* src = slabs + ((long long)i * parts * 256 + r) * 256 + c;
+  grid_dependency_wait();
   float f[8], g[8];
   raw_to_f32(load_raw8<float, true>(src, 0, 8), f);
   for (int q = 1; q < parts; ++q) {

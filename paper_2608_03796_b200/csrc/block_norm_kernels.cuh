@@ -733,27 +733,27 @@ block_norm_backward_rows_kernel(const NormBackward p) {
   }
 }
 
-// Column sums of the partial rows, in a fixed order: thread y of a block adds the rows y, y + 8, ...; then the eight
-// partial sums are added in order.
-struct NormColumns { void* out[3]; int type[3]; };
-__global__ void __launch_bounds__(256)
+// Column sums of the partial rows, in a fixed order: warp y of a block adds the rows y, y + 32, ... of 32 columns, then
+// each warp the 32 partial sums of a column. Starts while the kernel before it drains and waits for it before it reads.
+struct NormColumns { void* out[3]; int type[3]; int which[3]; };
+__global__ void __launch_bounds__(1024)
 block_norm_columns_kernel(const float* __restrict__ partial, int parts, int H, long long cpitch, const NormColumns p) {
-  __shared__ float sm[8][33];
-  const int which = blockIdx.y, c = blockIdx.x * 32 + threadIdx.x;
-  if (p.out[which] == nullptr) return;
+  __shared__ float sm[32][33];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, q = blockIdx.y;
+  grid_dependency_wait();
   float s = 0.f;
-  if (c < H) {
-    const float* src = partial + which * cpitch + c;
+  if (blockIdx.x * 32 + lane < H) {
+    const float* src = partial + p.which[q] * cpitch + blockIdx.x * 32 + lane;
 #pragma unroll 8
-    for (int i = threadIdx.y; i < parts; i += 8) s += src[(long long)i * 3 * cpitch];
+    for (int i = warp; i < parts; i += 32) s += src[(long long)i * 3 * cpitch];
   }
-  sm[threadIdx.y][threadIdx.x] = s;
+  sm[warp][lane] = s;
   __syncthreads();
-  if (threadIdx.y == 0 && c < H) {
+  s = sm[lane][warp];
 #pragma unroll
-    for (int i = 1; i < 8; ++i) s += sm[i][threadIdx.x];
-    any_store(p.out[which], p.type[which], c, s);
-  }
+  for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  const int c = blockIdx.x * 32 + warp;
+  if (lane == 0 && c < H) any_store(p.out[q], p.type[q], c, s);
 }
 
 }  // namespace kdkl

@@ -227,8 +227,9 @@ int kdkl_act8_dweight(const void* dy, int64_t ld_dy, const void* record, size_t 
   KDKL_BY_FORMAT(format, FMT, KDKL_BY_BOOL(type == KDKL_TYPE_F32, F32_OUT,
     rc = (launch_dweight<FMT, F32_OUT>(ty, tc, ts, to, tslab, p, di, st))));
   if (rc || plan.rest == 0) return rc;
-  act8_dweight_join_kernel<<<(unsigned)plan.rest * 32, 256, 0, st>>>(slab, plan.whole, plan.parts, p.h_tiles, (int)N, (int)H,
-                                                                     dweight, type, accumulate);
+  rc = launch_after(act8_dweight_join_kernel, dim3((unsigned)plan.rest * 32, 1, 1), 256, st, (const float*)slab, plan.whole,
+                    plan.parts, p.h_tiles, (int)N, (int)H, dweight, (int)type, (int)accumulate);
+  if (rc) return rc;
   KDKL_LAUNCHED("act8_dweight_join_kernel");
   return KDKL_OK;
 }

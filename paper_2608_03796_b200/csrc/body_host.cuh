@@ -1,5 +1,7 @@
 // Argument checks and dispatch that the host sides of the student-body operators share.
 #pragma once
+#include <string.h>
+
 #include "act8.cuh"
 #include "host_common.cuh"
 
@@ -36,6 +38,23 @@ inline dim3 rows_grid(long long T, long long H, const DeviceInfo& di, int per_sm
   if (gy > T) gy = T;
   if (gy > 65535) gy = 65535;
   return dim3((unsigned)gx, (unsigned)gy, 1);
+}
+
+// A launch that may start while the kernel before it on the stream drains (that kernel calls grid_dependency_wait).
+template <typename... P, typename... Q>
+inline int launch_after(void (*kern)(P...), dim3 grid, int threads, cudaStream_t st, Q... args) {
+  cudaLaunchConfig_t cfg;
+  memset(&cfg, 0, sizeof(cfg));
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3((unsigned)threads, 1, 1);
+  cfg.stream = st;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  KDKL_CUDA(cudaLaunchKernelEx(&cfg, kern, P(args)...));
+  return KDKL_OK;
 }
 
 #define KDKL_BY_BOOL(cond, NAME, ...)                                  \

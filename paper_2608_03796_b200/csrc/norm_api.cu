@@ -205,12 +205,14 @@ int kdkl_block_norm_backward(const kdkl_block_norm_args* a, void* cuda_stream) {
   if (has_post || has_pre || channel) {
     NormColumns c;
     memset(&c, 0, sizeof(c));
-    c.out[0] = has_post ? a->dpost_weight : nullptr; c.type[0] = a->weight_type;
-    c.out[1] = has_pre ? a->dpre_weight : nullptr; c.type[1] = a->weight_type;
-    c.out[2] = channel ? a->dgate : nullptr; c.type[2] = a->gate_type;
-    const dim3 grid((unsigned)((a->H + 31) / 32), 3, 1);
-    block_norm_columns_kernel<<<grid, dim3(32, 8, 1), 0, st>>>(at<float>(a->workspace, 0), parts, (int)a->H,
-                                                             act_codes_pitch(a->H), c);
+    int n = 0;
+    auto add = [&](int which, void* out, int type) { c.which[n] = which; c.out[n] = out; c.type[n] = type; ++n; };
+    if (has_post) add(0, a->dpost_weight, a->weight_type);
+    if (has_pre) add(1, a->dpre_weight, a->weight_type);
+    if (channel) add(2, a->dgate, a->gate_type);
+    rc = launch_after(block_norm_columns_kernel, dim3((unsigned)((a->H + 31) / 32), (unsigned)n, 1), 1024, st,
+                      (const float*)at<float>(a->workspace, 0), parts, (int)a->H, act_codes_pitch(a->H), c);
+    if (rc) return rc;
     KDKL_LAUNCHED("block_norm_columns_kernel");
   }
   return KDKL_OK;

@@ -47,6 +47,10 @@ __device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
 // microseconds; two seconds means a protocol error, which is reported, not spun on.
 constexpr uint64_t kWaitLimitNs = 2000000000ull;
 
+// For a kernel launched with programmatic stream serialisation: returns when the kernel before it has completed and its
+// writes can be read.
+__device__ __forceinline__ void grid_dependency_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 // One lane of a converged warp.
 __device__ __forceinline__ bool elect_one() {
   uint32_t r;
