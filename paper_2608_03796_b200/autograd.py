@@ -18,6 +18,15 @@ Algorithm 1, and a backward whose buffer set has been reused in the meantime (a 
 graph) raises instead of returning gradients of another batch. `weight_grad_fp32=True` hands the fp32 dW
 buffer over to the caller (the pool allocates a new one next time) instead of a bf16 copy; with `dweight_out`
 given, dW is accumulated into that fp32 tensor in place.
+
+The layers of a student's body whose backward pass reads activations kept in 8 bits (``body``):
+
+    y, x, kept = block_norm(x, branch, post_weight, pre_weight, gate, act8="int8", keep_y=True)
+    z = act8_linear(y, W_gate_up, record=kept)               # keeps nothing of its own
+    h, kept = gated_act(z, act="silu", act8="int8", keep_h=True)
+    branch = act8_linear(h, W_down, record=kept)
+
+Their outputs, records and gradients are allocated per call, as a graph needs them.
 """
 from __future__ import annotations
 
@@ -26,6 +35,7 @@ from typing import Optional
 import torch
 
 from . import binding as B
+from . import body
 
 _free: dict = {}          # key -> buffer sets (FusedChunkedKL holders) no live loss is using
 _probed: list = []        # buffer sets whose last step's status has not been looked at yet
@@ -194,3 +204,155 @@ class _FeatureLoss(torch.autograd.Function):
 def feature_loss(student, teacher, loss_mask=None, kind=B.FEATURE_MSE, weight=1.0) -> torch.Tensor:
     """Hidden-state feature loss (MSE or cosine) between student and cached teacher hidden states."""
     return _FeatureLoss.apply(student, teacher, loss_mask, kind, weight)
+
+
+def _flat(t: torch.Tensor, width: int) -> torch.Tensor:
+    """[..., width] as rows whose columns are neighbours and which do not overlap (a copy where they do)."""
+    t = t.reshape(-1, width)
+    apart, along = t.stride()
+    return t if (along == 1 or width == 1) and (apart >= width or t.shape[0] <= 1) else t.contiguous()
+
+
+def _shaped(t: torch.Tensor, shape) -> torch.Tensor:
+    """The memory of a contiguous tensor under another shape, not as a view of it: what a Function returns may then be
+    changed in place like any other tensor."""
+    return t if t.shape == shape else torch.empty(0, dtype=t.dtype, device=t.device).set_(t.untyped_storage(), 0, shape)
+
+
+def _recorded(*tensors) -> bool:
+    """Whether a backward pass can come (within a Function's forward, grad mode is off and does not say)."""
+    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+
+
+class _Act8Linear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, record, act8, keep):
+        N, H = weight.shape
+        rows = _flat(x, H)
+        if keep:
+            if record is None:
+                record = body.Act8Record(rows.shape[0], H, act8, device=x.device).store(rows)
+            elif (record.T, record.H) != tuple(rows.shape):
+                raise TypeError(f"act8_linear: the record is of shape {(record.T, record.H)}, the input of {tuple(rows.shape)}")
+            ctx.format = record.format
+        ctx.save_for_backward(weight, None if record is None else record.buffer)
+        ctx.shape = x.shape
+        return torch.matmul(rows, weight.t()).reshape(*x.shape[:-1], N)          # a plain library product
+
+    @staticmethod
+    def backward(ctx, dy):
+        weight, buffer = ctx.saved_tensors
+        N, H = weight.shape
+        rows = _flat(dy, N)
+        dx = torch.matmul(rows, weight).reshape(ctx.shape) if ctx.needs_input_grad[0] else None
+        dw = None
+        if ctx.needs_input_grad[1]:
+            record = body.Act8Record(rows.shape[0], H, ctx.format, buffer=buffer)
+            dw = body.Act8WeightGrad(rows.shape[0], N, H, dtype=weight.dtype, device=dy.device).run(rows, record)
+        return dx, dw, None, None, None
+
+
+def act8_linear(x, weight, record: Optional[body.Act8Record] = None, act8: str = "int8") -> torch.Tensor:
+    """x @ weight.T (bf16, x [..., H], weight [N, H]) that keeps x in 8 bits for the weight's gradient: in `record`, if
+    one that stands for x exists already (block_norm and gated_act leave them), else in one of format `act8`."""
+    if x.dtype != torch.bfloat16 or weight.dtype != torch.bfloat16:
+        raise TypeError(f"act8_linear: expected bf16, got {x.dtype} and {weight.dtype}")
+    if act8 not in ("int8", "e4m3"):
+        raise ValueError(f"act8_linear: expected a record format, got {act8!r}")
+    return _Act8Linear.apply(x, weight, record, act8, _recorded(weight))
+
+
+class _GatedAct(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, gate_up, act, act8, keep_h, needed):
+        F = gate_up.shape[-1] // 2
+        rows = _flat(gate_up, 2 * F)
+        op = body.GatedAct(rows.shape[0], F, act=act, act8=act8 if needed else None, dtype=gate_up.dtype,
+                           keep_h=keep_h and needed, device=gate_up.device)
+        h = _shaped(op.forward(rows[:, :F], rows[:, F:]), (*gate_up.shape[:-1], F))
+        if needed:
+            ctx.save_for_backward(op.gate_record.buffer, op.up_record.buffer)   # autograd frees them, layer by layer
+        record, op.h, op.h_record, op.gate_record, op.up_record = op.h_record, None, None, None, None
+        ctx.op, ctx.shape, ctx.format = op, gate_up.shape, act8
+        return h, record
+
+    @staticmethod
+    def backward(ctx, dh, _):
+        op, F = ctx.op, ctx.shape[-1] // 2
+        op.gate_record, op.up_record = (body.Act8Record(op.T, F, ctx.format, buffer=b) for b in ctx.saved_tensors)
+        op.dgate_up = None                                                      # a buffer of its own for every backward
+        op.backward(_flat(dh, F))
+        out, op.dgate_up, op.halves, op.gate_record, op.up_record = op.dgate_up, None, None, None, None
+        return out.reshape(ctx.shape), None, None, None, None
+
+
+def gated_act(gate_up, act: str = "silu", act8: str = "int8", keep_h: bool = False):
+    """act(gate) * up of a projection [..., 2 F] whose first half is the gate; the backward pass reads both halves from
+    8-bit records. With keep_h: (h, record of h), for the act8_linear that reads h."""
+    if gate_up.shape[-1] % 2:
+        raise TypeError(f"gated_act: expected an even width, got {gate_up.shape[-1]}")
+    if act8 not in ("int8", "e4m3"):
+        raise ValueError(f"gated_act: expected a record format, got {act8!r}")
+    h, record = _GatedAct.apply(gate_up, act, act8, keep_h, _recorded(gate_up))
+    return (h, record) if keep_h else h
+
+
+class _BlockNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, residual, branch, post_weight, pre_weight, gate, kind, act8, keep_y, args, train):
+        H = branch.shape[-1]
+        r, b = _flat(residual, H), _flat(branch, H)
+        op = body.BlockNorm(b.shape[0], H, dtype=branch.dtype, residual_dtype=residual.dtype, gate=kind, act8=act8,
+                            train=train, keep_y=keep_y, device=branch.device, **args)
+        flat_gate = None if gate is None else gate.reshape(-1).contiguous()
+        y, x = op.forward(r, b, post_weight=post_weight, pre_weight=pre_weight, gate=flat_gate)
+        ctx.shapes = residual.shape, branch.shape, None if gate is None else gate.shape
+        y, x = None if y is None else _shaped(y, branch.shape), _shaped(x, residual.shape)
+        if train:
+            # the branch and the sum, as records or as they are: autograd frees them layer by layer and, for tensors, checks
+            # that nobody has changed them in place
+            kept = (b, x) if act8 is None else (op.branch_record.buffer, op.sum_record.buffer)
+            ctx.save_for_backward(post_weight, pre_weight, flat_gate, *kept)
+        record = op.y_record
+        op.kept = op.y = op.sum = op.y_record = op.branch_record = op.sum_record = None
+        ctx.op, ctx.format = op, act8
+        ctx.set_materialize_grads(False)
+        return y, x, record
+
+    @staticmethod
+    def backward(ctx, dy, dx, _):
+        if dy is None and dx is None:
+            return (None,) * 10
+        op, (post_weight, pre_weight, gate, b, x) = ctx.op, ctx.saved_tensors
+        rs, bs, gs = ctx.shapes
+        H = bs[-1]
+        if dy is None and pre_weight is not None:
+            dy = torch.zeros(op.T, H, dtype=op.dtype, device=op.rho.device)
+        if ctx.format is not None:
+            op.branch_record, op.sum_record = (body.Act8Record(op.T, H, ctx.format, buffer=t) for t in (b, x))
+        op.kept = (b, x if ctx.format is not None else _flat(x, H), post_weight, pre_weight, gate)
+        op.workspace, op.grads = None, {}                                       # buffers of its own for every backward
+        d = op.backward(None if dy is None else _flat(dy, H), None if dx is None else _flat(dx, H))
+        op.kept = op.workspace = op.dresidual = op.dbranch = op.branch_record = op.sum_record = None
+        return (d.residual.reshape(rs), d.branch.reshape(bs), d.post_weight, d.pre_weight,
+                None if d.gate is None else d.gate.reshape(gs), None, None, None, None, None)
+
+
+def block_norm(residual, branch, post_weight=None, pre_weight=None, gate=None, *, gate_kind: Optional[str] = None,
+               act8: Optional[str] = None, keep_y: bool = False, eps: float = 1e-6, weight_offset: float = 0.0,
+               branch_scale: float = 1.0, residual_scale: float = 1.0):
+    """The join between two blocks (see body.BlockNorm): (y, x), y None without a pre_weight; with keep_y also the record
+    of y for the act8_linear that reads it. The gate is one per channel if its shape is [H], else one per token; gate_kind
+    says so where both fit. With act8 the backward pass reads 8-bit records of branch and x instead of the tensors."""
+    if residual.shape != branch.shape:
+        raise TypeError(f"block_norm: residual {tuple(residual.shape)} and branch {tuple(branch.shape)} differ")
+    if gate is None:
+        gate_kind = "none"
+    elif gate_kind is None:
+        gate_kind = "channel" if gate.shape == branch.shape[-1:] else "token"
+    if keep_y and (act8 is None or pre_weight is None):
+        raise ValueError("block_norm: keep_y needs act8 and a pre_weight")
+    args = dict(eps=eps, weight_offset=weight_offset, branch_scale=branch_scale, residual_scale=residual_scale)
+    y, x, record = _BlockNorm.apply(residual, branch, post_weight, pre_weight, gate, gate_kind, act8, keep_y, args,
+                                    _recorded(residual, branch, post_weight, pre_weight, gate))
+    return (y, x, record) if keep_y else (y, x)

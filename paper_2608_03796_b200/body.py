@@ -40,7 +40,8 @@ _device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStr
 def _rows(t: torch.Tensor, T: int, H: int, dtype, name: str):
     """(address, distance of rows) of a CUDA tensor [T, H] whose rows are contiguous but may lie apart. Refused here,
     as in binding: another device, type or shape, or columns that are not neighbours."""
-    if t.get_device() != _device() or t.dtype is not dtype or t.shape != (T, H):
+    at = t.get_device()
+    if at < 0 or at != _device() or t.dtype is not dtype or t.shape != (T, H):
         if not t.is_cuda or t.device.index != _device():
             raise TypeError(f"kdkl: {name}: expected a tensor on the current CUDA device, got one on {t.device}")
         if t.dtype != dtype:
@@ -59,7 +60,8 @@ def _stream() -> int:
 def _vector(t: Optional[torch.Tensor], n: int, dtype, name: str):
     if t is None:
         return None
-    if t.get_device() == _device() and t.dtype is dtype and t.shape == (n,) and (n <= 1 or t.stride(0) == 1):
+    at = t.get_device()
+    if at >= 0 and at == _device() and t.dtype is dtype and t.shape == (n,) and (n <= 1 or t.stride(0) == 1):
         return t.data_ptr()
     return B._dptr(t, dtype, (n,), name).value                          # says what is wrong
 
@@ -67,15 +69,19 @@ def _vector(t: Optional[torch.Tensor], n: int, dtype, name: str):
 class Act8Record:
     """Activations [T, H] in 8 bits (kdkl_act8_store / kdkl_act8_load). ``buffer`` is the record itself."""
 
-    def __init__(self, T: int, H: int, format: str = "int8", device="cuda"):
+    def __init__(self, T: int, H: int, format: str = "int8", device="cuda", buffer: Optional[torch.Tensor] = None):
+        """With `buffer`, the record that it holds already (one of the same shape and format wrote it)."""
         if format is None:
             raise ValueError("kdkl: a record needs a format")
         self.T, self.H, self.format, self.code = T, H, format, _lookup(FORMATS, format, "format")
         self.nbytes = B.lib().kdkl_act8_bytes(T, H)
         if self.nbytes == 0 and T != 0:
             raise ValueError(f"kdkl: no record of shape {(T, H)}")
-        self.buffer = torch.empty(self.nbytes, dtype=torch.uint8, device=device)
-        self.ptr = self.buffer.data_ptr()
+        if buffer is None:
+            buffer = torch.empty(self.nbytes, dtype=torch.uint8, device=device)
+        elif buffer.dtype != torch.uint8 or not buffer.is_contiguous() or buffer.numel() < self.nbytes:
+            raise TypeError(f"kdkl: a record of shape {(T, H)} is {self.nbytes} contiguous bytes")
+        self.buffer, self.ptr = buffer, buffer.data_ptr()
 
     def store(self, x: torch.Tensor) -> "Act8Record":
         ptr, ld = _rows(x, self.T, self.H, x.dtype, "x")
@@ -134,22 +140,23 @@ class GatedAct:
         self.T, self.F, self.dtype, self.type = T, F, dtype, TYPES[dtype]
         self.act, self.format = _lookup(ACTS, act, "act"), _lookup(FORMATS, act8, "act8")
         self.h = torch.empty(T, F, dtype=dtype, device=device)
+        self.device = self.h.device
         self.gate_record = self.up_record = self.h_record = None
-        self.records = (None, None, None, 0)
         self.dgate_up = None
         if act8 is not None:
             self.gate_record, self.up_record = Act8Record(T, F, act8, device), Act8Record(T, F, act8, device)
             self.h_record = Act8Record(T, F, act8, device) if keep_h else None
-            self.records = (self.gate_record.ptr, self.up_record.ptr, self.h_record.ptr if keep_h else None,
-                            self.gate_record.nbytes)
 
     def forward(self, gate: torch.Tensor, up: torch.Tensor) -> torch.Tensor:
         g, ld = _rows(gate, self.T, self.F, self.dtype, "gate")
         u, ld_u = _rows(up, self.T, self.F, self.dtype, "up")
         if ld_u != ld:
             raise TypeError(f"kdkl: gate and up must have their rows equally far apart, got {ld} and {ld_u}")
+        keep, also = self.gate_record, self.h_record
+        records = (None, None, None, 0) if keep is None else (keep.ptr, self.up_record.ptr,
+                                                              None if also is None else also.ptr, keep.nbytes)
         B._check(B.lib().kdkl_gated_act_forward(g, u, ld, self.type, self.T, self.F, self.act, self.format,
-                                                self.h.data_ptr(), self.F, *self.records, _stream()))
+                                                self.h.data_ptr(), self.F, *records, _stream()))
         return self.h
 
     def backward(self, dh: torch.Tensor):
@@ -157,12 +164,12 @@ class GatedAct:
         if self.gate_record is None:
             raise RuntimeError("kdkl: this gated activation keeps nothing for a backward pass (act8=None)")
         if self.dgate_up is None:
-            self.dgate_up = torch.empty(self.T, 2 * self.F, dtype=self.dtype, device=self.h.device)
+            self.dgate_up = torch.empty(self.T, 2 * self.F, dtype=self.dtype, device=self.device)
             self.halves = self.dgate_up[:, :self.F], self.dgate_up[:, self.F:]
         d, ld = _rows(dh, self.T, self.F, self.dtype, "dh")
         out = self.dgate_up.data_ptr()
         B._check(B.lib().kdkl_gated_act_backward(
-            self.records[0], self.records[1], self.records[3], self.format, d, ld, self.type, self.T, self.F, self.act,
+            self.gate_record.ptr, self.up_record.ptr, self.gate_record.nbytes, self.format, d, ld, self.type, self.T, self.F, self.act,
             out, out + self.F * self.dtype.itemsize, 2 * self.F, _stream()))
         return self.halves
 
@@ -220,24 +227,16 @@ class BlockNorm:
         self.sum = torch.empty(T, H, dtype=residual_dtype, device=device)
         a.y, a.sum = self.y.data_ptr(), self.sum.data_ptr()
         self.branch_record = self.sum_record = self.y_record = None
+        self.workspace = self.dresidual = self.dbranch = None               # made by the first backward call
         if train:
-            nbytes = B.lib().kdkl_block_norm_workspace_bytes(T, H)
-            if nbytes == 0:
+            self.workspace_bytes = B.lib().kdkl_block_norm_workspace_bytes(T, H)
+            if self.workspace_bytes == 0:
                 raise ValueError(f"kdkl: no block norm of shape {(T, H)}")
             self.rho = torch.empty(2, T, dtype=torch.float32, device=device)
             a.rho_post, a.rho_pre = self.rho[0].data_ptr(), self.rho[1].data_ptr()
-            self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
-            a.workspace, a.workspace_bytes = self.workspace.data_ptr(), nbytes
-            self.dresidual = torch.empty(T, H, dtype=residual_dtype, device=device)
-            self.dbranch = torch.empty(T, H, dtype=dtype, device=device)
-            a.dresidual, a.dbranch = self.dresidual.data_ptr(), self.dbranch.data_ptr()
         if keeps:
             self.branch_record, self.sum_record = Act8Record(T, H, act8, device), Act8Record(T, H, act8, device)
-            a.branch_record, a.sum_record = self.branch_record.ptr, self.sum_record.ptr
-            a.record_bytes = self.branch_record.nbytes
-            if keep_y:
-                self.y_record = Act8Record(T, H, act8, device)
-                a.y_record = self.y_record.ptr
+            self.y_record = Act8Record(T, H, act8, device) if keep_y else None
         self.grads = {}
 
     def forward(self, residual, branch, post_weight=None, pre_weight=None, gate=None):
@@ -246,9 +245,9 @@ class BlockNorm:
         a.residual, a.ld_residual = _rows(residual, self.T, self.H, self.residual_dtype, "residual")
         a.branch, a.ld_branch = _rows(branch, self.T, self.H, self.dtype, "branch")
         self._weights(post_weight, pre_weight, gate)
+        self._records()
         B._check(B.lib().kdkl_block_norm_forward(ctypes.byref(a), _stream()))
-        # what the backward call reads is kept alive here
-        self.kept = (branch, post_weight, pre_weight, gate)
+        self.kept = (branch, self.sum, post_weight, pre_weight, gate)           # what the backward call reads
         return (self.y if pre_weight is not None else None), self.sum
 
     def _weights(self, post_weight, pre_weight, gate):
@@ -266,6 +265,13 @@ class BlockNorm:
             a.gate_type = _lookup(TYPES, gate.dtype, "gate")
             a.gate = _vector(gate, H if a.gate_kind == 1 else self.T, gate.dtype, "gate")
 
+    def _records(self):
+        a = self.args
+        if a.format >= 0:
+            a.branch_record, a.sum_record = self.branch_record.ptr, self.sum_record.ptr
+            a.y_record = None if self.y_record is None else self.y_record.ptr
+            a.record_bytes = self.branch_record.nbytes
+
     def _grad(self, name, like):
         """The holder's gradient buffer for a weight or gate (made when first needed, or when its type changes)."""
         if like is None:
@@ -280,7 +286,19 @@ class BlockNorm:
         if not self.train:
             raise RuntimeError("kdkl: this block norm keeps nothing for a backward pass (train=False)")
         a = self.args
-        branch, post_weight, pre_weight, gate = self.kept
+        if self.workspace is None:
+            device = self.rho.device
+            self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=device)
+            self.dresidual = torch.empty(self.T, self.H, dtype=self.residual_dtype, device=device)
+            self.dbranch = torch.empty(self.T, self.H, dtype=self.dtype, device=device)
+            a.workspace, a.workspace_bytes = self.workspace.data_ptr(), self.workspace_bytes
+            a.dresidual, a.dbranch = self.dresidual.data_ptr(), self.dbranch.data_ptr()
+        branch, total, post_weight, pre_weight, gate = self.kept
+        self._weights(post_weight, pre_weight, gate)
+        self._records()
+        if a.format < 0:
+            a.branch, a.ld_branch = _rows(branch, self.T, self.H, self.dtype, "branch")
+            a.sum = _rows(total, self.T, self.H, self.residual_dtype, "sum")[0]
         if (dy is None) != (pre_weight is None):
             raise TypeError("kdkl: dy goes with a pre_weight")
         if dy is not None:

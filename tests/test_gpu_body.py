@@ -271,9 +271,8 @@ def _norm_case(T, H, dtype, rdtype, wdtype, kind, post, pre, fmt, how, with_dsum
     up = lambda t: None if t is None else t.to(_dev())                      # noqa: E731
     op = body.BlockNorm(T, H, dtype=dtype, residual_dtype=rdtype, gate=kind, act8=fmt, eps=eps, weight_offset=offset,
                         branch_scale=alpha, residual_scale=beta, keep_y=fmt is not None and pre)
-    for t in (op.y, op.sum, op.rho, op.dresidual, op.dbranch):
+    for t in (op.y, op.sum, op.rho):
         t.fill_(NAN)
-    op.workspace.fill_(0xFF)
     y, x = op.forward(_placed(r, how), _placed(b, how), post_weight=up(w1), pre_weight=up(w2), gate=up(gate))
     nps = lambda t: None if t is None else _np(t)                           # noqa: E731
     args = dict(w1=nps(w1), w2=nps(w2), gate=nps(gate), kind=kind, offset=offset, alpha=alpha, beta=beta)
