@@ -293,7 +293,7 @@ __device__ __forceinline__ void record_read8(int fmt, const ActRecord& r, long l
 }
 
 // ------------------------------------------------------------------ store and load
-// One thread per eight values; a block covers 2048 columns of the rows blockIdx.y, blockIdx.y + gridDim.y, ... Bound by
+// One thread per eight values; a block covers an even share of the columns, at most 2048, of the rows blockIdx.y, blockIdx.y + gridDim.y, ... Bound by
 // memory. Many short blocks keep more loads in flight than few long ones (128 or 64 an SM against 16: 5 to 10 %); two
 // rows asked for at once pay only where little is done with a row, in load.
 // 32768 x 4096 bf16, one B200: store 70 us (5.8 TB/s), load 64 us (6.4 TB/s, 0.99 of a copy).
@@ -301,7 +301,7 @@ template <typename T, int FMT, bool VEC>
 __global__ void __launch_bounds__(256)
 act8_store_kernel(const T* __restrict__ x, long long ld, long long rows, int H, ActRecord rec) {
   const long long cpitch = act_codes_pitch(H), spitch = act_scale_pitch(H);
-  const int c = (blockIdx.x * 256 + threadIdx.x) * 8;
+  const int c = (blockIdx.x * blockDim.x + threadIdx.x) * 8;
   for (long long t = blockIdx.y; t < rows; t += gridDim.y) {
     float f[8];
     load8<T, VEC>(x + t * ld, c, H, f);
@@ -313,7 +313,7 @@ __global__ void __launch_bounds__(256)
 act8_load_kernel(ActRecord rec, long long rows, int H, T* __restrict__ out, long long ld) {
   constexpr int U = 2;
   const long long cpitch = act_codes_pitch(H), spitch = act_scale_pitch(H);
-  const int c = (blockIdx.x * 256 + threadIdx.x) * 8;
+  const int c = (blockIdx.x * blockDim.x + threadIdx.x) * 8;
   if (c >= H) return;
   for (long long t0 = blockIdx.y; t0 < rows; t0 += (long long)U * gridDim.y) {
     uint2 codes[U];

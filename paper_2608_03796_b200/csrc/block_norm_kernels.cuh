@@ -110,6 +110,33 @@ __device__ __forceinline__ void block_sums_any(float (&x)[N], float* sm) {
   }
 }
 
+// Three sums at once: the first two steps of the butterfly also sort the sums by lane (lane 0: the first, 16: the
+// second, 8: the third), so that the rest reduces one value instead of three. At most 16 warps; `sm` holds 3 * 16 floats.
+__device__ __forceinline__ void block_sums3(float (&x)[3], float* sm) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  const bool up = lane & 16, mid = lane & 8;
+  float k = up ? x[1] : x[0];
+  k += __shfl_xor_sync(0xffffffffu, up ? x[0] : x[1], 16);
+  float third = x[2] + __shfl_xor_sync(0xffffffffu, x[2], 16);
+  const float give = mid ? k : third;
+  k = (mid ? third : k) + __shfl_xor_sync(0xffffffffu, give, 8);
+#pragma unroll
+  for (int o = 4; o; o >>= 1) k += __shfl_xor_sync(0xffffffffu, k, o);
+  if (warps > 1) {
+    const int which = mid ? 2 : up ? 1 : 0;
+    if ((lane & 7) == 0 && lane != 24) sm[which * 16 + warp] = k;
+    __syncthreads();
+    // lane group `which` of eight lanes adds the warps' values of its sum
+    const int q = lane & 7;
+    k = (lane < 24 && q < warps ? sm[(lane >> 3) * 16 + q] : 0.f) + (lane < 24 && q + 8 < warps ? sm[(lane >> 3) * 16 + q + 8] : 0.f);
+#pragma unroll
+    for (int o = 4; o; o >>= 1) k += __shfl_xor_sync(0xffffffffu, k, o);
+    x[0] = __shfl_sync(0xffffffffu, k, 0); x[1] = __shfl_sync(0xffffffffu, k, 8); x[2] = __shfl_sync(0xffffffffu, k, 16);
+  } else {
+    x[0] = __shfl_sync(0xffffffffu, k, 0); x[1] = __shfl_sync(0xffffffffu, k, 16); x[2] = __shfl_sync(0xffffffffu, k, 8);
+  }
+}
+
 struct NormForward {
   const void* residual; long long ld_residual;
   const void* branch; long long ld_branch;
@@ -582,7 +609,7 @@ template <typename A, typename R, int FMT, bool FULL>
 __global__ void __launch_bounds__(kRowsThreads)
 block_norm_backward_rows_kernel(const NormBackward p) {
   extern __shared__ __align__(16) uint8_t smem[];
-  __shared__ float sm[2][3 * 32];
+  __shared__ float sm[2][3 * 16];
   constexpr int kRB = 256 * (int)sizeof(R), kDy = kRB, kBranch = kRB + 512, kSum = kBranch + (FMT >= 0 ? 384 : 512);
   const int H = p.H, threads = blockDim.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const long long cpitch = act_codes_pitch(H), spitch = act_scale_pitch(H);
@@ -686,7 +713,7 @@ block_norm_backward_rows_kernel(const NormBackward p) {
       }
     }
     float s[3] = {sum2(a0), sum2(a1), sum2(a2)};
-    block_sums_any<3>(s, sm[parity]);
+    block_sums3(s, sm[parity]);
     const float k2 = rho2 * rho2 * s[0] * inv_h;             // d = e - k2 x
     const float dot = rho1 * p.alpha * (s[1] - k2 * s[2]);   // sum_h alpha Q b^ d
     if (token && threadIdx.x == 0) any_store(p.dgate_token, p.gate_type, t, dot);

@@ -39,9 +39,10 @@ int kdkl_act8_store(const void* x, int32_t type, int64_t ld, int64_t T, int64_t 
   DeviceInfo di;
   if ((rc = need_b200(&di))) return rc;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
+  const RowsShape shape = rows_shape(T, H, di, 128);
   const ActRecord rec = record_at(record, T, H);
   KDKL_BY_TYPE(type, E, KDKL_BY_FORMAT(format, FMT, KDKL_BY_BOOL(words(x, ld, T, H, type), VEC,
-    (act8_store_kernel<E, FMT, VEC><<<rows_grid(T, H, di, 128), 256, 0, st>>>(reinterpret_cast<const E*>(x), ld, T, (int)H, rec)))));
+    (act8_store_kernel<E, FMT, VEC><<<shape.grid, shape.threads, 0, st>>>(reinterpret_cast<const E*>(x), ld, T, (int)H, rec)))));
   KDKL_LAUNCHED("act8_store_kernel");
   return KDKL_OK;
 }
@@ -59,9 +60,10 @@ int kdkl_act8_load(const void* record, size_t record_bytes, int64_t T, int64_t H
   DeviceInfo di;
   if ((rc = need_b200(&di))) return rc;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
+  const RowsShape shape = rows_shape(T, H, di, 64);
   const ActRecord rec = record_at(record, T, H);
   KDKL_BY_TYPE(type, E, KDKL_BY_FORMAT(format, FMT, KDKL_BY_BOOL(words(out, ld, T, H, type), VEC,
-    (act8_load_kernel<E, FMT, VEC><<<rows_grid(T, H, di, 64), 256, 0, st>>>(rec, T, (int)H, reinterpret_cast<E*>(out), ld)))));
+    (act8_load_kernel<E, FMT, VEC><<<shape.grid, shape.threads, 0, st>>>(rec, T, (int)H, reinterpret_cast<E*>(out), ld)))));
   KDKL_LAUNCHED("act8_load_kernel");
   return KDKL_OK;
 }
@@ -87,9 +89,10 @@ int kdkl_gated_act_forward(const void* gate, const void* up_, int64_t ld, int32_
   DeviceInfo di;
   if ((rc = need_b200(&di))) return rc;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
+  const RowsShape shape = rows_shape(T, F, di, 128);
   const bool vec = words(gate, ld, T, F, type) && words(up_, ld, T, F, type) && words(h, ld_h, T, F, type);
   KDKL_BY_TYPE16(type, E, KDKL_BY_BOOL(act == KDKL_GATED_GELU, GELU, KDKL_BY_FORMAT_OR_NONE(format, FMT, KDKL_BY_BOOL(vec, VEC,
-    (gated_forward_kernel<E, GELU ? kActGelu : kActSilu, FMT, VEC><<<rows_grid(T, F, di, 128), 256, 0, st>>>(
+    (gated_forward_kernel<E, GELU ? kActGelu : kActSilu, FMT, VEC><<<shape.grid, shape.threads, 0, st>>>(
         reinterpret_cast<const E*>(gate), reinterpret_cast<const E*>(up_), ld, T, (int)F, reinterpret_cast<E*>(h), ld_h,
         record_at(gate_record, T, F), record_at(up_record, T, F), record_at(h_record, T, F)))))));
   KDKL_LAUNCHED("gated_forward_kernel");
@@ -112,9 +115,10 @@ int kdkl_gated_act_backward(const void* gate_record, const void* up_record, size
   DeviceInfo di;
   if ((rc = need_b200(&di))) return rc;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
+  const RowsShape shape = rows_shape(T, F, di, 128);
   const bool vec = words(dh, ld_dh, T, F, type) && words(dgate, ld, T, F, type) && words(dup, ld, T, F, type);
   KDKL_BY_TYPE16(type, E, KDKL_BY_BOOL(act == KDKL_GATED_GELU, GELU, KDKL_BY_FORMAT(format, FMT, KDKL_BY_BOOL(vec, VEC,
-    (gated_backward_kernel<E, GELU ? kActGelu : kActSilu, FMT, VEC><<<rows_grid(T, F, di, 128), 256, 0, st>>>(
+    (gated_backward_kernel<E, GELU ? kActGelu : kActSilu, FMT, VEC><<<shape.grid, shape.threads, 0, st>>>(
         record_at(gate_record, T, F), record_at(up_record, T, F), reinterpret_cast<const E*>(dh), ld_dh, T, (int)F,
         reinterpret_cast<E*>(dgate), reinterpret_cast<E*>(dup), ld))))));
   KDKL_LAUNCHED("gated_backward_kernel");

@@ -31,13 +31,18 @@ inline int need_b200(DeviceInfo* di) {
   if (rc) return rc;
   return di->cc_major == 10 ? KDKL_OK : KDKL_ERR_ARCH;
 }
-// Grid of the element-wise kernels: 2048 columns a block in x; in y as many rows as make `per_sm` blocks an SM.
-inline dim3 rows_grid(long long T, long long H, const DeviceInfo& di, int per_sm) {
-  const long long gx = (act_codes_pitch(H) + 2047) / 2048;
+// Launch shape of the element-wise kernels: the columns in even shares of at most 2048 a block; in y as many rows as make
+// `per_sm` blocks an SM.
+struct RowsShape { dim3 grid; int threads; };
+inline RowsShape rows_shape(long long T, long long H, const DeviceInfo& di, int per_sm) {
+  const long long groups = act_codes_pitch(H) / 8, gx = (groups + 255) / 256;
   long long gy = ((long long)di.sm_count * per_sm + gx - 1) / gx;
   if (gy > T) gy = T;
   if (gy > 65535) gy = 65535;
-  return dim3((unsigned)gx, (unsigned)gy, 1);
+  RowsShape r;
+  r.threads = (int)(((groups + gx - 1) / gx + 31) / 32 * 32);
+  r.grid = dim3((unsigned)gx, (unsigned)gy, 1);
+  return r;
 }
 
 // A launch that may start while the kernel before it on the stream drains (that kernel calls grid_dependency_wait).
