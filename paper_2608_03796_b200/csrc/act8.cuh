@@ -67,8 +67,8 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
 __device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
 
 // ------------------------------------------------------------------ eight values of a row
-// VEC: rows start on 16 bytes and H % 8 == 0, so that eight values are whole 16-byte words. Otherwise element by
-// element, and what lies past the row's end reads as 0 and is not written.
+// VEC: rows start on 16 bytes (fp32: 32) and H % 8 == 0, so that eight values are one aligned word of 16 or 32 bytes.
+// Otherwise element by element, and what lies past the row's end reads as 0 and is not written.
 __device__ __forceinline__ float to_f32(float x) { return x; }
 __device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ float to_f32(__half x) { return __half2float(x); }
@@ -124,10 +124,14 @@ template <typename T, bool VEC>
 __device__ __forceinline__ Raw8<T> load_raw8(const T* __restrict__ row, int c, int width) {
   Raw8<T> r;
   if (VEC) {
-    const uint4* p = reinterpret_cast<const uint4*>(row + c);
     if (c < width) {
-      r.v = __ldg(p);
-      if constexpr (sizeof(T) == 4) r.w = __ldg(p + 1);
+      if constexpr (sizeof(T) == 4) {
+        asm volatile("ld.global.nc.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=r"(r.v.x), "=r"(r.v.y), "=r"(r.v.z), "=r"(r.v.w), "=r"(r.w.x), "=r"(r.w.y), "=r"(r.w.z), "=r"(r.w.w)
+                     : "l"(row + c));
+      } else {
+        r.v = __ldg(reinterpret_cast<const uint4*>(row + c));
+      }
     } else {
       r.v = make_uint4(0u, 0u, 0u, 0u);
       if constexpr (sizeof(T) == 4) r.w = r.v;
@@ -148,9 +152,12 @@ template <typename T, bool VEC>
 __device__ __forceinline__ void store_raw8(T* __restrict__ row, int c, int width, const Raw8<T>& r) {
   if (VEC) {
     if (c < width) {
-      uint4* p = reinterpret_cast<uint4*>(row + c);
-      p[0] = r.v;
-      if constexpr (sizeof(T) == 4) p[1] = r.w;
+      if constexpr (sizeof(T) == 4) {
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(row + c), "r"(r.v.x), "r"(r.v.y),
+                     "r"(r.v.z), "r"(r.v.w), "r"(r.w.x), "r"(r.w.y), "r"(r.w.z), "r"(r.w.w) : "memory");
+      } else {
+        *reinterpret_cast<uint4*>(row + c) = r.v;
+      }
     }
   } else {
     float f[8];

@@ -479,12 +479,11 @@ act8_dweight_join_kernel(const float* __restrict__ slabs, int whole, int parts, 
   if (row >= N || col >= H) return;
   const float* src = slabs + ((long long)i * parts * 256 + r) * 256 + c;
   grid_dependency_wait();
-  float f[8], g[8];
-  raw_to_f32(load_raw8<float, true>(src, 0, 8), f);
-  for (int q = 1; q < parts; ++q) {
-    raw_to_f32(load_raw8<float, true>(src + (long long)q * 65536, 0, 8), g);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) f[j] += g[j];
+  float f[8] = {};
+  for (int q = 0; q < parts; ++q) {          // (from L2: the lines were written while this kernel was starting)
+    const float4 a = __ldcg(reinterpret_cast<const float4*>(src + (long long)q * 65536));
+    const float4 b = __ldcg(reinterpret_cast<const float4*>(src + (long long)q * 65536) + 1);
+    f[0] += a.x; f[1] += a.y; f[2] += a.z; f[3] += a.w; f[4] += b.x; f[5] += b.y; f[6] += b.z; f[7] += b.w;
   }
   const long long at = (long long)row * H + col;
   if (type == 1) {

@@ -772,7 +772,7 @@ block_norm_columns_kernel(const float* __restrict__ partial, int parts, int H, l
   if (blockIdx.x * 32 + lane < H) {
     const float* src = partial + p.which[q] * cpitch + blockIdx.x * 32 + lane;
 #pragma unroll 8
-    for (int i = warp; i < parts; i += 32) s += src[(long long)i * 3 * cpitch];
+    for (int i = warp; i < parts; i += 32) s += __ldcg(src + (long long)i * 3 * cpitch);   // from L2: written just now
   }
   sm[warp][lane] = s;
   __syncthreads();

@@ -127,8 +127,8 @@ int kdkl_gated_act_backward(const void* gate_record, const void* up_record, size
 
 // ------------------------------------------------------------------ weight gradient from a record
 // Rows that tensor maps can describe (16 bytes apart): the tensor-core kernel. Others: the FMA kernel.
-static bool dw_mapped(const void* dy, long long ld_dy, long long T, long long N, long long H, const void* out) {
-  return words(dy, ld_dy, T, N, KDKL_TYPE_BF16) && H % 8 == 0 && ((uintptr_t)out & 15) == 0;
+static bool dw_mapped(const void* dy, long long ld_dy, long long T, long long N, long long H, const void* out, int type) {
+  return words(dy, ld_dy, T, N, KDKL_TYPE_BF16) && words(out, H, N, H, type);
 }
 // Which tiles are cut, and into how many parts of the contraction: the choice with the least estimated cycles. A block
 // of 64 tokens takes a unit 600 cycles, starting a unit and draining its tile about five blocks; the slabs of cut tiles
@@ -192,7 +192,7 @@ int kdkl_act8_dweight(const void* dy, int64_t ld_dy, const void* record, size_t 
   cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
   const ActRecord rec = record_at(record, T, H);
   int* status = at<int>(workspace, 0);
-  if (T == 0 || !dw_mapped(dy, ld_dy, T, N, H, dweight)) {
+  if (T == 0 || !dw_mapped(dy, ld_dy, T, N, H, dweight, type)) {
     DweightParams p;
     p.dy = reinterpret_cast<const __nv_bfloat16*>(dy); p.ld_dy = ld_dy;
     p.rec = rec;

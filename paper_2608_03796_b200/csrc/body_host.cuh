@@ -19,9 +19,10 @@ inline ActRecord record_at(const void* record, long long T, long long H) {
   r.scales = record == nullptr ? nullptr : r.codes + act_scales_at(T, H);
   return r;
 }
-// Rows that can be read and written in 16-byte words: start, distance and width.
+// Rows whose groups of eight values are aligned words (16 bytes, 32 of fp32): start, distance and width.
 inline bool words(const void* p, long long ld, long long T, long long H, int type) {
-  return ((uintptr_t)p & 15) == 0 && (T <= 1 || (ld * type_bytes(type)) % 16 == 0) && H % 8 == 0;
+  const int word = 8 * type_bytes(type);
+  return (uintptr_t)p % word == 0 && (T <= 1 || (ld * type_bytes(type)) % word == 0) && H % 8 == 0;
 }
 inline bool shape_ok(long long T, long long H) {
   return T >= 0 && T <= 0x7fffff00ll && H >= 1 && H < (1ll << 30);

@@ -105,7 +105,10 @@ static int launch_rows(long long most, int threads, int smem, const P& p, const 
   return KDKL_OK;
 }
 
-static bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+static bool vectors_are_words(const kdkl_block_norm_args* a) {
+  return words(a->post_weight, 0, 1, a->H, a->weight_type) && words(a->pre_weight, 0, 1, a->H, a->weight_type) &&
+         (a->gate_kind != KDKL_GATE_CHANNEL || words(a->gate, 0, 1, a->H, a->gate_type));
+}
 
 // Threads a row and groups of eight columns a thread of the *_any kernels.
 #define KDKL_NORM_SHAPE(H, vec, VEC, THREADS, NV, ...)                                                       \
@@ -137,9 +140,8 @@ int kdkl_block_norm_forward(const kdkl_block_norm_args* a, void* cuda_stream) {
   p.T = a->T; p.H = (int)a->H; p.gate_kind = a->gate_kind;
   p.eps = a->eps; p.offset = a->weight_offset; p.alpha = a->branch_scale; p.beta = a->residual_scale;
   const bool vec = words(a->residual, a->ld_residual, a->T, a->H, a->residual_type) &&
-                   words(a->branch, a->ld_branch, a->T, a->H, a->type) && aligned16(a->sum) && aligned16(a->y) &&
-                   aligned16(a->post_weight) && aligned16(a->pre_weight) &&
-                   (a->gate_kind != KDKL_GATE_CHANNEL || aligned16(a->gate));
+                   words(a->branch, a->ld_branch, a->T, a->H, a->type) && words(a->sum, a->H, a->T, a->H, a->residual_type) &&
+                   words(a->y, a->H, a->T, a->H, a->type) && vectors_are_words(a);
   const bool any_record = a->format != KDKL_ACT8_NONE && (a->branch_record || a->sum_record || p.rec_y.codes);
   const long long most = (long long)di.sm_count * 8;
   const unsigned grid = (unsigned)(a->T < most ? a->T : most);
@@ -183,11 +185,12 @@ int kdkl_block_norm_backward(const kdkl_block_norm_args* a, void* cuda_stream) {
     p.T = a->T; p.H = (int)a->H; p.gate_kind = a->gate_kind;
     p.offset = a->weight_offset; p.alpha = a->branch_scale; p.beta = a->residual_scale;
     const bool kept = a->format != KDKL_ACT8_NONE ||
-                      (words(a->branch, a->ld_branch, a->T, a->H, a->type) && (!has_pre || aligned16(a->sum)));
+                      (words(a->branch, a->ld_branch, a->T, a->H, a->type) &&
+                       (!has_pre || words(a->sum, a->H, a->T, a->H, a->residual_type)));
     const bool vec = kept && a->H % 8 == 0 && (!has_pre || words(a->dy, a->ld_dy, a->T, a->H, a->type)) &&
-                     (!a->dsum || words(a->dsum, a->ld_dsum, a->T, a->H, a->residual_type)) && aligned16(a->dresidual) &&
-                     aligned16(a->dbranch) && aligned16(a->post_weight) && aligned16(a->pre_weight) &&
-                     (!channel || aligned16(a->gate));
+                     (!a->dsum || words(a->dsum, a->ld_dsum, a->T, a->H, a->residual_type)) &&
+                     words(a->dresidual, a->H, a->T, a->H, a->residual_type) && words(a->dbranch, a->H, a->T, a->H, a->type) &&
+                     vectors_are_words(a);
     if (vec && a->H <= kRowsMaxH) {
       const bool rec = a->format != KDKL_ACT8_NONE, full = has_post && has_pre && a->dsum;
       const int threads = rows_threads(a->H), smem = kRowsStages * (threads / 16) * rows_backward_chunk(type_bytes(a->residual_type), rec);

@@ -409,6 +409,68 @@ def test_other_stream_and_graph_replay():
     assert not torch.equal(got[0], want[0])
 
 
+def test_odd_addresses():
+    """Vectors and results that do not start on 16 or 32 bytes take the element-wise paths and give the same."""
+    T, H, N = 40, 264, 72
+    dev = _dev()
+
+    def off(t, by):                                                         # the same values, `by` elements off the boundary
+        base = torch.empty(t.numel() + 64, dtype=t.dtype, device=dev)
+        v = base[by:by + t.numel()].view(t.shape)
+        return v.copy_(t.to(dev))
+    r, b, dy, dx = (_randn(s, T, H) for s in range(4))
+    w, gate = (1 + 0.1 * _randn(5, H, dtype=F32)), (1 + 0.1 * _randn(6, H, dtype=F32))
+    results = []
+    for by_w, by_x in ((0, 0), (4, 0), (1, 0), (0, 8), (0, 3)):             # fp32: 16 and 4 bytes off; bf16: 16 and 6
+        op = body.BlockNorm(T, H, gate="channel", residual_dtype=F32)
+        y, x = op.forward(off(r.float(), by_w), off(b, by_x), off(w, by_w), off(w, by_w), off(gate, by_w))
+        d = op.backward(off(dy, by_x), off(dx.float(), by_w))
+        results.append([t.clone().double() for t in (y, x, *d)])
+    for other in results[1:]:
+        for s, t in zip(results[0], other):
+            assert ((s - t).norm() / s.norm()).item() <= 1e-3               # the same but for roundings at the last place
+    rec = body.Act8Record(T, H).store(off(r, 0))
+    want = body.Act8WeightGrad(T, N, H, dtype=F32).run(off(_randn(9, T, N), 0), rec)
+    for by in (4, 1):
+        out = off(torch.zeros(N, H), by)
+        body.Act8WeightGrad(T, N, H, dtype=F32).run(off(_randn(9, T, N), 0), rec, out=out)
+        assert ((out - want).norm() / want.norm()).item() <= 1e-5
+        for dtype in (F32, BF16):
+            x = _randn(11, T, H, dtype=dtype)
+            a = body.Act8Record(T, H).store(off(x, by)).load(off(torch.zeros(T, H, dtype=dtype), by))
+            assert torch.equal(a, body.Act8Record(T, H).store(off(x, 0)).load(dtype=dtype))
+
+
+def test_offsets_past_32_bits():
+    """A record of more than 2^32 codes, read and written to its end; the weight gradient over it."""
+    T, H, N = (1 << 20) + 77, 4128, 16
+    x = torch.empty(T, H, dtype=BF16, device=_dev())
+    g = torch.Generator(device=_dev()).manual_seed(1)
+    for t in range(0, T, 1 << 17):
+        x[t:t + (1 << 17)].normal_(generator=g)
+    rec = body.Act8Record(T, H).store(x)
+    assert rec.nbytes > 1 << 32
+    last = body.Act8Record(1000, H).store(x[-1000:]).load()
+    out = torch.empty_like(x)
+    rec.load(out)
+    assert torch.equal(out[-1000:], last)
+    assert torch.equal(out[:1000], body.Act8Record(1000, H).store(x[:1000]).load())
+    dy = _randn(3, T, N, scale=0.1).to(_dev())
+    got = body.Act8WeightGrad(T, N, H, dtype=F32).run(dy, rec)
+    want = torch.zeros(N, H, dtype=torch.float64, device=_dev())
+    for t in range(0, T, 1 << 17):
+        want += dy[t:t + (1 << 17)].double().t() @ out[t:t + (1 << 17)].double()
+    assert ((got.double() - want).norm() / want.norm()).item() <= 1e-5
+    op = body.BlockNorm(T, H, act8="int8")
+    w = torch.ones(H, dtype=BF16, device=_dev())
+    y, s = op.forward(x, x, w, w)
+    tail = body.BlockNorm(1000, H, act8="int8")
+    y2, s2 = tail.forward(x[-1000:], x[-1000:], w, w)
+    assert torch.equal(y[-1000:], y2) and torch.equal(s[-1000:], s2)
+    d, d2 = op.backward(x, x), tail.backward(x[-1000:], x[-1000:])
+    assert torch.equal(d.branch[-1000:], d2.branch) and torch.equal(d.residual[-1000:], d2.residual)
+
+
 def test_no_tokens():
     dev = _dev()
     e = torch.empty(0, 64, dtype=BF16, device=dev)
