@@ -173,13 +173,12 @@ __device__ __forceinline__ void store_raw8(T* __restrict__ row, int c, int width
 // magnitudes, infinities above all numbers and NaNs above those).
 template <int FMT>
 __device__ __forceinline__ uint32_t act_scale_byte(uint32_t amax_bits) {
-  if (amax_bits >= 0x7f800000u) return 255u;
-  // max|x| = (1 + m / 2^23) 2^(E - 127); Q = 1.984375 * 2^6 or 1.75 * 2^8
-  constexpr uint32_t kFrac = FMT == kFmtInt8 ? 0x7e0000u : 0x600000u;
+  // max|x| = (1 + m / 2^23) 2^(E - 127); Q = 1.984375 * 2^6 or 1.75 * 2^8: adding what carries into E where m is beyond
+  // Q's fraction gives E rounded up as needed
+  constexpr uint32_t kCarry = 0x7fffffu - (FMT == kFmtInt8 ? 0x7e0000u : 0x600000u);
   constexpr int kShift = FMT == kFmtInt8 ? 6 : 8;
-  int e = (int)(amax_bits >> 23) - 127 - kShift + ((amax_bits & 0x7fffffu) > kFrac ? 1 : 0);
-  if (e < kActMinExp) e = kActMinExp;     // zeros and subnormal maxima too
-  return (uint32_t)(e + 127);
+  const int byte = max((int)((amax_bits + kCarry) >> 23) - kShift, kActMinExp + 127);    // zeros and subnormal maxima too
+  return amax_bits >= 0x7f800000u ? 255u : (uint32_t)byte;
 }
 __device__ __forceinline__ float act_scale(uint32_t byte) {          // 2^e, NaN for byte 255
   return byte == 255u ? __uint_as_float(0x7fffffffu) : __uint_as_float(byte << 23);
