@@ -87,54 +87,51 @@ __device__ __forceinline__ void block_sums(float (&x)[N], float* sm) {
   }
 }
 
-// the same with a number of threads that is known at run time (whole warps)
-template <int N>
-__device__ __forceinline__ void block_sums_any(float (&x)[N], float* sm) {
-#pragma unroll
-  for (int k = 0; k < N; ++k)
-#pragma unroll
-    for (int o = 16; o; o >>= 1) x[k] += __shfl_xor_sync(0xffffffffu, x[k], o);
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-  if (warps == 1) return;
-  if (lane == 0)
-#pragma unroll
-    for (int k = 0; k < N; ++k) sm[k * 32 + warp] = x[k];
+// The same where the number of threads is known at run time only (whole warps, at most 16): after the barrier every
+// thread reads and adds the warps' values itself, which is quicker than five more dependent shuffles. `sm` holds 16
+// floats a sum, 16-byte aligned; those of warps that do not exist stay 0 (clear_sums).
+__device__ __forceinline__ void clear_sums(float* sm, int n) {
+  for (int i = threadIdx.x; i < n; i += blockDim.x) sm[i] = 0.f;
   __syncthreads();
-#pragma unroll
-  for (int k = 0; k < N; ++k) {
-    float s = (lane & 15) < warps ? sm[k * 32 + (lane & 15)] : 0.f;    // at most 16 warps
-    if (warps > 8) s += __shfl_xor_sync(0xffffffffu, s, 8);
-#pragma unroll
-    for (int o = 4; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    x[k] = __shfl_sync(0xffffffffu, s, 0);
-  }
 }
-
+__device__ __forceinline__ float sum_of_warps(const float* sm) {
+  const float4* p = reinterpret_cast<const float4*>(sm);
+  const float4 a = p[0], b = p[1];
+  float s = ((a.x + a.y) + (a.z + a.w)) + ((b.x + b.y) + (b.z + b.w));
+  if (blockDim.x > 256) {
+    const float4 c = p[2], d = p[3];
+    s += ((c.x + c.y) + (c.z + c.w)) + ((d.x + d.y) + (d.z + d.w));
+  }
+  return s;
+}
+__device__ __forceinline__ float block_sum(float x, float* sm) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  if (blockDim.x == 32) return x;
+  if ((threadIdx.x & 31) == 0) sm[threadIdx.x >> 5] = x;
+  __syncthreads();
+  return sum_of_warps(sm);
+}
 // Three sums at once: the first two steps of the butterfly also sort the sums by lane (lane 0: the first, 16: the
-// second, 8: the third), so that the rest reduces one value instead of three. At most 16 warps; `sm` holds 3 * 16 floats.
+// second, 8: the third), so that the rest reduces one value instead of three.
 __device__ __forceinline__ void block_sums3(float (&x)[3], float* sm) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  const int lane = threadIdx.x & 31;
   const bool up = lane & 16, mid = lane & 8;
   float k = up ? x[1] : x[0];
   k += __shfl_xor_sync(0xffffffffu, up ? x[0] : x[1], 16);
-  float third = x[2] + __shfl_xor_sync(0xffffffffu, x[2], 16);
+  const float third = x[2] + __shfl_xor_sync(0xffffffffu, x[2], 16);
   const float give = mid ? k : third;
   k = (mid ? third : k) + __shfl_xor_sync(0xffffffffu, give, 8);
 #pragma unroll
   for (int o = 4; o; o >>= 1) k += __shfl_xor_sync(0xffffffffu, k, o);
-  if (warps > 1) {
-    const int which = mid ? 2 : up ? 1 : 0;
-    if ((lane & 7) == 0 && lane != 24) sm[which * 16 + warp] = k;
-    __syncthreads();
-    // lane group `which` of eight lanes adds the warps' values of its sum
-    const int q = lane & 7;
-    k = (lane < 24 && q < warps ? sm[(lane >> 3) * 16 + q] : 0.f) + (lane < 24 && q + 8 < warps ? sm[(lane >> 3) * 16 + q + 8] : 0.f);
-#pragma unroll
-    for (int o = 4; o; o >>= 1) k += __shfl_xor_sync(0xffffffffu, k, o);
-    x[0] = __shfl_sync(0xffffffffu, k, 0); x[1] = __shfl_sync(0xffffffffu, k, 8); x[2] = __shfl_sync(0xffffffffu, k, 16);
-  } else {
+  if (blockDim.x == 32) {
     x[0] = __shfl_sync(0xffffffffu, k, 0); x[1] = __shfl_sync(0xffffffffu, k, 16); x[2] = __shfl_sync(0xffffffffu, k, 8);
+    return;
   }
+  if ((lane & 7) == 0 && lane != 24) sm[(mid ? 32 : up ? 16 : 0) + (threadIdx.x >> 5)] = k;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 3; ++i) x[i] = sum_of_warps(sm + 16 * i);
 }
 
 struct NormForward {
@@ -388,9 +385,6 @@ __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool l
 __device__ __forceinline__ void cp_async8(uint32_t dst, const void* src, bool live) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(live ? 8 : 0) : "memory");
 }
-__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src, bool live) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(live ? 4 : 0) : "memory");
-}
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
@@ -433,11 +427,11 @@ __device__ __forceinline__ void v8_write_record(const ActRecord& r, long long t,
 }
 
 // What the next row brings waits in shared memory, in places that only their own thread touches: per group of eight
-// columns and warp one chunk of 32 lanes' places, field after field, so that every address is one of three lane offsets
+// columns and warp one chunk of 32 lanes' places, field after field, so that every address is one of two lane offsets
 // plus a constant.
 struct Places {
-  uint32_t l16, l8, l4;
-  __device__ __forceinline__ Places(uint32_t chunk, int lane) : l16(chunk + lane * 16), l8(chunk + lane * 8), l4(chunk + lane * 4) {}
+  uint32_t l16, l8;
+  __device__ __forceinline__ Places(uint32_t chunk, int lane) : l16(chunk + lane * 16), l8(chunk + lane * 8) {}
 };
 // A row's values [c, c + 8) of 2 or 4 bytes; 4-byte values take two places 512 bytes apart.
 template <typename T, int AT> __device__ __forceinline__ void fetch8(const Places& s, const T* row, int c, bool live) {
@@ -453,15 +447,11 @@ template <typename T, int AT> __device__ __forceinline__ V8 take8(const Places& 
   raw_to_f32(r, f);
   return v8_of(f);
 }
-// Eight codes and, 256 bytes on, the word that holds the group's scale byte.
-template <int AT> __device__ __forceinline__ void fetch_record8(const Places& s, const uint8_t* codes, const uint8_t* scales,
-                                                                int c, bool live) {
-  const uint32_t k = live ? c : 0;
-  cp_async8(s.l8 + AT, codes + k, live);
-  cp_async4(s.l4 + AT + 256, scales + ((k >> 5) & ~3u), live);
+// Eight codes. (The scale bytes come into registers a row ahead: copies of 4 bytes a lane cost a tenth of the kernel.)
+template <int AT> __device__ __forceinline__ void fetch_codes8(const Places& s, const uint8_t* codes, int c, bool live) {
+  cp_async8(s.l8 + AT, codes + (uint32_t)(live ? c : 0), live);
 }
-template <int FMT, int AT> __device__ __forceinline__ V8 take_record8(const Places& s, int shift) {
-  const uint32_t byte = (ld_shared_u32(s.l4 + AT + 256) >> shift) & 0xffu;
+template <int FMT, int AT> __device__ __forceinline__ V8 take_record8(const Places& s, uint32_t byte) {
   const uint2 codes = ld_shared_v2(s.l8 + AT);
   float f[8];
   act_values<FMT>(codes, byte, f);
@@ -470,7 +460,7 @@ template <int FMT, int AT> __device__ __forceinline__ V8 take_record8(const Plac
 // Bytes of a chunk: fields for 32 lanes.
 __host__ __device__ constexpr int rows_forward_chunk(int residual_bytes) { return 512 + 256 * residual_bytes; }
 __host__ __device__ constexpr int rows_backward_chunk(int residual_bytes, bool rec) {
-  return 256 * residual_bytes + 512 + (rec ? 2 * 384 : 512 + 256 * residual_bytes);
+  return 256 * residual_bytes + 512 + (rec ? 2 * 256 : 512 + 256 * residual_bytes);
 }
 
 // FMT -1: no records. FULL: both norms (and, backward, a gradient along the residual stream) are there, which spares the
@@ -479,8 +469,9 @@ template <typename A, typename R, int FMT, bool FULL>
 __global__ void __launch_bounds__(kRowsThreads)
 block_norm_forward_rows_kernel(const NormForward p) {
   extern __shared__ __align__(16) uint8_t smem[];
-  __shared__ float sm[4][32];
+  __shared__ __align__(16) float sm[4][16];
   constexpr int kResidual = 512;        // field offsets: branch, residual
+  clear_sums(sm[0], 64);
   const int H = p.H, threads = blockDim.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const long long cpitch = act_codes_pitch(H), spitch = act_scale_pitch(H);
   const float inv_h = 1.f / (float)H;
@@ -546,9 +537,7 @@ block_norm_forward_rows_kernel(const NormForward p) {
     }
     float rho1 = 1.f;
     if (has_post) {
-      float s[1] = {sum2(acc)};
-      block_sums_any<1>(s, sm[parity]);
-      rho1 = rsqrtf(fmaf(s[0], inv_h, p.eps));
+      rho1 = rsqrtf(fmaf(block_sum(sum2(acc), sm[parity]), inv_h, p.eps));
     }
     const float2 scale = both(rho1 * gate_t);
     acc = both(0.f);
@@ -574,9 +563,7 @@ block_norm_forward_rows_kernel(const NormForward p) {
     }
     float rho2 = 1.f;
     if (has_pre) {
-      float s[1] = {sum2(acc)};
-      block_sums_any<1>(s, sm[parity + 1]);
-      rho2 = rsqrtf(fmaf(s[0], inv_h, p.eps));
+      rho2 = rsqrtf(fmaf(block_sum(sum2(acc), sm[parity + 1]), inv_h, p.eps));
       A* y_row = reinterpret_cast<A*>(p.y) + t * H;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
@@ -609,8 +596,9 @@ template <typename A, typename R, int FMT, bool FULL>
 __global__ void __launch_bounds__(kRowsThreads)
 block_norm_backward_rows_kernel(const NormBackward p) {
   extern __shared__ __align__(16) uint8_t smem[];
-  __shared__ float sm[2][3 * 16];
-  constexpr int kRB = 256 * (int)sizeof(R), kDy = kRB, kBranch = kRB + 512, kSum = kBranch + (FMT >= 0 ? 384 : 512);
+  __shared__ __align__(16) float sm[2][3 * 16];
+  clear_sums(sm[0], 96);
+  constexpr int kRB = 256 * (int)sizeof(R), kDy = kRB, kBranch = kRB + 512, kSum = kBranch + (FMT >= 0 ? 256 : 512);
   const int H = p.H, threads = blockDim.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const long long cpitch = act_codes_pitch(H), spitch = act_scale_pitch(H);
   const float inv_h = 1.f / (float)H;
@@ -621,7 +609,7 @@ block_norm_backward_rows_kernel(const NormBackward p) {
   const uint32_t chunk = smem_u32(smem) + warp * kChunk;
   const uint32_t stage_bytes = (threads >> 4) * kChunk;
   float rho1_next = 1.f, rho2_next = 1.f;
-  uint32_t gate_next = 0u;
+  uint32_t gate_next = 0u, byte_b[2] = {1u, 1u}, byte_x[2] = {1u, 1u};   // (bytes of columns that do not exist)
   auto places = [&](int i, int stage) { return Places(chunk + stage * stage_bytes + i * (stage_bytes / 2), lane); };
   auto fetch = [&](long long t, int stage) {
     if (t < p.T) {
@@ -632,8 +620,8 @@ block_norm_backward_rows_kernel(const NormBackward p) {
       if (has_dx) fetch8<R, 0>(at[i], reinterpret_cast<const R*>(p.dsum) + t * p.ld_dsum, c[i], live);
       if (has_pre) fetch8<A, kDy>(at[i], reinterpret_cast<const A*>(p.dy) + t * p.ld_dy, c[i], live);
       if constexpr (FMT >= 0) {
-        fetch_record8<kBranch>(at[i], p.rec_branch.codes + t * cpitch, p.rec_branch.scales + t * spitch, c[i], live);
-        if (has_pre) fetch_record8<kSum>(at[i], p.rec_sum.codes + t * cpitch, p.rec_sum.scales + t * spitch, c[i], live);
+        fetch_codes8<kBranch>(at[i], p.rec_branch.codes + t * cpitch, c[i], live);
+        if (has_pre) fetch_codes8<kSum>(at[i], p.rec_sum.codes + t * cpitch, c[i], live);
       } else {
         fetch8<A, kBranch>(at[i], reinterpret_cast<const A*>(p.branch) + t * p.ld_branch, c[i], live);
         if (has_pre) fetch8<R, kSum>(at[i], reinterpret_cast<const R*>(p.sum) + t * p.ld_sum, c[i], live);
@@ -647,6 +635,14 @@ block_norm_backward_rows_kernel(const NormBackward p) {
     if (has_post) rho1_next = p.rho_post[t];
     if (has_pre) rho2_next = p.rho_pre[t];
     if (token) gate_next = any_bits(p.gate, t);
+    if constexpr (FMT >= 0) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        if (c[i] >= H) continue;
+        byte_b[i] = __ldg(p.rec_branch.scales + t * spitch + (c[i] >> 5));
+        if (has_pre) byte_x[i] = __ldg(p.rec_sum.scales + t * spitch + (c[i] >> 5));
+      }
+    }
   };
   constexpr int S = kRowsStages;
 #pragma unroll
@@ -675,10 +671,10 @@ block_norm_backward_rows_kernel(const NormBackward p) {
       for (int j = 0; j < 4; ++j) w2[i].p[j] = add2(w.p[j], both(p.offset));
     }
   }
-  const int shift0 = ((c[0] >> 5) & 3) * 8, shift1 = ((c[1] >> 5) & 3) * 8;
   int parity = 0;
   for (long long t = blockIdx.x; t < p.T; t += gridDim.x, parity ^= 1) {
     const float rho1 = rho1_next, rho2 = rho2_next, gate_t = token ? any_value(gate_next, p.gate.type) : 1.f;
+    const uint32_t now_b[2] = {byte_b[0], byte_b[1]}, now_x[2] = {byte_x[0], byte_x[1]};
     fetch(t + (long long)(S - 1) * gridDim.x, stage == 0 ? S - 1 : stage - 1);
     factors(t + gridDim.x);
     cp_async_wait<S - 1>();
@@ -689,10 +685,10 @@ block_norm_backward_rows_kernel(const NormBackward p) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       e[i] = has_dx ? take8<R, 0>(at[i]) : v8_all(0.f);
-      if constexpr (FMT >= 0) b[i] = take_record8<FMT, kBranch>(at[i], i == 0 ? shift0 : shift1);
+      if constexpr (FMT >= 0) b[i] = take_record8<FMT, kBranch>(at[i], now_b[i]);
       else b[i] = take8<A, kBranch>(at[i]);
       if (has_pre) {
-        if constexpr (FMT >= 0) x[i] = take_record8<FMT, kSum>(at[i], i == 0 ? shift0 : shift1);
+        if constexpr (FMT >= 0) x[i] = take_record8<FMT, kSum>(at[i], now_x[i]);
         else x[i] = take8<R, kSum>(at[i]);
         const V8 dy = take8<A, kDy>(at[i]);
 #pragma unroll
