@@ -22,6 +22,8 @@
 
 #include <type_traits>
 
+#include "sm100_prims.cuh"
+
 namespace kdkl {
 
 constexpr int kActGroup = 32;
@@ -308,6 +310,8 @@ __global__ void __launch_bounds__(256)
 act8_store_kernel(const T* __restrict__ x, long long ld, long long rows, int H, ActRecord rec) {
   const long long cpitch = act_codes_pitch(H), spitch = act_scale_pitch(H);
   const int c = (blockIdx.x * blockDim.x + threadIdx.x) * 8;
+  grid_dependents_launch();
+  grid_dependency_wait();
   for (long long t = blockIdx.y; t < rows; t += gridDim.y) {
     float f[8];
     load8<T, VEC>(x + t * ld, c, H, f);
@@ -320,6 +324,8 @@ act8_load_kernel(ActRecord rec, long long rows, int H, T* __restrict__ out, long
   constexpr int U = 2;
   const long long cpitch = act_codes_pitch(H), spitch = act_scale_pitch(H);
   const int c = (blockIdx.x * blockDim.x + threadIdx.x) * 8;
+  grid_dependents_launch();
+  grid_dependency_wait();
   if (c >= H) return;
   for (long long t0 = blockIdx.y; t0 < rows; t0 += (long long)U * gridDim.y) {
     uint2 codes[U];

@@ -48,6 +48,8 @@ act8_dweight_simple_kernel(const DweightParams p) {
   const long long cpitch = act_codes_pitch(p.H), spitch = act_scale_pitch(p.H);
   const int n0 = blockIdx.y * 64, h0 = blockIdx.x * 64;
   const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
+  grid_dependents_launch();
+  grid_dependency_wait();
   clear_status(p.status);
   float acc[4][4] = {};
   for (long long t0 = 0; t0 < p.T; t0 += 16) {
@@ -187,7 +189,7 @@ act8_dweight_kernel(const __grid_constant__ CUtensorMap tmY, const __grid_consta
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();
   const bool leader = rank == 0u;
-  clear_status(p.status);
+  grid_dependents_launch();
   if (threadIdx.x == 0) {
     for (int s = 0; s < C::STAGES; ++s) {
       mbar_init(full(s), 1 + 2 * C::CONVERT_TEAM);
@@ -206,6 +208,8 @@ act8_dweight_kernel(const __grid_constant__ CUtensorMap tmY, const __grid_consta
   cluster_sync_all();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
+  grid_dependency_wait();
+  clear_status(p.status);
 
   const int worker = blockIdx.x >> 1, workers = gridDim.x >> 1;
   const int units = p.whole + p.rest * p.parts;
@@ -476,9 +480,10 @@ act8_dweight_join_kernel(const float* __restrict__ slabs, int whole, int parts, 
                          void* __restrict__ out, int type, int accumulate) {
   const int i = blockIdx.x >> 5, r = (blockIdx.x & 31) * 8 + (threadIdx.x >> 5), c = (threadIdx.x & 31) * 8;
   const int tile = whole + i, row = (tile / h_tiles) * 256 + r, col = (tile % h_tiles) * 256 + c;
-  if (row >= N || col >= H) return;
   const float* src = slabs + ((long long)i * parts * 256 + r) * 256 + c;
+  grid_dependents_launch();
   grid_dependency_wait();
+  if (row >= N || col >= H) return;
   float f[8] = {};
   for (int q = 0; q < parts; ++q) {          // (from L2: the lines were written while this kernel was starting)
     const float4 a = __ldcg(reinterpret_cast<const float4*>(src + (long long)q * 65536));

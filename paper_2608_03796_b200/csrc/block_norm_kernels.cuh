@@ -155,6 +155,8 @@ block_norm_forward_any_kernel(const NormForward p) {
   const int H = p.H;
   const long long cpitch = act_codes_pitch(H), spitch = act_scale_pitch(H);
   const float inv_h = 1.f / (float)H;
+  grid_dependents_launch();
+  grid_dependency_wait();
   for (long long t = blockIdx.x; t < p.T; t += gridDim.x, parity ^= 2) {
     const A* brow = reinterpret_cast<const A*>(p.branch) + t * p.ld_branch;
     const R* rrow = reinterpret_cast<const R*>(p.residual) + t * p.ld_residual;
@@ -261,6 +263,8 @@ block_norm_backward_any_kernel(const NormBackward p) {
   const long long cpitch = act_codes_pitch(H), spitch = act_scale_pitch(H);
   const float inv_h = 1.f / (float)H;
   float dw1[NV][8], dw2[NV][8], dgt[NV][8];
+  grid_dependents_launch();
+  grid_dependency_wait();
 #pragma unroll
   for (int i = 0; i < NV; ++i)
 #pragma unroll
@@ -488,6 +492,8 @@ block_norm_forward_rows_kernel(const NormForward p) {
       fetch8<R, kResidual>(at[i], r, c[i], c[i] < H);
     }
   };
+  grid_dependents_launch();
+  grid_dependency_wait();
   fetch(blockIdx.x);
   V8 k[2], w2[2];                       // alpha (w1 + o) gate_c;  w2 + o
 #pragma unroll
@@ -645,6 +651,8 @@ block_norm_backward_rows_kernel(const NormBackward p) {
     }
   };
   constexpr int S = kRowsStages;
+  grid_dependents_launch();
+  grid_dependency_wait();
 #pragma unroll
   for (int k = 0; k < S - 1; ++k) fetch(blockIdx.x + (long long)k * gridDim.x, k);
   factors(blockIdx.x);
@@ -763,6 +771,7 @@ __global__ void __launch_bounds__(1024)
 block_norm_columns_kernel(const float* __restrict__ partial, int parts, int H, long long cpitch, const NormColumns p) {
   __shared__ float sm[32][33];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, q = blockIdx.y;
+  grid_dependents_launch();
   grid_dependency_wait();
   float s = 0.f;
   if (blockIdx.x * 32 + lane < H) {

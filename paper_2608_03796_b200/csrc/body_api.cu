@@ -42,9 +42,8 @@ int kdkl_act8_store(const void* x, int32_t type, int64_t ld, int64_t T, int64_t 
   const RowsShape shape = rows_shape(T, H, di, 128);
   const ActRecord rec = record_at(record, T, H);
   KDKL_BY_TYPE(type, E, KDKL_BY_FORMAT(format, FMT, KDKL_BY_BOOL(words(x, ld, T, H, type), VEC,
-    (act8_store_kernel<E, FMT, VEC><<<shape.grid, shape.threads, 0, st>>>(reinterpret_cast<const E*>(x), ld, T, (int)H, rec)))));
-  KDKL_LAUNCHED("act8_store_kernel");
-  return KDKL_OK;
+    rc = (launch("act8_store_kernel", act8_store_kernel<E, FMT, VEC>, shape.grid, shape.threads, 0, st, reinterpret_cast<const E*>(x), ld, T, (int)H, rec)))));
+  return rc;
 }
 
 int kdkl_act8_load(const void* record, size_t record_bytes, int64_t T, int64_t H, int32_t format, void* out,
@@ -63,9 +62,8 @@ int kdkl_act8_load(const void* record, size_t record_bytes, int64_t T, int64_t H
   const RowsShape shape = rows_shape(T, H, di, 64);
   const ActRecord rec = record_at(record, T, H);
   KDKL_BY_TYPE(type, E, KDKL_BY_FORMAT(format, FMT, KDKL_BY_BOOL(words(out, ld, T, H, type), VEC,
-    (act8_load_kernel<E, FMT, VEC><<<shape.grid, shape.threads, 0, st>>>(rec, T, (int)H, reinterpret_cast<E*>(out), ld)))));
-  KDKL_LAUNCHED("act8_load_kernel");
-  return KDKL_OK;
+    rc = (launch("act8_load_kernel", act8_load_kernel<E, FMT, VEC>, shape.grid, shape.threads, 0, st, rec, T, (int)H, reinterpret_cast<E*>(out), ld)))));
+  return rc;
 }
 
 // ------------------------------------------------------------------ gated activation
@@ -92,11 +90,10 @@ int kdkl_gated_act_forward(const void* gate, const void* up_, int64_t ld, int32_
   const RowsShape shape = rows_shape(T, F, di, 128);
   const bool vec = words(gate, ld, T, F, type) && words(up_, ld, T, F, type) && words(h, ld_h, T, F, type);
   KDKL_BY_TYPE16(type, E, KDKL_BY_BOOL(act == KDKL_GATED_GELU, GELU, KDKL_BY_FORMAT_OR_NONE(format, FMT, KDKL_BY_BOOL(vec, VEC,
-    (gated_forward_kernel<E, GELU ? kActGelu : kActSilu, FMT, VEC><<<shape.grid, shape.threads, 0, st>>>(
+    rc = (launch("gated_forward_kernel", gated_forward_kernel<E, GELU ? kActGelu : kActSilu, FMT, VEC>, shape.grid, shape.threads, 0, st,
         reinterpret_cast<const E*>(gate), reinterpret_cast<const E*>(up_), ld, T, (int)F, reinterpret_cast<E*>(h), ld_h,
         record_at(gate_record, T, F), record_at(up_record, T, F), record_at(h_record, T, F)))))));
-  KDKL_LAUNCHED("gated_forward_kernel");
-  return KDKL_OK;
+  return rc;
 }
 
 int kdkl_gated_act_backward(const void* gate_record, const void* up_record, size_t record_bytes, int32_t format,
@@ -118,11 +115,10 @@ int kdkl_gated_act_backward(const void* gate_record, const void* up_record, size
   const RowsShape shape = rows_shape(T, F, di, 128);
   const bool vec = words(dh, ld_dh, T, F, type) && words(dgate, ld, T, F, type) && words(dup, ld, T, F, type);
   KDKL_BY_TYPE16(type, E, KDKL_BY_BOOL(act == KDKL_GATED_GELU, GELU, KDKL_BY_FORMAT(format, FMT, KDKL_BY_BOOL(vec, VEC,
-    (gated_backward_kernel<E, GELU ? kActGelu : kActSilu, FMT, VEC><<<shape.grid, shape.threads, 0, st>>>(
+    rc = (launch("gated_backward_kernel", gated_backward_kernel<E, GELU ? kActGelu : kActSilu, FMT, VEC>, shape.grid, shape.threads, 0, st,
         record_at(gate_record, T, F), record_at(up_record, T, F), reinterpret_cast<const E*>(dh), ld_dh, T, (int)F,
         reinterpret_cast<E*>(dgate), reinterpret_cast<E*>(dup), ld))))));
-  KDKL_LAUNCHED("gated_backward_kernel");
-  return KDKL_OK;
+  return rc;
 }
 
 // ------------------------------------------------------------------ weight gradient from a record
@@ -167,9 +163,8 @@ static int launch_dweight(const CUtensorMap& ty, const CUtensorMap& tc, const CU
     if (di.dev >= 0 && di.dev < kMaxDevices) attr_set[di.dev] = true;
   }
   const int units = p.whole + p.rest * p.parts, most = di.sm_count / 2;
-  kern<<<2 * (units < most ? units : most), DwCfg::THREADS, DwCfg::SMEM_BYTES, st>>>(ty, tc, ts, to, tslab, p);
-  KDKL_LAUNCHED("act8_dweight_kernel");
-  return KDKL_OK;
+  return launch("act8_dweight_kernel", kern, dim3(2 * (units < most ? units : most), 1, 1), DwCfg::THREADS,
+                DwCfg::SMEM_BYTES, st, ty, tc, ts, to, tslab, p);
 }
 
 extern "C" {
@@ -201,9 +196,8 @@ int kdkl_act8_dweight(const void* dy, int64_t ld_dy, const void* record, size_t 
     p.status = status;
     const dim3 grid((unsigned)((H + 63) / 64), (unsigned)((N + 63) / 64), 1);
     if (grid.y > 65535) return KDKL_ERR_SHAPE;
-    KDKL_BY_FORMAT(format, FMT, (act8_dweight_simple_kernel<FMT><<<grid, 256, 0, st>>>(p)));
-    KDKL_LAUNCHED("act8_dweight_simple_kernel");
-    return KDKL_OK;
+    KDKL_BY_FORMAT(format, FMT, rc = (launch("act8_dweight_simple_kernel", act8_dweight_simple_kernel<FMT>, grid, 256, 0, st, p)));
+    return rc;
   }
   const DwPlan plan = dw_plan(T, N, H);
   float* slab = at<float>(workspace, 256);
@@ -231,11 +225,8 @@ int kdkl_act8_dweight(const void* dy, int64_t ld_dy, const void* record, size_t 
   KDKL_BY_FORMAT(format, FMT, KDKL_BY_BOOL(type == KDKL_TYPE_F32, F32_OUT,
     rc = (launch_dweight<FMT, F32_OUT>(ty, tc, ts, to, tslab, p, di, st))));
   if (rc || plan.rest == 0) return rc;
-  rc = launch_after(act8_dweight_join_kernel, dim3((unsigned)plan.rest * 32, 1, 1), 256, st, (const float*)slab, plan.whole,
-                    plan.parts, p.h_tiles, (int)N, (int)H, dweight, (int)type, (int)accumulate);
-  if (rc) return rc;
-  KDKL_LAUNCHED("act8_dweight_join_kernel");
-  return KDKL_OK;
+  return launch("act8_dweight_join_kernel", act8_dweight_join_kernel, dim3((unsigned)plan.rest * 32, 1, 1), 256, 0, st, slab,
+                plan.whole, plan.parts, p.h_tiles, N, H, dweight, type, accumulate);
 }
 
 }  // extern "C"

@@ -46,20 +46,24 @@ inline RowsShape rows_shape(long long T, long long H, const DeviceInfo& di, int 
   return r;
 }
 
-// A launch that may start while the kernel before it on the stream drains (that kernel calls grid_dependency_wait).
+// A launch that may start while the kernel before it on the stream drains (every kernel launched so begins with
+// grid_dependency_wait). Measured on one B200: 1 to 2 us less between kernels of 5 to 15 us.
 template <typename... P, typename... Q>
-inline int launch_after(void (*kern)(P...), dim3 grid, int threads, cudaStream_t st, Q... args) {
+inline int launch(const char* name, void (*kern)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, const Q&... args) {
   cudaLaunchConfig_t cfg;
   memset(&cfg, 0, sizeof(cfg));
   cfg.gridDim = grid;
   cfg.blockDim = dim3((unsigned)threads, 1, 1);
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  KDKL_CUDA(cudaLaunchKernelEx(&cfg, kern, P(args)...));
+  cudaError_t e = cudaLaunchKernelEx(&cfg, kern, P(args)...);
+  if (e != cudaSuccess) return cuda_fail(name, e);
+  ++g_launches;
   return KDKL_OK;
 }
 

@@ -37,6 +37,8 @@ gated_forward_kernel(const T* __restrict__ gate, const T* __restrict__ up, long 
                      T* __restrict__ h, long long ld_h, ActRecord rec_gate, ActRecord rec_up, ActRecord rec_h) {
   const long long cpitch = act_codes_pitch(F), spitch = act_scale_pitch(F);
   const int c = (blockIdx.x * blockDim.x + threadIdx.x) * 8;
+  grid_dependents_launch();
+  grid_dependency_wait();
   for (long long t = blockIdx.y; t < rows; t += gridDim.y) {
     float g[8], u[8], o[8];
     load8<T, VEC>(gate + t * ld, c, F, g);
@@ -65,6 +67,8 @@ gated_backward_kernel(ActRecord rec_gate, ActRecord rec_up, const T* __restrict_
                       int F, T* __restrict__ dgate, T* __restrict__ dup, long long ld) {
   const long long cpitch = act_codes_pitch(F), spitch = act_scale_pitch(F);
   const int c = (blockIdx.x * blockDim.x + threadIdx.x) * 8;
+  grid_dependents_launch();
+  grid_dependency_wait();
   if (c >= F) return;
   for (long long t = blockIdx.y; t < rows; t += gridDim.y) {
     float g[8], u[8], d[8], dg[8], du[8];

@@ -100,9 +100,7 @@ static int launch_rows(long long most, int threads, int smem, const P& p, const 
   }
   const long long held = (long long)di.sm_count * fit;
   *blocks = (int)(most < held ? most : held);
-  KERN<<<*blocks, threads, smem, st>>>(p);
-  KDKL_LAUNCHED(name);
-  return KDKL_OK;
+  return launch(name, KERN, dim3((unsigned)*blocks, 1, 1), threads, (size_t)smem, st, p);
 }
 
 static bool vectors_are_words(const kdkl_block_norm_args* a) {
@@ -156,9 +154,9 @@ int kdkl_block_norm_forward(const kdkl_block_norm_args* a, void* cuda_stream) {
   }
   KDKL_BY_TYPE16(a->type, A, KDKL_BY_BOOL(a->residual_type == KDKL_TYPE_F32, WIDE,
     KDKL_BY_BOOL(any_record, REC, KDKL_NORM_SHAPE(a->H, vec, VEC, THREADS, NV,
-      (block_norm_forward_any_kernel<A, std::conditional_t<WIDE, float, A>, REC, THREADS, NV, VEC><<<grid, THREADS, 0, st>>>(p))))));
-  KDKL_LAUNCHED("block_norm_forward_any_kernel");
-  return KDKL_OK;
+      rc = (launch("block_norm_forward_any_kernel", block_norm_forward_any_kernel<A, std::conditional_t<WIDE, float, A>, REC, THREADS, NV, VEC>,
+                   dim3(grid, 1, 1), THREADS, 0, st, p))))));
+  return rc;
 }
 
 int kdkl_block_norm_backward(const kdkl_block_norm_args* a, void* cuda_stream) {
@@ -201,8 +199,10 @@ int kdkl_block_norm_backward(const kdkl_block_norm_args* a, void* cuda_stream) {
     } else {
       KDKL_BY_TYPE16(a->type, A, KDKL_BY_BOOL(a->residual_type == KDKL_TYPE_F32, WIDE,
         KDKL_BY_BOOL(a->format != KDKL_ACT8_NONE, REC, KDKL_NORM_SHAPE(a->H, vec, VEC, THREADS, NV,
-          (block_norm_backward_any_kernel<A, std::conditional_t<WIDE, float, A>, REC, THREADS, NV, VEC><<<(unsigned)parts, THREADS, 0, st>>>(p))))));
-      KDKL_LAUNCHED("block_norm_backward_any_kernel");
+          rc = (launch("block_norm_backward_any_kernel",
+                       block_norm_backward_any_kernel<A, std::conditional_t<WIDE, float, A>, REC, THREADS, NV, VEC>,
+                       dim3((unsigned)parts, 1, 1), THREADS, 0, st, p))))));
+      if (rc) return rc;
     }
   }
   if (has_post || has_pre || channel) {
@@ -213,10 +213,8 @@ int kdkl_block_norm_backward(const kdkl_block_norm_args* a, void* cuda_stream) {
     if (has_post) add(0, a->dpost_weight, a->weight_type);
     if (has_pre) add(1, a->dpre_weight, a->weight_type);
     if (channel) add(2, a->dgate, a->gate_type);
-    rc = launch_after(block_norm_columns_kernel, dim3((unsigned)((a->H + 31) / 32), (unsigned)n, 1), 1024, st,
-                      (const float*)at<float>(a->workspace, 0), parts, (int)a->H, act_codes_pitch(a->H), c);
-    if (rc) return rc;
-    KDKL_LAUNCHED("block_norm_columns_kernel");
+    return launch("block_norm_columns_kernel", block_norm_columns_kernel, dim3((unsigned)((a->H + 31) / 32), (unsigned)n, 1),
+                  1024, 0, st, at<float>(a->workspace, 0), parts, a->H, act_codes_pitch(a->H), c);
   }
   return KDKL_OK;
 }

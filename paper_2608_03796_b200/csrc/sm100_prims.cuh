@@ -47,9 +47,11 @@ __device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
 // microseconds; two seconds means a protocol error, which is reported, not spun on.
 constexpr uint64_t kWaitLimitNs = 2000000000ull;
 
-// For a kernel launched with programmatic stream serialisation: returns when the kernel before it has completed and its
-// writes can be read.
+// Programmatic stream serialisation: a kernel may be launched while the one before it on the stream drains. It calls
+// grid_dependency_wait before it touches memory (returns when all that came before has completed and can be read), and
+// grid_dependents_launch when the next one may be launched, here at its start: whatever follows waits in the same way.
 __device__ __forceinline__ void grid_dependency_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void grid_dependents_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 // One lane of a converged warp.
 __device__ __forceinline__ bool elect_one() {
