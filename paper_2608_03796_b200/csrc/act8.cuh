@@ -69,8 +69,13 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
 __device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
 
 // ------------------------------------------------------------------ eight values of a row
-// VEC: rows start on 16 bytes (fp32: 32) and H % 8 == 0, so that eight values are one aligned word of 16 or 32 bytes.
-// Otherwise element by element, and what lies past the row's end reads as 0 and is not written.
+// Which eight columns a thread has depends on the rows. VEC: they start on 16 bytes (fp32: 32) and H % 8 == 0, so that a
+// thread's columns c .. c + 7 are one aligned word of 16 or 32 bytes and four lanes share a group of a record.
+// Otherwise a warp's lanes take neighbouring columns and a thread every 32nd, c, c + 32, .., c + 224: element by element,
+// but still whole lines a warp, and a group of a record is a warp's. What lies past the row's end reads as 0 and is not
+// written. first_column gives c of the v-th thread of a row (whole warps).
+template <bool VEC> __device__ __forceinline__ int first_column(int v) { return VEC ? 8 * v : (v & ~31) * 8 + (v & 31); }
+template <bool VEC> __device__ __forceinline__ int column(int c, int i) { return VEC ? c + i : c + 32 * i; }
 __device__ __forceinline__ float to_f32(float x) { return x; }
 __device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ float to_f32(__half x) { return __half2float(x); }
@@ -121,7 +126,7 @@ template <> __device__ __forceinline__ Raw8<float> f32_to_raw<float>(const float
   return r;
 }
 
-// columns [c, c + 8) of a row of `width` values; c is a multiple of 8
+// a thread's eight columns of a row of `width` values
 template <typename T, bool VEC>
 __device__ __forceinline__ Raw8<T> load_raw8(const T* __restrict__ row, int c, int width) {
   Raw8<T> r;
@@ -141,7 +146,7 @@ __device__ __forceinline__ Raw8<T> load_raw8(const T* __restrict__ row, int c, i
   } else {
     float f[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = c + i < width ? to_f32(row[c + i]) : 0.f;
+    for (int i = 0; i < 8; ++i) f[i] = column<VEC>(c, i) < width ? to_f32(row[column<VEC>(c, i)]) : 0.f;
     r = f32_to_raw<T>(f);                 // back to the type it came from: exact
   }
   return r;
@@ -166,7 +171,7 @@ __device__ __forceinline__ void store_raw8(T* __restrict__ row, int c, int width
     raw_to_f32(r, f);
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      if (c + i < width) row[c + i] = from_f32<T>(f[i]);
+      if (column<VEC>(c, i) < width) row[column<VEC>(c, i)] = from_f32<T>(f[i]);
   }
 }
 
@@ -266,38 +271,74 @@ __device__ __forceinline__ void act_values(const uint2& codes, uint32_t byte, fl
   }
 }
 
-// Write eight values (columns [c, c + 8) of row t; the four lanes of a group call together) into a record; c < Hp.
-// Values past the row's end are 0.
-template <int FMT>
-__device__ __forceinline__ void record_write8(const ActRecord& r, long long t, long long cpitch, long long spitch, int c,
-                                              const float (&f)[8], bool write) {
-  const uint32_t byte = act_scale_byte<FMT>(group_max(abs_max_bits(f)));
-  const uint2 codes = act_codes<FMT>(f, byte);
-  if (write) *reinterpret_cast<uint2*>(r.codes + t * cpitch + c) = codes;
-  if (write && (c & 31) == 0) r.scales[t * spitch + (c >> 5)] = (uint8_t)byte;
+// One code and what it stands for.
+template <int FMT> __device__ __forceinline__ uint32_t act_code(float x, uint32_t byte) {
+  float f[8] = {x, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  return act_codes<FMT>(f, byte).x & 0xffu;
 }
+template <int FMT> __device__ __forceinline__ float act_value(uint32_t code, uint32_t byte) {
+  float f[8];
+  act_values<FMT>(make_uint2(code, 0u), byte, f);
+  return f[0];
+}
+
+// Write a thread's eight values of row t into a record; the whole warp calls. Values past the row's end are 0.
+template <int FMT, bool VEC>
+__device__ __forceinline__ void record_write8(const ActRecord& r, long long t, long long cpitch, long long spitch, int c,
+                                              const float (&f)[8]) {
+  uint8_t* codes = r.codes + t * cpitch;
+  uint8_t* scales = r.scales + t * spitch;
+  if (VEC) {
+    const uint32_t byte = act_scale_byte<FMT>(group_max(abs_max_bits(f)));
+    const uint2 v = act_codes<FMT>(f, byte);
+    if (c < cpitch) *reinterpret_cast<uint2*>(codes + c) = v;
+    if (c < cpitch && (c & 31) == 0) scales[c >> 5] = (uint8_t)byte;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int col = column<VEC>(c, i);
+      const uint32_t byte = act_scale_byte<FMT>(__reduce_max_sync(0xffffffffu, __float_as_uint(f[i]) & 0x7fffffffu));
+      const uint32_t code = act_code<FMT>(f[i], byte);
+      if (col < cpitch) codes[col] = (uint8_t)code;
+      if (col < cpitch && (col & 31) == 0) scales[col >> 5] = (uint8_t)byte;
+    }
+  }
+}
+// eight neighbouring codes and their scale byte, for act_values
 __device__ __forceinline__ void record_fetch8(const ActRecord& r, long long t, long long cpitch, long long spitch, int c,
                                               uint2& codes, uint32_t& byte) {
   codes = __ldg(reinterpret_cast<const uint2*>(r.codes + t * cpitch + c));
   byte = __ldg(r.scales + t * spitch + (c >> 5));
 }
-template <int FMT>
+// a thread's eight values; 0 past the end
+template <int FMT, bool VEC>
 __device__ __forceinline__ void record_read8(const ActRecord& r, long long t, long long cpitch, long long spitch, int c,
                                              float (&f)[8]) {
-  const uint2 codes = __ldg(reinterpret_cast<const uint2*>(r.codes + t * cpitch + c));
-  act_values<FMT>(codes, __ldg(r.scales + t * spitch + (c >> 5)), f);
+  if (VEC) {
+    uint2 codes = make_uint2(0u, 0u);
+    uint32_t byte = 1u;
+    if (c < cpitch) record_fetch8(r, t, cpitch, spitch, c, codes, byte);
+    act_values<FMT>(codes, byte, f);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int col = column<VEC>(c, i);
+      f[i] = col < cpitch ? act_value<FMT>(__ldg(r.codes + t * cpitch + col), __ldg(r.scales + t * spitch + (col >> 5))) : 0.f;
+    }
+  }
 }
-
 // The same with a format that is known at run time, uniform over a launch.
+template <bool VEC>
 __device__ __forceinline__ void record_write8(int fmt, const ActRecord& r, long long t, long long cpitch, long long spitch,
-                                              int c, const float (&f)[8], bool write) {
-  if (fmt == kFmtInt8) record_write8<kFmtInt8>(r, t, cpitch, spitch, c, f, write);
-  else record_write8<kFmtE4M3>(r, t, cpitch, spitch, c, f, write);
+                                              int c, const float (&f)[8]) {
+  if (fmt == kFmtInt8) record_write8<kFmtInt8, VEC>(r, t, cpitch, spitch, c, f);
+  else record_write8<kFmtE4M3, VEC>(r, t, cpitch, spitch, c, f);
 }
+template <bool VEC>
 __device__ __forceinline__ void record_read8(int fmt, const ActRecord& r, long long t, long long cpitch, long long spitch,
                                              int c, float (&f)[8]) {
-  if (fmt == kFmtInt8) record_read8<kFmtInt8>(r, t, cpitch, spitch, c, f);
-  else record_read8<kFmtE4M3>(r, t, cpitch, spitch, c, f);
+  if (fmt == kFmtInt8) record_read8<kFmtInt8, VEC>(r, t, cpitch, spitch, c, f);
+  else record_read8<kFmtE4M3, VEC>(r, t, cpitch, spitch, c, f);
 }
 
 // ------------------------------------------------------------------ store and load
@@ -309,43 +350,51 @@ template <typename T, int FMT, bool VEC>
 __global__ void __launch_bounds__(256)
 act8_store_kernel(const T* __restrict__ x, long long ld, long long rows, int H, ActRecord rec) {
   const long long cpitch = act_codes_pitch(H), spitch = act_scale_pitch(H);
-  const int c = (blockIdx.x * blockDim.x + threadIdx.x) * 8;
+  const int c = first_column<VEC>(blockIdx.x * blockDim.x + threadIdx.x);
   grid_dependents_launch();
   grid_dependency_wait();
   for (long long t = blockIdx.y; t < rows; t += gridDim.y) {
     float f[8];
     load8<T, VEC>(x + t * ld, c, H, f);
-    record_write8<FMT>(rec, t, cpitch, spitch, c, f, c < cpitch);
+    record_write8<FMT, VEC>(rec, t, cpitch, spitch, c, f);
   }
 }
 template <typename T, int FMT, bool VEC>
 __global__ void __launch_bounds__(256)
 act8_load_kernel(ActRecord rec, long long rows, int H, T* __restrict__ out, long long ld) {
-  constexpr int U = 2;
   const long long cpitch = act_codes_pitch(H), spitch = act_scale_pitch(H);
-  const int c = (blockIdx.x * blockDim.x + threadIdx.x) * 8;
+  const int c = first_column<VEC>(blockIdx.x * blockDim.x + threadIdx.x);
   grid_dependents_launch();
   grid_dependency_wait();
   if (c >= H) return;
-  for (long long t0 = blockIdx.y; t0 < rows; t0 += (long long)U * gridDim.y) {
-    uint2 codes[U];
-    uint32_t bytes[U];
+  auto put = [&](float (&f)[8], long long t) {
+    if constexpr (std::is_same<T, __half>::value) {       // a code rounded up past the largest fp16 value
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const long long t = t0 + (long long)u * gridDim.y;
-      if (t < rows) record_fetch8(rec, t, cpitch, spitch, c, codes[u], bytes[u]);
+      for (int i = 0; i < 8; ++i) f[i] = f[i] > 65504.f ? 65504.f : f[i] < -65504.f ? -65504.f : f[i];
     }
+    store_raw8<T, VEC>(out + t * ld, c, H, f32_to_raw<T>(f));
+  };
+  constexpr int U = VEC ? 2 : 1;
+  for (long long t0 = blockIdx.y; t0 < rows; t0 += (long long)U * gridDim.y) {
+    float f[8];
+    if constexpr (VEC) {
+      uint2 codes[U];
+      uint32_t bytes[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const long long t = t0 + (long long)u * gridDim.y;
-      if (t >= rows) break;
-      float f[8];
-      act_values<FMT>(codes[u], bytes[u], f);
-      if constexpr (std::is_same<T, __half>::value) {     // a code rounded up past the largest fp16 value
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = f[i] > 65504.f ? 65504.f : f[i] < -65504.f ? -65504.f : f[i];
+      for (int u = 0; u < U; ++u) {
+        const long long t = t0 + (long long)u * gridDim.y;
+        if (t < rows) record_fetch8(rec, t, cpitch, spitch, c, codes[u], bytes[u]);
       }
-      store_raw8<T, VEC>(out + t * ld, c, H, f32_to_raw<T>(f));
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const long long t = t0 + (long long)u * gridDim.y;
+        if (t >= rows) break;
+        act_values<FMT>(codes[u], bytes[u], f);
+        put(f, t);
+      }
+    } else {
+      record_read8<FMT, VEC>(rec, t0, cpitch, spitch, c, f);
+      put(f, t0);
     }
   }
 }

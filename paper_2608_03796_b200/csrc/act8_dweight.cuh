@@ -62,7 +62,7 @@ act8_dweight_simple_kernel(const DweightParams p) {
       const long long t = t0 + threadIdx.x / 8;
       const int c = h0 + (threadIdx.x % 8) * 8;
       float f[8] = {};
-      if (t < p.T && c < cpitch) record_read8<FMT>(p.rec, t, cpitch, spitch, c, f);
+      if (t < p.T && c < cpitch) record_read8<FMT, true>(p.rec, t, cpitch, spitch, c, f);
 #pragma unroll
       for (int j = 0; j < 8; ++j) b[threadIdx.x / 8][(threadIdx.x % 8) * 8 + j] = f[j];
     }

@@ -53,7 +53,7 @@ __device__ __forceinline__ void any_load8(const AnyVec& v, int c, int width, flo
     else load8<__half, true>(reinterpret_cast<const __half*>(v.p), c, width, f);
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = c + i < width ? any_at(v, c + i) : 0.f;
+    for (int i = 0; i < 8; ++i) f[i] = column<VEC>(c, i) < width ? any_at(v, column<VEC>(c, i)) : 0.f;
   }
 }
 __device__ __forceinline__ void any_store(void* p, int type, long long i, float x) {
@@ -157,17 +157,33 @@ block_norm_forward_any_kernel(const NormForward p) {
   const float inv_h = 1.f / (float)H;
   grid_dependents_launch();
   grid_dependency_wait();
+  float k[NV][8], w2[NV][8];            // alpha (w1 + o) gate_c;  w2 + o
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = first_column<VEC>(threadIdx.x + i * THREADS);
+    float w[8], g[8];
+    if (p.post.p != nullptr) any_load8<VEC>(p.post, c, H, w);
+    if (p.gate_kind == kGateChannel) any_load8<VEC>(p.gate, c, H, g);
+    if (p.pre.p != nullptr) any_load8<VEC>(p.pre, c, H, w2[i]);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      k[i][j] = p.alpha;
+      if (p.post.p != nullptr) k[i][j] *= w[j] + p.offset;
+      if (p.gate_kind == kGateChannel) k[i][j] *= g[j];
+      w2[i][j] = p.pre.p != nullptr ? w2[i][j] + p.offset : 0.f;
+    }
+  }
   for (long long t = blockIdx.x; t < p.T; t += gridDim.x, parity ^= 2) {
     const A* brow = reinterpret_cast<const A*>(p.branch) + t * p.ld_branch;
     const R* rrow = reinterpret_cast<const R*>(p.residual) + t * p.ld_residual;
     float b[NV][8], x[NV][8];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int c = (threadIdx.x + i * THREADS) * 8;
+      const int c = first_column<VEC>(threadIdx.x + i * THREADS);
       load8<A, VEC>(brow, c, H, b[i]);
       load8<R, VEC>(rrow, c, H, x[i]);
       if constexpr (REC) {
-        if (p.rec_branch.codes != nullptr) record_write8(p.format, p.rec_branch, t, cpitch, spitch, c, b[i], c < cpitch);
+        if (p.rec_branch.codes != nullptr) record_write8<VEC>(p.format, p.rec_branch, t, cpitch, spitch, c, b[i]);
       }
     }
     float rho1 = 1.f;
@@ -180,24 +196,16 @@ block_norm_forward_any_kernel(const NormForward p) {
       block_sums<1, THREADS>(s, sm[parity]);
       rho1 = 1.f / sqrtf(fmaf(s[0], inv_h, p.eps));
     }
-    float scale = p.alpha * rho1;
+    float scale = rho1;
     if (p.gate_kind == kGateToken) scale *= any_at(p.gate, t);
     float s[1] = {0.f};
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = (threadIdx.x + i * THREADS) * 8;
-      float w[8], g[8];
-      if (p.post.p != nullptr) any_load8<VEC>(p.post, c, H, w);
-      if (p.gate_kind == kGateChannel) any_load8<VEC>(p.gate, c, H, g);
+    for (int i = 0; i < NV; ++i)
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        float k = scale;
-        if (p.post.p != nullptr) k *= w[j] + p.offset;
-        if (p.gate_kind == kGateChannel) k *= g[j];
-        x[i][j] = fmaf(k, b[i][j], p.beta * x[i][j]);
+        x[i][j] = fmaf(scale * k[i][j], b[i][j], p.beta * x[i][j]);
         s[0] = fmaf(x[i][j], x[i][j], s[0]);
       }
-    }
     float rho2 = 1.f;
     if (p.pre.p != nullptr) {
       block_sums<1, THREADS>(s, sm[parity + 1]);
@@ -209,28 +217,26 @@ block_norm_forward_any_kernel(const NormForward p) {
     }
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int c = (threadIdx.x + i * THREADS) * 8;
+      const int c = first_column<VEC>(threadIdx.x + i * THREADS);
       const Raw8<R> raw = f32_to_raw<R>(x[i]);
       store_raw8<R, VEC>(reinterpret_cast<R*>(p.sum) + t * H, c, H, raw);
       if constexpr (REC) {
         if (p.rec_sum.codes != nullptr) {             // what a record of the returned sum would hold
           float v[8];
           raw_to_f32(raw, v);
-          record_write8(p.format, p.rec_sum, t, cpitch, spitch, c, v, c < cpitch);
+          record_write8<VEC>(p.format, p.rec_sum, t, cpitch, spitch, c, v);
         }
       }
       if (p.pre.p != nullptr) {
-        float w[8];
-        any_load8<VEC>(p.pre, c, H, w);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[i][j] *= rho2 * (w[j] + p.offset);
+        for (int j = 0; j < 8; ++j) x[i][j] *= rho2 * w2[i][j];
         const Raw8<A> yr = f32_to_raw<A>(x[i]);
         store_raw8<A, VEC>(reinterpret_cast<A*>(p.y) + t * H, c, H, yr);
         if constexpr (REC) {
           if (p.rec_y.codes != nullptr) {
             float v[8];
             raw_to_f32(yr, v);
-            record_write8(p.format, p.rec_y, t, cpitch, spitch, c, v, c < cpitch);
+            record_write8<VEC>(p.format, p.rec_y, t, cpitch, spitch, c, v);
           }
         }
       }
@@ -255,126 +261,106 @@ struct NormBackward {
   float offset, alpha, beta;
 };
 
+// With Q = gate_c (w1 + o), sigma = alpha rho1 gate_t, u = dy rho2 and x, b as kept (not normalised):
+//   e = dx + u (w2 + o),  c2 = rho2 mean(u x (w2 + o)),  d = e - rho2 c2 x
+//   A = sum_t sigma d b     (per column; dw1 = gate_c A, dgate_c = (w1 + o) A),   dw2 = sum_t u x
+//   db = sigma Q d - rho1^2 c1 b
+// so a column needs one sum for the gate and the post weight together.
 template <typename A, typename R, bool REC, int THREADS, int NV, bool VEC>
 __global__ void __launch_bounds__(THREADS)
 block_norm_backward_any_kernel(const NormBackward p) {
-  __shared__ float sm[2][4 * 32];
+  __shared__ float sm[2][3 * 32];
   const int H = p.H;
   const long long cpitch = act_codes_pitch(H), spitch = act_scale_pitch(H);
   const float inv_h = 1.f / (float)H;
-  float dw1[NV][8], dw2[NV][8], dgt[NV][8];
+  const bool has_post = p.post.p != nullptr, has_pre = p.pre.p != nullptr;
+  const bool channel = p.gate_kind == kGateChannel, token = p.gate_kind == kGateToken;
+  float q[NV][8], w2[NV][8], sum_a[NV][8], sum_w[NV][8];     
   grid_dependents_launch();
   grid_dependency_wait();
 #pragma unroll
-  for (int i = 0; i < NV; ++i)
+  for (int i = 0; i < NV; ++i) {
+    const int c = first_column<VEC>(threadIdx.x + i * THREADS);
+    float g[8];
+    if (has_post) any_load8<VEC>(p.post, c, H, q[i]);
+    if (channel) any_load8<VEC>(p.gate, c, H, g);
+    if (has_pre) any_load8<VEC>(p.pre, c, H, w2[i]);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) dw1[i][j] = dw2[i][j] = dgt[i][j] = 0.f;
-  const bool has_post = p.post.p != nullptr, has_pre = p.pre.p != nullptr;
-  const bool channel = p.gate_kind == kGateChannel, token = p.gate_kind == kGateToken;
+    for (int j = 0; j < 8; ++j) {
+      q[i][j] = has_post ? q[i][j] + p.offset : 1.f;
+      if (channel) q[i][j] *= g[j];
+      w2[i][j] = has_pre ? w2[i][j] + p.offset : 0.f;
+      sum_a[i][j] = sum_w[i][j] = 0.f;
+    }
+  }
   int parity = 0;
   for (long long t = blockIdx.x; t < p.T; t += gridDim.x, parity ^= 1) {
     const float rho1 = has_post ? p.rho_post[t] : 1.f, rho2 = has_pre ? p.rho_pre[t] : 1.f;
-    const float scale = token ? p.alpha * any_at(p.gate, t) : p.alpha;
-    float d[NV][8], gy[NV][8], bh[NV][8], xh[NV][8];
-    float s[4] = {0.f, 0.f, 0.f, 0.f};   // gy x^;  q b^ (dx + rho2 gy);  q b^ x^   with q = alpha gate_c (w1 + o)
+    const float gate_t = token ? any_at(p.gate, t) : 1.f;
+    float e[NV][8], b[NV][8], x[NV][8];
+    float s[3] = {0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int c = (threadIdx.x + i * THREADS) * 8;
+      const int c = first_column<VEC>(threadIdx.x + i * THREADS);
       if constexpr (REC) {
-        if (c < cpitch) {
-          record_read8(p.format, p.rec_branch, t, cpitch, spitch, c, bh[i]);
-          if (has_pre) record_read8(p.format, p.rec_sum, t, cpitch, spitch, c, xh[i]);
-        } else {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) bh[i][j] = xh[i][j] = 0.f;
-        }
+        record_read8<VEC>(p.format, p.rec_branch, t, cpitch, spitch, c, b[i]);
+        if (has_pre) record_read8<VEC>(p.format, p.rec_sum, t, cpitch, spitch, c, x[i]);
       } else {
-        load8<A, VEC>(reinterpret_cast<const A*>(p.branch) + t * p.ld_branch, c, H, bh[i]);
-        if (has_pre) load8<R, VEC>(reinterpret_cast<const R*>(p.sum) + t * p.ld_sum, c, H, xh[i]);
+        load8<A, VEC>(reinterpret_cast<const A*>(p.branch) + t * p.ld_branch, c, H, b[i]);
+        if (has_pre) load8<R, VEC>(reinterpret_cast<const R*>(p.sum) + t * p.ld_sum, c, H, x[i]);
       }
-      if (p.dsum != nullptr) {
-        load8<R, VEC>(reinterpret_cast<const R*>(p.dsum) + t * p.ld_dsum, c, H, d[i]);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) d[i][j] = 0.f;
-      }
-      float q[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) q[j] = p.alpha;
-      if (has_post) {
-        float w[8];
-        any_load8<VEC>(p.post, c, H, w);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) q[j] *= w[j] + p.offset;
-      }
-      if (channel) {
-        float g[8];
-        any_load8<VEC>(p.gate, c, H, g);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) q[j] *= g[j];
-      }
-      if (has_pre) {
-        float w[8], dy[8];
-        any_load8<VEC>(p.pre, c, H, w);
-        load8<A, VEC>(reinterpret_cast<const A*>(p.dy) + t * p.ld_dy, c, H, dy);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          xh[i][j] *= rho2;
-          dw2[i][j] = fmaf(dy[j], xh[i][j], dw2[i][j]);
-          gy[i][j] = dy[j] * (w[j] + p.offset);
-          s[0] = fmaf(gy[i][j], xh[i][j], s[0]);
-          d[i][j] = fmaf(rho2, gy[i][j], d[i][j]);
-        }
-      }
+      float dy[8];
+      if (p.dsum != nullptr) load8<R, VEC>(reinterpret_cast<const R*>(p.dsum) + t * p.ld_dsum, c, H, e[i]);
+      if (has_pre) load8<A, VEC>(reinterpret_cast<const A*>(p.dy) + t * p.ld_dy, c, H, dy);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        bh[i][j] *= rho1;
-        const float qb = q[j] * bh[i][j];
-        s[1] = fmaf(qb, d[i][j], s[1]);
-        if (has_pre) s[2] = fmaf(qb, xh[i][j], s[2]);
+        if (p.dsum == nullptr) e[i][j] = 0.f;
+        if (has_pre) {
+          const float u = dy[j] * rho2, ux = u * x[i][j];
+          sum_w[i][j] += ux;
+          s[0] = fmaf(ux, w2[i][j], s[0]);
+          e[i][j] = fmaf(u, w2[i][j], e[i][j]);
+        } else {
+          x[i][j] = 0.f;
+        }
+        const float qb = q[i][j] * b[i][j];
+        s[1] = fmaf(qb, e[i][j], s[1]);
+        s[2] = fmaf(qb, x[i][j], s[2]);
       }
     }
-    block_sums<4, THREADS>(s, sm[parity]);
-    const float c2 = s[0] * inv_h;
-    const float dot = s[1] - c2 * rho2 * s[2];         // sum_h q b^ d
-    const float c1 = has_post ? dot * (token ? any_at(p.gate, t) : 1.f) * inv_h : 0.f;
+    block_sums<3, THREADS>(s, sm[parity]);
+    const float k2 = rho2 * rho2 * s[0] * inv_h, dot = rho1 * p.alpha * (s[1] - k2 * s[2]);
     if (token && threadIdx.x == 0) any_store(p.dgate_token, p.gate_type, t, dot);
+    const float sigma = p.alpha * rho1 * gate_t, tau = has_post ? -rho1 * rho1 * dot * gate_t * inv_h : 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int c = (threadIdx.x + i * THREADS) * 8;
-      float k[8], o[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) k[j] = scale;
-      if (channel) {
-        float g[8];
-        any_load8<VEC>(p.gate, c, H, g);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) k[j] *= g[j];
-      }
-      float w[8];
-      if (has_post) any_load8<VEC>(p.post, c, H, w);
+      const int c = first_column<VEC>(threadIdx.x + i * THREADS);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float wj = has_post ? w[j] + p.offset : 1.f;
-        const float dj = has_pre ? fmaf(-c2 * rho2, xh[i][j], d[i][j]) : d[i][j];
-        const float dn = k[j] * dj;
-        if (has_post) dw1[i][j] = fmaf(dn, bh[i][j], dw1[i][j]);
-        if (channel) dgt[i][j] = fmaf(p.alpha * dj * wj, bh[i][j], dgt[i][j]);
-        d[i][j] = p.beta * dj;
-        o[j] = rho1 * fmaf(-c1, bh[i][j], dn * wj);
+        const float d = fmaf(-k2, x[i][j], e[i][j]), sd = d * sigma;
+        sum_a[i][j] = fmaf(sd, b[i][j], sum_a[i][j]);
+        e[i][j] = p.beta * d;
+        b[i][j] = fmaf(q[i][j], sd, tau * b[i][j]);
       }
-      store_raw8<R, VEC>(reinterpret_cast<R*>(p.dresidual) + t * H, c, H, f32_to_raw<R>(d[i]));
-      store_raw8<A, VEC>(reinterpret_cast<A*>(p.dbranch) + t * H, c, H, f32_to_raw<A>(o));
+      store_raw8<R, VEC>(reinterpret_cast<R*>(p.dresidual) + t * H, c, H, f32_to_raw<R>(e[i]));
+      store_raw8<A, VEC>(reinterpret_cast<A*>(p.dbranch) + t * H, c, H, f32_to_raw<A>(b[i]));
     }
   }
   float* out = p.partial + (long long)blockIdx.x * 3 * cpitch;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int c = (threadIdx.x + i * THREADS) * 8;
-    if (c >= cpitch) continue;
-    if (has_post) store_raw8<float, true>(out, c, (int)cpitch, f32_to_raw<float>(dw1[i]));
-    if (has_pre) store_raw8<float, true>(out + cpitch, c, (int)cpitch, f32_to_raw<float>(dw2[i]));
-    if (channel) store_raw8<float, true>(out + 2 * cpitch, c, (int)cpitch, f32_to_raw<float>(dgt[i]));
+    const int c = first_column<VEC>(threadIdx.x + i * THREADS);
+    if (c >= H) continue;
+    float w[8], g[8], v[8];
+    if (has_post) any_load8<VEC>(p.post, c, H, w);
+    if (channel) any_load8<VEC>(p.gate, c, H, g);
+    if (has_pre) store_raw8<float, VEC>(out + cpitch, c, (int)cpitch, f32_to_raw<float>(sum_w[i]));
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = channel ? sum_a[i][j] * g[j] : sum_a[i][j];
+    if (has_post) store_raw8<float, VEC>(out, c, (int)cpitch, f32_to_raw<float>(v));
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = has_post ? sum_a[i][j] * (w[j] + p.offset) : sum_a[i][j];
+    if (channel) store_raw8<float, VEC>(out + 2 * cpitch, c, (int)cpitch, f32_to_raw<float>(v));
   }
 }
 
@@ -427,7 +413,7 @@ __device__ __forceinline__ void v8_write_record(const ActRecord& r, long long t,
                                                 int c, const V8& v) {
   float f[8];
   v8_to(v, f);
-  record_write8<FMT>(r, t, cpitch, spitch, c, f, c < cpitch);
+  record_write8<FMT, true>(r, t, cpitch, spitch, c, f);
 }
 
 // What the next row brings waits in shared memory, in places that only their own thread touches: per group of eight
@@ -563,7 +549,7 @@ block_norm_forward_rows_kernel(const NormForward p) {
         if (p.rec_sum.codes != nullptr) {              // what a record of the returned sum would hold
           float f[8];
           raw_to_f32(raw, f);
-          record_write8<FMT>(p.rec_sum, t, cpitch, spitch, c[i], f, c[i] < cpitch);
+          record_write8<FMT, true>(p.rec_sum, t, cpitch, spitch, c[i], f);
         }
       }
     }
@@ -581,7 +567,7 @@ block_norm_forward_rows_kernel(const NormForward p) {
           if (p.rec_y.codes != nullptr) {
             float f[8];
             raw_to_f32(raw, f);
-            record_write8<FMT>(p.rec_y, t, cpitch, spitch, c[i], f, c[i] < cpitch);
+            record_write8<FMT, true>(p.rec_y, t, cpitch, spitch, c[i], f);
           }
         }
       }
@@ -593,11 +579,6 @@ block_norm_forward_rows_kernel(const NormForward p) {
   }
 }
 
-// With Q = gate_c (w1 + o), sigma = alpha rho1 gate_t, u = dy rho2 and x, b as kept (not normalised):
-//   e = dx + u w2',  c2 = rho2 mean(u x w2'),  d = e - rho2 c2 x
-//   A = sum_t sigma d b     (per column; dw1 = gate_c A, dgate_c = (w1 + o) A),   dw2 = sum_t u x
-//   db = sigma Q d - rho1^2 c1 b
-// so a column needs one sum for the gate and the post weight together.
 template <typename A, typename R, int FMT, bool FULL>
 __global__ void __launch_bounds__(kRowsThreads)
 block_norm_backward_rows_kernel(const NormBackward p) {

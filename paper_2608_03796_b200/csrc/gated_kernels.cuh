@@ -36,7 +36,7 @@ __global__ void __launch_bounds__(256)
 gated_forward_kernel(const T* __restrict__ gate, const T* __restrict__ up, long long ld, long long rows, int F,
                      T* __restrict__ h, long long ld_h, ActRecord rec_gate, ActRecord rec_up, ActRecord rec_h) {
   const long long cpitch = act_codes_pitch(F), spitch = act_scale_pitch(F);
-  const int c = (blockIdx.x * blockDim.x + threadIdx.x) * 8;
+  const int c = first_column<VEC>(blockIdx.x * blockDim.x + threadIdx.x);
   grid_dependents_launch();
   grid_dependency_wait();
   for (long long t = blockIdx.y; t < rows; t += gridDim.y) {
@@ -51,11 +51,11 @@ gated_forward_kernel(const T* __restrict__ gate, const T* __restrict__ up, long 
     const Raw8<T> raw = f32_to_raw<T>(o);
     store_raw8<T, VEC>(h + t * ld_h, c, F, raw);
     if constexpr (FMT >= 0) {
-      record_write8<FMT>(rec_gate, t, cpitch, spitch, c, g, c < cpitch);
-      record_write8<FMT>(rec_up, t, cpitch, spitch, c, u, c < cpitch);
+      record_write8<FMT, VEC>(rec_gate, t, cpitch, spitch, c, g);
+      record_write8<FMT, VEC>(rec_up, t, cpitch, spitch, c, u);
       if (rec_h.codes != nullptr) {                    // what a record of h, as it was returned, would hold
         raw_to_f32(raw, o);
-        record_write8<FMT>(rec_h, t, cpitch, spitch, c, o, c < cpitch);
+        record_write8<FMT, VEC>(rec_h, t, cpitch, spitch, c, o);
       }
     }
   }
@@ -66,15 +66,25 @@ __global__ void __launch_bounds__(256)
 gated_backward_kernel(ActRecord rec_gate, ActRecord rec_up, const T* __restrict__ dh, long long ld_dh, long long rows,
                       int F, T* __restrict__ dgate, T* __restrict__ dup, long long ld) {
   const long long cpitch = act_codes_pitch(F), spitch = act_scale_pitch(F);
-  const int c = (blockIdx.x * blockDim.x + threadIdx.x) * 8;
+  const int c = first_column<VEC>(blockIdx.x * blockDim.x + threadIdx.x);
   grid_dependents_launch();
   grid_dependency_wait();
   if (c >= F) return;
   for (long long t = blockIdx.y; t < rows; t += gridDim.y) {
     float g[8], u[8], d[8], dg[8], du[8];
-    record_read8<FMT>(rec_gate, t, cpitch, spitch, c, g);
-    record_read8<FMT>(rec_up, t, cpitch, spitch, c, u);
-    load8<T, VEC>(dh + t * ld_dh, c, F, d);
+    if constexpr (VEC) {                               // c < F: both records' words at once
+      uint2 codes_g, codes_u;
+      uint32_t byte_g, byte_u;
+      record_fetch8(rec_gate, t, cpitch, spitch, c, codes_g, byte_g);
+      record_fetch8(rec_up, t, cpitch, spitch, c, codes_u, byte_u);
+      load8<T, VEC>(dh + t * ld_dh, c, F, d);
+      act_values<FMT>(codes_g, byte_g, g);
+      act_values<FMT>(codes_u, byte_u, u);
+    } else {
+      record_read8<FMT, VEC>(rec_gate, t, cpitch, spitch, c, g);
+      record_read8<FMT, VEC>(rec_up, t, cpitch, spitch, c, u);
+      load8<T, VEC>(dh + t * ld_dh, c, F, d);
+    }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       float slope;
