@@ -82,19 +82,21 @@ class Act8Record:
         elif buffer.dtype != torch.uint8 or not buffer.is_contiguous() or buffer.numel() < self.nbytes:
             raise TypeError(f"kdkl: a record of shape {(T, H)} is {self.nbytes} contiguous bytes")
         self.buffer, self.ptr = buffer, buffer.data_ptr()
+        L = B.lib()
+        self._store, self._load = L.kdkl_act8_store, L.kdkl_act8_load
 
     def store(self, x: torch.Tensor) -> "Act8Record":
         ptr, ld = _rows(x, self.T, self.H, x.dtype, "x")
-        B._check(B.lib().kdkl_act8_store(ptr, _lookup(TYPES, x.dtype, "x"), ld, self.T, self.H, self.code, self.ptr,
-                                         self.nbytes, _stream()))
+        B._check(self._store(ptr, _lookup(TYPES, x.dtype, "x"), ld, self.T, self.H, self.code, self.ptr, self.nbytes,
+                             _stream()))
         return self
 
     def load(self, out: Optional[torch.Tensor] = None, dtype=torch.bfloat16) -> torch.Tensor:
         if out is None:
             out = torch.empty(self.T, self.H, dtype=dtype, device=self.buffer.device)
         ptr, ld = _rows(out, self.T, self.H, out.dtype, "out")
-        B._check(B.lib().kdkl_act8_load(self.ptr, self.nbytes, self.T, self.H, self.code, ptr,
-                                        _lookup(TYPES, out.dtype, "out"), ld, _stream()))
+        B._check(self._load(self.ptr, self.nbytes, self.T, self.H, self.code, ptr, _lookup(TYPES, out.dtype, "out"), ld,
+                            _stream()))
         return out
 
 
@@ -110,19 +112,21 @@ class Act8WeightGrad:
             raise ValueError(f"kdkl: no weight gradient of shape {(T, N, H)}")
         self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
         self.dweight = torch.empty(N, H, dtype=dtype, device=device)
+        self._run, self._own = B.lib().kdkl_act8_dweight, (self.dweight.data_ptr(), self.workspace.data_ptr(), nbytes)
 
     def run(self, dy: torch.Tensor, record: Act8Record, out: Optional[torch.Tensor] = None,
             accumulate: bool = False) -> torch.Tensor:
         """With `accumulate`, += into `out` (or into the holder's own buffer)."""
         if (record.T, record.H) != (self.T, self.H):
             raise TypeError(f"kdkl: record: expected shape {(self.T, self.H)}, got {(record.T, record.H)}")
+        to, workspace, nbytes = self._own
         if out is None:
             out = self.dweight
+        else:
+            to = B._dptr(out, self.dtype, (self.N, self.H), "out")
         ptr, ld = _rows(dy, self.T, self.N, torch.bfloat16, "dy")
-        B._check(B.lib().kdkl_act8_dweight(
-            ptr, ld, record.ptr, record.nbytes, self.T, self.N, self.H, record.code,
-            B._dptr(out, self.dtype, (self.N, self.H), "out"), self.type, 1 if accumulate else 0,
-            self.workspace.data_ptr(), self.workspace.numel(), _stream()))
+        B._check(self._run(ptr, ld, record.ptr, record.nbytes, self.T, self.N, self.H, record.code, to, self.type,
+                           1 if accumulate else 0, workspace, nbytes, _stream()))
         return out
 
     def status(self):
@@ -140,7 +144,8 @@ class GatedAct:
         self.T, self.F, self.dtype, self.type = T, F, dtype, TYPES[dtype]
         self.act, self.format = _lookup(ACTS, act, "act"), _lookup(FORMATS, act8, "act8")
         self.h = torch.empty(T, F, dtype=dtype, device=device)
-        self.device = self.h.device
+        self.device, self._h = self.h.device, self.h.data_ptr()
+        self._forward, self._backward = B.lib().kdkl_gated_act_forward, B.lib().kdkl_gated_act_backward
         self.gate_record = self.up_record = self.h_record = None
         self.dgate_up = None
         if act8 is not None:
@@ -155,8 +160,8 @@ class GatedAct:
         keep, also = self.gate_record, self.h_record
         records = (None, None, None, 0) if keep is None else (keep.ptr, self.up_record.ptr,
                                                               None if also is None else also.ptr, keep.nbytes)
-        B._check(B.lib().kdkl_gated_act_forward(g, u, ld, self.type, self.T, self.F, self.act, self.format,
-                                                self.h.data_ptr(), self.F, *records, _stream()))
+        B._check(self._forward(g, u, ld, self.type, self.T, self.F, self.act, self.format, self._h, self.F, *records,
+                               _stream()))
         return self.h
 
     def backward(self, dh: torch.Tensor):
@@ -168,7 +173,7 @@ class GatedAct:
             self.halves = self.dgate_up[:, :self.F], self.dgate_up[:, self.F:]
         d, ld = _rows(dh, self.T, self.F, self.dtype, "dh")
         out = self.dgate_up.data_ptr()
-        B._check(B.lib().kdkl_gated_act_backward(
+        B._check(self._backward(
             self.gate_record.ptr, self.up_record.ptr, self.gate_record.nbytes, self.format, d, ld, self.type, self.T, self.F, self.act,
             out, out + self.F * self.dtype.itemsize, 2 * self.F, _stream()))
         return self.halves
@@ -238,6 +243,8 @@ class BlockNorm:
             self.branch_record, self.sum_record = Act8Record(T, H, act8, device), Act8Record(T, H, act8, device)
             self.y_record = Act8Record(T, H, act8, device) if keep_y else None
         self.grads = {}
+        self._ref = ctypes.byref(a)
+        self._forward, self._backward = B.lib().kdkl_block_norm_forward, B.lib().kdkl_block_norm_backward
 
     def forward(self, residual, branch, post_weight=None, pre_weight=None, gate=None):
         """(y, x); y is None without a pre_weight."""
@@ -246,7 +253,7 @@ class BlockNorm:
         a.branch, a.ld_branch = _rows(branch, self.T, self.H, self.dtype, "branch")
         self._weights(post_weight, pre_weight, gate)
         self._records()
-        B._check(B.lib().kdkl_block_norm_forward(ctypes.byref(a), _stream()))
+        B._check(self._forward(self._ref, _stream()))
         self.kept = (branch, self.sum, post_weight, pre_weight, gate)           # what the backward call reads
         return (self.y if pre_weight is not None else None), self.sum
 
@@ -312,5 +319,5 @@ class BlockNorm:
         a.dpost_weight = None if d.post_weight is None else d.post_weight.data_ptr()
         a.dpre_weight = None if d.pre_weight is None else d.pre_weight.data_ptr()
         a.dgate = None if d.gate is None else d.gate.data_ptr()
-        B._check(B.lib().kdkl_block_norm_backward(ctypes.byref(a), _stream()))
+        B._check(self._backward(self._ref, _stream()))
         return d
