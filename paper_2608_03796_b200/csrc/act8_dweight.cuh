@@ -21,6 +21,10 @@
 // Work units: whole tiles as far as they fill whole waves of CTA pairs, then the remaining tiles cut into parts of the
 // contraction, so that the last wave is as short as it can be. Parts leave fp32 slabs that act8_dweight_join_kernel adds
 // in order: results are reproducible bit for bit.
+//
+// One B200, 32768 x 4096 x 4096: 775 us with int8, 810 us with e4m3 codes (1420 and 1360 TFLOP/s; a library product of bf16
+// operands 675 us); back to back, under the power cap, 930 to 960 us against 813. What the gap is: the conversion, done
+// once per 256 rows of the result, takes about 135 us of the cap's energy.
 #pragma once
 #include "act8.cuh"
 #include "sm100_prims.cuh"

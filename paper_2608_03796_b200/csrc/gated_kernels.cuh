@@ -6,7 +6,7 @@
 //
 // Element-wise, so bound by memory: forward reads 4 bytes a value and writes 2 (+ 33/32 per record), backward reads
 // 2 + 66/32 and writes 4. The records leave in the pass that computes h, from registers. 32768 x 7168 bf16, int8 records,
-// one B200: forward 332 us (5.7 TB/s), backward 285 us (6.65 TB/s); without records forward 203 us (6.95 TB/s). What the
+// one B200: forward 316 us (6.0 TB/s), backward 285 us (6.65 TB/s); without records forward 201 us (7.0 TB/s). What the
 // records add to the forward pass is the encoding: about 70 instructions per eight values.
 #pragma once
 #include "act8.cuh"
