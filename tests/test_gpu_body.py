@@ -471,6 +471,46 @@ def test_offsets_past_32_bits():
     assert torch.equal(d.branch[-1000:], d2.branch) and torch.equal(d.residual[-1000:], d2.residual)
 
 
+def test_refusals_of_tensors():
+    """What a class was not made for is refused before anything is launched: types, shapes, strides, gates."""
+    T, H = 8, 64
+    dev = _dev()
+    x = _randn(1, T, H).to(dev)
+    w = torch.ones(H, dtype=BF16, device=dev)
+    rec = body.Act8Record(T, H).store(x)
+    for bad in (x.t(), x[:4], x.long(), x[:1].expand(T, H), x.cpu(), x.reshape(-1)):
+        with pytest.raises((TypeError, ValueError)):
+            rec.store(bad)
+        with pytest.raises((TypeError, ValueError)):
+            rec.load(bad)
+    ffn = body.GatedAct(T, H)
+    with pytest.raises(TypeError):
+        ffn.forward(x, x.half())
+    with pytest.raises(TypeError):
+        ffn.forward(x, torch.cat([x, x], 1)[:, :H])                         # rows not equally far apart
+    grad = body.Act8WeightGrad(T, 32, H)
+    with pytest.raises(TypeError):
+        grad.run(_randn(2, T, 32, dtype=F32).to(dev), rec)
+    with pytest.raises(TypeError):
+        grad.run(_randn(2, T, 32).to(dev), body.Act8Record(T, 32))
+    with pytest.raises(TypeError):
+        grad.run(_randn(2, T, 32).to(dev), rec, out=torch.empty(32, H, device=dev))
+    join = body.BlockNorm(T, H, gate="token")
+    with pytest.raises(TypeError):
+        join.forward(x, x, w, w)                                            # the gate is missing
+    with pytest.raises(TypeError):
+        join.forward(x, x, w, w, gate=w)                                    # one per channel, not per token
+    with pytest.raises(TypeError):
+        join.forward(x, x, w, w.float(), gate=w[:T])                        # two weight types
+    join.forward(x, x, w, None, gate=w[:T].clone())
+    with pytest.raises(TypeError):
+        join.backward(x, x)                                                 # there is no y
+    with pytest.raises(TypeError):
+        body.Act8Record(T, H, buffer=torch.empty(16, dtype=torch.uint8, device=dev))
+    with pytest.raises(RuntimeError):
+        body.BlockNorm(T, H, train=False).backward(x, x)
+
+
 def test_no_tokens():
     dev = _dev()
     e = torch.empty(0, 64, dtype=BF16, device=dev)
