@@ -17,10 +17,11 @@
 // in its registers until the end, leave as one partial row per block, and a second kernel adds the partial rows in a
 // fixed order: bitwise reproducible.
 //
-// Two kernels each way. The *_rows kernels take rows that are whole 16-byte words, up to kRowsMaxH columns: the next
+// Two kernels each way. The *_rows kernels take rows that are whole words; rows wider than a block's 8192 columns are
+// shared by a cluster, whose blocks leave their sums in one another's shared memory: the next
 // rows travel to shared memory (cp.async, slots that only their own thread touches, so no barrier) while a row is
 // worked on, what depends on the column alone is formed once, and two values go through an instruction. The *_any
-// kernels take everything else: odd widths and addresses, and wider rows.
+// kernels take everything else: odd widths and addresses.
 // 32768 x 4096 bf16, one B200: forward 172 us (6.2 TB/s), leaving int8 records 238 us (5.7 TB/s); backward 290 us (5.6 TB/s),
 // from int8 records 280 us (4.8 TB/s). The backward kernel holds 128 registers a thread, so 16 warps an SM, and its
 // reduction shows: without it (and wrong) it would take 255 us. 16384 x 4095 (any): forward 178, backward 556 us.
@@ -90,34 +91,53 @@ __device__ __forceinline__ void block_sums(float (&x)[N], float* sm) {
   }
 }
 
-// The same where the number of threads is known at run time only (whole warps, at most 16): after the barrier every
-// thread reads and adds the warps' values itself, which is quicker than five more dependent shuffles. `sm` holds 16
-// floats a sum, 16-byte aligned; those of warps that do not exist stay 0 (clear_sums).
+// The same where the number of threads is known at run time only (whole warps, at most 16), over the C blocks of a
+// cluster that share a row: after the barrier every thread reads and adds the warps' values itself, which is quicker than
+// five more dependent shuffles. `sm` holds 16 floats a sum and block, 16-byte aligned, in every block; those of warps that
+// do not exist stay 0 (clear_sums).
+template <int C> __device__ __forceinline__ void row_barrier() {
+  if (C == 1) __syncthreads(); else cluster_sync_all();
+}
+template <int C>
 __device__ __forceinline__ void clear_sums(float* sm, int n) {
   for (int i = threadIdx.x; i < n; i += blockDim.x) sm[i] = 0.f;
-  __syncthreads();
+  row_barrier<C>();
 }
+template <int C>
+__device__ __forceinline__ void leave_sum(float* at, float x) {             // at this place in every block of the cluster
+  if (C == 1) { *at = x; return; }
+#pragma unroll
+  for (int q = 0; q < C; ++q)
+    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(map_to_cta(smem_u32(at), q)), "f"(x) : "memory");
+}
+template <int C>
 __device__ __forceinline__ float sum_of_warps(const float* sm) {
-  const float4* p = reinterpret_cast<const float4*>(sm);
-  const float4 a = p[0], b = p[1];
-  float s = ((a.x + a.y) + (a.z + a.w)) + ((b.x + b.y) + (b.z + b.w));
-  if (blockDim.x > 256) {
-    const float4 c = p[2], d = p[3];
-    s += ((c.x + c.y) + (c.z + c.w)) + ((d.x + d.y) + (d.z + d.w));
+  float s = 0.f;
+#pragma unroll
+  for (int q = 0; q < C; ++q) {
+    const float4* p = reinterpret_cast<const float4*>(sm + 16 * q);
+    const float4 a = p[0], b = p[1];
+    s += ((a.x + a.y) + (a.z + a.w)) + ((b.x + b.y) + (b.z + b.w));
+    if (blockDim.x > 256) {
+      const float4 c = p[2], d = p[3];
+      s += ((c.x + c.y) + (c.z + c.w)) + ((d.x + d.y) + (d.z + d.w));
+    }
   }
   return s;
 }
-__device__ __forceinline__ float block_sum(float x, float* sm) {
+template <int C>
+__device__ __forceinline__ float block_sum(float x, float* sm, int rank) {
 #pragma unroll
   for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-  if (blockDim.x == 32) return x;
-  if ((threadIdx.x & 31) == 0) sm[threadIdx.x >> 5] = x;
-  __syncthreads();
-  return sum_of_warps(sm);
+  if (C == 1 && blockDim.x == 32) return x;
+  if ((threadIdx.x & 31) == 0) leave_sum<C>(sm + 16 * rank + (threadIdx.x >> 5), x);
+  row_barrier<C>();
+  return sum_of_warps<C>(sm);
 }
 // Three sums at once: the first two steps of the butterfly also sort the sums by lane (lane 0: the first, 16: the
 // second, 8: the third), so that the rest reduces one value instead of three.
-__device__ __forceinline__ void block_sums3(float (&x)[3], float* sm) {
+template <int C>
+__device__ __forceinline__ void block_sums3(float (&x)[3], float* sm, int rank) {
   const int lane = threadIdx.x & 31;
   const bool up = lane & 16, mid = lane & 8;
   float k = up ? x[1] : x[0];
@@ -127,14 +147,14 @@ __device__ __forceinline__ void block_sums3(float (&x)[3], float* sm) {
   k = (mid ? third : k) + __shfl_xor_sync(0xffffffffu, give, 8);
 #pragma unroll
   for (int o = 4; o; o >>= 1) k += __shfl_xor_sync(0xffffffffu, k, o);
-  if (blockDim.x == 32) {
+  if (C == 1 && blockDim.x == 32) {
     x[0] = __shfl_sync(0xffffffffu, k, 0); x[1] = __shfl_sync(0xffffffffu, k, 16); x[2] = __shfl_sync(0xffffffffu, k, 8);
     return;
   }
-  if ((lane & 7) == 0 && lane != 24) sm[(mid ? 32 : up ? 16 : 0) + (threadIdx.x >> 5)] = k;
-  __syncthreads();
+  if ((lane & 7) == 0 && lane != 24) leave_sum<C>(sm + (mid ? 32 : up ? 16 : 0) * C + 16 * rank + (threadIdx.x >> 5), k);
+  row_barrier<C>();
 #pragma unroll
-  for (int i = 0; i < 3; ++i) x[i] = sum_of_warps(sm + 16 * i);
+  for (int i = 0; i < 3; ++i) x[i] = sum_of_warps<C>(sm + 16 * C * i);
 }
 
 struct NormForward {
@@ -150,7 +170,7 @@ struct NormForward {
   float eps, offset, alpha, beta;
 };
 
-template <typename A, typename R, bool REC, int THREADS, int NV, bool VEC>
+template <typename A, typename R, bool REC, int THREADS, int NV>
 __global__ void __launch_bounds__(THREADS)
 block_norm_forward_any_kernel(const NormForward p) {
   __shared__ float sm[4][32];           // post and pre, alternating by row (see block_sums)
@@ -163,11 +183,11 @@ block_norm_forward_any_kernel(const NormForward p) {
   float k[NV][8], w2[NV][8];            // alpha (w1 + o) gate_c;  w2 + o
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int c = first_column<VEC>(threadIdx.x + i * THREADS);
+    const int c = first_column<false>(threadIdx.x + i * THREADS);
     float w[8], g[8];
-    if (p.post.p != nullptr) any_load8<VEC>(p.post, c, H, w);
-    if (p.gate_kind == kGateChannel) any_load8<VEC>(p.gate, c, H, g);
-    if (p.pre.p != nullptr) any_load8<VEC>(p.pre, c, H, w2[i]);
+    if (p.post.p != nullptr) any_load8<false>(p.post, c, H, w);
+    if (p.gate_kind == kGateChannel) any_load8<false>(p.gate, c, H, g);
+    if (p.pre.p != nullptr) any_load8<false>(p.pre, c, H, w2[i]);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       k[i][j] = p.alpha;
@@ -182,11 +202,11 @@ block_norm_forward_any_kernel(const NormForward p) {
     float b[NV][8], x[NV][8];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int c = first_column<VEC>(threadIdx.x + i * THREADS);
-      load8<A, VEC>(brow, c, H, b[i]);
-      load8<R, VEC>(rrow, c, H, x[i]);
+      const int c = first_column<false>(threadIdx.x + i * THREADS);
+      load8<A, false>(brow, c, H, b[i]);
+      load8<R, false>(rrow, c, H, x[i]);
       if constexpr (REC) {
-        if (p.rec_branch.codes != nullptr) record_write8<VEC>(p.format, p.rec_branch, t, cpitch, spitch, c, b[i]);
+        if (p.rec_branch.codes != nullptr) record_write8<false>(p.format, p.rec_branch, t, cpitch, spitch, c, b[i]);
       }
     }
     float rho1 = 1.f;
@@ -220,26 +240,26 @@ block_norm_forward_any_kernel(const NormForward p) {
     }
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int c = first_column<VEC>(threadIdx.x + i * THREADS);
+      const int c = first_column<false>(threadIdx.x + i * THREADS);
       const Raw8<R> raw = f32_to_raw<R>(x[i]);
-      store_raw8<R, VEC>(reinterpret_cast<R*>(p.sum) + t * H, c, H, raw);
+      store_raw8<R, false>(reinterpret_cast<R*>(p.sum) + t * H, c, H, raw);
       if constexpr (REC) {
         if (p.rec_sum.codes != nullptr) {             // what a record of the returned sum would hold
           float v[8];
           raw_to_f32(raw, v);
-          record_write8<VEC>(p.format, p.rec_sum, t, cpitch, spitch, c, v);
+          record_write8<false>(p.format, p.rec_sum, t, cpitch, spitch, c, v);
         }
       }
       if (p.pre.p != nullptr) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) x[i][j] *= rho2 * w2[i][j];
         const Raw8<A> yr = f32_to_raw<A>(x[i]);
-        store_raw8<A, VEC>(reinterpret_cast<A*>(p.y) + t * H, c, H, yr);
+        store_raw8<A, false>(reinterpret_cast<A*>(p.y) + t * H, c, H, yr);
         if constexpr (REC) {
           if (p.rec_y.codes != nullptr) {
             float v[8];
             raw_to_f32(yr, v);
-            record_write8<VEC>(p.format, p.rec_y, t, cpitch, spitch, c, v);
+            record_write8<false>(p.format, p.rec_y, t, cpitch, spitch, c, v);
           }
         }
       }
@@ -269,7 +289,7 @@ struct NormBackward {
 //   A = sum_t sigma d b     (per column; dw1 = gate_c A, dgate_c = (w1 + o) A),   dw2 = sum_t u x
 //   db = sigma Q d - rho1^2 c1 b
 // so a column needs one sum for the gate and the post weight together.
-template <typename A, typename R, bool REC, int THREADS, int NV, bool VEC>
+template <typename A, typename R, bool REC, int THREADS, int NV>
 __global__ void __launch_bounds__(THREADS)
 block_norm_backward_any_kernel(const NormBackward p) {
   __shared__ float sm[2][3 * 32];
@@ -283,11 +303,11 @@ block_norm_backward_any_kernel(const NormBackward p) {
   grid_dependency_wait();
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int c = first_column<VEC>(threadIdx.x + i * THREADS);
+    const int c = first_column<false>(threadIdx.x + i * THREADS);
     float g[8];
-    if (has_post) any_load8<VEC>(p.post, c, H, q[i]);
-    if (channel) any_load8<VEC>(p.gate, c, H, g);
-    if (has_pre) any_load8<VEC>(p.pre, c, H, w2[i]);
+    if (has_post) any_load8<false>(p.post, c, H, q[i]);
+    if (channel) any_load8<false>(p.gate, c, H, g);
+    if (has_pre) any_load8<false>(p.pre, c, H, w2[i]);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       q[i][j] = has_post ? q[i][j] + p.offset : 1.f;
@@ -304,17 +324,17 @@ block_norm_backward_any_kernel(const NormBackward p) {
     float s[3] = {0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int c = first_column<VEC>(threadIdx.x + i * THREADS);
+      const int c = first_column<false>(threadIdx.x + i * THREADS);
       if constexpr (REC) {
-        record_read8<VEC>(p.format, p.rec_branch, t, cpitch, spitch, c, b[i]);
-        if (has_pre) record_read8<VEC>(p.format, p.rec_sum, t, cpitch, spitch, c, x[i]);
+        record_read8<false>(p.format, p.rec_branch, t, cpitch, spitch, c, b[i]);
+        if (has_pre) record_read8<false>(p.format, p.rec_sum, t, cpitch, spitch, c, x[i]);
       } else {
-        load8<A, VEC>(reinterpret_cast<const A*>(p.branch) + t * p.ld_branch, c, H, b[i]);
-        if (has_pre) load8<R, VEC>(reinterpret_cast<const R*>(p.sum) + t * p.ld_sum, c, H, x[i]);
+        load8<A, false>(reinterpret_cast<const A*>(p.branch) + t * p.ld_branch, c, H, b[i]);
+        if (has_pre) load8<R, false>(reinterpret_cast<const R*>(p.sum) + t * p.ld_sum, c, H, x[i]);
       }
       float dy[8];
-      if (p.dsum != nullptr) load8<R, VEC>(reinterpret_cast<const R*>(p.dsum) + t * p.ld_dsum, c, H, e[i]);
-      if (has_pre) load8<A, VEC>(reinterpret_cast<const A*>(p.dy) + t * p.ld_dy, c, H, dy);
+      if (p.dsum != nullptr) load8<R, false>(reinterpret_cast<const R*>(p.dsum) + t * p.ld_dsum, c, H, e[i]);
+      if (has_pre) load8<A, false>(reinterpret_cast<const A*>(p.dy) + t * p.ld_dy, c, H, dy);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         if (p.dsum == nullptr) e[i][j] = 0.f;
@@ -337,7 +357,7 @@ block_norm_backward_any_kernel(const NormBackward p) {
     const float sigma = p.alpha * rho1 * gate_t, tau = has_post ? -rho1 * rho1 * dot * gate_t * inv_h : 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int c = first_column<VEC>(threadIdx.x + i * THREADS);
+      const int c = first_column<false>(threadIdx.x + i * THREADS);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const float d = fmaf(-k2, x[i][j], e[i][j]), sd = d * sigma;
@@ -345,32 +365,33 @@ block_norm_backward_any_kernel(const NormBackward p) {
         e[i][j] = p.beta * d;
         b[i][j] = fmaf(q[i][j], sd, tau * b[i][j]);
       }
-      store_raw8<R, VEC>(reinterpret_cast<R*>(p.dresidual) + t * H, c, H, f32_to_raw<R>(e[i]));
-      store_raw8<A, VEC>(reinterpret_cast<A*>(p.dbranch) + t * H, c, H, f32_to_raw<A>(b[i]));
+      store_raw8<R, false>(reinterpret_cast<R*>(p.dresidual) + t * H, c, H, f32_to_raw<R>(e[i]));
+      store_raw8<A, false>(reinterpret_cast<A*>(p.dbranch) + t * H, c, H, f32_to_raw<A>(b[i]));
     }
   }
   float* out = p.partial + (long long)blockIdx.x * 3 * cpitch;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int c = first_column<VEC>(threadIdx.x + i * THREADS);
+    const int c = first_column<false>(threadIdx.x + i * THREADS);
     if (c >= H) continue;
     float w[8], g[8], v[8];
-    if (has_post) any_load8<VEC>(p.post, c, H, w);
-    if (channel) any_load8<VEC>(p.gate, c, H, g);
-    if (has_pre) store_raw8<float, VEC>(out + cpitch, c, (int)cpitch, f32_to_raw<float>(sum_w[i]));
+    if (has_post) any_load8<false>(p.post, c, H, w);
+    if (channel) any_load8<false>(p.gate, c, H, g);
+    if (has_pre) store_raw8<float, false>(out + cpitch, c, (int)cpitch, f32_to_raw<float>(sum_w[i]));
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = channel ? sum_a[i][j] * g[j] : sum_a[i][j];
-    if (has_post) store_raw8<float, VEC>(out, c, (int)cpitch, f32_to_raw<float>(v));
+    if (has_post) store_raw8<float, false>(out, c, (int)cpitch, f32_to_raw<float>(v));
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = has_post ? sum_a[i][j] * (w[j] + p.offset) : sum_a[i][j];
-    if (channel) store_raw8<float, VEC>(out + 2 * cpitch, c, (int)cpitch, f32_to_raw<float>(v));
+    if (channel) store_raw8<float, false>(out + 2 * cpitch, c, (int)cpitch, f32_to_raw<float>(v));
   }
 }
 
 // ------------------------------------------------------------------ rows of whole 16-byte words
 // A thread has two groups of eight columns: that halves what a row costs per value in sums, factors and addresses
 // (with one group a thread both kernels were bound by instructions, 63 and 54 a value).
-constexpr int kRowsThreads = 512, kRowsMaxH = 2 * 8 * kRowsThreads, kRowsStages = 3;
+constexpr int kRowsThreads = 512, kRowsMaxH = 2 * 8 * kRowsThreads;   // kRowsMaxH: columns a block
+constexpr int kRowsMaxCluster = 4;      // wider rows are shared by a cluster of 2 or 4 blocks
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool live) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
@@ -455,21 +476,29 @@ __host__ __device__ constexpr int rows_forward_chunk(int residual_bytes) { retur
 __host__ __device__ constexpr int rows_backward_chunk(int residual_bytes, bool rec) {
   return 256 * residual_bytes + 512 + (rec ? 2 * 256 : 512 + 256 * residual_bytes);
 }
+// Rows of the backward kernel that are worked on or on their way: three, two where the widest block's 32 chunks of three
+// would not fit the shared memory (an fp32 residual without records).
+__host__ __device__ constexpr int rows_backward_stages(int residual_bytes, bool rec) {
+  return 3 * 32 * rows_backward_chunk(residual_bytes, rec) <= 200 * 1024 ? 3 : 2;
+}
 
 // FMT -1: no records. FULL: both norms (and, backward, a gradient along the residual stream) are there, which spares the
-// loop its questions.
-template <typename A, typename R, int FMT, bool FULL>
+// loop its questions. C: blocks that share a row (a cluster); block `rank` of them has the columns of its threads' numbers
+// threadIdx.x + (2 rank) blockDim.x and threadIdx.x + (2 rank + 1) blockDim.x.
+template <typename A, typename R, int FMT, bool FULL, int C>
 __global__ void __launch_bounds__(kRowsThreads)
 block_norm_forward_rows_kernel(const NormForward p) {
   extern __shared__ __align__(16) uint8_t smem[];
-  __shared__ __align__(16) float sm[4][16];
+  __shared__ __align__(16) float sm[4][16 * C];
   constexpr int kResidual = 512;        // field offsets: branch, residual
-  clear_sums(sm[0], 64);
+  clear_sums<C>(sm[0], 64 * C);
   const int H = p.H, threads = blockDim.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const long long cpitch = act_codes_pitch(H), spitch = act_scale_pitch(H);
   const float inv_h = 1.f / (float)H;
   const bool has_post = FULL || p.post.p != nullptr, has_pre = FULL || p.pre.p != nullptr, token = p.gate_kind == kGateToken;
-  const int c[2] = {(int)threadIdx.x * 8, (int)(threadIdx.x + threads) * 8};
+  const int rank = C == 1 ? 0 : (int)cluster_ctarank();
+  const long long first = blockIdx.x / C, step = gridDim.x / C;
+  const int c[2] = {(int)(threadIdx.x + 2 * rank * threads) * 8, (int)(threadIdx.x + (2 * rank + 1) * threads) * 8};
   const uint32_t chunk = smem_u32(smem) + warp * rows_forward_chunk(sizeof(R));
   const Places at[2] = {Places(chunk, lane), Places(chunk + (threads >> 5) * rows_forward_chunk(sizeof(R)), lane)};
   auto fetch = [&](long long t) {
@@ -483,7 +512,7 @@ block_norm_forward_rows_kernel(const NormForward p) {
   };
   grid_dependents_launch();
   grid_dependency_wait();
-  fetch(blockIdx.x);
+  fetch(first);
   V8 k[2], w2[2];                       // alpha (w1 + o) gate_c;  w2 + o
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
@@ -507,8 +536,8 @@ block_norm_forward_rows_kernel(const NormForward p) {
     }
   }
   int parity = 0;
-  uint32_t gate_next = token ? any_bits(p.gate, blockIdx.x) : 0u;
-  for (long long t = blockIdx.x; t < p.T; t += gridDim.x, parity ^= 2) {
+  uint32_t gate_next = token ? any_bits(p.gate, first) : 0u;
+  for (long long t = first; t < p.T; t += step, parity ^= 2) {
     const float gate_t = token ? any_value(gate_next, p.gate.type) : 1.f;
     cp_async_wait_all();
     V8 b[2], x[2];
@@ -520,9 +549,9 @@ block_norm_forward_rows_kernel(const NormForward p) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) { acc = fma2(b[i].p[j], b[i].p[j], acc); x[i].p[j] = mul2(x[i].p[j], both(p.beta)); }
     }
-    if (t + gridDim.x < p.T) {          // the row is in registers: its places take the next one
-      fetch(t + gridDim.x);
-      if (token) gate_next = any_bits(p.gate, t + gridDim.x);
+    if (t + step < p.T) {               // the row is in registers: its places take the next one
+      fetch(t + step);
+      if (token) gate_next = any_bits(p.gate, t + step);
     }
     if constexpr (FMT >= 0) {
       if (p.rec_branch.codes != nullptr) {
@@ -532,7 +561,7 @@ block_norm_forward_rows_kernel(const NormForward p) {
     }
     float rho1 = 1.f;
     if (has_post) {
-      rho1 = rsqrtf(fmaf(block_sum(sum2(acc), sm[parity]), inv_h, p.eps));
+      rho1 = rsqrtf(fmaf(block_sum<C>(sum2(acc), sm[parity], rank), inv_h, p.eps));
     }
     const float2 scale = both(rho1 * gate_t);
     acc = both(0.f);
@@ -558,7 +587,7 @@ block_norm_forward_rows_kernel(const NormForward p) {
     }
     float rho2 = 1.f;
     if (has_pre) {
-      rho2 = rsqrtf(fmaf(block_sum(sum2(acc), sm[parity + 1]), inv_h, p.eps));
+      rho2 = rsqrtf(fmaf(block_sum<C>(sum2(acc), sm[parity + 1], rank), inv_h, p.eps));
       A* y_row = reinterpret_cast<A*>(p.y) + t * H;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
@@ -575,26 +604,28 @@ block_norm_forward_rows_kernel(const NormForward p) {
         }
       }
     }
-    if (threadIdx.x == 0) {
+    if (threadIdx.x == 0 && rank == 0) {
       if (p.rho_post != nullptr) p.rho_post[t] = rho1;
       if (p.rho_pre != nullptr) p.rho_pre[t] = rho2;
     }
   }
 }
 
-template <typename A, typename R, int FMT, bool FULL>
+template <typename A, typename R, int FMT, bool FULL, int C>
 __global__ void __launch_bounds__(kRowsThreads)
 block_norm_backward_rows_kernel(const NormBackward p) {
   extern __shared__ __align__(16) uint8_t smem[];
-  __shared__ __align__(16) float sm[2][3 * 16];
-  clear_sums(sm[0], 96);
+  __shared__ __align__(16) float sm[2][3 * 16 * C];
+  clear_sums<C>(sm[0], 96 * C);
   constexpr int kRB = 256 * (int)sizeof(R), kDy = kRB, kBranch = kRB + 512, kSum = kBranch + (FMT >= 0 ? 256 : 512);
   const int H = p.H, threads = blockDim.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const long long cpitch = act_codes_pitch(H), spitch = act_scale_pitch(H);
   const float inv_h = 1.f / (float)H;
   const bool has_post = FULL || p.post.p != nullptr, has_pre = FULL || p.pre.p != nullptr, token = p.gate_kind == kGateToken;
   const bool has_dx = FULL || p.dsum != nullptr;
-  const int c[2] = {(int)threadIdx.x * 8, (int)(threadIdx.x + threads) * 8};
+  const int rank = C == 1 ? 0 : (int)cluster_ctarank();
+  const long long first = blockIdx.x / C, step = gridDim.x / C;
+  const int c[2] = {(int)(threadIdx.x + 2 * rank * threads) * 8, (int)(threadIdx.x + (2 * rank + 1) * threads) * 8};
   constexpr int kChunk = rows_backward_chunk(sizeof(R), FMT >= 0);
   const uint32_t chunk = smem_u32(smem) + warp * kChunk;
   const uint32_t stage_bytes = (threads >> 4) * kChunk;
@@ -634,12 +665,12 @@ block_norm_backward_rows_kernel(const NormBackward p) {
       }
     }
   };
-  constexpr int S = kRowsStages;
+  constexpr int S = rows_backward_stages(sizeof(R), FMT >= 0);
   grid_dependents_launch();
   grid_dependency_wait();
 #pragma unroll
-  for (int k = 0; k < S - 1; ++k) fetch(blockIdx.x + (long long)k * gridDim.x, k);
-  factors(blockIdx.x);
+  for (int k = 0; k < S - 1; ++k) fetch(first + k * step, k);
+  factors(first);
   int stage = 0;
   V8 q[2], w2[2], sum_a[2], sum_w[2];
 #pragma unroll
@@ -664,11 +695,11 @@ block_norm_backward_rows_kernel(const NormBackward p) {
     }
   }
   int parity = 0;
-  for (long long t = blockIdx.x; t < p.T; t += gridDim.x, parity ^= 1) {
+  for (long long t = first; t < p.T; t += step, parity ^= 1) {
     const float rho1 = rho1_next, rho2 = rho2_next, gate_t = token ? any_value(gate_next, p.gate.type) : 1.f;
     const uint32_t now_b[2] = {byte_b[0], byte_b[1]}, now_x[2] = {byte_x[0], byte_x[1]};
-    fetch(t + (long long)(S - 1) * gridDim.x, stage == 0 ? S - 1 : stage - 1);
-    factors(t + gridDim.x);
+    fetch(t + (S - 1) * step, stage == 0 ? S - 1 : stage - 1);
+    factors(t + step);
     cp_async_wait<S - 1>();
     const Places at[2] = {places(0, stage), places(1, stage)};
     stage = stage + 1 == S ? 0 : stage + 1;
@@ -701,10 +732,10 @@ block_norm_backward_rows_kernel(const NormBackward p) {
       }
     }
     float s[3] = {sum2(a0), sum2(a1), sum2(a2)};
-    block_sums3(s, sm[parity]);
+    block_sums3<C>(s, sm[parity], rank);
     const float k2 = rho2 * rho2 * s[0] * inv_h;             // d = e - k2 x
     const float dot = rho1 * p.alpha * (s[1] - k2 * s[2]);   // sum_h alpha Q b^ d
-    if (token && threadIdx.x == 0) any_store(p.dgate_token, p.gate_type, t, dot);
+    if (token && threadIdx.x == 0 && rank == 0) any_store(p.dgate_token, p.gate_type, t, dot);
     const float sigma = p.alpha * rho1 * gate_t;
     const float tau = has_post ? -rho1 * rho1 * dot * gate_t * inv_h : 0.f;
     R* dr_row = reinterpret_cast<R*>(p.dresidual) + t * H;
@@ -722,7 +753,7 @@ block_norm_backward_rows_kernel(const NormBackward p) {
       store_raw8<A, true>(db_row, c[i], H, v8_raw<A>(b[i]));
     }
   }
-  float* out = p.partial + (long long)blockIdx.x * 3 * cpitch;
+  float* out = p.partial + first * 3 * cpitch;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     if (c[i] >= H) continue;

@@ -11,11 +11,16 @@ using namespace kdkl;
 
 // ------------------------------------------------------------------ block norm
 static constexpr long long kNormMaxH = 32768;
-// Threads of the *_rows kernels: two groups of eight columns each.
-static int rows_threads(long long H) { return (int)((act_codes_pitch(H) / 16 + 31) / 32 * 32); }
+// Blocks of the *_rows kernels that share a row, and their threads: two groups of eight columns each.
+static int rows_cluster(long long H) { return H <= kRowsMaxH ? 1 : H <= 2 * kRowsMaxH ? 2 : 4; }
+static int rows_threads(long long H) {
+  const long long per = 16 * rows_cluster(H);
+  return (int)(((act_codes_pitch(H) + per - 1) / per + 31) / 32 * 32);
+}
+static_assert(kNormMaxH <= (long long)kRowsMaxCluster * kRowsMaxH, "the widest rows");
 // The most blocks of the backward kernels, each of which leaves one partial row: what 1024 threads an SM amount to.
 static long long norm_parts(long long T, long long H) {
-  const int threads = H <= kRowsMaxH ? rows_threads(H) : 2 * kRowsThreads;
+  const int threads = rows_threads(H);
   const long long most = (long long)sm_count_or_default() * (1024 / threads > 16 ? 16 : 1024 / threads);
   return T < most ? T : most;
 }
@@ -77,12 +82,12 @@ static int check_norm(const kdkl_block_norm_args* a, bool backward) {
   return KDKL_OK;
 }
 
-// Launches a *_rows kernel with as many blocks as the device holds at once (at most `most`: one per row, one per partial
-// row). The shared memory a kernel may use beyond 48 KiB, its static part included, is an attribute of its copy on the
+// Launches a *_rows kernel with as many blocks, or clusters of C, as the device holds at once (at most `most`: one per row,
+// one per partial row). The shared memory a kernel may use beyond 48 KiB, its static part included, is an attribute of its copy on the
 // device, raised when a launch needs more than any before; how many blocks fit an SM is asked once per number of warps.
-template <auto KERN, typename P>
+template <auto KERN, int C, typename P>
 static int launch_rows(long long most, int threads, int smem, const P& p, const char* name, const DeviceInfo& di,
-                       cudaStream_t st, int* blocks) {
+                       cudaStream_t st, int* rows) {
   struct Known { int allowed; int fit[kRowsThreads / 32 + 1]; };
   static Known known[kMaxDevices];
   Known fresh;
@@ -98,10 +103,19 @@ static int launch_rows(long long most, int threads, int smem, const P& p, const 
     if (fit < 1) fit = 1;
     k.fit[threads / 32] = fit;
   }
-  const long long held = (long long)di.sm_count * fit;
-  *blocks = (int)(most < held ? most : held);
-  return launch(name, KERN, dim3((unsigned)*blocks, 1, 1), threads, (size_t)smem, st, p);
+  const long long held = (long long)di.sm_count * fit / C;
+  *rows = (int)(most < held ? most : held);
+  return launch_cluster(C, name, KERN, dim3((unsigned)*rows * C, 1, 1), threads, (size_t)smem, st, p);
 }
+
+// (rows wider than a block's: without the FULL variants)
+#define KDKL_BY_CLUSTER(H, full, C, FULL, ...)                                                                   \
+  do {                                                                                                           \
+    const int c__ = rows_cluster(H);                                                                             \
+    if (c__ == 4) { constexpr int C = 4; constexpr bool FULL = false; __VA_ARGS__; }                             \
+    else if (c__ == 2) { constexpr int C = 2; constexpr bool FULL = false; __VA_ARGS__; }                        \
+    else { constexpr int C = 1; KDKL_BY_BOOL(full, FULL, __VA_ARGS__); }                                         \
+  } while (0)
 
 static bool vectors_are_words(const kdkl_block_norm_args* a) {
   return words(a->post_weight, 0, 1, a->H, a->weight_type) && words(a->pre_weight, 0, 1, a->H, a->weight_type) &&
@@ -109,11 +123,10 @@ static bool vectors_are_words(const kdkl_block_norm_args* a) {
 }
 
 // Threads a row and groups of eight columns a thread of the *_any kernels.
-#define KDKL_NORM_SHAPE(H, vec, VEC, THREADS, NV, ...)                                                       \
-  do {                                                                                                       \
-    if ((vec)) { constexpr bool VEC = true; constexpr int THREADS = 1024, NV = 4; __VA_ARGS__; }             \
-    else if ((H) <= 4096) { constexpr bool VEC = false; constexpr int THREADS = 512, NV = 1; __VA_ARGS__; }  \
-    else { constexpr bool VEC = false; constexpr int THREADS = 1024, NV = 4; __VA_ARGS__; }                  \
+#define KDKL_NORM_SHAPE(H, THREADS, NV, ...)                                              \
+  do {                                                                                    \
+    if ((H) <= 4096) { constexpr int THREADS = 512, NV = 1; __VA_ARGS__; }                \
+    else { constexpr int THREADS = 1024, NV = 4; __VA_ARGS__; }                           \
   } while (0)
 
 extern "C" {
@@ -143,18 +156,18 @@ int kdkl_block_norm_forward(const kdkl_block_norm_args* a, void* cuda_stream) {
   const bool any_record = a->format != KDKL_ACT8_NONE && (a->branch_record || a->sum_record || p.rec_y.codes);
   const long long most = (long long)di.sm_count * 8;
   const unsigned grid = (unsigned)(a->T < most ? a->T : most);
-  if (vec && a->H <= kRowsMaxH) {
+  if (vec) {
     const int fmt = any_record ? a->format : KDKL_ACT8_NONE;
     const bool full = a->post_weight && a->pre_weight;
     const int threads = rows_threads(a->H), smem = threads / 16 * rows_forward_chunk(type_bytes(a->residual_type));
     int blocks;
-    KDKL_BY_TYPE16(a->type, A, KDKL_BY_BOOL(a->residual_type == KDKL_TYPE_F32, WIDE, KDKL_BY_FORMAT_OR_NONE(fmt, FMT, KDKL_BY_BOOL(full, FULL,
-      return (launch_rows<block_norm_forward_rows_kernel<A, std::conditional_t<WIDE, float, A>, FMT, FULL>>(
+    KDKL_BY_TYPE16(a->type, A, KDKL_BY_BOOL(a->residual_type == KDKL_TYPE_F32, WIDE, KDKL_BY_FORMAT_OR_NONE(fmt, FMT, KDKL_BY_CLUSTER(a->H, full, C, FULL,
+      return (launch_rows<block_norm_forward_rows_kernel<A, std::conditional_t<WIDE, float, A>, FMT, FULL, C>, C>(
           a->T, threads, smem, p, "block_norm_forward_rows_kernel", di, st, &blocks))))));
   }
   KDKL_BY_TYPE16(a->type, A, KDKL_BY_BOOL(a->residual_type == KDKL_TYPE_F32, WIDE,
-    KDKL_BY_BOOL(any_record, REC, KDKL_NORM_SHAPE(a->H, vec, VEC, THREADS, NV,
-      rc = (launch("block_norm_forward_any_kernel", block_norm_forward_any_kernel<A, std::conditional_t<WIDE, float, A>, REC, THREADS, NV, VEC>,
+    KDKL_BY_BOOL(any_record, REC, KDKL_NORM_SHAPE(a->H, THREADS, NV,
+      rc = (launch("block_norm_forward_any_kernel", block_norm_forward_any_kernel<A, std::conditional_t<WIDE, float, A>, REC, THREADS, NV>,
                    dim3(grid, 1, 1), THREADS, 0, st, p))))));
   return rc;
 }
@@ -189,18 +202,19 @@ int kdkl_block_norm_backward(const kdkl_block_norm_args* a, void* cuda_stream) {
                      (!a->dsum || words(a->dsum, a->ld_dsum, a->T, a->H, a->residual_type)) &&
                      words(a->dresidual, a->H, a->T, a->H, a->residual_type) && words(a->dbranch, a->H, a->T, a->H, a->type) &&
                      vectors_are_words(a);
-    if (vec && a->H <= kRowsMaxH) {
+    if (vec) {
       const bool rec = a->format != KDKL_ACT8_NONE, full = has_post && has_pre && a->dsum;
-      const int threads = rows_threads(a->H), smem = kRowsStages * (threads / 16) * rows_backward_chunk(type_bytes(a->residual_type), rec);
-      KDKL_BY_TYPE16(a->type, A, KDKL_BY_BOOL(a->residual_type == KDKL_TYPE_F32, WIDE, KDKL_BY_FORMAT_OR_NONE(a->format, FMT, KDKL_BY_BOOL(full, FULL,
-        rc = (launch_rows<block_norm_backward_rows_kernel<A, std::conditional_t<WIDE, float, A>, FMT, FULL>>(
+      const int threads = rows_threads(a->H), rb = type_bytes(a->residual_type);
+      const int smem = rows_backward_stages(rb, rec) * (threads / 16) * rows_backward_chunk(rb, rec);
+      KDKL_BY_TYPE16(a->type, A, KDKL_BY_BOOL(a->residual_type == KDKL_TYPE_F32, WIDE, KDKL_BY_FORMAT_OR_NONE(a->format, FMT, KDKL_BY_CLUSTER(a->H, full, C, FULL,
+        rc = (launch_rows<block_norm_backward_rows_kernel<A, std::conditional_t<WIDE, float, A>, FMT, FULL, C>, C>(
             parts, threads, smem, p, "block_norm_backward_rows_kernel", di, st, &parts))))));
       if (rc) return rc;
     } else {
       KDKL_BY_TYPE16(a->type, A, KDKL_BY_BOOL(a->residual_type == KDKL_TYPE_F32, WIDE,
-        KDKL_BY_BOOL(a->format != KDKL_ACT8_NONE, REC, KDKL_NORM_SHAPE(a->H, vec, VEC, THREADS, NV,
+        KDKL_BY_BOOL(a->format != KDKL_ACT8_NONE, REC, KDKL_NORM_SHAPE(a->H, THREADS, NV,
           rc = (launch("block_norm_backward_any_kernel",
-                       block_norm_backward_any_kernel<A, std::conditional_t<WIDE, float, A>, REC, THREADS, NV, VEC>,
+                       block_norm_backward_any_kernel<A, std::conditional_t<WIDE, float, A>, REC, THREADS, NV>,
                        dim3((unsigned)parts, 1, 1), THREADS, 0, st, p))))));
       if (rc) return rc;
     }

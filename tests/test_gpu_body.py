@@ -341,6 +341,15 @@ def test_norm_types(dtype, rdtype, wdtype, fmt):
     _norm_case(70, 1000, dtype, rdtype, wdtype, "token", True, True, fmt, "odd", with_dsum=False, alpha=-1.5, beta=0.0)
 
 
+@pytest.mark.parametrize("T,H", [(20, 8192), (5, 4104), (9, 12288), (7, 16392), (3, 32768)])
+@pytest.mark.parametrize("fmt", [None, "int8"])
+def test_norm_wide_rows(T, H, fmt):
+    """An fp32 residual stream at the widths that need most shared memory, and rows shared by two and four blocks."""
+    _norm_case(T, H, BF16, F32, F32, "channel", True, True, fmt, "plain")
+    _norm_case(T, H, F16, F16, F32, "token", True, False, fmt, "plain", with_dsum=True)
+    _norm_case(T, H, BF16, BF16, F32, "none", False, True, fmt, "wide", with_dsum=False)
+
+
 def test_norm_of_zero_rows_and_of_a_sum_that_cancels():
     """A row of zeros has rho = eps^-1/2 and finite results; a residual that the branch cancels exactly gives y = 0."""
     T, H, eps = 4, 256, 1e-5
