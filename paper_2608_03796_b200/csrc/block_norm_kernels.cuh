@@ -18,13 +18,14 @@
 // fixed order: bitwise reproducible.
 //
 // Two kernels each way. The *_rows kernels take rows that are whole words; rows wider than a block's 8192 columns are
-// shared by a cluster, whose blocks leave their sums in one another's shared memory: the next
-// rows travel to shared memory (cp.async, slots that only their own thread touches, so no barrier) while a row is
-// worked on, what depends on the column alone is formed once, and two values go through an instruction. The *_any
-// kernels take everything else: odd widths and addresses.
-// 32768 x 4096 bf16, one B200: forward 172 us (6.2 TB/s), leaving int8 records 238 us (5.7 TB/s); backward 290 us (5.6 TB/s),
-// from int8 records 280 us (4.8 TB/s). The backward kernel holds 128 registers a thread, so 16 warps an SM, and its
-// reduction shows: without it (and wrong) it would take 255 us. 16384 x 4095 (any): forward 178, backward 556 us.
+// shared by a cluster, whose blocks leave their sums in one another's shared memory. The next rows travel to shared memory
+// (cp.async, places that only their own thread touches, so no barrier) while a row is worked on, what depends on the
+// column alone is formed once, and two values go through an instruction. The *_any kernels take everything else: odd
+// widths and addresses.
+// 32768 x 4096 bf16, one B200: forward 167 us (6.4 TB/s), leaving int8 records 240 us (5.6 TB/s); backward 286 us (5.6 TB/s),
+// from int8 records 281 us (4.8 TB/s). The backward kernel holds 128 registers a thread, so 16 warps an SM, and its
+// reduction shows: without it (and wrong) it would take 255 us. 8192 x 16384, two blocks a row: forward 358, backward
+// 402 us. 16384 x 4095 (any): forward 178, backward 556 us.
 #pragma once
 #include "act8.cuh"
 #include "sm100_prims.cuh"
@@ -485,8 +486,10 @@ __host__ __device__ constexpr int rows_backward_stages(int residual_bytes, bool 
 // FMT -1: no records. FULL: both norms (and, backward, a gradient along the residual stream) are there, which spares the
 // loop its questions. C: blocks that share a row (a cluster); block `rank` of them has the columns of its threads' numbers
 // threadIdx.x + (2 rank) blockDim.x and threadIdx.x + (2 rank + 1) blockDim.x.
+// (Without records at most 96 registers a thread, so that a third block of 192 threads fits an SM: 138 -> 115 us at
+// 32768 x 2816. With records the 113 that the compiler takes are quicker: 240 against 258 us at 32768 x 4096.)
 template <typename A, typename R, int FMT, bool FULL, int C>
-__global__ void __launch_bounds__(kRowsThreads)
+__global__ void __launch_bounds__(FMT < 0 ? 640 : kRowsThreads)
 block_norm_forward_rows_kernel(const NormForward p) {
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ __align__(16) float sm[4][16 * C];
