@@ -24,8 +24,8 @@
 // widths and addresses.
 // 32768 x 4096 bf16, one B200: forward 167 us (6.4 TB/s), leaving int8 records 240 us (5.6 TB/s); backward 286 us (5.6 TB/s),
 // from int8 records 281 us (4.8 TB/s). The backward kernel holds 128 registers a thread, so 16 warps an SM, and its
-// reduction shows: without it (and wrong) it would take 255 us. 8192 x 16384, two blocks a row: forward 358, backward
-// 402 us. 16384 x 4095 (any): forward 178, backward 556 us.
+// reduction shows: a form that took 298 us took 255 with it left out (and a wrong result). 8192 x 16384, two blocks a
+// row: forward 358, backward 402 us. 16384 x 4095 (any): forward 178, backward 556 us.
 #pragma once
 #include "act8.cuh"
 #include "sm100_prims.cuh"
