@@ -126,18 +126,21 @@ template <> __device__ __forceinline__ Raw8<float> f32_to_raw<float>(const float
   return r;
 }
 
-// a thread's eight columns of a row of `width` values
+// Loads here are coherent ones, never ld.global.nc (nor const __restrict__, which lets the compiler choose it): a kernel
+// that may start while the one before it drains (grid_dependency_wait) reads what is written during its own lifetime, and
+// the non-coherent path is defined only for memory that nobody writes in that time.
+// A thread's eight columns of a row of `width` values:
 template <typename T, bool VEC>
-__device__ __forceinline__ Raw8<T> load_raw8(const T* __restrict__ row, int c, int width) {
+__device__ __forceinline__ Raw8<T> load_raw8(const T* row, int c, int width) {
   Raw8<T> r;
   if (VEC) {
     if (c < width) {
       if constexpr (sizeof(T) == 4) {
-        asm volatile("ld.global.nc.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+        asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                      : "=r"(r.v.x), "=r"(r.v.y), "=r"(r.v.z), "=r"(r.v.w), "=r"(r.w.x), "=r"(r.w.y), "=r"(r.w.z), "=r"(r.w.w)
                      : "l"(row + c));
       } else {
-        r.v = __ldg(reinterpret_cast<const uint4*>(row + c));
+        r.v = *reinterpret_cast<const uint4*>(row + c);
       }
     } else {
       r.v = make_uint4(0u, 0u, 0u, 0u);
@@ -152,11 +155,11 @@ __device__ __forceinline__ Raw8<T> load_raw8(const T* __restrict__ row, int c, i
   return r;
 }
 template <typename T, bool VEC>
-__device__ __forceinline__ void load8(const T* __restrict__ row, int c, int width, float (&f)[8]) {
+__device__ __forceinline__ void load8(const T* row, int c, int width, float (&f)[8]) {
   raw_to_f32(load_raw8<T, VEC>(row, c, width), f);
 }
 template <typename T, bool VEC>
-__device__ __forceinline__ void store_raw8(T* __restrict__ row, int c, int width, const Raw8<T>& r) {
+__device__ __forceinline__ void store_raw8(T* row, int c, int width, const Raw8<T>& r) {
   if (VEC) {
     if (c < width) {
       if constexpr (sizeof(T) == 4) {
@@ -307,8 +310,8 @@ __device__ __forceinline__ void record_write8(const ActRecord& r, long long t, l
 // eight neighbouring codes and their scale byte, for act_values
 __device__ __forceinline__ void record_fetch8(const ActRecord& r, long long t, long long cpitch, long long spitch, int c,
                                               uint2& codes, uint32_t& byte) {
-  codes = __ldg(reinterpret_cast<const uint2*>(r.codes + t * cpitch + c));
-  byte = __ldg(r.scales + t * spitch + (c >> 5));
+  codes = *reinterpret_cast<const uint2*>(r.codes + t * cpitch + c);
+  byte = r.scales[t * spitch + (c >> 5)];
 }
 // a thread's eight values; 0 past the end
 template <int FMT, bool VEC>
@@ -323,7 +326,7 @@ __device__ __forceinline__ void record_read8(const ActRecord& r, long long t, lo
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int col = column<VEC>(c, i);
-      f[i] = col < cpitch ? act_value<FMT>(__ldg(r.codes + t * cpitch + col), __ldg(r.scales + t * spitch + (col >> 5))) : 0.f;
+      f[i] = col < cpitch ? act_value<FMT>(r.codes[t * cpitch + col], r.scales[t * spitch + (col >> 5)]) : 0.f;
     }
   }
 }
@@ -348,7 +351,7 @@ __device__ __forceinline__ void record_read8(int fmt, const ActRecord& r, long l
 // 32768 x 4096 bf16, one B200: store 70 us (5.8 TB/s), load 64 us (6.4 TB/s, 0.99 of a copy).
 template <typename T, int FMT, bool VEC>
 __global__ void __launch_bounds__(256)
-act8_store_kernel(const T* __restrict__ x, long long ld, long long rows, int H, ActRecord rec) {
+act8_store_kernel(const T* x, long long ld, long long rows, int H, ActRecord rec) {
   const long long cpitch = act_codes_pitch(H), spitch = act_scale_pitch(H);
   const int c = first_column<VEC>(blockIdx.x * blockDim.x + threadIdx.x);
   grid_dependents_launch();

@@ -480,8 +480,8 @@ act8_dweight_kernel(const __grid_constant__ CUtensorMap tmY, const __grid_consta
 // The tiles that were cut: out (= or +=) slab 0 + slab 1 + ... in that order, rounded once. One block per 8 rows of a
 // tile, 32 threads a row. H % 8 == 0. Starts while the products drain and waits for them before it reads.
 __global__ void __launch_bounds__(256)
-act8_dweight_join_kernel(const float* __restrict__ slabs, int whole, int parts, int h_tiles, int N, int H,
-                         void* __restrict__ out, int type, int accumulate) {
+act8_dweight_join_kernel(const float* slabs, int whole, int parts, int h_tiles, int N, int H,
+                         void* out, int type, int accumulate) {
   const int i = blockIdx.x >> 5, r = (blockIdx.x & 31) * 8 + (threadIdx.x >> 5), c = (threadIdx.x & 31) * 8;
   const int tile = whole + i, row = (tile / h_tiles) * 256 + r, col = (tile % h_tiles) * 256 + c;
   const float* src = slabs + ((long long)i * parts * 256 + r) * 256 + c;

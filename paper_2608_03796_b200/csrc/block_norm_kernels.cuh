@@ -43,7 +43,7 @@ __device__ __forceinline__ float any_at(const AnyVec& v, long long i) {
 }
 // one element as bits, and what they stand for: apart, so that nothing waits for the load before its value is used
 __device__ __forceinline__ uint32_t any_bits(const AnyVec& v, long long i) {
-  return v.type == 1 ? __ldg(reinterpret_cast<const uint32_t*>(v.p) + i) : __ldg(reinterpret_cast<const uint16_t*>(v.p) + i);
+  return v.type == 1 ? reinterpret_cast<const uint32_t*>(v.p)[i] : reinterpret_cast<const uint16_t*>(v.p)[i];
 }
 __device__ __forceinline__ float any_value(uint32_t bits, int type) {
   if (type == 1) return __uint_as_float(bits);
@@ -663,8 +663,8 @@ block_norm_backward_rows_kernel(const NormBackward p) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         if (c[i] >= H) continue;
-        byte_b[i] = __ldg(p.rec_branch.scales + t * spitch + (c[i] >> 5));
-        if (has_pre) byte_x[i] = __ldg(p.rec_sum.scales + t * spitch + (c[i] >> 5));
+        byte_b[i] = p.rec_branch.scales[t * spitch + (c[i] >> 5)];
+        if (has_pre) byte_x[i] = p.rec_sum.scales[t * spitch + (c[i] >> 5)];
       }
     }
   };
@@ -786,7 +786,7 @@ block_norm_backward_rows_kernel(const NormBackward p) {
 // each warp the 32 partial sums of a column. Starts while the kernel before it drains and waits for it before it reads.
 struct NormColumns { void* out[3]; int type[3]; int which[3]; };
 __global__ void __launch_bounds__(1024)
-block_norm_columns_kernel(const float* __restrict__ partial, int parts, int H, long long cpitch, const NormColumns p) {
+block_norm_columns_kernel(const float* partial, int parts, int H, long long cpitch, const NormColumns p) {
   __shared__ float sm[32][33];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, q = blockIdx.y;
   grid_dependents_launch();

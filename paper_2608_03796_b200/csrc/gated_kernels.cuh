@@ -33,7 +33,7 @@ __device__ __forceinline__ float gate_sigmoid(float g, float& slope) {
 
 template <typename T, int ACT, int FMT /* -1: nothing is kept */, bool VEC>
 __global__ void __launch_bounds__(256)
-gated_forward_kernel(const T* __restrict__ gate, const T* __restrict__ up, long long ld, long long rows, int F,
+gated_forward_kernel(const T* gate, const T* up, long long ld, long long rows, int F,
                      T* __restrict__ h, long long ld_h, ActRecord rec_gate, ActRecord rec_up, ActRecord rec_h) {
   const long long cpitch = act_codes_pitch(F), spitch = act_scale_pitch(F);
   const int c = first_column<VEC>(blockIdx.x * blockDim.x + threadIdx.x);
@@ -63,7 +63,7 @@ gated_forward_kernel(const T* __restrict__ gate, const T* __restrict__ up, long 
 
 template <typename T, int ACT, int FMT, bool VEC>
 __global__ void __launch_bounds__(256)
-gated_backward_kernel(ActRecord rec_gate, ActRecord rec_up, const T* __restrict__ dh, long long ld_dh, long long rows,
+gated_backward_kernel(ActRecord rec_gate, ActRecord rec_up, const T* dh, long long ld_dh, long long rows,
                       int F, T* __restrict__ dgate, T* __restrict__ dup, long long ld) {
   const long long cpitch = act_codes_pitch(F), spitch = act_scale_pitch(F);
   const int c = first_column<VEC>(blockIdx.x * blockDim.x + threadIdx.x);
