@@ -53,8 +53,14 @@ def _rows(t: torch.Tensor, T: int, H: int, dtype, name: str):
     return t.data_ptr(), (apart if T > 1 else H)
 
 
-def _stream() -> int:
-    return _raw_stream(_device())
+def _stream(at: int, what: str) -> int:
+    """The current stream, for a holder whose own memory is on CUDA device `at` (-1: on the host). The kernels get that
+    memory as stored addresses, so a holder from elsewhere is refused here, as binding refuses any such tensor."""
+    now = _device()
+    if at != now:
+        raise TypeError(f"kdkl: {what}: its memory is on {'the host' if at < 0 else f'cuda:{at}'}, but the current device is "
+                        f"cuda:{now} (one process per GPU: torch.cuda.set_device first)")
+    return _raw_stream(now)
 
 
 def _vector(t: Optional[torch.Tensor], n: int, dtype, name: str):
@@ -81,14 +87,14 @@ class Act8Record:
             buffer = torch.empty(self.nbytes, dtype=torch.uint8, device=device)
         elif buffer.dtype != torch.uint8 or not buffer.is_contiguous() or buffer.numel() < self.nbytes:
             raise TypeError(f"kdkl: a record of shape {(T, H)} is {self.nbytes} contiguous bytes")
-        self.buffer, self.ptr = buffer, buffer.data_ptr()
+        self.buffer, self.ptr, self.at = buffer, buffer.data_ptr(), buffer.get_device()
         L = B.lib()
         self._store, self._load = L.kdkl_act8_store, L.kdkl_act8_load
 
     def store(self, x: torch.Tensor) -> "Act8Record":
         ptr, ld = _rows(x, self.T, self.H, x.dtype, "x")
         B._check(self._store(ptr, _lookup(TYPES, x.dtype, "x"), ld, self.T, self.H, self.code, self.ptr, self.nbytes,
-                             _stream()))
+                             _stream(self.at, "record")))
         return self
 
     def load(self, out: Optional[torch.Tensor] = None, dtype=torch.bfloat16) -> torch.Tensor:
@@ -96,7 +102,7 @@ class Act8Record:
             out = torch.empty(self.T, self.H, dtype=dtype, device=self.buffer.device)
         ptr, ld = _rows(out, self.T, self.H, out.dtype, "out")
         B._check(self._load(self.ptr, self.nbytes, self.T, self.H, self.code, ptr, _lookup(TYPES, out.dtype, "out"), ld,
-                            _stream()))
+                            _stream(self.at, "record")))
         return out
 
 
@@ -112,6 +118,7 @@ class Act8WeightGrad:
             raise ValueError(f"kdkl: no weight gradient of shape {(T, N, H)}")
         self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
         self.dweight = torch.empty(N, H, dtype=dtype, device=device)
+        self.at = self.dweight.get_device()
         self._run, self._own = B.lib().kdkl_act8_dweight, (self.dweight.data_ptr(), self.workspace.data_ptr(), nbytes)
 
     def run(self, dy: torch.Tensor, record: Act8Record, out: Optional[torch.Tensor] = None,
@@ -125,8 +132,10 @@ class Act8WeightGrad:
         else:
             to = B._dptr(out, self.dtype, (self.N, self.H), "out")
         ptr, ld = _rows(dy, self.T, self.N, torch.bfloat16, "dy")
+        stream = _stream(record.at, "record")
         B._check(self._run(ptr, ld, record.ptr, record.nbytes, self.T, self.N, self.H, record.code, to, self.type,
-                           1 if accumulate else 0, workspace, nbytes, _stream()))
+                           1 if accumulate else 0, workspace, nbytes,
+                           stream if self.at == record.at else _stream(self.at, "weight gradient")))
         return out
 
     def status(self):
@@ -144,7 +153,7 @@ class GatedAct:
         self.T, self.F, self.dtype, self.type = T, F, dtype, TYPES[dtype]
         self.act, self.format = _lookup(ACTS, act, "act"), _lookup(FORMATS, act8, "act8")
         self.h = torch.empty(T, F, dtype=dtype, device=device)
-        self.device, self._h = self.h.device, self.h.data_ptr()
+        self.device, self.at, self._h = self.h.device, self.h.get_device(), self.h.data_ptr()
         self._forward, self._backward = B.lib().kdkl_gated_act_forward, B.lib().kdkl_gated_act_backward
         self.gate_record = self.up_record = self.h_record = None
         self.dgate_up = None
@@ -161,7 +170,7 @@ class GatedAct:
         records = (None, None, None, 0) if keep is None else (keep.ptr, self.up_record.ptr,
                                                               None if also is None else also.ptr, keep.nbytes)
         B._check(self._forward(g, u, ld, self.type, self.T, self.F, self.act, self.format, self._h, self.F, *records,
-                               _stream()))
+                               _stream(self.at, "gated activation")))
         return self.h
 
     def backward(self, dh: torch.Tensor):
@@ -172,10 +181,13 @@ class GatedAct:
             self.dgate_up = torch.empty(self.T, 2 * self.F, dtype=self.dtype, device=self.device)
             self.halves = self.dgate_up[:, :self.F], self.dgate_up[:, self.F:]
         d, ld = _rows(dh, self.T, self.F, self.dtype, "dh")
+        for kept in (self.gate_record, self.up_record):
+            if kept.at != self.at:                                          # (autograd's hooks may have moved it)
+                _stream(kept.at, "record")
         out = self.dgate_up.data_ptr()
         B._check(self._backward(
             self.gate_record.ptr, self.up_record.ptr, self.gate_record.nbytes, self.format, d, ld, self.type, self.T, self.F, self.act,
-            out, out + self.F * self.dtype.itemsize, 2 * self.F, _stream()))
+            out, out + self.F * self.dtype.itemsize, 2 * self.F, _stream(self.at, "gated activation")))
         return self.halves
 
 
@@ -230,7 +242,7 @@ class BlockNorm:
         a.T, a.H = T, H
         self.y = torch.empty(T, H, dtype=dtype, device=device)
         self.sum = torch.empty(T, H, dtype=residual_dtype, device=device)
-        a.y, a.sum = self.y.data_ptr(), self.sum.data_ptr()
+        a.y, a.sum, self.at = self.y.data_ptr(), self.sum.data_ptr(), self.y.get_device()
         self.branch_record = self.sum_record = self.y_record = None
         self.workspace = self.dresidual = self.dbranch = None               # made by the first backward call
         if train:
@@ -253,7 +265,7 @@ class BlockNorm:
         a.branch, a.ld_branch = _rows(branch, self.T, self.H, self.dtype, "branch")
         self._weights(post_weight, pre_weight, gate)
         self._records()
-        B._check(self._forward(self._ref, _stream()))
+        B._check(self._forward(self._ref, _stream(self.at, "block norm")))
         self.kept = (branch, self.sum, post_weight, pre_weight, gate)           # what the backward call reads
         return (self.y if pre_weight is not None else None), self.sum
 
@@ -275,6 +287,9 @@ class BlockNorm:
     def _records(self):
         a = self.args
         if a.format >= 0:
+            for kept in (self.branch_record, self.sum_record, self.y_record):
+                if kept is not None and kept.at != self.at:                 # (autograd's hooks may have moved it)
+                    _stream(kept.at, "record")
             a.branch_record, a.sum_record = self.branch_record.ptr, self.sum_record.ptr
             a.y_record = None if self.y_record is None else self.y_record.ptr
             a.record_bytes = self.branch_record.nbytes
@@ -319,5 +334,5 @@ class BlockNorm:
         a.dpost_weight = None if d.post_weight is None else d.post_weight.data_ptr()
         a.dpre_weight = None if d.pre_weight is None else d.pre_weight.data_ptr()
         a.dgate = None if d.gate is None else d.gate.data_ptr()
-        B._check(self._backward(self._ref, _stream()))
+        B._check(self._backward(self._ref, _stream(self.at, "block norm")))
         return d
