@@ -43,6 +43,21 @@ __device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
   return ok != 0;
 }
 
+// The same for a barrier that the other CTA of a pair arrives on (mbar_arrive_pair): a wait's default scope is the CTA.
+// This one acquires, for the cluster, what that CTA had in its shared memory when it arrived.
+__device__ __forceinline__ bool mbar_try_wait_pair(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.relaxed.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  if (ok) asm volatile("fence.acquire.sync_restrict::shared::cluster.cluster;" ::: "memory");
+  return ok != 0;
+}
+
 // Wait limit: no legitimate wait in these kernels lasts longer than a few hundred
 // microseconds; two seconds means a protocol error, which is reported, not spun on.
 constexpr uint64_t kWaitLimitNs = 2000000000ull;
@@ -66,13 +81,15 @@ template <int N> __device__ __forceinline__ void regs_dec() { asm volatile("setm
 
 // Bounded wait. Returns false when the CTA has aborted (flag set by any role) or the
 // limit expired (then it sets the flag itself and records `where` in the status word).
+template <bool PAIR = false>
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag,
                                           int* status_word, int where, uint64_t limit_ns = kWaitLimitNs) {
-  if (mbar_try_wait(bar, parity)) return true;
+  auto try_wait = [&] { return PAIR ? mbar_try_wait_pair(bar, parity) : mbar_try_wait(bar, parity); };
+  if (try_wait()) return true;
   const uint64_t t0 = globaltimer_ns();
   uint32_t spins = 0;
   while (true) {
-    if (mbar_try_wait(bar, parity)) return true;
+    if (try_wait()) return true;
     if ((++spins & 63u) == 0u) {
       if (*abort_flag) return false;
       if (globaltimer_ns() - t0 > limit_ns) {
@@ -220,6 +237,13 @@ __device__ __forceinline__ uint32_t map_to_cta(uint32_t smem_addr, uint32_t rank
 }
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_bar) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
+// The same arrival where the other CTA's thread goes by it to use this CTA's memory (an arrival's default scope is the
+// CTA): releases, for the cluster, what is in this CTA's shared memory. An arrival with .release.cluster would release
+// everything, which is a full memory barrier.
+__device__ __forceinline__ void mbar_arrive_pair(uint32_t cluster_bar) {
+  asm volatile("fence.release.sync_restrict::shared::cta.cluster;" ::: "memory");
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
 // TMA load into this CTA's shared memory whose completion is signalled on a barrier that may
 // belong to the other CTA of the pair (no multicast: every CTA fetches its own boxes).

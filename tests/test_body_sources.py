@@ -26,3 +26,17 @@ def test_kernels_that_start_early_read_coherently(name):
     assert not re.search(r"\.nc\b", code) and "__ldg" not in code
     for declaration in re.findall(r"[^,;(){}]*__restrict__", code):
         assert "const" not in declaration, declaration
+
+
+def test_the_pairs_leader_acquires_what_the_peer_wrote():
+    """The leader's MMAs read the peer CTA's shared memory and overwrite its tensor memory: what tells the leader that it
+    may has to be released and acquired for the cluster. An arrival's and a wait's default scope is the CTA."""
+    code = _code("act8_dweight.cuh")
+    assert "mbar_arrive_cluster(" not in code
+    for barrier in ("full", "tempty"):
+        assert f"mbar_wait<true>({barrier}(" in code and f"mbar_wait({barrier}(" not in code
+        assert f"mbar_arrive_pair(map_to_cta({barrier}(" in code
+    prims = _code("sm100_prims.cuh")
+    for part in ("fence.release.sync_restrict::shared::cta.cluster", "mbarrier.arrive.relaxed.cluster",
+                 "mbarrier.try_wait.parity.relaxed.cluster", "fence.acquire.sync_restrict::shared::cluster.cluster"):
+        assert part in prims
