@@ -411,7 +411,8 @@ int kdkl_gated_act_backward(const void* gate_record, const void* up_record, size
  * dY^T x~, dY [T, N] bf16 with rows ld_dy apart, x~ [T, H] what the record stands for; sums in fp32, rounded once to
  * `type` (F32 or BF16). T = 0 writes zeros (nothing when accumulating).
  * workspace: device, 256-byte aligned, kdkl_act8_dweight_workspace_bytes(); its first words are a status block readable
- * with kdkl_status (KDKL_ERR_TIMEOUT). Bitwise reproducible. */
+ * with kdkl_status (KDKL_ERR_TIMEOUT: a wait ran out and the result is not whole), that of the last call: every call clears
+ * it. Bitwise reproducible. */
 size_t kdkl_act8_dweight_workspace_bytes(int64_t T, int64_t N, int64_t H, int32_t type);
 int kdkl_act8_dweight(const void* dy_bf16, int64_t ld_dy, const void* record, size_t record_bytes, int64_t T, int64_t N,
                       int64_t H, int32_t format, void* dweight, int32_t type, int32_t accumulate, void* workspace,

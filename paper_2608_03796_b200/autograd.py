@@ -39,6 +39,8 @@ from . import body
 
 _free: dict = {}          # key -> buffer sets (FusedChunkedKL holders) no live loss is using
 _probed: list = []        # buffer sets whose last step's status has not been looked at yet
+_idle: list = []          # _StepStatus objects that wait for nothing
+_captured: list = []      # (what, status words) of steps that a CUDA graph repeats
 
 
 def clear_cache() -> None:
@@ -47,6 +49,7 @@ def clear_cache() -> None:
         check_status()
     finally:
         _free.clear()
+        _captured.clear()
 
 
 def _probe(op) -> None:
@@ -71,17 +74,50 @@ def _collect(op) -> None:
         _probed.remove(op)
     code, where = int(op.probe[0]), int(op.probe[1])
     if code not in (0, -10):                                      # -10: out-of-range teacher indices were ignored
-        raise B.KdklError(code, f"device status of an earlier fused_chunked_kl step, detail {where}")
+        what = getattr(op, "what", "fused_chunked_kl")
+        if isinstance(op, _StepStatus):
+            _idle.append(op)
+        raise B.KdklError(code, f"device status of an earlier {what} step, detail {where}")
+    if isinstance(op, _StepStatus):
+        _idle.append(op)
+
+
+class _StepStatus:
+    """The status of one step whose workspace is not kept: 16 bytes of pinned memory and an event."""
+    what = ""
+
+
+def _watch(workspace, what: str) -> None:
+    """Remembers the status words that the step just enqueued leaves in `workspace` for check_status, and looks at those
+    of earlier such steps that have ended."""
+    if torch.cuda.is_current_stream_capturing():
+        words = torch.empty(4, dtype=torch.int32, device=workspace.device)     # every replay writes them again
+        words.copy_(workspace[:16].view(torch.int32))
+        _captured.append((what, words))
+        return
+    op = _idle.pop() if _idle else _StepStatus()
+    op.what, op.workspace = what, workspace
+    _probe(op)
+    op.workspace = None
+    for earlier in [q for q in _probed if isinstance(q, _StepStatus) and q is not op]:
+        if not earlier.probe_event.query():
+            break                                             # (in the order of the steps)
+        _collect(earlier)
 
 
 def check_status() -> None:
-    """Raises if any step whose status has not been looked at yet failed on the device (waits for those steps)."""
+    """Raises if any step whose status has not been looked at yet failed on the device (waits for those steps), or the last
+    replay of a step that a CUDA graph repeats."""
     first = None
     for op in list(_probed):                   # every pending status is collected, the first failure is raised
         try:
             _collect(op)
         except B.KdklError as e:
             first = first or e
+    for what, words in _captured:
+        code, where = words[:2].tolist()
+        if code == -8:                         # KDKL_ERR_TIMEOUT (before the first replay the words are anything)
+            first = first or B.KdklError(code, f"device status of a captured {what} step, detail {where}")
     if first is not None:
         raise first
 
@@ -226,7 +262,7 @@ def _recorded(*tensors) -> bool:
 
 class _Act8Linear(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, weight, record, act8, keep):
+    def forward(ctx, x, weight, record, act8, keep, sync_status):
         N, H = weight.shape
         rows = _flat(x, H)
         if keep:
@@ -234,7 +270,7 @@ class _Act8Linear(torch.autograd.Function):
                 record = body.Act8Record(rows.shape[0], H, act8, device=x.device).store(rows)
             elif (record.T, record.H) != tuple(rows.shape):
                 raise TypeError(f"act8_linear: the record is of shape {(record.T, record.H)}, the input of {tuple(rows.shape)}")
-            ctx.format = record.format
+            ctx.format, ctx.sync_status = record.format, sync_status
         ctx.save_for_backward(weight, None if record is None else record.buffer)
         ctx.shape = x.shape
         return torch.matmul(rows, weight.t()).reshape(*x.shape[:-1], N)          # a plain library product
@@ -248,18 +284,28 @@ class _Act8Linear(torch.autograd.Function):
         dw = None
         if ctx.needs_input_grad[1]:
             record = body.Act8Record(rows.shape[0], H, ctx.format, buffer=buffer)
-            dw = body.Act8WeightGrad(rows.shape[0], N, H, dtype=weight.dtype, device=dy.device).run(rows, record)
-        return dx, dw, None, None, None
+            op = body.Act8WeightGrad(rows.shape[0], N, H, dtype=weight.dtype, device=dy.device)
+            dw = op.run(rows, record)
+            if ctx.sync_status:
+                code, detail = op.status()
+                if code != 0:
+                    raise B.KdklError(code, f"device status of an act8_linear step, detail {detail}")
+            else:
+                _watch(op.workspace, "act8_linear")
+        return dx, dw, None, None, None, None
 
 
-def act8_linear(x, weight, record: Optional[body.Act8Record] = None, act8: str = "int8") -> torch.Tensor:
+def act8_linear(x, weight, record: Optional[body.Act8Record] = None, act8: str = "int8",
+                sync_status: bool = False) -> torch.Tensor:
     """x @ weight.T (bf16, x [..., H], weight [N, H]) that keeps x in 8 bits for the weight's gradient: in `record`, if
-    one that stands for x exists already (block_norm and gated_act leave them), else in one of format `act8`."""
+    one that stands for x exists already (block_norm and gated_act leave them), else in one of format `act8`. A wait that
+    runs out in the weight gradient's kernel is reported as the loss reports its steps: by check_status, by a later
+    step, or by the backward call itself with sync_status (which waits for the kernel)."""
     if x.dtype != torch.bfloat16 or weight.dtype != torch.bfloat16:
         raise TypeError(f"act8_linear: expected bf16, got {x.dtype} and {weight.dtype}")
     if act8 not in ("int8", "e4m3"):
         raise ValueError(f"act8_linear: expected a record format, got {act8!r}")
-    return _Act8Linear.apply(x, weight, record, act8, _recorded(weight))
+    return _Act8Linear.apply(x, weight, record, act8, _recorded(weight), bool(sync_status))
 
 
 class _GatedAct(torch.autograd.Function):

@@ -139,6 +139,7 @@ class Act8WeightGrad:
         return out
 
     def status(self):
+        """(code, detail) of the last run, which waits for it; every run starts with a clear status."""
         return B.kdkl_status(self.workspace)
 
 
