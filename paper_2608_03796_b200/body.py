@@ -9,8 +9,8 @@ read them in the backward pass.
     d = join.backward(dy, dx)                           # d.residual, d.branch, d.post_weight, d.pre_weight, d.gate
 
 The classes hold outputs, records and workspaces of one shape: calls allocate nothing, only enqueue on the current
-stream, and return the holder's own buffers, which the next call overwrites. Marshalling only; autograd entries
-that allocate their outputs are in ``autograd``. Formats are "int8", "e4m3" or None (nothing is kept in 8 bits).
+stream, and return the holder's own buffers, which the next call overwrites (a graph of autograd's that has saved one of
+them raises then). Marshalling only; autograd entries that allocate their outputs are in ``autograd``. Formats are "int8", "e4m3" or None (nothing is kept in 8 bits).
 """
 from __future__ import annotations
 
@@ -35,6 +35,9 @@ def _lookup(table, key, name):
 
 
 _device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+# The library writes through addresses, which autograd does not see: a graph that has saved a tensor would use the new
+# values without a word. Every call therefore says which tensors it has written.
+_written = torch.autograd.graph.increment_version
 
 
 def _rows(t: torch.Tensor, T: int, H: int, dtype, name: str):
@@ -95,6 +98,7 @@ class Act8Record:
         ptr, ld = _rows(x, self.T, self.H, x.dtype, "x")
         B._check(self._store(ptr, _lookup(TYPES, x.dtype, "x"), ld, self.T, self.H, self.code, self.ptr, self.nbytes,
                              _stream(self.at, "record")))
+        _written(self.buffer)
         return self
 
     def load(self, out: Optional[torch.Tensor] = None, dtype=torch.bfloat16) -> torch.Tensor:
@@ -103,6 +107,7 @@ class Act8Record:
         ptr, ld = _rows(out, self.T, self.H, out.dtype, "out")
         B._check(self._load(self.ptr, self.nbytes, self.T, self.H, self.code, ptr, _lookup(TYPES, out.dtype, "out"), ld,
                             _stream(self.at, "record")))
+        _written(out)
         return out
 
 
@@ -136,6 +141,7 @@ class Act8WeightGrad:
         B._check(self._run(ptr, ld, record.ptr, record.nbytes, self.T, self.N, self.H, record.code, to, self.type,
                            1 if accumulate else 0, workspace, nbytes,
                            stream if self.at == record.at else _stream(self.at, "weight gradient")))
+        _written(out)
         return out
 
     def status(self):
@@ -167,11 +173,14 @@ class GatedAct:
         u, ld_u = _rows(up, self.T, self.F, self.dtype, "up")
         if ld_u != ld:
             raise TypeError(f"kdkl: gate and up must have their rows equally far apart, got {ld} and {ld_u}")
-        keep, also = self.gate_record, self.h_record
-        records = (None, None, None, 0) if keep is None else (keep.ptr, self.up_record.ptr,
-                                                              None if also is None else also.ptr, keep.nbytes)
+        keep, also, written = self.gate_record, self.h_record, [self.h]
+        records = (None, None, None, 0)
+        if keep is not None:
+            records = (keep.ptr, self.up_record.ptr, None if also is None else also.ptr, keep.nbytes)
+            written += [keep.buffer, self.up_record.buffer] if also is None else [keep.buffer, self.up_record.buffer, also.buffer]
         B._check(self._forward(g, u, ld, self.type, self.T, self.F, self.act, self.format, self._h, self.F, *records,
                                _stream(self.at, "gated activation")))
+        _written(written)
         return self.h
 
     def backward(self, dh: torch.Tensor):
@@ -189,6 +198,7 @@ class GatedAct:
         B._check(self._backward(
             self.gate_record.ptr, self.up_record.ptr, self.gate_record.nbytes, self.format, d, ld, self.type, self.T, self.F, self.act,
             out, out + self.F * self.dtype.itemsize, 2 * self.F, _stream(self.at, "gated activation")))
+        _written(self.dgate_up)
         return self.halves
 
 
@@ -265,8 +275,10 @@ class BlockNorm:
         a.residual, a.ld_residual = _rows(residual, self.T, self.H, self.residual_dtype, "residual")
         a.branch, a.ld_branch = _rows(branch, self.T, self.H, self.dtype, "branch")
         self._weights(post_weight, pre_weight, gate)
-        self._records()
+        written = self._records()
+        written += (self.sum,) if pre_weight is None else (self.sum, self.y)
         B._check(self._forward(self._ref, _stream(self.at, "block norm")))
+        _written(written)
         self.kept = (branch, self.sum, post_weight, pre_weight, gate)           # what the backward call reads
         return (self.y if pre_weight is not None else None), self.sum
 
@@ -286,14 +298,18 @@ class BlockNorm:
             a.gate = _vector(gate, H if a.gate_kind == 1 else self.T, gate.dtype, "gate")
 
     def _records(self):
-        a = self.args
+        """Their memory goes into the arguments and is returned."""
+        a, buffers = self.args, []
         if a.format >= 0:
             for kept in (self.branch_record, self.sum_record, self.y_record):
-                if kept is not None and kept.at != self.at:                 # (autograd's hooks may have moved it)
-                    _stream(kept.at, "record")
+                if kept is not None:
+                    if kept.at != self.at:                                  # (autograd's hooks may have moved it)
+                        _stream(kept.at, "record")
+                    buffers.append(kept.buffer)
             a.branch_record, a.sum_record = self.branch_record.ptr, self.sum_record.ptr
             a.y_record = None if self.y_record is None else self.y_record.ptr
             a.record_bytes = self.branch_record.nbytes
+        return buffers
 
     def _grad(self, name, like):
         """The holder's gradient buffer for a weight or gate (made when first needed, or when its type changes)."""
@@ -336,4 +352,5 @@ class BlockNorm:
         a.dpre_weight = None if d.pre_weight is None else d.pre_weight.data_ptr()
         a.dgate = None if d.gate is None else d.gate.data_ptr()
         B._check(self._backward(self._ref, _stream(self.at, "block norm")))
+        _written([t for t in d if t is not None])
         return d

@@ -54,3 +54,30 @@ def test_holders_on_another_device_are_refused_before_a_launch(monkeypatch):
     for call in (lambda: grad.run(x, rec), lambda: ffn.backward(x), lambda: join.backward(x, x)):
         with pytest.raises(TypeError, match="record"):
             call()
+
+
+def test_what_a_call_writes_is_marked_as_changed(monkeypatch):
+    """Autograd's version counters, by which a graph knows that a tensor it has saved was changed, without a launch."""
+    T, H, N = 4, 64, 8
+    monkeypatch.setattr(body, "_rows", lambda t, T, H, dtype, name: (P, H))
+    monkeypatch.setattr(body, "_vector", lambda t, n, dtype, name: P)
+    monkeypatch.setattr(body, "_stream", lambda at, what: 0)
+    x, w = torch.zeros(T, H, dtype=torch.bfloat16), torch.ones(H, dtype=torch.bfloat16)
+    rec = body.Act8Record(T, H, device="cpu")
+    grad = body.Act8WeightGrad(T, N, H, device="cpu")
+    ffn = body.GatedAct(T, H, device="cpu", keep_h=True)
+    join = body.BlockNorm(T, H, act8="int8", gate="channel", keep_y=True, device="cpu")
+    rec._store = rec._load = grad._run = ffn._forward = ffn._backward = join._forward = join._backward = lambda *args: 0
+    out, dy = torch.empty(T, H, dtype=torch.bfloat16), torch.zeros(T, N, dtype=torch.bfloat16)
+    ffn.forward(x, x), ffn.backward(x), join.forward(x, x, w, w, w), join.backward(x, x)
+    for call, written in ((lambda: rec.store(x), [rec.buffer]), (lambda: rec.load(out), [out]),
+                          (lambda: grad.run(dy, rec), [grad.dweight]),
+                          (lambda: ffn.forward(x, x), [ffn.h, ffn.gate_record.buffer, ffn.up_record.buffer, ffn.h_record.buffer]),
+                          (lambda: ffn.backward(x), [ffn.dgate_up, *ffn.halves]),
+                          (lambda: join.forward(x, x, w, w, w), [join.y, join.sum, join.branch_record.buffer,
+                                                                 join.sum_record.buffer, join.y_record.buffer]),
+                          (lambda: join.backward(x, x), [join.dresidual, join.dbranch, *join.grads.values()])):
+        before = [t._version for t in written]
+        call()
+        assert all(t._version > v for t, v in zip(written, before))
+    assert x._version == w._version == 0                                    # inputs are not
