@@ -30,12 +30,47 @@ Their outputs, records and gradients are allocated per call, as a graph needs th
 """
 from __future__ import annotations
 
+import functools
 from typing import Optional
 
 import torch
 
 from . import binding as B
 from . import body
+
+
+class _NoSecondDerivative(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, name, anchor, *grads):
+        ctx.name = name
+        return tuple(g.view_as(g) for g in grads)
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError(f"{ctx.name}: the backward pass is computed by kernels that have no derivative, so there are no "
+                           "second derivatives through it")
+
+
+def _first_derivative_only(name):
+    """For the backward pass of a Function whose kernels autograd cannot differentiate. Under create_graph its gradients
+    come back as ever, but a graph that depends on them raises when it is differentiated: their dependence on the saved
+    tensors would otherwise be missing in silence (whether or not the upstream gradient needs a graph itself)."""
+    def wrap(backward):
+        @functools.wraps(backward)
+        def once(ctx, *grads):
+            if not torch.is_grad_enabled():
+                return backward(ctx, *grads)
+            with torch.no_grad():
+                out = backward(ctx, *grads)
+            outs = list(out if isinstance(out, tuple) else (out,))
+            at = [i for i, t in enumerate(outs) if isinstance(t, torch.Tensor)]
+            if at:
+                for i, t in zip(at, _NoSecondDerivative.apply(name, torch.empty(0, requires_grad=True), *(outs[i] for i in at))):
+                    outs[i] = t
+            return tuple(outs)
+        return once
+    return wrap
+
 
 _free: dict = {}          # key -> buffer sets (FusedChunkedKL holders) no live loss is using
 _probed: list = []        # buffer sets whose last step's status has not been looked at yet
@@ -170,6 +205,7 @@ class _FusedChunkedKL(torch.autograd.Function):
         return loss
 
     @staticmethod
+    @_first_derivative_only("fused_chunked_kl")
     def backward(ctx, grad):
         hidden, weight = ctx.saved_tensors
         op = ctx.op
@@ -226,6 +262,7 @@ class _FeatureLoss(torch.autograd.Function):
         return loss.squeeze(0)
 
     @staticmethod
+    @_first_derivative_only("feature_loss")
     def backward(ctx, g):
         # one more pass of the same kernel writes grad * d loss / d student; the upstream gradient stays on the device
         student, teacher, ws = ctx.saved_tensors
@@ -276,6 +313,7 @@ class _Act8Linear(torch.autograd.Function):
         return torch.matmul(rows, weight.t()).reshape(*x.shape[:-1], N)          # a plain library product
 
     @staticmethod
+    @_first_derivative_only("act8_linear")
     def backward(ctx, dy):
         weight, buffer = ctx.saved_tensors
         N, H = weight.shape
@@ -323,6 +361,7 @@ class _GatedAct(torch.autograd.Function):
         return h, record
 
     @staticmethod
+    @_first_derivative_only("gated_act")
     def backward(ctx, dh, _):
         op, F = ctx.op, ctx.shape[-1] // 2
         op.gate_record, op.up_record = (body.Act8Record(op.T, F, ctx.format, buffer=b) for b in ctx.saved_tensors)
@@ -366,6 +405,7 @@ class _BlockNorm(torch.autograd.Function):
         return y, x, record
 
     @staticmethod
+    @_first_derivative_only("block_norm")
     def backward(ctx, dy, dx, _):
         if dy is None and dx is None:
             return (None,) * 10
