@@ -265,7 +265,7 @@ class BlockNorm:
         if keeps:
             self.branch_record, self.sum_record = Act8Record(T, H, act8, device), Act8Record(T, H, act8, device)
             self.y_record = Act8Record(T, H, act8, device) if keep_y else None
-        self.grads = {}
+        self.grads, self.kept = {}, None
         self._ref = ctypes.byref(a)
         self._forward, self._backward = B.lib().kdkl_block_norm_forward, B.lib().kdkl_block_norm_backward
 
@@ -279,7 +279,8 @@ class BlockNorm:
         written += (self.sum,) if pre_weight is None else (self.sum, self.y)
         B._check(self._forward(self._ref, _stream(self.at, "block norm")))
         _written(written)
-        self.kept = (branch, self.sum, post_weight, pre_weight, gate)           # what the backward call reads
+        if self.train:                                                      # what the backward call reads
+            self.kept = (*((branch, self.sum) if a.format < 0 else (None, None)), post_weight, pre_weight, gate)
         return (self.y if pre_weight is not None else None), self.sum
 
     def _weights(self, post_weight, pre_weight, gate):
@@ -324,6 +325,8 @@ class BlockNorm:
         """Gradients of the last forward call's inputs from those of y (None without a pre norm) and of x."""
         if not self.train:
             raise RuntimeError("kdkl: this block norm keeps nothing for a backward pass (train=False)")
+        if self.kept is None:
+            raise RuntimeError("kdkl: this block norm's backward call comes before any forward call")
         a = self.args
         if self.workspace is None:
             device = self.rho.device

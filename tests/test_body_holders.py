@@ -81,3 +81,10 @@ def test_what_a_call_writes_is_marked_as_changed(monkeypatch):
         call()
         assert all(t._version > v for t, v in zip(written, before))
     assert x._version == w._version == 0                                    # inputs are not
+
+
+def test_a_block_norms_backward_call_before_any_forward_call():
+    x = torch.zeros(4, 64, dtype=torch.bfloat16)
+    for act8 in (None, "int8"):
+        with pytest.raises(RuntimeError, match="before any forward"):
+            body.BlockNorm(4, 64, act8=act8, device="cpu").backward(x, x)
