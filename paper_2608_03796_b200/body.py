@@ -163,7 +163,7 @@ class GatedAct:
         self.device, self.at, self._h = self.h.device, self.h.get_device(), self.h.data_ptr()
         self._forward, self._backward = B.lib().kdkl_gated_act_forward, B.lib().kdkl_gated_act_backward
         self.gate_record = self.up_record = self.h_record = None
-        self.dgate_up = None
+        self.dgate_up, self.stored = None, False
         if act8 is not None:
             self.gate_record, self.up_record = Act8Record(T, F, act8, device), Act8Record(T, F, act8, device)
             self.h_record = Act8Record(T, F, act8, device) if keep_h else None
@@ -181,12 +181,15 @@ class GatedAct:
         B._check(self._forward(g, u, ld, self.type, self.T, self.F, self.act, self.format, self._h, self.F, *records,
                                _stream(self.at, "gated activation")))
         _written(written)
+        self.stored = True
         return self.h
 
     def backward(self, dh: torch.Tensor):
         """(dgate, dup), the halves of one [T, 2 F] buffer."""
         if self.gate_record is None:
             raise RuntimeError("kdkl: this gated activation keeps nothing for a backward pass (act8=None)")
+        if not self.stored:
+            raise RuntimeError("kdkl: this gated activation's backward call comes before any forward call")
         if self.dgate_up is None:
             self.dgate_up = torch.empty(self.T, 2 * self.F, dtype=self.dtype, device=self.device)
             self.halves = self.dgate_up[:, :self.F], self.dgate_up[:, self.F:]

@@ -33,6 +33,7 @@ def test_holders_on_another_device_are_refused_before_a_launch(monkeypatch):
             r._store = r._load = reached
         grad._run = ffn._forward = ffn._backward = join._forward = join._backward = reached
         plain._forward = plain._backward = reached
+        ffn.stored = True
         join.kept = plain.kept = (x, x, w, w, None)
         return rec, held, grad, ffn, join, plain
     rec, held, grad, ffn, join, plain = holders()
@@ -88,3 +89,9 @@ def test_a_block_norms_backward_call_before_any_forward_call():
     for act8 in (None, "int8"):
         with pytest.raises(RuntimeError, match="before any forward"):
             body.BlockNorm(4, 64, act8=act8, device="cpu").backward(x, x)
+
+
+def test_a_gated_activations_backward_call_before_any_forward_call():
+    """Its records hold nothing yet."""
+    with pytest.raises(RuntimeError, match="before any forward"):
+        body.GatedAct(4, 64, device="cpu").backward(torch.zeros(4, 64, dtype=torch.bfloat16))
