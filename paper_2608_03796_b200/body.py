@@ -274,6 +274,8 @@ class BlockNorm:
 
     def forward(self, residual, branch, post_weight=None, pre_weight=None, gate=None):
         """(y, x); y is None without a pre_weight."""
+        if pre_weight is None and self.y_record is not None:
+            raise ValueError("kdkl: keep_y needs a pre_weight: without one there is no y, and its record would stay another call's")
         a = self.args
         a.residual, a.ld_residual = _rows(residual, self.T, self.H, self.residual_dtype, "residual")
         a.branch, a.ld_branch = _rows(branch, self.T, self.H, self.dtype, "branch")

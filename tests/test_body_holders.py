@@ -95,3 +95,10 @@ def test_a_gated_activations_backward_call_before_any_forward_call():
     """Its records hold nothing yet."""
     with pytest.raises(RuntimeError, match="before any forward"):
         body.GatedAct(4, 64, device="cpu").backward(torch.zeros(4, 64, dtype=torch.bfloat16))
+
+
+def test_a_record_of_y_needs_a_y():
+    """Without a pre norm there is no y: its record would go on holding the call's before, or nothing."""
+    x, w = torch.zeros(4, 64, dtype=torch.bfloat16), torch.ones(64, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="keep_y"):
+        body.BlockNorm(4, 64, act8="int8", keep_y=True, device="cpu").forward(x, x, post_weight=w)
