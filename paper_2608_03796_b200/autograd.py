@@ -435,7 +435,12 @@ def block_norm(residual, branch, post_weight=None, pre_weight=None, gate=None, *
     if gate is None:
         gate_kind = "none"
     elif gate_kind is None:
+        lead = branch.shape[:-1]
         gate_kind = "channel" if gate.shape == branch.shape[-1:] else "token"
+        if gate_kind == "token" and gate.dim() > 1 and gate.shape[-1] == gate.numel() == branch.shape[-1] \
+                and gate.shape not in (lead, (*lead, 1)):
+            raise TypeError(f"block_norm: a gate of shape {tuple(gate.shape)} beside a branch of {tuple(branch.shape)}: give it one "
+                            "dimension if it is one per channel, or say gate_kind")
     if keep_y and (act8 is None or pre_weight is None):
         raise ValueError("block_norm: keep_y needs act8 and a pre_weight")
     args = dict(eps=eps, weight_offset=weight_offset, branch_scale=branch_scale, residual_scale=residual_scale)
