@@ -83,19 +83,21 @@ static int check_norm(const kdkl_block_norm_args* a, bool backward) {
 }
 
 // Launches a *_rows kernel with as many blocks, or clusters of C, as the device holds at once (at most `most`: one per row,
-// one per partial row). The shared memory a kernel may use beyond 48 KiB, its static part included, is an attribute of its copy on the
-// device, raised when a launch needs more than any before; how many blocks fit an SM is asked once per number of warps.
+// one per partial row). The shared memory a kernel may use is an attribute of its copy on the device, set once, to what its
+// widest rows take (`smem_widest`) - one value whatever the launch, so that threads that launch it for the first time at the
+// same time, at different widths, cannot leave it too small for each other. How many blocks fit an SM is asked once per
+// number of warps.
 template <auto KERN, int C, typename P>
-static int launch_rows(long long most, int threads, int smem, const P& p, const char* name, const DeviceInfo& di,
+static int launch_rows(long long most, int threads, int smem, int smem_widest, const P& p, const char* name, const DeviceInfo& di,
                        cudaStream_t st, int* rows) {
-  struct Known { int allowed; int fit[kRowsThreads / 32 + 1]; };
+  struct Known { bool allowed; int fit[kRowsThreads / 32 + 1]; };
   static Known known[kMaxDevices];
   Known fresh;
   memset(&fresh, 0, sizeof(fresh));
   Known& k = di.dev >= 0 && di.dev < kMaxDevices ? known[di.dev] : fresh;
-  if (smem > 40 * 1024 && smem > k.allowed) {
-    KDKL_CUDA(cudaFuncSetAttribute(KERN, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-    k.allowed = smem;
+  if (!k.allowed) {
+    KDKL_CUDA(cudaFuncSetAttribute(KERN, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_widest));
+    k.allowed = true;
   }
   int fit = k.fit[threads / 32];
   if (fit == 0) {
@@ -159,11 +161,11 @@ int kdkl_block_norm_forward(const kdkl_block_norm_args* a, void* cuda_stream) {
   if (vec) {
     const int fmt = any_record ? a->format : KDKL_ACT8_NONE;
     const bool full = a->post_weight && a->pre_weight;
-    const int threads = rows_threads(a->H), smem = threads / 16 * rows_forward_chunk(type_bytes(a->residual_type));
+    const int threads = rows_threads(a->H), chunk = rows_forward_chunk(type_bytes(a->residual_type));
     int blocks;
     KDKL_BY_TYPE16(a->type, A, KDKL_BY_BOOL(a->residual_type == KDKL_TYPE_F32, WIDE, KDKL_BY_FORMAT_OR_NONE(fmt, FMT, KDKL_BY_CLUSTER(a->H, full, C, FULL,
       return (launch_rows<block_norm_forward_rows_kernel<A, std::conditional_t<WIDE, float, A>, FMT, FULL, C>, C>(
-          a->T, threads, smem, p, "block_norm_forward_rows_kernel", di, st, &blocks))))));
+          a->T, threads, threads / 16 * chunk, kRowsThreads / 16 * chunk, p, "block_norm_forward_rows_kernel", di, st, &blocks))))));
   }
   KDKL_BY_TYPE16(a->type, A, KDKL_BY_BOOL(a->residual_type == KDKL_TYPE_F32, WIDE,
     KDKL_BY_BOOL(any_record, REC, KDKL_NORM_SHAPE(a->H, THREADS, NV,
@@ -205,10 +207,10 @@ int kdkl_block_norm_backward(const kdkl_block_norm_args* a, void* cuda_stream) {
     if (vec) {
       const bool rec = a->format != KDKL_ACT8_NONE, full = has_post && has_pre && a->dsum;
       const int threads = rows_threads(a->H), rb = type_bytes(a->residual_type);
-      const int smem = rows_backward_stages(rb, rec) * (threads / 16) * rows_backward_chunk(rb, rec);
+      const int row = rows_backward_stages(rb, rec) * rows_backward_chunk(rb, rec);
       KDKL_BY_TYPE16(a->type, A, KDKL_BY_BOOL(a->residual_type == KDKL_TYPE_F32, WIDE, KDKL_BY_FORMAT_OR_NONE(a->format, FMT, KDKL_BY_CLUSTER(a->H, full, C, FULL,
         rc = (launch_rows<block_norm_backward_rows_kernel<A, std::conditional_t<WIDE, float, A>, FMT, FULL, C>, C>(
-            parts, threads, smem, p, "block_norm_backward_rows_kernel", di, st, &parts))))));
+            parts, threads, threads / 16 * row, kRowsThreads / 16 * row, p, "block_norm_backward_rows_kernel", di, st, &parts))))));
       if (rc) return rc;
     } else {
       KDKL_BY_TYPE16(a->type, A, KDKL_BY_BOOL(a->residual_type == KDKL_TYPE_F32, WIDE,
