@@ -377,12 +377,17 @@ int kdkl_teacher_topk_stored(const void* hidden_bf16, const void* weight_bf16, i
  *   e    = smallest integer with max |x| <= Q 2^e over the 32 values (Q = 127 or 448), at least -126
  *   code = x 2^-e rounded to nearest even, as an integer of 8 bits (INT8) or as an e4m3 value (E4M3)
  * A group that holds an infinity or a NaN reads back as NaN in all its 32 places. Error of a value: at most half a
- * step, |x - x~| <= max |x| / 127 (INT8), or |x| / 16 + max |x| 2^-17 (E4M3); finite values read back as finite ones.
- * Decoded values are exact in bf16.
+ * step, |x - x~| <= max |x| / 127 (INT8), or |x| / 16 + max |x| 2^-17 (E4M3), but for the two ends of the range:
+ *   - where a code rounded up would stand for 2^128, the code below is taken, so that finite values read back as finite
+ *     ones: 63 2^122 (INT8, off by at most a step of 2^122) and 240 2^120 (E4M3, off by at most |x| / 16);
+ *   - where e has stopped at -126, the step goes by that: |x - x~| <= 2^-127 (INT8), |x| / 16 + 2^-136 (E4M3).
+ * Decoded values are exact in bf16, except E4M3 ones below 2^-126 at the smallest e, down to 2^-135: bf16 ends at 2^-133,
+ * and load to bf16 and the weight gradient's tensor-core form round them to it.
  * `record`: device, 256-byte aligned, kdkl_act8_bytes(T, H) bytes (H + H / 32 bytes a token, both rounded up): codes
  * [T, Hp], Hp = H rounded up to 32, padding codes 0; at the next multiple of 256 bytes the scale bytes e + 127
  * (255: not finite) [T, Sp], Sp = Hp / 32 rounded up to 16. `format` and T, H must be those the record was written with.
- * store: x [T, H] of `type`, rows ld >= H apart, is read once. load: out [T, H] of `type`, rows ld apart. */
+ * store: x [T, H] of `type`, rows ld >= H apart, is read once. load: out [T, H] of `type`, rows ld apart (F16:
+ * values beyond 65504 read back as 65504). */
 #define KDKL_ACT8_NONE (-1)
 #define KDKL_ACT8_INT8 0
 #define KDKL_ACT8_E4M3 1

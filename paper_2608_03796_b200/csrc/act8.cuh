@@ -4,11 +4,11 @@
 //   x[t, h] ~ code[t, h] * 2^e[t, h / 32],   code = int8 (-127 .. 127) or e4m3 (|code| <= 448)
 //   e = the smallest integer with max |x| <= Q 2^e over the 32 values, Q = 127 or 448, at least kActMinExp
 //   code = x 2^-e rounded to nearest even (exact scaling: nothing saturates); stored scale byte = e + 127
-//   (where rounding up would pass the largest finite fp32 number, the code below it is taken)
+//   (where rounding up would pass the largest finite fp32 number, the code below it is taken: 63 2^122 or 240 2^120)
 // A group that holds an infinity or a NaN stores byte 255 and reads back as NaN in all its 32 places.
 // Why a power of two per 32 and not one fp32 factor per row or per 128: 7 or 4 significant bits times a power of two
-// are exact in bf16, so a record is a bf16 operand of the tensor cores without a second rounding, and scaling by it
-// is exact everywhere. What the coarser factor loses (a factor of at most 2 in the int8 step) the shorter group gains
+// are exact in bf16 (down to its last subnormal, 2^-133: e4m3 codes at e = -126 go on to 2^-135), so a record is a bf16
+// operand of the tensor cores without a second rounding, and scaling by it is exact everywhere. What the coarser factor loses (a factor of at most 2 in the int8 step) the shorter group gains
 // back: the largest of 32 normal values is about 2.1 deviations, of 128 about 2.8.
 //
 // Layout in one buffer: codes [T, Hp] with Hp = H rounded up to 32 (padding codes are 0), then at the next multiple of

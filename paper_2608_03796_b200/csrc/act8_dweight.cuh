@@ -124,7 +124,8 @@ struct DwParams {
   int* status;
 };
 
-// Four bf16 values from four codes, times `scale` (a power of two in both halves). Exact. e4m3 codes arrive as their
+// Four bf16 values from four codes, times `scale` (a power of two in both halves). Exact, but for e4m3 values below bf16's
+// last subnormal (2^-133 to 2^-135, at the smallest exponent), which round to a multiple of it. e4m3 codes arrive as their
 // value times 2^-120, so their scale carries 2^120.
 template <int FMT>
 __device__ __forceinline__ void codes_to_bf16x4(uint32_t codes, uint32_t scale, uint32_t (&o)[2]) {
