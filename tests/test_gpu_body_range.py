@@ -80,3 +80,18 @@ def test_the_weight_gradient_at_the_smallest_exponent(fmt, T, N, H):
     got = body.Act8WeightGrad(T, N, H, dtype=F32).run(dy.cuda(), rec).double().cpu().numpy()
     d = dy.double().numpy()
     assert (np.abs(got - d.T @ kept) <= (T * 2.0 ** -24 + 2.0 ** -22) * (np.abs(d).T @ np.abs(kept))).all()
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("T,N,H", [(40, 64, 96), (333, 136, 264), (40, 33, 65)])
+def test_the_weight_gradient_across_exponents(fmt, T, N, H):
+    """Groups from 2^-60 to 2^100 in size side by side, each group of columns of one size, so that the bound by the terms'
+    magnitudes is that group's; dY of 2^-20. (An e4m3 operand's scale is split in two factors above 2^7.)"""
+    g = torch.Generator().manual_seed(4)
+    sizes = torch.tensor([2.0 ** e for e in (-60, -3, 0, 6, 8, 9, 30, 64, 100)])
+    x = torch.randn(T, H, generator=g) * sizes[torch.arange(H) // 32 % len(sizes)]
+    rec = body.Act8Record(T, H, fmt).store(x.cuda())
+    dy = (torch.randn(T, N, generator=g) * 2.0 ** -20).to(BF16)
+    kept, d = O.record_values(x.double().numpy(), fmt), dy.double().numpy()
+    got = body.Act8WeightGrad(T, N, H, dtype=F32).run(dy.cuda(), rec).double().cpu().numpy()
+    assert (np.abs(got - d.T @ kept) <= (T * 2.0 ** -24 + 2.0 ** -22) * (np.abs(d).T @ np.abs(kept))).all()
