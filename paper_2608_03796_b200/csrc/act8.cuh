@@ -8,8 +8,9 @@
 // A group that holds an infinity or a NaN stores byte 255 and reads back as NaN in all its 32 places.
 // Why a power of two per 32 and not one fp32 factor per row or per 128: 7 or 4 significant bits times a power of two
 // are exact in bf16 (down to its last subnormal, 2^-133: e4m3 codes at e = -126 go on to 2^-135), so a record is a bf16
-// operand of the tensor cores without a second rounding, and scaling by it is exact everywhere. What the coarser factor loses (a factor of at most 2 in the int8 step) the shorter group gains
-// back: the largest of 32 normal values is about 2.1 deviations, of 128 about 2.8.
+// operand of the tensor cores without a second rounding, and scaling by it is exact everywhere. What the coarser factor
+// loses (a factor of at most 2 in the int8 step) the shorter group gains back: the largest of 32 normal values is about
+// 2.1 deviations, of 128 about 2.8.
 //
 // Layout in one buffer: codes [T, Hp] with Hp = H rounded up to 32 (padding codes are 0), then at the next multiple of
 // 256 bytes the scale bytes [T, Sp] with Sp = Hp / 32 rounded up to 16: both are tensor-map pitches.
@@ -129,6 +130,13 @@ template <> __device__ __forceinline__ Raw8<float> f32_to_raw<float>(const float
 // Loads here are coherent ones, never ld.global.nc (nor const __restrict__, which lets the compiler choose it): a kernel
 // that may start while the one before it drains (grid_dependency_wait) reads what is written during its own lifetime, and
 // the non-coherent path is defined only for memory that nobody writes in that time.
+// (Bytes by an instruction of their own: from plain C++ loads the compiler takes 5 to 13 registers more in the element-wise
+// kernels, a block less an SM. Gated backward 16384 x 7167, int8: 851 against 1380 us.)
+__device__ __forceinline__ uint32_t ld_global_u8(const uint8_t* p) {
+  uint32_t v;
+  asm volatile("ld.global.u8 %0, [%1];" : "=r"(v) : "l"(p));
+  return v;
+}
 // A thread's eight columns of a row of `width` values:
 template <typename T, bool VEC>
 __device__ __forceinline__ Raw8<T> load_raw8(const T* row, int c, int width) {
@@ -311,7 +319,7 @@ __device__ __forceinline__ void record_write8(const ActRecord& r, long long t, l
 __device__ __forceinline__ void record_fetch8(const ActRecord& r, long long t, long long cpitch, long long spitch, int c,
                                               uint2& codes, uint32_t& byte) {
   codes = *reinterpret_cast<const uint2*>(r.codes + t * cpitch + c);
-  byte = r.scales[t * spitch + (c >> 5)];
+  byte = ld_global_u8(r.scales + t * spitch + (c >> 5));
 }
 // a thread's eight values; 0 past the end
 template <int FMT, bool VEC>
@@ -326,7 +334,7 @@ __device__ __forceinline__ void record_read8(const ActRecord& r, long long t, lo
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int col = column<VEC>(c, i);
-      f[i] = col < cpitch ? act_value<FMT>(r.codes[t * cpitch + col], r.scales[t * spitch + (col >> 5)]) : 0.f;
+      f[i] = col < cpitch ? act_value<FMT>(ld_global_u8(r.codes + t * cpitch + col), ld_global_u8(r.scales + t * spitch + (col >> 5))) : 0.f;
     }
   }
 }
@@ -349,8 +357,9 @@ __device__ __forceinline__ void record_read8(int fmt, const ActRecord& r, long l
 // memory. Many short blocks keep more loads in flight than few long ones (128 or 64 an SM against 16: 5 to 10 %); two
 // rows asked for at once pay only where little is done with a row, in load.
 // 32768 x 4096 bf16, one B200: store 70 us (5.8 TB/s), load 64 us (6.4 TB/s, 0.99 of a copy).
+// Element by element at most 40 registers, for a sixth block an SM: 16384 x 4095 bf16, e4m3: 139 against 161 us.
 template <typename T, int FMT, bool VEC>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, VEC ? 0 : 6)
 act8_store_kernel(const T* x, long long ld, long long rows, int H, ActRecord rec) {
   const long long cpitch = act_codes_pitch(H), spitch = act_scale_pitch(H);
   const int c = first_column<VEC>(blockIdx.x * blockDim.x + threadIdx.x);

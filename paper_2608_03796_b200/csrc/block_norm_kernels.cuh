@@ -663,8 +663,8 @@ block_norm_backward_rows_kernel(const NormBackward p) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         if (c[i] >= H) continue;
-        byte_b[i] = p.rec_branch.scales[t * spitch + (c[i] >> 5)];
-        if (has_pre) byte_x[i] = p.rec_sum.scales[t * spitch + (c[i] >> 5)];
+        byte_b[i] = ld_global_u8(p.rec_branch.scales + t * spitch + (c[i] >> 5));
+        if (has_pre) byte_x[i] = ld_global_u8(p.rec_sum.scales + t * spitch + (c[i] >> 5));
       }
     }
   };
