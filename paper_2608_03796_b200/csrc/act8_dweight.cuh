@@ -22,8 +22,8 @@
 // contraction, so that the last wave is as short as it can be. Parts leave fp32 slabs that act8_dweight_join_kernel adds
 // in order: results are reproducible bit for bit.
 //
-// One B200, 32768 x 4096 x 4096: 775 us with int8, 810 us with e4m3 codes (1420 and 1360 TFLOP/s; a library product of bf16
-// operands 675 us); back to back, under the power cap, 930 to 960 us against 813. What the gap is: the conversion, done
+// One B200, 32768 x 4096 x 4096: 780 to 805 us with int8, 800 to 828 us with e4m3 codes (1410 and 1375 TFLOP/s at best; a
+// library product of bf16 operands 675 us); back to back, under the power cap, 955 to 985 us against 813. What the gap is: the conversion, done
 // once per 256 rows of the result, takes about 135 us of the cap's energy.
 #pragma once
 #include "act8.cuh"
@@ -43,7 +43,8 @@ __device__ __forceinline__ void clear_status(int* status) {
 }
 
 // Any alignment and width: rows of dY or of the result that tensor maps cannot describe (not 16 bytes apart).
-// 64 x 64 tiles of fp32 FMAs.
+// 64 x 64 tiles of fp32 FMAs, so 15 to 40 times the tensor-core form's time: 333 x 2817 x 2816 takes 188 us (12 aligned),
+// 4096 x 2816 x 2815 2281.
 
 template <int FMT>
 __global__ void __launch_bounds__(256)

@@ -22,10 +22,12 @@
 // (cp.async, places that only their own thread touches, so no barrier) while a row is worked on, what depends on the
 // column alone is formed once, and two values go through an instruction. The *_any kernels take everything else: odd
 // widths and addresses.
-// 32768 x 4096 bf16, one B200: forward 167 us (6.4 TB/s), leaving int8 records 240 us (5.6 TB/s); backward 286 us (5.6 TB/s),
-// from int8 records 281 us (4.8 TB/s). The backward kernel holds 128 registers a thread, so 16 warps an SM, and its
-// reduction shows: a form that took 298 us took 255 with it left out (and a wrong result). 8192 x 16384, two blocks a
-// row: forward 358, backward 402 us. 16384 x 4095 (any): forward 178, backward 556 us.
+// 32768 x 4096 bf16, one B200, in a loop over inputs beyond the L2: forward 180 us (6.0 TB/s), leaving int8 records 255 us
+// (5.3 TB/s); backward with its column sums 297 us (5.4 TB/s), from int8 records 291 us (4.6 TB/s). The backward kernel holds
+// 128 registers a thread, so 16 warps an SM, and its reduction shows: a form that took 298 us took 255 with it left out (and
+// a wrong result). 8192 x 16384, two blocks a row: forward 366, backward 402 us; with int8 records 434 and 570.
+// The any kernels: 16384 x 4095 without records forward 175, backward 556 us, with int8 records 599 and 995. Above 4096 columns
+// their arrays do not fit the 64 registers that 1024 threads have, and go to memory: 16384 x 4097 takes 6765 and 9850 us.
 #pragma once
 #include "act8.cuh"
 #include "sm100_prims.cuh"

@@ -6,8 +6,10 @@
 //
 // Element-wise, so bound by memory: forward reads 4 bytes a value and writes 2 (+ 33/32 per record), backward reads
 // 2 + 66/32 and writes 4. The records leave in the pass that computes h, from registers. 32768 x 7168 bf16, int8 records,
-// one B200: forward 316 us (6.0 TB/s), backward 285 us (6.65 TB/s); without records forward 201 us (7.0 TB/s). What the
-// records add to the forward pass is the encoding: about 70 instructions per eight values.
+// one B200, in a loop over inputs beyond the L2: forward 340 us (5.6 TB/s), backward 318 us (5.95 TB/s), a pass of both 657;
+// without records forward 207 us (6.8 TB/s: two thirds of it reads, of which a plain sum of two tensors does 7.1, a copy 6.6).
+// What the records add to the forward pass is the encoding: about 70 instructions per eight values. Element by element (odd
+// widths) 16384 x 7167 takes 1119 and 851 us.
 #pragma once
 #include "act8.cuh"
 
