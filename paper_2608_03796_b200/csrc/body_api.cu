@@ -128,7 +128,9 @@ static bool dw_mapped(const void* dy, long long ld_dy, long long T, long long N,
 }
 // Which tiles are cut, and into how many parts of the contraction: the choice with the least estimated cycles. A block
 // of 64 tokens takes a unit 600 cycles, starting a unit and draining its tile about five blocks; the slabs of cut tiles
-// one more launch, and being written and read once at about 2600 bytes a cycle.
+// one more launch, and being written and read once at about 2600 bytes a cycle. (600 is what the long loop takes; the other
+// figures and the bound of 16 parts are estimates. With one or two tiles in all, 16 parts leave most pairs idle:
+// 32768 x 256 x 256 takes 24 us, its bytes 4.)
 struct DwPlan { int whole, rest, parts; };
 static DwPlan dw_plan(long long T, long long N, long long H) {
   const long long tiles = ((N + 255) / 256) * ((H + 255) / 256), kb = (T + 63) / 64;
