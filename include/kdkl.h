@@ -480,6 +480,87 @@ size_t kdkl_block_norm_workspace_bytes(int64_t T, int64_t H);
 int kdkl_block_norm_forward(const kdkl_block_norm_args* args, void* cuda_stream);
 int kdkl_block_norm_backward(const kdkl_block_norm_args* args, void* cuda_stream);
 
+/* Layer norm per token over the H columns, with the gradients of its weight and bias:
+ *   mu = mean(x), rho = 1 / sqrt(mean((x - mu)^2) + eps), y = (x - mu) rho weight + bias
+ *   dx = rho (g - mean(g) - xh mean(g xh)), g = dy weight, xh = (x - mu) rho;  dweight = sum_t dy xh, dbias = sum_t dy
+ * weight NULL: ones; bias NULL: zeros. Everything is computed in fp32 and rounded once; the variance is taken around the
+ * mean. The sums over tokens are taken in a fixed order: bitwise reproducible. x is of x_type, y and dy of y_type
+ * (the same, or any where x is F32), dx of x_type, weight, bias and their gradients of weight_type.
+ * With a format the forward pass leaves records of x and y (each optional: y's for the weight gradient of the layer that
+ * reads y), and the backward pass reads x's record in x's place, with the forward pass's mu and rho.
+ * One struct serves both calls; a call reads the fields it needs. Outputs [T, H] are contiguous. */
+typedef struct kdkl_layer_norm_args {
+  int32_t struct_size;        /* sizeof(kdkl_layer_norm_args) */
+  int32_t x_type, y_type, weight_type;
+  int32_t format;             /* KDKL_ACT8_*; NONE: the tensor x is kept instead */
+  float eps;
+  int64_t T, H;
+  const void* x;              /* forward, and backward without records; rows ld_x apart */
+  int64_t ld_x;
+  const void* weight;         /* [H] or NULL */
+  const void* bias;           /* [H] or NULL */
+  void* y;                    /* forward out */
+  float* mean;                /* [T]; forward out (optional, both or none), backward in */
+  float* rho;                 /* [T]; the same */
+  void* x_record;             /* forward out (optional), backward in, with a format */
+  void* y_record;             /* forward out (optional), with a format */
+  size_t record_bytes;        /* size of each record: at least kdkl_act8_bytes(T, H) */
+  const void* dy;             /* backward in; rows ld_dy apart */
+  int64_t ld_dy;
+  void* dx;                   /* backward out */
+  void* dweight;              /* required with weight */
+  void* dbias;                /* required with bias */
+  void* workspace;            /* backward; 256-byte aligned, kdkl_layer_norm_workspace_bytes(T, H) */
+  size_t workspace_bytes;
+} kdkl_layer_norm_args;
+size_t kdkl_layer_norm_workspace_bytes(int64_t T, int64_t H);
+int kdkl_layer_norm_forward(const kdkl_layer_norm_args* args, void* cuda_stream);
+int kdkl_layer_norm_backward(const kdkl_layer_norm_args* args, void* cuda_stream);
+
+/* Rotary positions of queries [T, q_heads, head_dim] and keys [T, k_heads, head_dim] (either may have no heads). The first
+ * rotary_dim columns of a head are pairs - columns (i, i + rotary_dim / 2), or (2 i, 2 i + 1) INTERLEAVED - and pair i of
+ * a token at position n is turned by n turns[i] whole turns and multiplied by `magnitude`; the other columns are copied:
+ *   (a, b) -> magnitude (a cos - b sin, b cos + a sin)
+ * inverse = 1 turns the other way, which is the backward pass. The angle is formed in fp64: positions may be as far as one
+ * likes, negative ones too. A tensor's tokens and heads lie token and head strides apart (in elements), its columns are
+ * neighbours; an output's must not overlap. An output may be its own input (same strides): then it is changed in place. Otherwise
+ * outputs must not alias inputs. head_dim and rotary_dim are even; heads, tokens and halves that start on 16 or 8 bytes go by
+ * words of that size, others element by element.
+ *
+ * kdkl_rotary_table (host, no device work): turns [rotary_dim / 2] and the factor for f_i = base^(-2 i / rotary_dim) radians
+ * a position, changed for contexts longer than a model was trained on:
+ *   LINEAR  f_i / factor
+ *   NTK     base factor^(d / (d - 2)) in base's place, d = rotary_dim
+ *   YARN    k f_i + (1 - k) f_i / factor, k = clamp((original_length f_i / (2 pi) - 1) / 31, 0, 1); magnitude 0.1 ln(factor) + 1 */
+#define KDKL_ROTARY_HALF 0
+#define KDKL_ROTARY_INTERLEAVED 1
+#define KDKL_ROTARY_PLAIN 0
+#define KDKL_ROTARY_LINEAR 1
+#define KDKL_ROTARY_NTK 2
+#define KDKL_ROTARY_YARN 3
+#define KDKL_ROTARY_MAX_DIM 1024
+#define KDKL_ROTARY_MAX_HEADS 4096
+typedef struct kdkl_rotary_args {
+  int32_t struct_size;        /* sizeof(kdkl_rotary_args) */
+  int32_t type;               /* KDKL_TYPE_* of all four tensors */
+  int32_t layout;             /* KDKL_ROTARY_HALF or _INTERLEAVED */
+  int32_t head_dim, rotary_dim;
+  int32_t q_heads, k_heads;
+  int32_t wide_positions;     /* 0: int32, 1: int64 */
+  int32_t inverse;
+  float magnitude;
+  int64_t T;
+  const void* positions;      /* [T], device */
+  const double* turns;        /* [rotary_dim / 2], device */
+  const void* q; int64_t q_token, q_head;
+  void* q_out; int64_t q_out_token, q_out_head;
+  const void* k; int64_t k_token, k_head;
+  void* k_out; int64_t k_out_token, k_out_head;
+} kdkl_rotary_args;
+int kdkl_rotary_table(int32_t rotary_dim, double base, int32_t scaling, double factor, double original_length,
+                      double* turns_host, float* magnitude_host);
+int kdkl_rotary(const kdkl_rotary_args* args, void* cuda_stream);
+
 /* Exercises the bounded wait every kernel of this library uses on its mbarriers: one thread waits on
  * a barrier that nothing completes, gives up after limit_ns (1 .. 1e9) and the kernel returns normally.
  * status: device int32[2], zeroed by the caller; afterwards {KDKL_ERR_TIMEOUT, 99}. The context stays

@@ -25,6 +25,8 @@ The layers of a student's body whose backward pass reads activations kept in 8 b
     z = act8_linear(y, W_gate_up, record=kept)               # keeps nothing of its own
     h, kept = gated_act(z, act="silu", act8="int8", keep_h=True)
     branch = act8_linear(h, W_down, record=kept)
+    y, kept = layer_norm(x, weight, bias, act8="int8", keep_y=True)
+    q, k = rotary(q, k, positions, body.Rotary(D))
 
 Their outputs, records and gradients are allocated per call, as a graph needs them.
 """
@@ -447,3 +449,81 @@ def block_norm(residual, branch, post_weight=None, pre_weight=None, gate=None, *
     y, x, record = _BlockNorm.apply(residual, branch, post_weight, pre_weight, gate, gate_kind, act8, keep_y, args,
                                     _recorded(residual, branch, post_weight, pre_weight, gate))
     return (y, x, record) if keep_y else (y, x)
+
+
+class _LayerNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, out_dtype, act8, keep_y, eps, train):
+        H = x.shape[-1]
+        rows = _flat(x, H)
+        op = body.LayerNorm(rows.shape[0], H, dtype=out_dtype, x_dtype=x.dtype, act8=act8, eps=eps, train=train,
+                            keep_y=keep_y and train, device=x.device)
+        y = _shaped(op.forward(rows, weight, bias), x.shape)
+        if train:
+            ctx.save_for_backward(weight, bias, rows if act8 is None else op.x_record.buffer)
+        record = op.y_record
+        op.kept = op.y = op.y_record = op.x_record = None
+        ctx.op, ctx.format, ctx.shape = op, act8, x.shape
+        return y, record
+
+    @staticmethod
+    @_first_derivative_only("layer_norm")
+    def backward(ctx, dy, _):
+        op, (weight, bias, x) = ctx.op, ctx.saved_tensors
+        if ctx.format is not None:
+            op.x_record, x = body.Act8Record(op.T, op.H, ctx.format, buffer=x), None
+        op.kept = (x, weight, bias)
+        op.workspace, op.dx, op.grads = None, None, {}                          # buffers of its own for every backward
+        d = op.backward(_flat(dy, op.H))
+        op.kept = op.workspace = op.dx = op.x_record = None
+        return d.x.reshape(ctx.shape), d.weight, d.bias, None, None, None, None, None
+
+
+def layer_norm(x, weight=None, bias=None, *, eps: float = 1e-5, out_dtype=None, act8: Optional[str] = None,
+               keep_y: bool = False):
+    """Layer norm over the last dimension (see body.LayerNorm); x may be fp32 with an out_dtype of its own. With act8 the
+    backward pass reads an 8-bit record of x instead of x; with keep_y: (y, record of y), for the act8_linear that reads y."""
+    if keep_y and act8 is None:
+        raise ValueError("layer_norm: keep_y needs act8")
+    y, record = _LayerNorm.apply(x, weight, bias, out_dtype or x.dtype, act8, keep_y, eps, _recorded(x, weight, bias))
+    return (y, record) if keep_y else y
+
+
+class _Rotary(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, positions, rope):
+        ctx.save_for_backward(positions)
+        ctx.rope = rope
+        ctx.set_materialize_grads(False)
+        out = _rotate(rope.forward, q, k, positions)
+        return out if k is not None else out[0]
+
+    @staticmethod
+    @_first_derivative_only("rotary")
+    def backward(ctx, dq, dk=None):
+        positions, = ctx.saved_tensors
+        if dq is None:                                                          # one of the two may have no gradient
+            return (None, None if dk is None else _rotate(ctx.rope.backward, dk, None, positions)[0], None, None)
+        return (*_rotate(ctx.rope.backward, dq, dk, positions), None, None)
+
+
+def _rotate(turn, q, k, positions):
+    """One call on [..., heads, D] tensors, into outputs of its own."""
+    places = positions.reshape(-1).contiguous()
+
+    def rows(t):
+        t = t.reshape(-1, *t.shape[-2:])
+        return t if t.stride(-1) == 1 else t.contiguous()
+    flat = [None if t is None else rows(t) for t in (q, k)]
+    out = [None if t is None else torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k)]
+    turn(*flat, places, out=[None if t is None else t.view(f.shape) for t, f in zip(out, flat)])
+    return tuple(out)
+
+
+def rotary(q, k, positions, rope: body.Rotary):
+    """(q, k) turned by their tokens' positions: q [..., heads, D], k [..., kv heads, D] or None (then q alone is returned),
+    positions [...] of int32 or int64."""
+    for t in (q, k):
+        if t is not None and t.shape[:-2] != positions.shape:
+            raise TypeError(f"rotary: positions {tuple(positions.shape)} beside heads of {tuple(t.shape)}")
+    return _Rotary.apply(q, k, positions, rope)

@@ -34,6 +34,8 @@ EXPORTS = [
     "kdkl_debug_guard_bytes", "kdkl_act8_bytes", "kdkl_act8_store", "kdkl_act8_load", "kdkl_gated_act_forward",
     "kdkl_gated_act_backward", "kdkl_act8_dweight_workspace_bytes", "kdkl_act8_dweight",
     "kdkl_block_norm_workspace_bytes", "kdkl_block_norm_forward", "kdkl_block_norm_backward",
+    "kdkl_layer_norm_workspace_bytes", "kdkl_layer_norm_forward", "kdkl_layer_norm_backward",
+    "kdkl_rotary_table", "kdkl_rotary",
 ]
 
 FEATURE_MSE, FEATURE_COSINE = 0, 1
@@ -145,6 +147,17 @@ def lib() -> ctypes.CDLL:
     L.kdkl_block_norm_forward.argtypes = [vp, vp]
     L.kdkl_block_norm_backward.restype = ctypes.c_int
     L.kdkl_block_norm_backward.argtypes = [vp, vp]
+    L.kdkl_layer_norm_workspace_bytes.restype = sz
+    L.kdkl_layer_norm_workspace_bytes.argtypes = [i64, i64]
+    L.kdkl_layer_norm_forward.restype = ctypes.c_int
+    L.kdkl_layer_norm_forward.argtypes = [vp, vp]
+    L.kdkl_layer_norm_backward.restype = ctypes.c_int
+    L.kdkl_layer_norm_backward.argtypes = [vp, vp]
+    L.kdkl_rotary_table.restype = ctypes.c_int
+    L.kdkl_rotary_table.argtypes = [i32, ctypes.c_double, i32, ctypes.c_double, ctypes.c_double,
+                                    ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_float)]
+    L.kdkl_rotary.restype = ctypes.c_int
+    L.kdkl_rotary.argtypes = [vp, vp]
     L.kdkl_wait_selftest.restype = ctypes.c_int
     L.kdkl_wait_selftest.argtypes = [vp, i64, vp]
     L.kdkl_last_error.restype = ctypes.c_char_p

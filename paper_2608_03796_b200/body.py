@@ -7,6 +7,8 @@ read them in the backward pass.
     ffn = GatedAct(T, F); h = ffn.forward(gate, up); dgate, dup = ffn.backward(dh)
     join = BlockNorm(T, H); y, x = join.forward(residual, branch, post_weight=w1, pre_weight=w2)
     d = join.backward(dy, dx)                           # d.residual, d.branch, d.post_weight, d.pre_weight, d.gate
+    norm = LayerNorm(T, H); y = norm.forward(x, w, b); d = norm.backward(dy)          # d.x, d.weight, d.bias
+    rope = Rotary(D); q_, k_ = rope.forward(q, k, positions); dq, dk = rope.backward(dq_, dk_, positions)
 
 The classes hold outputs, records and workspaces of one shape: calls allocate nothing, only enqueue on the current
 stream, and return the holder's own buffers, which the next call overwrites (a graph of autograd's that has saved one of
@@ -362,3 +364,205 @@ class BlockNorm:
         B._check(self._backward(self._ref, _stream(self.at, "block norm")))
         _written([t for t in d if t is not None])
         return d
+
+
+class kdkl_layer_norm_args(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("struct_size", "x_type", "y_type", "weight_type", "format")]
+                + [("eps", ctypes.c_float), ("T", ctypes.c_int64), ("H", ctypes.c_int64), ("x", ctypes.c_void_p), ("ld_x", ctypes.c_int64)]
+                + [(n, ctypes.c_void_p) for n in ("weight", "bias", "y", "mean", "rho", "x_record", "y_record")]
+                + [("record_bytes", ctypes.c_size_t), ("dy", ctypes.c_void_p), ("ld_dy", ctypes.c_int64)]
+                + [(n, ctypes.c_void_p) for n in ("dx", "dweight", "dbias", "workspace")] + [("workspace_bytes", ctypes.c_size_t)])
+
+
+class LayerNormGrads(NamedTuple):
+    x: torch.Tensor
+    weight: Optional[torch.Tensor]
+    bias: Optional[torch.Tensor]
+
+
+class LayerNorm:
+    """y = (x - mean(x)) * rsqrt(var(x) + eps) * weight + bias per row of x [T, H] (kdkl_layer_norm_forward / _backward);
+    weight None: ones, bias None: zeros. `dtype` is that of y and dy, `x_dtype` of x and dx (dtype's own, or fp32). With
+    act8 given, forward leaves a record of x, which backward reads; otherwise backward reads the tensor, which the caller
+    leaves in place. keep_y: a record of y too (``y_record``, for the layer that reads y). train=False keeps nothing."""
+
+    def __init__(self, T: int, H: int, *, dtype=torch.bfloat16, x_dtype=None, act8: Optional[str] = None, eps: float = 1e-5,
+                 train: bool = True, keep_y: bool = False, device="cuda"):
+        x_dtype = x_dtype or dtype
+        if dtype not in TYPES or x_dtype not in (dtype, torch.float32):
+            raise ValueError(f"kdkl: a layer norm is bf16, fp16 or fp32, its input the same or fp32, not {dtype}, {x_dtype}")
+        if keep_y and not (train and act8 is not None):
+            raise ValueError("kdkl: keep_y needs act8, in training")
+        self.T, self.H, self.dtype, self.x_dtype, self.train = T, H, dtype, x_dtype, train
+        a = self.args = kdkl_layer_norm_args()
+        a.struct_size = ctypes.sizeof(a)
+        a.x_type, a.y_type, a.weight_type = TYPES[x_dtype], TYPES[dtype], 0
+        a.format = _lookup(FORMATS, act8, "act8") if train else -1
+        a.eps, a.T, a.H = eps, T, H
+        self.y = torch.empty(T, H, dtype=dtype, device=device)
+        a.y, self.at = self.y.data_ptr(), self.y.get_device()
+        self.x_record = self.y_record = self.workspace = self.dx = self.kept = None
+        if train:
+            self.workspace_bytes = B.lib().kdkl_layer_norm_workspace_bytes(T, H)
+            if self.workspace_bytes == 0:
+                raise ValueError(f"kdkl: no layer norm of shape {(T, H)}")
+            self.stats = torch.empty(2, T, dtype=torch.float32, device=device)
+            a.mean, a.rho = self.stats[0].data_ptr(), self.stats[1].data_ptr()
+            if act8 is not None:
+                self.x_record = Act8Record(T, H, act8, device)
+                self.y_record = Act8Record(T, H, act8, device) if keep_y else None
+        self.grads = {}
+        self._ref = ctypes.byref(a)
+        self._forward, self._backward = B.lib().kdkl_layer_norm_forward, B.lib().kdkl_layer_norm_backward
+
+    def forward(self, x, weight=None, bias=None) -> torch.Tensor:
+        a = self.args
+        a.x, a.ld_x = _rows(x, self.T, self.H, self.x_dtype, "x")
+        self._affine(weight, bias)
+        written = self._records()
+        B._check(self._forward(self._ref, _stream(self.at, "layer norm")))
+        _written([self.y, *written])
+        if self.train:                                                      # what the backward call reads
+            self.kept = (x if a.format < 0 else None, weight, bias)
+        return self.y
+
+    def _affine(self, weight, bias):
+        a, given = self.args, weight if weight is not None else bias
+        if given is None:
+            a.weight = a.bias = None
+            return
+        a.weight_type = _lookup(TYPES, given.dtype, "weight")
+        a.weight, a.bias = _vector(weight, self.H, given.dtype, "weight"), _vector(bias, self.H, given.dtype, "bias")
+
+    def _records(self):
+        a, kept = self.args, [r for r in (self.x_record, self.y_record) if r is not None]
+        for r in kept:
+            if r.at != self.at:                                             # (autograd's hooks may have moved it)
+                _stream(r.at, "record")
+            a.record_bytes = r.nbytes
+        a.x_record = None if self.x_record is None else self.x_record.ptr
+        a.y_record = None if self.y_record is None else self.y_record.ptr
+        return [r.buffer for r in kept]
+
+    def _grad(self, name, like):
+        if like is None:
+            return None
+        t = self.grads.get(name)
+        if t is None or t.dtype != like.dtype:
+            t = self.grads[name] = torch.empty_like(like)
+        return t
+
+    def backward(self, dy) -> LayerNormGrads:
+        """Gradients of the last forward call's inputs."""
+        if not self.train:
+            raise RuntimeError("kdkl: this layer norm keeps nothing for a backward pass (train=False)")
+        if self.kept is None:
+            raise RuntimeError("kdkl: this layer norm's backward call comes before any forward call")
+        a = self.args
+        if self.workspace is None:
+            self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=self.stats.device)
+            a.workspace, a.workspace_bytes = self.workspace.data_ptr(), self.workspace_bytes
+        if self.dx is None:
+            self.dx = torch.empty(self.T, self.H, dtype=self.x_dtype, device=self.stats.device)
+            a.dx = self.dx.data_ptr()
+        x, weight, bias = self.kept
+        self._affine(weight, bias)
+        self._records()
+        if a.format < 0:
+            a.x, a.ld_x = _rows(x, self.T, self.H, self.x_dtype, "x")
+        a.dy, a.ld_dy = _rows(dy, self.T, self.H, self.dtype, "dy")
+        d = LayerNormGrads(self.dx, self._grad("weight", weight), self._grad("bias", bias))
+        a.dweight = None if d.weight is None else d.weight.data_ptr()
+        a.dbias = None if d.bias is None else d.bias.data_ptr()
+        B._check(self._backward(self._ref, _stream(self.at, "layer norm")))
+        _written([t for t in d if t is not None])
+        return d
+
+
+LAYOUTS = {"half": 0, "interleaved": 1}
+SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
+_POSITIONS = {torch.int32: 0, torch.int64: 1}
+
+
+class kdkl_rotary_args(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("struct_size", "type", "layout", "head_dim", "rotary_dim", "q_heads", "k_heads",
+                                               "wide_positions", "inverse")]
+                + [("magnitude", ctypes.c_float), ("T", ctypes.c_int64), ("positions", ctypes.c_void_p), ("turns", ctypes.c_void_p)]
+                + [f for n in ("q", "q_out", "k", "k_out")
+                   for f in ((n, ctypes.c_void_p), (n + "_token", ctypes.c_int64), (n + "_head", ctypes.c_int64))])
+
+
+class Rotary:
+    """Rotary positions of queries [T, heads, D] and keys [T, kv heads, D] (kdkl_rotary). The first `rotary_dim` columns of a
+    head (all by default) are pairs - "half": (i, i + rotary_dim / 2), "interleaved": (2 i, 2 i + 1) - turned by
+    position * base ** (-2 i / rotary_dim) radians. `scaling` ("linear", "ntk", "yarn", by `factor`) is for contexts longer
+    than `original_length`, the one that was trained on; see kdkl_rotary_table for the formulas.
+
+    Tokens and heads may lie any distance apart (the halves of one projection, or x.transpose(0, 1) of heads before
+    tokens); columns are neighbours. Outputs are the holder's own buffers, made for each new shape, or those given as `out`
+    (which may be the inputs themselves: then they are changed in place)."""
+
+    def __init__(self, D: int, rotary_dim: Optional[int] = None, *, base: float = 10000.0, layout: str = "half",
+                 scaling: str = "none", factor: float = 1.0, original_length: int = 0, device="cuda"):
+        R = D if rotary_dim is None else rotary_dim
+        if D % 2 or R % 2 or not 2 <= R <= D <= 1024:
+            raise ValueError(f"kdkl: heads of {D} columns, {R} of them turned: both are even, and at most 1024")
+        a = self.args = kdkl_rotary_args()
+        turns, magnitude = (ctypes.c_double * (R // 2))(), ctypes.c_float()
+        kind = _lookup(SCALINGS, scaling, "scaling")
+        if B.lib().kdkl_rotary_table(R, base, kind, factor, original_length, turns, ctypes.byref(magnitude)) != 0:
+            raise ValueError(f"kdkl: no rotary positions with base {base}, scaling {scaling!r} by {factor} of {original_length}")
+        self.D, self.R = D, R
+        a.struct_size = ctypes.sizeof(a)
+        a.layout, a.head_dim, a.rotary_dim, a.magnitude = _lookup(LAYOUTS, layout, "layout"), D, R, magnitude.value
+        self.turns = torch.tensor(list(turns), dtype=torch.float64).to(device)
+        a.turns, self.at = self.turns.data_ptr(), self.turns.get_device()
+        self._call, self._own = B.lib().kdkl_rotary, {}
+
+    def forward(self, q, k, positions, out=None):
+        """(q, k) turned; k may be None."""
+        return self._run(q, k, positions, out, 0)
+
+    def backward(self, dq, dk, positions, out=None):
+        """Gradients of q and k from those of their turned forms."""
+        return self._run(dq, dk, positions, out, 1)
+
+    def _run(self, q, k, positions, out, inverse):
+        a = kdkl_rotary_args.from_buffer_copy(self.args)     # a call's own: several threads may share a table
+        T = positions.shape[0] if positions.dim() == 1 else -1
+        now = _device()
+        if positions.get_device() != now or positions.dtype not in _POSITIONS or T < 0 or (T > 1 and positions.stride(0) != 1):
+            raise TypeError(f"kdkl: positions: expected contiguous int32 or int64 [T] on the current CUDA device, got "
+                            f"{positions.dtype} {tuple(positions.shape)} on {positions.device}")
+        outs = out if out is not None else (self._buffer(inverse, 0, q), self._buffer(inverse, 1, k))
+        a.T, a.positions, a.wide_positions, a.inverse = T, positions.data_ptr(), _POSITIONS[positions.dtype], inverse
+        a.type = _lookup(TYPES, q.dtype, "q")
+        a.q_heads, a.q, a.q_token, a.q_head = self._heads(q, T, q.dtype, "q", now)
+        n, a.q_out, a.q_out_token, a.q_out_head = self._heads(outs[0], T, q.dtype, "q's output", now)
+        same = n == a.q_heads
+        if k is not None:
+            a.k_heads, a.k, a.k_token, a.k_head = self._heads(k, T, q.dtype, "k", now)
+            n, a.k_out, a.k_out_token, a.k_out_head = self._heads(outs[1], T, q.dtype, "k's output", now)
+            same = same and n == a.k_heads
+        else:
+            a.k_heads, outs = 0, (outs[0], None)
+        if not same:
+            raise TypeError("kdkl: an output has another number of heads than its input")
+        B._check(self._call(ctypes.byref(a), _stream(self.at, "rotary table")))
+        _written(outs[0] if k is None else list(outs))
+        return outs
+
+    def _heads(self, t, T, dtype, name, now):
+        """(heads, address, distance of tokens, distance of heads)"""
+        if t.get_device() != now or t.dtype is not dtype or t.dim() != 3 or t.shape[0] != T or t.shape[2] != self.D or t.stride(2) != 1:
+            raise TypeError(f"kdkl: {name}: expected {dtype} [{T}, heads, {self.D}] on the current CUDA device, columns contiguous, "
+                            f"got {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}")
+        return t.shape[1], t.data_ptr(), t.stride(0), t.stride(1)
+
+    def _buffer(self, inverse, which, like):
+        if like is None:
+            return None
+        t = self._own.get((inverse, which))
+        if t is None or t.shape != like.shape or t.dtype is not like.dtype or t.device != like.device:
+            t = self._own[inverse, which] = torch.empty(like.shape, dtype=like.dtype, device=like.device)
+        return t

@@ -1,0 +1,382 @@
+// Layer norm, forward and backward, with the gradients of its weight and bias.
+//
+//   mu = mean(x), rho = 1 / sqrt(mean((x - mu)^2) + eps), xh = (x - mu) rho, y = xh w + b
+//   dx = rho (dy w - mean(dy w) - xh mean(dy w xh)),  dw = sum_t dy xh,  db = sum_t dy
+//
+// The variance is taken around the mean of the values in registers, never as a difference of two sums: a warp takes the
+// mean of its own columns and the squares around it, and the warps' (sum, squares) pairs are joined exactly,
+//   sum (x - mu)^2 = sum_i [ q_i + n_i (mu_i - mu)^2 ],
+// so that a row costs one barrier. Everything is computed in fp32 and rounded once.
+//
+// Three shapes, by width: rows of at most 512 columns belong to a warp (no barrier); up to 8192 columns a block has the
+// row in registers, eight columns a thread; wider rows are read again from the caches for the second look at them.
+// In the first two the backward pass keeps the columns' sums of dw and db in registers over all rows of a warp or block
+// and leaves one partial row each, which a second kernel adds in a fixed order; of wider rows they are taken by a kernel
+// of their own that goes down the columns.
+#pragma once
+#include "act8.cuh"
+
+namespace kdkl {
+
+constexpr int kLnWarpCols = 512, kLnBlockCols = 8192;
+constexpr int kLnWarpThreads = 256, kLnWideThreads = 1024;
+
+struct LnParams {
+  const void* x;  long long ld_x;
+  const void* weight; const void* bias; int weight_type;
+  void* y;                       // contiguous
+  float* mean; float* rho;       // [T]; forward: out or null
+  ActRecord x_record, y_record;  // codes null: none
+  int format;
+  const void* dy; long long ld_dy;
+  void* dx;
+  float* part;                   // [parts][2][H]
+  long long T; int H;
+  float eps;
+};
+
+__device__ __forceinline__ float ln_warp_sum(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+
+// eight values of the weight or bias, of a type known at run time (uniform)
+template <bool VEC>
+__device__ __forceinline__ void load8_typed(const void* p, int type, int c, int H, float (&f)[8]) {
+  if (type == 0) load8<__nv_bfloat16, VEC>(reinterpret_cast<const __nv_bfloat16*>(p), c, H, f);
+  else if (type == 1) load8<float, VEC>(reinterpret_cast<const float*>(p), c, H, f);
+  else load8<__half, VEC>(reinterpret_cast<const __half*>(p), c, H, f);
+}
+template <bool VEC>
+__device__ __forceinline__ void load_affine(const LnParams& p, int c, float (&w)[8], float (&b)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) { w[i] = 1.f; b[i] = 0.f; }
+  if (p.weight != nullptr) load8_typed<VEC>(p.weight, p.weight_type, c, p.H, w);
+  if (p.bias != nullptr) load8_typed<VEC>(p.bias, p.weight_type, c, p.H, b);
+}
+template <bool VEC> __device__ __forceinline__ int columns_of(int c, int H) {      // how many of a thread's eight exist
+  int n = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) n += column<VEC>(c, i) < H ? 1 : 0;
+  return n;
+}
+
+// (sum, squares around its own mean) of the warps of a block -> mean and squares of the row, known to every thread.
+// slots: [2][32] pairs and [32] counts in shared memory; `par` alternates from row to row, which spares a second barrier.
+struct LnJoin { float mean, squares; };
+__device__ __forceinline__ LnJoin ln_join(float2 (*slots)[32], const float* counts, int par, int warps, float s, float q, float H) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (lane == 0) slots[par][warp] = make_float2(s, q);
+  __syncthreads();
+  const bool has = lane < warps;
+  const float2 v = has ? slots[par][lane] : make_float2(0.f, 0.f);
+  const float n = has ? counts[lane] : 0.f;
+  LnJoin r;
+  r.mean = ln_warp_sum(v.x) / H;         // a division: equal values have themselves for their mean
+  const float off = n > 0.f ? v.x / n - r.mean : 0.f;
+  r.squares = ln_warp_sum(fmaf(n * off, off, v.y));
+  return r;
+}
+__device__ __forceinline__ float2 ln_join2(float2 (*slots)[32], int par, int warps, float a, float b) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (lane == 0) slots[par][warp] = make_float2(a, b);
+  __syncthreads();
+  const float2 v = lane < warps ? slots[par][lane] : make_float2(0.f, 0.f);
+  return make_float2(ln_warp_sum(v.x), ln_warp_sum(v.y));
+}
+
+// WARP: G groups of eight columns a lane, a row a warp; otherwise one group a thread, a row a block.
+template <typename X, typename Y, int G, bool WARP, bool VEC>
+__global__ void __launch_bounds__(WARP ? kLnWarpThreads : 1024)
+layer_norm_forward_kernel(const LnParams p) {
+  __shared__ float2 slots[2][32];
+  __shared__ float counts[32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int tpr = WARP ? 32 : blockDim.x, me = WARP ? lane : threadIdx.x, warps = blockDim.x >> 5;
+  const long long first = WARP ? (long long)blockIdx.x * warps + warp : blockIdx.x;
+  const long long step = WARP ? (long long)gridDim.x * warps : gridDim.x;
+  const long long cpitch = act_codes_pitch(p.H), spitch = act_scale_pitch(p.H);
+  const float inv_H = 1.f / (float)p.H;
+  int c[G], have = 0;
+#pragma unroll
+  for (int g = 0; g < G; ++g) { c[g] = first_column<VEC>(me + g * tpr); have += columns_of<VEC>(c[g], p.H); }
+  const float n_warp = ln_warp_sum((float)have);
+  if (!WARP && lane == 0) counts[warp] = n_warp;
+  grid_dependents_launch();
+  grid_dependency_wait();
+  float w[G][8], b[G][8];
+#pragma unroll
+  for (int g = 0; g < G; ++g) load_affine<VEC>(p, c[g], w[g], b[g]);
+  int par = 0;
+  Raw8<X> raw[G];
+  const X* x = reinterpret_cast<const X*>(p.x);
+#pragma unroll
+  for (int g = 0; g < G; ++g)
+    if (first < p.T) raw[g] = load_raw8<X, VEC>(x + first * p.ld_x, c[g], p.H);
+  for (long long t = first; t < p.T; t += step, par ^= 1) {
+    float f[G][8], s = 0.f;
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      raw_to_f32(raw[g], f[g]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s += f[g][i];
+    }
+    if (t + step < p.T) {                                  // the next row is on its way while this one is worked on
+#pragma unroll
+      for (int g = 0; g < G; ++g) raw[g] = load_raw8<X, VEC>(x + (t + step) * p.ld_x, c[g], p.H);
+    }
+    s = ln_warp_sum(s);
+    const float mine = n_warp > 0.f ? s / n_warp : 0.f;
+    float q = 0.f;
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float d = (VEC ? c[g] : column<VEC>(c[g], i)) < p.H ? f[g][i] - mine : 0.f;
+        q = fmaf(d, d, q);
+      }
+    q = ln_warp_sum(q);
+    float mean = mine, squares = q;
+    if (!WARP) {
+      const LnJoin j = ln_join(slots, counts, par, warps, s, q, (float)p.H);
+      mean = j.mean; squares = j.squares;
+    }
+    const float rho = 1.f / sqrtf(fmaf(squares, inv_H, p.eps));
+    if (me == 0 && p.mean != nullptr) { p.mean[t] = mean; p.rho[t] = rho; }
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      float y[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i] = fmaf((f[g][i] - mean) * rho, w[g][i], b[g][i]);
+      const Raw8<Y> out = f32_to_raw<Y>(y);
+      store_raw8<Y, VEC>(reinterpret_cast<Y*>(p.y) + t * p.H, c[g], p.H, out);
+      if (p.x_record.codes != nullptr) record_write8<VEC>(p.format, p.x_record, t, cpitch, spitch, c[g], f[g]);
+      if (p.y_record.codes != nullptr) {                   // of y as it is returned
+        raw_to_f32(out, y);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (column<VEC>(c[g], i) >= p.H) y[i] = 0.f;     // padding codes are zeros
+        record_write8<VEC>(p.format, p.y_record, t, cpitch, spitch, c[g], y);
+      }
+    }
+  }
+}
+
+// Rows wider than a block's registers: three looks at the row, the second and third from the caches.
+template <typename X, typename Y, bool VEC>
+__global__ void __launch_bounds__(kLnWideThreads)
+layer_norm_forward_wide_kernel(const LnParams p) {
+  __shared__ float2 slots[2][32];
+  const int warps = blockDim.x >> 5, cols = blockDim.x * 8;
+  const long long cpitch = act_codes_pitch(p.H), spitch = act_scale_pitch(p.H);
+  const float inv_H = 1.f / (float)p.H;
+  const int c0 = first_column<VEC>(threadIdx.x);
+  grid_dependents_launch();
+  grid_dependency_wait();
+  for (long long t = blockIdx.x; t < p.T; t += gridDim.x) {
+    const X* row = reinterpret_cast<const X*>(p.x) + t * p.ld_x;
+    float f[8], s = 0.f, q = 0.f;
+    for (int base = 0; base < p.H; base += cols) {
+      load8<X, VEC>(row, base + c0, p.H, f);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s += f[i];
+    }
+    const float mean = ln_join2(slots, 0, warps, ln_warp_sum(s), 0.f).x / (float)p.H;
+    for (int base = 0; base < p.H; base += cols) {
+      load8<X, VEC>(row, base + c0, p.H, f);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float d = column<VEC>(base + c0, i) < p.H ? f[i] - mean : 0.f;
+        q = fmaf(d, d, q);
+      }
+    }
+    const float rho = 1.f / sqrtf(fmaf(ln_join2(slots, 1, warps, ln_warp_sum(q), 0.f).x, inv_H, p.eps));
+    if (threadIdx.x == 0 && p.mean != nullptr) { p.mean[t] = mean; p.rho[t] = rho; }
+    for (int base = 0; base < p.H; base += cols) {         // the same trips for every thread: records are a warp's work
+      const int c = base + c0;
+      float w[8], b[8], y[8];
+      load8<X, VEC>(row, c, p.H, f);
+      load_affine<VEC>(p, c, w, b);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i] = fmaf((f[i] - mean) * rho, w[i], b[i]);
+      const Raw8<Y> out = f32_to_raw<Y>(y);
+      store_raw8<Y, VEC>(reinterpret_cast<Y*>(p.y) + t * p.H, c, p.H, out);
+      if (p.x_record.codes != nullptr) record_write8<VEC>(p.format, p.x_record, t, cpitch, spitch, c, f);
+      if (p.y_record.codes != nullptr) {
+        raw_to_f32(out, y);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (column<VEC>(c, i) >= p.H) y[i] = 0.f;
+        record_write8<VEC>(p.format, p.y_record, t, cpitch, spitch, c, y);
+      }
+    }
+  }
+}
+
+// x of the backward pass: the tensor, or what its record stands for
+template <typename X, bool REC, bool VEC>
+__device__ __forceinline__ void ln_x8(const LnParams& p, long long t, long long cpitch, long long spitch, int c, float (&f)[8]) {
+  if (REC) record_read8<VEC>(p.format, p.x_record, t, cpitch, spitch, c, f);
+  else load8<X, VEC>(reinterpret_cast<const X*>(p.x) + t * p.ld_x, c, p.H, f);
+}
+
+template <typename X, typename Y, int G, bool WARP, bool REC, bool VEC>
+__global__ void __launch_bounds__(WARP ? kLnWarpThreads : 1024)
+layer_norm_backward_kernel(const LnParams p) {
+  __shared__ float2 slots[2][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int tpr = WARP ? 32 : blockDim.x, me = WARP ? lane : threadIdx.x, warps = blockDim.x >> 5;
+  const long long first = WARP ? (long long)blockIdx.x * warps + warp : blockIdx.x;
+  const long long step = WARP ? (long long)gridDim.x * warps : gridDim.x;
+  const long long cpitch = act_codes_pitch(p.H), spitch = act_scale_pitch(p.H);
+  const float inv_H = 1.f / (float)p.H;
+  int c[G];
+#pragma unroll
+  for (int g = 0; g < G; ++g) c[g] = first_column<VEC>(me + g * tpr);
+  grid_dependents_launch();
+  grid_dependency_wait();
+  float w[G][8], aw[G][8], ab[G][8];
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { w[g][i] = 1.f; aw[g][i] = 0.f; ab[g][i] = 0.f; }
+    if (p.weight != nullptr) load8_typed<VEC>(p.weight, p.weight_type, c[g], p.H, w[g]);
+  }
+  int par = 0;
+  for (long long t = first; t < p.T; t += step, par ^= 1) {
+    const float mean = p.mean[t], rho = p.rho[t];
+    float xh[G][8], d[G][8], s1 = 0.f, s2 = 0.f;
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      ln_x8<X, REC, VEC>(p, t, cpitch, spitch, c[g], xh[g]);
+      load8<Y, VEC>(reinterpret_cast<const Y*>(p.dy) + t * p.ld_dy, c[g], p.H, d[g]);   // 0 past the row's end
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        xh[g][i] = (xh[g][i] - mean) * rho;
+        aw[g][i] = fmaf(d[g][i], xh[g][i], aw[g][i]);
+        ab[g][i] += d[g][i];
+        d[g][i] *= w[g][i];
+        s1 += d[g][i];
+        s2 = fmaf(d[g][i], xh[g][i], s2);
+      }
+    }
+    s1 = ln_warp_sum(s1); s2 = ln_warp_sum(s2);
+    if (!WARP) { const float2 s = ln_join2(slots, par, warps, s1, s2); s1 = s.x; s2 = s.y; }
+    s1 *= inv_H; s2 *= inv_H;
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      float o[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) o[i] = rho * (d[g][i] - fmaf(xh[g][i], s2, s1));
+      store_raw8<X, VEC>(reinterpret_cast<X*>(p.dx) + t * p.H, c[g], p.H, f32_to_raw<X>(o));
+    }
+  }
+  if (p.part != nullptr) {
+    const long long slot = WARP ? (long long)blockIdx.x * warps + warp : blockIdx.x;
+    float* part = p.part + slot * 2 * p.H;
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int col = column<VEC>(c[g], i);
+        if (col < p.H) { part[col] = aw[g][i]; part[p.H + col] = ab[g][i]; }
+      }
+  }
+}
+
+template <typename X, typename Y, bool REC, bool VEC>
+__global__ void __launch_bounds__(kLnWideThreads)
+layer_norm_backward_wide_kernel(const LnParams p) {
+  __shared__ float2 slots[2][32];
+  const int warps = blockDim.x >> 5, cols = blockDim.x * 8;
+  const long long cpitch = act_codes_pitch(p.H), spitch = act_scale_pitch(p.H);
+  const float inv_H = 1.f / (float)p.H;
+  const int c0 = first_column<VEC>(threadIdx.x);
+  grid_dependents_launch();
+  grid_dependency_wait();
+  int par = 0;
+  for (long long t = blockIdx.x; t < p.T; t += gridDim.x, par ^= 1) {
+    const float mean = p.mean[t], rho = p.rho[t];
+    const Y* dy = reinterpret_cast<const Y*>(p.dy) + t * p.ld_dy;
+    float x[8], d[8], w[8], s1 = 0.f, s2 = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = 1.f;
+    for (int base = 0; base < p.H; base += cols) {
+      const int c = base + c0;
+      ln_x8<X, REC, VEC>(p, t, cpitch, spitch, c, x);
+      load8<Y, VEC>(dy, c, p.H, d);
+      if (p.weight != nullptr) load8_typed<VEC>(p.weight, p.weight_type, c, p.H, w);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float e = d[i] * w[i];
+        s1 += e;
+        s2 = fmaf(e, (x[i] - mean) * rho, s2);
+      }
+    }
+    const float2 s = ln_join2(slots, par, warps, ln_warp_sum(s1), ln_warp_sum(s2));
+    s1 = s.x * inv_H; s2 = s.y * inv_H;
+    for (int base = 0; base < p.H; base += cols) {
+      const int c = base + c0;
+      ln_x8<X, REC, VEC>(p, t, cpitch, spitch, c, x);
+      load8<Y, VEC>(dy, c, p.H, d);
+      if (p.weight != nullptr) load8_typed<VEC>(p.weight, p.weight_type, c, p.H, w);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) d[i] = rho * (d[i] * w[i] - fmaf((x[i] - mean) * rho, s2, s1));
+      store_raw8<X, VEC>(reinterpret_cast<X*>(p.dx) + t * p.H, c, p.H, f32_to_raw<X>(d));
+    }
+  }
+}
+
+// Column sums of wide rows: a block has 2048 columns (256 threads) of the rows blockIdx.y, + gridDim.y, ...
+template <typename X, typename Y, bool REC, bool VEC>
+__global__ void __launch_bounds__(256)
+layer_norm_columns_kernel(const LnParams p) {
+  const long long cpitch = act_codes_pitch(p.H), spitch = act_scale_pitch(p.H);
+  const int c = blockIdx.x * 2048 + first_column<VEC>(threadIdx.x);
+  float aw[8], ab[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) aw[i] = ab[i] = 0.f;
+  grid_dependents_launch();
+  grid_dependency_wait();
+  for (long long t = blockIdx.y; t < p.T; t += gridDim.y) {
+    float x[8], d[8];
+    const float mean = p.mean[t], rho = p.rho[t];
+    ln_x8<X, REC, VEC>(p, t, cpitch, spitch, c, x);
+    load8<Y, VEC>(reinterpret_cast<const Y*>(p.dy) + t * p.ld_dy, c, p.H, d);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { aw[i] = fmaf(d[i], (x[i] - mean) * rho, aw[i]); ab[i] += d[i]; }
+  }
+  float* part = p.part + (long long)blockIdx.y * 2 * p.H;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int col = column<VEC>(c, i);
+    if (col < p.H) { part[col] = aw[i]; part[p.H + col] = ab[i]; }
+  }
+}
+
+// dw and db from the partial rows, in a fixed order: 32 columns a block, 32 warps share the rows.
+__global__ void __launch_bounds__(1024)
+layer_norm_reduce_kernel(const float* part, long long parts, int H, void* dweight, void* dbias, int type) {
+  __shared__ float sums[32][33];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, which = blockIdx.y;
+  const int col = blockIdx.x * 32 + lane;
+  grid_dependents_launch();
+  grid_dependency_wait();
+  float s = 0.f;
+  if (col < H)
+    for (long long r = warp; r < parts; r += 32) s += part[(r * 2 + which) * H + col];
+  sums[warp][lane] = s;
+  __syncthreads();
+  if (warp != 0) return;
+  s = 0.f;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) s += sums[i][lane];
+  void* out = which == 0 ? dweight : dbias;
+  if (col >= H || out == nullptr) return;
+  if (type == 0) reinterpret_cast<__nv_bfloat16*>(out)[col] = __float2bfloat16_rn(s);
+  else if (type == 1) reinterpret_cast<float*>(out)[col] = s;
+  else reinterpret_cast<__half*>(out)[col] = __float2half_rn(s);
+}
+
+}  // namespace kdkl
