@@ -561,6 +561,49 @@ int kdkl_rotary_table(int32_t rotary_dim, double base, int32_t scaling, double f
                       double* turns_host, float* magnitude_host);
 int kdkl_rotary(const kdkl_rotary_args* args, void* cuda_stream);
 
+/* The gated linear layer h = act(x Wg^T) (x Wu^T), weight [2 F, H] = Wg above Wu, in one kernel: gate and up never reach
+ * memory in 16 bits. bf16, sums in fp32, one rounding; H and F are multiples of 8, rows start on 16 bytes.
+ * What the backward pass takes gate and up from:
+ *   format NONE        nothing is kept; a kernel forms the product of x and the weight once more
+ *   INT8 or E4M3       records of gate and up that the forward call leaves (and, if h_record is not NULL, one of h as it
+ *                      was returned); the weight gradient then reads a record of x, which whoever made x left
+ * backward: dgate = dh up act'(gate), dup = dh act(gate), rounded to bf16 into dgate_up [T, 2 F]; dx = dgate_up weight (bf16);
+ * dweight (= or, with accumulate, +=) dgate_up^T x, of dweight_type. dx and dweight may be NULL. T = 0: dweight becomes
+ * zeros. Bitwise reproducible. Up to 8 tokens without a format do without tensor cores (serving's single tokens).
+ * workspace: 256 bytes forward, kdkl_gated_linear_workspace_bytes() backward, 256-byte aligned; its first words are a status
+ * block readable with kdkl_status (KDKL_ERR_TIMEOUT), that of the last call.
+ * One struct serves both calls; a call reads the fields it needs. */
+typedef struct kdkl_gated_linear_args {
+  int32_t struct_size;        /* sizeof(kdkl_gated_linear_args) */
+  int32_t act;                /* KDKL_GATED_* */
+  int32_t format;             /* KDKL_ACT8_* */
+  int32_t dweight_type;       /* BF16 or F32 */
+  int32_t accumulate;
+  int32_t reserved;
+  int64_t T, H, F;
+  const void* x;              /* forward, and backward without records: [T, H], rows ld_x apart */
+  int64_t ld_x;
+  const void* weight;         /* [2 F, H] contiguous */
+  void* h;                    /* forward out [T, F], rows ld_h apart */
+  int64_t ld_h;
+  void* gate_record;          /* with a format: forward out, backward in; of [T, F] */
+  void* up_record;
+  void* h_record;             /* forward out, or NULL */
+  size_t record_bytes;        /* of each of the three */
+  const void* x_record;       /* backward, with a format and dweight: of [T, H] */
+  size_t x_record_bytes;
+  const void* dh;             /* backward in [T, F], rows ld_dh apart */
+  int64_t ld_dh;
+  void* dgate_up;             /* backward out [T, 2 F] contiguous */
+  void* dx;                   /* backward out [T, H] contiguous, or NULL */
+  void* dweight;              /* backward out [2 F, H], or NULL */
+  void* workspace;
+  size_t workspace_bytes;
+} kdkl_gated_linear_args;
+size_t kdkl_gated_linear_workspace_bytes(int64_t T, int64_t H, int64_t F, int32_t dweight_type);
+int kdkl_gated_linear_forward(const kdkl_gated_linear_args* args, void* cuda_stream);
+int kdkl_gated_linear_backward(const kdkl_gated_linear_args* args, void* cuda_stream);
+
 /* Exercises the bounded wait every kernel of this library uses on its mbarriers: one thread waits on
  * a barrier that nothing completes, gives up after limit_ns (1 .. 1e9) and the kernel returns normally.
  * status: device int32[2], zeroed by the caller; afterwards {KDKL_ERR_TIMEOUT, 99}. The context stays

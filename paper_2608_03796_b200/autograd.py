@@ -27,6 +27,7 @@ The layers of a student's body whose backward pass reads activations kept in 8 b
     branch = act8_linear(h, W_down, record=kept)
     y, kept = layer_norm(x, weight, bias, act8="int8", keep_y=True)
     q, k = rotary(q, k, positions, body.Rotary(D))
+    h, kept = gated_linear(y, W_gate_up, act8="int8", record=kept, keep_h=True)     # act8_linear and gated_act in one kernel
 
 Their outputs, records and gradients are allocated per call, as a graph needs them.
 """
@@ -527,3 +528,69 @@ def rotary(q, k, positions, rope: body.Rotary):
         if t is not None and t.shape[:-2] != positions.shape:
             raise TypeError(f"rotary: positions {tuple(positions.shape)} beside heads of {tuple(t.shape)}")
     return _Rotary.apply(q, k, positions, rope)
+
+
+def _words16(t: torch.Tensor) -> torch.Tensor:
+    """Rows that start on 16 bytes, as the tensor cores' loads need them (a copy where they do not)."""
+    return t if t.data_ptr() % 16 == 0 and (t.shape[0] <= 1 or t.stride(0) % 8 == 0) else t.clone(memory_format=torch.contiguous_format)
+
+
+class _GatedLinear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, record, act, act8, keep_h, train, sync_status):
+        H, F = weight.shape[1], weight.shape[0] // 2
+        rows, w = _words16(_flat(x, H)), _words16(weight.contiguous())
+        op = body.GatedLinear(rows.shape[0], H, F, act=act, act8=act8, train=train, keep_h=keep_h and train, device=x.device)
+        h = _shaped(op.forward(rows, w), (*x.shape[:-1], F))
+        _watch(op.head, "gated_linear")
+        if train:
+            if act8 is not None and record is None and ctx.needs_input_grad[1]:
+                record = body.Act8Record(rows.shape[0], H, act8, device=x.device).store(rows)
+            kept = (rows,) if act8 is None else (op.gate_record.buffer, op.up_record.buffer, None if record is None else record.buffer)
+            ctx.save_for_backward(w, *kept)
+            ctx.format, ctx.shape, ctx.sync_status = act8, x.shape, sync_status
+        h_record = op.h_record
+        op.h = op.kept = op.gate_record = op.up_record = op.h_record = None
+        ctx.op = op
+        return h, h_record
+
+    @staticmethod
+    @_first_derivative_only("gated_linear")
+    def backward(ctx, dh, _):
+        op, (weight, *kept), record = ctx.op, ctx.saved_tensors, None
+        if ctx.format is None:
+            op.kept = (kept[0], weight)
+        else:
+            op.kept = (None, weight)
+            op.gate_record, op.up_record = (body.Act8Record(op.T, op.F, ctx.format, buffer=b) for b in kept[:2])
+            record = None if kept[2] is None else body.Act8Record(op.T, op.H, ctx.format, buffer=kept[2])
+        op.workspace = op.dgate_up = op.dx = op.dweight = None                  # buffers of its own for every backward
+        dx, dw = op.backward(_words16(_flat(dh, op.F)), record, want_dx=ctx.needs_input_grad[0], want_dweight=ctx.needs_input_grad[1])
+        if ctx.sync_status:
+            code, detail = op.status()
+            if code != 0:
+                raise B.KdklError(code, f"device status of a gated_linear step, detail {detail}")
+        else:
+            _watch(op.workspace, "gated_linear")
+        op.kept = op.workspace = op.dgate_up = op.dx = op.dweight = op.gate_record = op.up_record = op.last = None
+        return None if dx is None else dx.reshape(ctx.shape), dw, None, None, None, None, None, None
+
+
+def gated_linear(x, weight, act: str = "silu", act8: Optional[str] = None, record: Optional[body.Act8Record] = None,
+                 keep_h: bool = False, sync_status: bool = False):
+    """act(x @ Wg.T) * (x @ Wu.T) in one kernel (see body.GatedLinear); x [..., H] and the stacked weight [2 F, H] are bf16.
+    With act8 the backward pass reads 8-bit records of gate and up and, for the weight, of x: `record`, if one that stands
+    for x exists already (layer_norm and block_norm leave them), else its own; with keep_h also (h, record of h). Without,
+    it keeps x and forms gate and up again. Waits that ran out are reported as act8_linear reports them."""
+    if x.dtype != torch.bfloat16 or weight.dtype != torch.bfloat16:
+        raise TypeError(f"gated_linear: expected bf16, got {x.dtype} and {weight.dtype}")
+    if weight.dim() != 2 or weight.shape[0] % 2 or weight.shape[1] != x.shape[-1]:
+        raise TypeError(f"gated_linear: expected a weight [2 F, {x.shape[-1]}], got {tuple(weight.shape)}")
+    if act8 not in (None, "int8", "e4m3"):
+        raise ValueError(f"gated_linear: expected a record format or None, got {act8!r}")
+    if keep_h and act8 is None:
+        raise ValueError("gated_linear: keep_h needs act8")
+    if record is not None and act8 is not None and (record.T, record.H, record.format) != (x.numel() // max(1, x.shape[-1]), x.shape[-1], act8):
+        raise TypeError(f"gated_linear: the record is of {(record.T, record.H, record.format)}, the input of {tuple(x.shape)}, act8 {act8}")
+    h, h_record = _GatedLinear.apply(x, weight, record, act, act8, keep_h, _recorded(x, weight), bool(sync_status))
+    return (h, h_record) if keep_h else h

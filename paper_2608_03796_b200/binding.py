@@ -35,7 +35,8 @@ EXPORTS = [
     "kdkl_gated_act_backward", "kdkl_act8_dweight_workspace_bytes", "kdkl_act8_dweight",
     "kdkl_block_norm_workspace_bytes", "kdkl_block_norm_forward", "kdkl_block_norm_backward",
     "kdkl_layer_norm_workspace_bytes", "kdkl_layer_norm_forward", "kdkl_layer_norm_backward",
-    "kdkl_rotary_table", "kdkl_rotary",
+    "kdkl_rotary_table", "kdkl_rotary", "kdkl_gated_linear_workspace_bytes", "kdkl_gated_linear_forward",
+    "kdkl_gated_linear_backward",
 ]
 
 FEATURE_MSE, FEATURE_COSINE = 0, 1
@@ -158,6 +159,12 @@ def lib() -> ctypes.CDLL:
                                     ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_float)]
     L.kdkl_rotary.restype = ctypes.c_int
     L.kdkl_rotary.argtypes = [vp, vp]
+    L.kdkl_gated_linear_workspace_bytes.restype = sz
+    L.kdkl_gated_linear_workspace_bytes.argtypes = [i64, i64, i64, i32]
+    L.kdkl_gated_linear_forward.restype = ctypes.c_int
+    L.kdkl_gated_linear_forward.argtypes = [vp, vp]
+    L.kdkl_gated_linear_backward.restype = ctypes.c_int
+    L.kdkl_gated_linear_backward.argtypes = [vp, vp]
     L.kdkl_wait_selftest.restype = ctypes.c_int
     L.kdkl_wait_selftest.argtypes = [vp, i64, vp]
     L.kdkl_last_error.restype = ctypes.c_char_p

@@ -8,6 +8,7 @@ read them in the backward pass.
     join = BlockNorm(T, H); y, x = join.forward(residual, branch, post_weight=w1, pre_weight=w2)
     d = join.backward(dy, dx)                           # d.residual, d.branch, d.post_weight, d.pre_weight, d.gate
     norm = LayerNorm(T, H); y = norm.forward(x, w, b); d = norm.backward(dy)          # d.x, d.weight, d.bias
+    ffn = GatedLinear(T, H, F); h = ffn.forward(x, W_gate_up); dx, dW = ffn.backward(dh)
     rope = Rotary(D); q_, k_ = rope.forward(q, k, positions); dq, dk = rope.backward(dq_, dk_, positions)
 
 The classes hold outputs, records and workspaces of one shape: calls allocate nothing, only enqueue on the current
@@ -566,3 +567,125 @@ class Rotary:
         if t is None or t.shape != like.shape or t.dtype is not like.dtype or t.device != like.device:
             t = self._own[inverse, which] = torch.empty(like.shape, dtype=like.dtype, device=like.device)
         return t
+
+
+class kdkl_gated_linear_args(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("struct_size", "act", "format", "dweight_type", "accumulate", "reserved")]
+                + [(n, ctypes.c_int64) for n in ("T", "H", "F")]
+                + [("x", ctypes.c_void_p), ("ld_x", ctypes.c_int64), ("weight", ctypes.c_void_p), ("h", ctypes.c_void_p),
+                   ("ld_h", ctypes.c_int64)]
+                + [(n, ctypes.c_void_p) for n in ("gate_record", "up_record", "h_record")]
+                + [("record_bytes", ctypes.c_size_t), ("x_record", ctypes.c_void_p), ("x_record_bytes", ctypes.c_size_t),
+                   ("dh", ctypes.c_void_p), ("ld_dh", ctypes.c_int64)]
+                + [(n, ctypes.c_void_p) for n in ("dgate_up", "dx", "dweight", "workspace")] + [("workspace_bytes", ctypes.c_size_t)])
+
+
+class GatedLinear:
+    """h = act(x @ Wg.T) * (x @ Wu.T) of x [T, H] and the stacked weight [2 F, H] (Wg above Wu), in one kernel
+    (kdkl_gated_linear_forward / _backward). bf16; H and F are multiples of 8.
+
+    With act8 given, forward leaves records of gate and up, which backward reads, together with a record of x that
+    whoever made x left; keep_h: a record of h too (``h_record``, for the layer that reads h). With act8=None nothing
+    is kept beside x itself, which the caller leaves in place, and backward forms gate and up again. train=False: no
+    backward call. `dtype` is that of the weight's gradient (bf16 or fp32)."""
+
+    def __init__(self, T: int, H: int, F: int, *, act: str = "silu", act8: Optional[str] = None, train: bool = True,
+                 keep_h: bool = False, dtype=torch.bfloat16, device="cuda"):
+        if dtype not in (torch.bfloat16, torch.float32):
+            raise ValueError(f"kdkl: weight gradients are bf16 or fp32, not {dtype}")
+        if keep_h and not (train and act8 is not None):
+            raise ValueError("kdkl: keep_h needs act8, in training")
+        self.T, self.H, self.F, self.dtype, self.train, self.act8 = T, H, F, dtype, train, act8
+        a = self.args = kdkl_gated_linear_args()
+        a.struct_size, a.T, a.H, a.F = ctypes.sizeof(a), T, H, F
+        a.act, a.format, a.dweight_type = _lookup(ACTS, act, "act"), _lookup(FORMATS, act8, "act8") if train else -1, TYPES[dtype]
+        self.workspace_bytes = B.lib().kdkl_gated_linear_workspace_bytes(T, H, F, a.dweight_type)
+        if self.workspace_bytes == 0:
+            raise ValueError(f"kdkl: no gated linear layer of shape {(T, H, F)}")
+        self.h = torch.empty(T, F, dtype=torch.bfloat16, device=device)
+        self.head = torch.zeros(256, dtype=torch.uint8, device=device)          # the forward call's status
+        self.device, self.at = self.h.device, self.h.get_device()
+        a.h, a.ld_h = self.h.data_ptr(), F
+        self.gate_record = self.up_record = self.h_record = self.kept = None
+        if a.format >= 0:
+            self.gate_record, self.up_record = Act8Record(T, F, act8, device), Act8Record(T, F, act8, device)
+            self.h_record = Act8Record(T, F, act8, device) if keep_h else None
+        self.workspace = self.dgate_up = self.dx = self.dweight = None          # made by the first backward call
+        self._ref, self.last = ctypes.byref(a), self.head
+        self._forward, self._backward = B.lib().kdkl_gated_linear_forward, B.lib().kdkl_gated_linear_backward
+
+    def forward(self, x: torch.Tensor, weight: torch.Tensor) -> torch.Tensor:
+        a = self.args
+        a.x, a.ld_x = _rows(x, self.T, self.H, torch.bfloat16, "x")
+        self._weight(weight)
+        written = self._records()
+        a.workspace, a.workspace_bytes = self.head.data_ptr(), 256
+        B._check(self._forward(self._ref, _stream(self.at, "gated linear layer")))
+        _written([self.h, *written])
+        self.last = self.head
+        if self.train:                                                      # what the backward call reads
+            self.kept = (x if a.format < 0 else None, weight)
+        return self.h
+
+    def _weight(self, weight):
+        ptr, apart = _rows(weight, 2 * self.F, self.H, torch.bfloat16, "weight")
+        if apart != self.H:
+            raise TypeError(f"kdkl: weight: expected a contiguous tensor, got strides {weight.stride()}")
+        self.args.weight = ptr
+
+    def _records(self):
+        a, kept = self.args, [r for r in (self.gate_record, self.up_record, self.h_record) if r is not None]
+        for r in kept:
+            if r.at != self.at:                                             # (autograd's hooks may have moved it)
+                _stream(r.at, "record")
+            a.record_bytes = r.nbytes
+        a.gate_record, a.up_record, a.h_record = (None if r is None else r.ptr for r in (self.gate_record, self.up_record, self.h_record))
+        return [r.buffer for r in kept]
+
+    def backward(self, dh: torch.Tensor, record: Optional[Act8Record] = None, *, out: Optional[torch.Tensor] = None,
+                 accumulate: bool = False, want_dx: bool = True, want_dweight: bool = True):
+        """(dx, dweight) of the last forward call's inputs. `record` is that of x, needed with act8 for the weight's gradient,
+        which goes to `out` if given; with `accumulate` it is added to what is there."""
+        if not self.train:
+            raise RuntimeError("kdkl: this gated linear layer keeps nothing for a backward pass (train=False)")
+        if self.kept is None:
+            raise RuntimeError("kdkl: this gated linear layer's backward call comes before any forward call")
+        a, bf16 = self.args, torch.bfloat16
+        if want_dweight and a.format >= 0:
+            if record is None or (record.T, record.H, record.code) != (self.T, self.H, a.format):
+                raise TypeError(f"kdkl: record: expected one of x, {(self.T, self.H)} {self.act8}, got "
+                                f"{None if record is None else (record.T, record.H, record.format)}")
+            if record.at != self.at:
+                _stream(record.at, "record")
+            a.x_record, a.x_record_bytes = record.ptr, record.nbytes
+        if self.workspace is None:
+            self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=self.device)
+        if self.dgate_up is None:
+            self.dgate_up = torch.empty(self.T, 2 * self.F, dtype=bf16, device=self.device)
+        if want_dx and self.dx is None:
+            self.dx = torch.empty(self.T, self.H, dtype=bf16, device=self.device)
+        if not want_dweight:
+            out = None
+        elif out is not None:
+            B._dptr(out, self.dtype, (2 * self.F, self.H), "out")
+        else:
+            if self.dweight is None:
+                self.dweight = torch.empty(2 * self.F, self.H, dtype=self.dtype, device=self.device)
+            out = self.dweight
+        x, weight = self.kept
+        self._weight(weight)
+        self._records()
+        if a.format < 0:
+            a.x, a.ld_x = _rows(x, self.T, self.H, bf16, "x")
+        a.dh, a.ld_dh = _rows(dh, self.T, self.F, bf16, "dh")
+        a.dgate_up, a.dx = self.dgate_up.data_ptr(), self.dx.data_ptr() if want_dx else None
+        a.dweight, a.accumulate = None if out is None else out.data_ptr(), 1 if accumulate else 0
+        a.workspace, a.workspace_bytes = self.workspace.data_ptr(), self.workspace_bytes
+        B._check(self._backward(self._ref, _stream(self.at, "gated linear layer")))
+        _written([t for t in (self.dgate_up, self.dx if want_dx else None, out) if t is not None])
+        self.last = self.workspace
+        return (self.dx if want_dx else None), out
+
+    def status(self):
+        """(code, detail) of the last call, which waits for it; every call starts with a clear status."""
+        return B.kdkl_status(self.last)

@@ -12,26 +12,9 @@
 // widths) 16384 x 7167 takes 1119 and 851 us.
 #pragma once
 #include "act8.cuh"
+#include "gated_math.cuh"
 
 namespace kdkl {
-
-constexpr int kActSilu = 0, kActGelu = 1;
-
-// sigmoid(k(g)) and k'(g)
-template <int ACT>
-__device__ __forceinline__ float gate_sigmoid(float g, float& slope) {
-  float k = g;
-  slope = 1.f;
-  if (ACT == kActGelu) {
-    constexpr float c = 1.5957691216057308f;          // 2 sqrt(2 / pi)
-    const float g2 = g * g;
-    k = c * g * fmaf(0.044715f, g2, 1.f);
-    slope = c * fmaf(3.f * 0.044715f, g2, 1.f);
-  }
-  // from exp(-|k|), so that the quotient stays in [1, 2] and the far negative side keeps its relative accuracy
-  const float e = __expf(-fabsf(k));
-  return __fdividef(k >= 0.f ? 1.f : e, 1.f + e);
-}
 
 template <typename T, int ACT, int FMT /* -1: nothing is kept */, bool VEC>
 __global__ void __launch_bounds__(256)

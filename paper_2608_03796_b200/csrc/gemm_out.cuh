@@ -1,0 +1,111 @@
+// Products that write a gradient, out [M, N] = A B with B stored [K, N]: which tiles, how many parts of the contraction, and
+// the launch. A is K-major ([M, K]) or MN-major ([K, M]). The result is bf16 or fp32, written or added to.
+#pragma once
+#include "gemm_host.cuh"
+
+namespace kdkl {
+
+// out = (part[0] + part[1] + ..., in that order) row_scale [+ out], rounded once. A row's scale of 0 gives zeros. One thread
+// per four columns.
+template <bool BF16>
+__global__ void __launch_bounds__(256)
+out_join_kernel(const float* part, long long slab, int splits, long long n4, int row_n4, const float* row_scale, void* out,
+                int accumulate) {
+  const long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x;
+  if (i >= n4) return;
+  float4 a = reinterpret_cast<const float4*>(part)[i];
+  for (int s = 1; s < splits; ++s) {
+    const float4 b = reinterpret_cast<const float4*>(part + s * slab)[i];
+    a.x += b.x; a.y += b.y; a.z += b.z; a.w += b.w;
+  }
+  if (row_scale != nullptr) {
+    const float r = row_scale[i / row_n4];
+    a = r == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(a.x * r, a.y * r, a.z * r, a.w * r);
+  }
+  if (BF16) {
+    uint2* o = reinterpret_cast<uint2*>(out) + i;
+    if (accumulate) {
+      const uint2 w = *o;
+      a.x += __uint_as_float(w.x << 16); a.y += __uint_as_float(w.x & 0xffff0000u);
+      a.z += __uint_as_float(w.y << 16); a.w += __uint_as_float(w.y & 0xffff0000u);
+    }
+    *o = make_uint2(pack_bf16x2(a.x, a.y), pack_bf16x2(a.z, a.w));
+  } else {
+    float4* o = reinterpret_cast<float4*>(out) + i;
+    if (accumulate) { const float4 w = *o; a.x += w.x; a.y += w.y; a.z += w.z; a.w += w.w; }
+    *o = a;
+  }
+}
+
+// The plan with the least estimated cycles: waves of units, a unit taking its k-blocks (512 cycles of tensor work each, 1024
+// in a WIDE tile, by the nominal rate) and about six more to start and to drain its tile; parts of a contraction cost
+// the slabs' way through memory (2600 bytes a cycle) and one more launch.
+struct OutPlan { bool wide; int splits; };
+inline OutPlan out_plan(long long M, long long N, long long K, int sm_count, bool joined) {
+  const long long workers = sm_count < 2 ? 1 : sm_count / 2, kb = (K + BK - 1) / BK, mt = (M + kTileM - 1) / kTileM;
+  OutPlan best = {false, 1};
+  double least = 1e300;
+  for (int wide = 0; wide <= 1; ++wide) {
+    const long long tiles = mt * n_tiles_for(N, wide != 0);
+    for (int sp = 1; sp <= 16; ++sp) {
+      if (sp > 1 && kb / sp < 8) break;
+      if ((kb + sp - 1) / sp * (sp - 1) >= kb) continue;     // the last part would be empty
+      const long long waves = (tiles * sp + workers - 1) / workers;
+      double cost = (double)waves * ((kb + sp - 1) / sp + 6) * (wide ? 1024.0 : 512.0);
+      if (sp > 1 || joined) cost += 4000.0 + (double)M * N * (8.0 * sp + 2.0) / 2600.0;
+      if (cost < least) { least = cost; best = OutPlan{wide != 0, sp}; }
+    }
+  }
+  return best;
+}
+inline size_t out_slab_bytes(const OutPlan& plan, long long M, long long N, bool joined) {
+  return plan.splits > 1 || joined ? up((size_t)plan.splits * up((size_t)M, 32) * N * 4, 256) : 0;
+}
+
+struct OutGemm {
+  const void* a; long long lda;       // elements; a_mn: stored [K, M]
+  const void* b; long long ldb;       // [K, N]
+  long long M, N, K;
+  void* out; bool bf16; int accumulate;
+  OutPlan plan;
+  float* slab;                        // out_slab_bytes
+  int* status;
+  const int* go;
+  const uint8_t* m_live; const uint8_t* k_live;
+  const float* row_scale;             // joined
+};
+template <bool A_MN>
+inline int launch_out(const OutGemm& o, const DeviceInfo& di, cudaStream_t st) {
+  CUtensorMap ta, tb, tc;
+  int rc;
+  if (A_MN) rc = make_tmap_bf16(&ta, o.a, (uint64_t)o.M, (uint64_t)o.K, (uint64_t)o.lda * 2, 64, BK);
+  else      rc = make_tmap_bf16(&ta, o.a, (uint64_t)o.K, (uint64_t)o.M, (uint64_t)o.lda * 2, BK, BM);
+  if (rc) return rc;
+  if ((rc = make_tmap_bf16(&tb, o.b, (uint64_t)o.N, (uint64_t)o.K, (uint64_t)o.ldb * 2, 64, BK))) return rc;
+  const bool joined = o.plan.splits > 1 || o.row_scale != nullptr || (o.bf16 && o.accumulate);
+  GemmParams p;
+  memset(&p, 0, sizeof(p));
+  p.M = (int)o.M; p.N = (int)o.N; p.K = (int)o.K;
+  p.m_tiles = (int)((o.M + kTileM - 1) / kTileM); p.n_tiles = (int)n_tiles_for(o.N, o.plan.wide);
+  const long long rows = (long long)up((size_t)o.M, 32);   // of a part: output boxes are 32 rows high
+  p.k_splits = o.plan.splits; p.split_rows = (int)rows;
+  p.status = o.status; p.go = o.go; p.m_live = o.m_live; p.k_live = o.plan.splits == 1 ? o.k_live : nullptr;
+  const bool f32 = joined || !o.bf16;
+  if (joined) rc = make_tmap_out_f32(&tc, o.slab, (uint64_t)o.N, (uint64_t)(o.plan.splits * rows), (uint64_t)o.N);
+  else if (o.bf16) rc = make_tmap_out_bf16(&tc, o.out, (uint64_t)o.N, (uint64_t)o.M, (uint64_t)o.N);
+  else { rc = make_tmap_out_f32(&tc, o.out, (uint64_t)o.N, (uint64_t)o.M, (uint64_t)o.N); p.accumulate = o.accumulate; }
+  if (rc) return rc;
+  if (f32) rc = o.plan.wide ? launch_gemm<EPI_STORE_F32, A_MN, true, true>(ta, tb, tc, p, di, st)
+                            : launch_gemm<EPI_STORE_F32, A_MN, true, false>(ta, tb, tc, p, di, st);
+  else     rc = o.plan.wide ? launch_gemm<EPI_STORE_BF16, A_MN, true, true>(ta, tb, tc, p, di, st)
+                            : launch_gemm<EPI_STORE_BF16, A_MN, true, false>(ta, tb, tc, p, di, st);
+  if (rc || !joined) return rc;
+  const long long n4 = o.M * o.N / 4;
+  const unsigned grid = (unsigned)((n4 + 255) / 256);
+  if (o.bf16) out_join_kernel<true><<<grid, 256, 0, st>>>(o.slab, rows * o.N, o.plan.splits, n4, (int)(o.N / 4), o.row_scale, o.out, o.accumulate);
+  else out_join_kernel<false><<<grid, 256, 0, st>>>(o.slab, rows * o.N, o.plan.splits, n4, (int)(o.N / 4), o.row_scale, o.out, o.accumulate);
+  KDKL_LAUNCHED("out_join_kernel");
+  return KDKL_OK;
+}
+
+}  // namespace kdkl

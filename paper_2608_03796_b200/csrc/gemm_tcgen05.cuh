@@ -28,9 +28,20 @@
 //                   reads them back instead of projecting again)
 //   EPI_LSE_E       EPI_LSE that also stores the unnormalised exponentials 2^(z log2e / tau - 64) in bf16, for the
 //                   single-pass forward + backward (no second projection: G is made from them once log Z is known)
+//   EPI_LSE_SUM, EPI_LSE_E_SUM
+//                   the same two that also leave each row's sum of raw logits (label smoothing)
+//   EPI_LABEL_G     backward of the label loss: G = a_t exp(z/tau - logZ) - c_t, less b_t at the label, cast to bf16
+//   EPI_GATED, EPI_GATED_ACT8
+//                   gate and up projection of a gated layer in one tile: of its 256 accumulator columns 128 are gate, from
+//                   the rows of B that the leader stages, and 128 up, from the peer's, of the same 128 features (B is a
+//                   [2, features, K] tensor). act(gate) * up leaves in bf16; ACT8 also leaves 8-bit records
+//   EPI_GATED_BACK  the same product again; from the upstream gradient d: d up act'(gate) and d act(gate), into a
+//                   [rows, 2, features] output
 #pragma once
 #include <cuda_bf16.h>
 
+#include "act8.cuh"
+#include "gated_math.cuh"
 #include "sm100_prims.cuh"
 
 namespace kdkl {
@@ -68,7 +79,8 @@ struct GemmCfg {
                                     2 * MAX_LIVE_KB /*live k-block list*/ + 2 * MAX_LIVE_M /*live row-tile list*/;
 };
 
-enum { EPI_STORE_F32 = 0, EPI_STORE_BF16 = 1, EPI_LSE = 2, EPI_DLOGITS = 3, EPI_TOPK = 4, EPI_LSE_E = 5, EPI_LSE_Z = 6 };
+enum { EPI_STORE_F32 = 0, EPI_STORE_BF16 = 1, EPI_LSE = 2, EPI_DLOGITS = 3, EPI_TOPK = 4, EPI_LSE_E = 5, EPI_LSE_Z = 6,
+       EPI_LSE_SUM = 7, EPI_LSE_E_SUM = 8, EPI_LABEL_G = 9, EPI_GATED = 10, EPI_GATED_ACT8 = 11, EPI_GATED_BACK = 12 };
 
 // EPI_LSE_E stores e = 2^(z log2e / tau - kExpBias) in bf16: representable for scaled logits in about
 // [-62, 190] (bf16 has fp32's exponent range), i.e. far below any weight that matters and far above any sane logit.
@@ -120,6 +132,15 @@ struct GemmParams {
   int* cand_idx;             // [rows, cand_cap]
   float* cand_val;           // [rows, cand_cap] raw logits
   int cand_cap;
+  // EPI_LSE_SUM, EPI_LSE_E_SUM: sums of raw logits, as part_m. EPI_LABEL_G: coefA any sign; coefB at the label (idx_sorted,
+  // nvalid with Ktop = 1)
+  float* part_z;             // [n_tiles, part_stride]
+  const float* coefC;        // [rows]
+  // EPI_GATED*: N is the number of features, n_tiles counts tiles of 128 of them
+  int act, format;           // kActSilu / kActGelu; kFmtInt8 / kFmtE4M3
+  ActRecord rec_gate, rec_up, rec_h;   // EPI_GATED_ACT8; rec_h optional
+  const __nv_bfloat16* dh;   // EPI_GATED_BACK [rows, N], 16-byte aligned rows
+  long long ld_dh;
 };
 
 __device__ __forceinline__ int lower_bound_i32(const int* a, int n, int key) {
@@ -152,6 +173,138 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
 
 __device__ __forceinline__ int kblocks_all(int K) { return (K + BK - 1) / BK; }
 
+constexpr int kGatedN = 128;                   // features of a gated tile
+
+// 32 values of a row (one group of a record) as codes and scale byte; the whole warp calls.
+template <int FMT>
+__device__ __forceinline__ uint32_t record_row32(const ActRecord& r, bool write, long long code_at, const uint32_t (&v)[32]) {
+  uint32_t top = 0u;
+#pragma unroll
+  for (int j = 0; j < 32; ++j) top = max(top, v[j] & 0x7fffffffu);
+  const uint32_t byte = act_scale_byte<FMT>(top);
+  uint32_t w[8];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(v[8 * k + i]);
+    const uint2 c = act_codes<FMT>(f, byte);
+    w[2 * k] = c.x; w[2 * k + 1] = c.y;
+  }
+  if (write) {
+    uint4* to = reinterpret_cast<uint4*>(r.codes + code_at);
+    to[0] = make_uint4(w[0], w[1], w[2], w[3]);
+    to[1] = make_uint4(w[4], w[5], w[6], w[7]);
+  }
+  return byte;
+}
+
+// A thread has one row: 128 gate columns at taddr and the same features' 128 up columns behind them, 32 at a time. Outputs
+// leave through the warp's two swizzled boxes as in the plain store. What lies past the last feature reads as zero (the
+// tensor map of B fills it) and is clipped by the output's map.
+template <int EPI>
+__device__ __forceinline__ void gated_epilogue(const GemmParams& p, const CUtensorMap& tmC, uint32_t taddr, int row, bool row_ok,
+                                               int box_row0, int nt, int lane, uint32_t boxes, uint32_t& nbox) {
+  constexpr bool kBack = EPI == EPI_GATED_BACK, kAct8 = EPI == EPI_GATED_ACT8;
+  const bool gelu = p.act == kActGelu;
+  const long long cpitch = act_codes_pitch(p.N), spitch = act_scale_pitch(p.N);
+  uint32_t bytes_gate = 0u, bytes_up = 0u, bytes_h = 0u;
+#pragma unroll 1
+  for (int w = 0; w < kGatedN / 32; ++w) {
+    const int col0 = nt * kGatedN + w * 32;
+    if (col0 >= p.N && (w & 1) == 0) break;    // uniform; a pair of windows (one box) is always completed
+    uint32_t g[32], u[32];
+    __syncwarp();
+    tmem_ld32(taddr + w * 32, g);
+    tmem_ld32(taddr + kGatedN + w * 32, u);
+    uint4 d[4];
+    if (kBack) {
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        d[c] = row_ok && col0 + 8 * c < p.N ? *reinterpret_cast<const uint4*>(p.dh + row * p.ld_dh + col0 + 8 * c) : make_uint4(0u, 0u, 0u, 0u);
+    }
+    tmem_ld_wait();
+    if ((w & 1) == 0) {
+      if (lane == 0) { if (kBack) bulk_wait_read<0>(); else bulk_wait_read<1>(); }
+      __syncwarp();
+    }
+    uint32_t va[16], vb[16];
+    if (kBack) {
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        float f[8], a[8], b[8];
+        words_to_f32(d[c], f, __nv_bfloat16());
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float gate = __uint_as_float(g[8 * c + i]);
+          const GateAct t = gelu ? gate_act<kActGelu>(gate) : gate_act<kActSilu>(gate);
+          a[i] = f[i] * __uint_as_float(u[8 * c + i]) * t.slope;
+          b[i] = f[i] * gate * t.sigmoid;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          va[4 * c + i] = pack_bf16x2(a[2 * i], a[2 * i + 1]);
+          vb[4 * c + i] = pack_bf16x2(b[2 * i], b[2 * i + 1]);
+        }
+      }
+    } else {
+      if (kAct8) {
+        const bool write = row_ok && col0 < cpitch;
+        const long long at = row * cpitch + col0;
+        const uint32_t bg = p.format == kFmtInt8 ? record_row32<kFmtInt8>(p.rec_gate, write, at, g) : record_row32<kFmtE4M3>(p.rec_gate, write, at, g);
+        const uint32_t bu = p.format == kFmtInt8 ? record_row32<kFmtInt8>(p.rec_up, write, at, u) : record_row32<kFmtE4M3>(p.rec_up, write, at, u);
+        bytes_gate |= bg << (8 * w); bytes_up |= bu << (8 * w);
+      }
+      float slope;
+#pragma unroll
+      for (int j = 0; j < 32; ++j) {
+        const float gate = __uint_as_float(g[j]);
+        const float s = gelu ? gate_sigmoid<kActGelu>(gate, slope) : gate_sigmoid<kActSilu>(gate, slope);
+        g[j] = __float_as_uint(gate * s * __uint_as_float(u[j]));
+      }
+#pragma unroll
+      for (int j = 0; j < 16; ++j) va[j] = pack_bf16x2(__uint_as_float(g[2 * j]), __uint_as_float(g[2 * j + 1]));
+      if (kAct8 && p.rec_h.codes != nullptr) {             // of h as it is returned
+#pragma unroll
+        for (int j = 0; j < 16; ++j) { u[2 * j] = va[j] << 16; u[2 * j + 1] = va[j] & 0xffff0000u; }
+        const bool write = row_ok && col0 < cpitch;
+        const long long at = row * cpitch + col0;
+        bytes_h |= (p.format == kFmtInt8 ? record_row32<kFmtInt8>(p.rec_h, write, at, u) : record_row32<kFmtE4M3>(p.rec_h, write, at, u)) << (8 * w);
+      }
+    }
+    const uint32_t box = boxes + (kBack ? 0u : (nbox & 1u) * 4096u);     // BACK fills both boxes at once
+    const uint32_t srow = box + lane * 128;
+    const int cbase = (w & 1) * 4;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      st_shared_v4(srow + (((cbase + c) ^ (lane & 7)) << 4), va[4 * c], va[4 * c + 1], va[4 * c + 2], va[4 * c + 3]);
+      if (kBack) st_shared_v4(srow + 4096 + (((cbase + c) ^ (lane & 7)) << 4), vb[4 * c], vb[4 * c + 1], vb[4 * c + 2], vb[4 * c + 3]);
+    }
+    if ((w & 1) == 1) {
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) {
+        if (box_row0 < p.M) {
+          if (kBack) {
+            tma_store_3d(&tmC, box, col0 - 32, box_row0, 0);
+            tma_store_3d(&tmC, box + 4096, col0 - 32, box_row0, 1);
+          } else {
+            tma_store_2d(&tmC, box, col0 - 32, box_row0);
+          }
+        }
+        bulk_commit();
+      }
+      ++nbox;
+    }
+  }
+  if (kAct8 && row_ok) {                       // the four scale bytes of the tile's groups (the pitch is a multiple of 16)
+    const long long at = row * spitch + nt * 4;
+    *reinterpret_cast<uint32_t*>(p.rec_gate.scales + at) = bytes_gate;
+    *reinterpret_cast<uint32_t*>(p.rec_up.scales + at) = bytes_up;
+    if (p.rec_h.codes != nullptr) *reinterpret_cast<uint32_t*>(p.rec_h.scales + at) = bytes_h;
+  }
+}
+
 template <int EPI, bool A_MN, bool B_MN, int NCTA, bool WIDE = false>
 __global__ void __launch_bounds__(GEMM_THREADS, 1)
 gemm_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
@@ -161,6 +314,8 @@ gemm_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
   constexpr int TILE_M = Cfg::TILE_M, B_ROWS = Cfg::B_ROWS, TILE_N = Cfg::TILE_N, N_HALVES = Cfg::N_HALVES;
   constexpr int HALF_ROWS = B_ROWS / N_HALVES;            // rows of B this CTA stages per accumulator half
   constexpr uint32_t HALF_BYTES = HALF_ROWS * BK * 2;
+  constexpr bool kGated = EPI == EPI_GATED || EPI == EPI_GATED_ACT8 || EPI == EPI_GATED_BACK;
+  static_assert(!kGated || (NCTA == 2 && !A_MN && !B_MN && !WIDE), "a gated tile is a pair's");
   extern __shared__ uint8_t smem_raw[];
   const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* smem_al = smem_raw + (smem_base - smem_u32(smem_raw));
@@ -195,7 +350,7 @@ gemm_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
     mbar_fence_init();
     tma_prefetch_desc(&tmA);
     tma_prefetch_desc(&tmB);
-    if (EPI != EPI_LSE && EPI != EPI_TOPK) tma_prefetch_desc(&tmC);
+    if (EPI != EPI_LSE && EPI != EPI_LSE_SUM && EPI != EPI_TOPK) tma_prefetch_desc(&tmC);
   }
   if (warp == 1) {
     if (NCTA == 2) { tmem_alloc_pair(smem_u32(tmem_slot), TMEM_COLS); tmem_relinquish_pair(); }
@@ -298,6 +453,13 @@ gemm_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
           // that consumed it have been committed.
           if (leader) mbar_arrive_expect_tx(full_bar(s), NCTA * STAGE_BYTES);
           const int k0 = kb * BK;
+          if constexpr (kGated) {
+            load(sa, &tmA, k0, m0, fb);
+            tma_load_3d_pair(sb, &tmB, k0, nt * kGatedN, (int)cta_rank, fb);
+            issued |= 1u << s;
+            last_par = (last_par & ~(1u << s)) | (ph << s);
+            continue;
+          }
           if (!A_MN) {
             load(sa, &tmA, k0, m0, fb);
           } else {
@@ -391,8 +553,10 @@ gemm_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
     // ------------------------------------------------------------ epilogue (warps 2..5)
     const int lg = warp & 3;                   // TMEM lane group this warp may read
     const int row_in_tile = lg * 32 + lane;
-    constexpr bool kBf16Out = (EPI == EPI_STORE_BF16 || EPI == EPI_DLOGITS || EPI == EPI_LSE_E);
-    constexpr bool kLse = (EPI == EPI_LSE || EPI == EPI_LSE_E || EPI == EPI_LSE_Z);
+    constexpr bool kSum = (EPI == EPI_LSE_SUM || EPI == EPI_LSE_E_SUM);
+    constexpr bool kExp = (EPI == EPI_LSE_E || EPI == EPI_LSE_E_SUM);
+    constexpr bool kBf16Out = (EPI == EPI_STORE_BF16 || EPI == EPI_DLOGITS || EPI == EPI_LABEL_G || kExp);
+    constexpr bool kLse = (EPI == EPI_LSE || EPI == EPI_LSE_Z || EPI == EPI_LSE_SUM || kExp);
     constexpr bool kStore = (EPI == EPI_STORE_F32 || EPI == EPI_LSE_Z || kBf16Out);
     uint32_t lt = 0, nbox = 0;
     bool ok = true;
@@ -440,11 +604,12 @@ gemm_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
       int cur = 0, nv = 0, next_idx = 0x7fffffff;
       const int* idxrow = nullptr;
       float row_b = 0.f, row_off = -INFINITY, row_thr = INFINITY;
+      float row_a = 0.f, row_c = 0.f, z_run = 0.f;
       bool row_zero = false;                   // EPI_LSE_E: a row without gradient stores zeros, not exponentials
-      if (EPI == EPI_LSE_E) { if (row_ok && p.coefA != nullptr) row_zero = p.coefA[row] == 0.f; }
+      if (kExp) { if (row_ok && p.coefA != nullptr) row_zero = p.coefA[row] == 0.f; }
       if (EPI == EPI_TOPK) { if (row_ok) row_thr = p.thr[row]; }
       const bool neg_a = EPI == EPI_DLOGITS && p.neg_a != nullptr && *p.neg_a != 0;   // uniform over the call
-      if (kLse || EPI == EPI_DLOGITS) {
+      if (kLse || EPI == EPI_DLOGITS || EPI == EPI_LABEL_G) {
         if (row_ok) {
           idxrow = p.idx_sorted + (long long)row * p.Ktop;
           nv = p.nvalid[row];
@@ -454,6 +619,10 @@ gemm_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
             const float a = p.coefA[row];
             row_b = p.coefB[row];
             row_off = a != 0.f ? log2f(fabsf(a)) - p.lz2[row] : -INFINITY;   // sign: see neg_a
+          }
+          if (EPI == EPI_LABEL_G) {
+            row_a = p.coefA[row]; row_b = p.coefB[row]; row_c = p.coefC[row];
+            row_off = nv > 0 ? -p.lz2[row] : -INFINITY;                      // ignored tokens: exact zeros
           }
         }
       }
@@ -467,8 +636,11 @@ gemm_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
       float m_run = -INFINITY, s_run = 0.f;
       const int box_row0 = m0 + lg * 32;       // first output row of this warp's boxes
       const bool box_ok = box_row0 < p.M;      // warp-uniform
+      if constexpr (kGated) {
+        gated_epilogue<EPI>(p, tmC, taddr, row, row_ok, box_row0, nt, lane, staging0 + (warp - 2) * STAGING_WARP_BYTES, nbox);
+      }
 #pragma unroll 1
-      for (int w = 0; w < TILE_N / 32; ++w) {
+      for (int w = 0; !kGated && w < TILE_N / 32; ++w) {
         const int col0 = n0 + w * 32;
         // uniform: whole window past the edge. bf16 outputs are staged as pairs of windows
         // (64 columns = one 128-byte row), so a pair is always completed.
@@ -500,7 +672,13 @@ gemm_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
             }
             const float m_new = fmaxf(m_run, wmax * p.scale_log2);
             float acc_s = 0.f;
-            if (EPI == EPI_LSE_E) {
+            if (kSum) {
+              float zs = 0.f;
+#pragma unroll
+              for (int j = 0; j < 32; ++j) zs += full_w || col0 + j < p.N ? __uint_as_float(r[j]) : 0.f;
+              z_run += zs;
+            }
+            if (kExp) {
               // keep the window's exponentials (relative to the running maximum) in place of the logits:
               // e = 2^(s - bias) = 2^(s - m_new) * 2^(m_new - bias), one multiply instead of a second ex2
 #pragma unroll
@@ -564,11 +742,24 @@ gemm_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
             if (EPI == EPI_STORE_BF16) {
 #pragma unroll
               for (int j = 0; j < 16; ++j) v[j] = pack_bf16x2(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1]));
-            } else if (EPI == EPI_LSE_E) {
+            } else if (kExp) {
               // unnormalised exponentials with a fixed bias: G = A_t * e - b_t p is formed from them later
 #pragma unroll
               for (int j = 0; j < 16; ++j)
                 v[j] = pack_bf16x2(__uint_as_float(r[2 * j]) * e_fac, __uint_as_float(r[2 * j + 1]) * e_fac);
+            } else if (EPI == EPI_LABEL_G) {
+              float g[32];
+#pragma unroll
+              for (int j = 0; j < 32; ++j)
+                g[j] = fmaf(row_a, ex2_approx(fmaf(__uint_as_float(r[j]), p.scale_log2, row_off)), -row_c);
+              if (next_idx < col0 + 32) {      // the one label of the row
+                const int off = next_idx - col0;
+#pragma unroll
+                for (int j = 0; j < 32; ++j) g[j] -= (off == j) ? row_b : 0.f;
+                next_idx = 0x7fffffff;
+              }
+#pragma unroll
+              for (int j = 0; j < 16; ++j) v[j] = pack_bf16x2(g[2 * j], g[2 * j + 1]);
             } else {  // EPI_DLOGITS
               // a_t * 2^(s - lz2) = 2^(s + (log2 a_t - lz2)): the row coefficient rides in the exponent
               // (a_t = 0 for ignored tokens gives -inf, hence exact zeros)
@@ -621,10 +812,11 @@ gemm_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
         if (row_ok) {
           p.part_m[(long long)nt * p.part_stride + row] = m_run;
           p.part_s[(long long)nt * p.part_stride + row] = s_run;
+          if (kSum) p.part_z[(long long)nt * p.part_stride + row] = z_run;
         }
       }
     }
-    if (EPI != EPI_LSE && EPI != EPI_TOPK && lane == 0) bulk_wait_all();   // every output box has been written
+    if (EPI != EPI_LSE && EPI != EPI_LSE_SUM && EPI != EPI_TOPK && lane == 0) bulk_wait_all();   // every output box has been written
   }
 
   // ---------------------------------------------------------------- teardown

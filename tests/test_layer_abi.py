@@ -160,3 +160,43 @@ def test_kernels_that_start_early_read_coherently(name):
     code = _code(name)
     assert "grid_dependency_wait" in code and "__restrict__" not in code
     assert not re.search(r"\.nc\b", code) and "__ldg" not in code
+
+
+def _gated(backward=False, **kw):
+    a = body.kdkl_gated_linear_args()
+    fields = dict(struct_size=ctypes.sizeof(a), act=0, format=-1, dweight_type=0, accumulate=0, T=16, H=64, F=64, x=P, ld_x=64, weight=P,
+                  h=P, ld_h=64, gate_record=Q, up_record=Q, h_record=None, record_bytes=BIG, x_record=Q, x_record_bytes=BIG, dh=P,
+                  ld_dh=64, dgate_up=P, dx=P, dweight=P, workspace=Q, workspace_bytes=BIG)
+    fields.update(kw)
+    for k, v in fields.items():
+        setattr(a, k, v)
+    f = B.lib().kdkl_gated_linear_backward if backward else B.lib().kdkl_gated_linear_forward
+    return f(ctypes.byref(a), None)
+
+
+def test_gated_linear_refusals():
+    for back in (False, True):
+        assert _gated(back, struct_size=1) == ARG and _gated(back, act=2) == ARG and _gated(back, format=2) == ARG
+        for bad in (dict(T=-1), dict(H=0), dict(H=60), dict(F=4), dict(F=0), dict(F=1 << 29), dict(ld_x=56)):
+            assert _gated(back, **bad) == SHAPE, bad
+        assert _gated(back, weight=None) == NULL and _gated(back, workspace=None) == NULL and _gated(back, x=None) == NULL
+        assert _gated(back, weight=P + 2) == ALIGN and _gated(back, workspace=Q + 16) == ALIGN and _gated(back, x=P + 8) == ALIGN
+        assert _gated(back, ld_x=68) == ALIGN and _gated(back, workspace_bytes=255) == SPACE
+        assert _gated(back, format=0, gate_record=None) == NULL and _gated(back, format=1, up_record=None) == NULL
+        assert _gated(back, format=0, record_bytes=64) == SPACE and _gated(back, format=0, up_record=Q + 16) == ALIGN
+    assert _gated(h=None) == NULL and _gated(ld_h=63) == SHAPE and _gated(h=P + 8) == ALIGN and _gated(T=0, x=None, h=None) == 0
+    assert _gated(format=0, h_record=Q + 32) == ALIGN
+    assert _gated(True, dh=None) == NULL and _gated(True, dgate_up=None) == NULL and _gated(True, format=0, x_record=None) == NULL
+    assert _gated(True, dweight_type=2) == ARG and _gated(True, accumulate=2) == ARG
+    assert _gated(True, ld_dh=32) == SHAPE and _gated(True, dx=P + 4) == ALIGN and _gated(True, dweight=P + 4) == ALIGN
+    assert _gated(True, format=0, x_record_bytes=8) == SPACE
+    size = B.lib().kdkl_gated_linear_workspace_bytes
+    assert size(16, 60, 64, 0) == 0 and size(16, 64, 64, 2) == 0 and size(-1, 64, 64, 0) == 0 and size(0, 64, 64, 1) >= 256
+    with pytest.raises(ValueError):
+        body.GatedLinear(4, 60, 64, device="cpu")
+    with pytest.raises(ValueError):
+        body.GatedLinear(4, 64, 64, dtype=torch.float16, device="cpu")
+    with pytest.raises(ValueError):
+        body.GatedLinear(4, 64, 64, keep_h=True, device="cpu")
+    with pytest.raises(RuntimeError, match="keeps nothing"):
+        body.GatedLinear(4, 64, 64, train=False, device="cpu").backward(torch.zeros(4, 64))
