@@ -358,6 +358,67 @@ int kdkl_teacher_topk_stored(const void* hidden_bf16, const void* weight_bf16, i
                              int32_t K, float temperature, void* workspace, size_t workspace_bytes,
                              int32_t* topk_idx, float* topk_val, float* lse, void* cuda_stream);
 
+/* The label loss over the LM head: softmax cross entropy against one label a token, with label smoothing s, a z term lambda
+ * and token weights, in pieces of the vocabulary, without the T x V logits. z = W h / temperature, q = softmax(z), y the label:
+ *   l = lse - (1 - s) z_y - (s / V) sum_v z_v + lambda lse^2,   lse = log sum_v e^(z_v)
+ *   dl/dz_v = (1 + 2 lambda lse) q_v - (1 - s) [v = y] - s / V
+ *   loss = sum_t w_t l_t / D over the counted tokens; D = their number (MEAN; 0 gives loss 0 and zero gradients), 1 (SUM), or
+ *   *denom_device. (Weights count in the sum, not in D.)
+ * A token whose label is ignore_index is not counted: its losses, lse and gradients are zeros, and row tiles of 256 tokens
+ * without a counted one are skipped. So is one whose label lies outside [0, V), which kdkl_status reports (KDKL_ERR_INDEX). Hidden
+ * states of tokens that are not counted take part in products with zeros: they have to be finite.
+ * Three calls on one struct:
+ *   forward    one sweep; the loss, and losses and lse [T] of the tokens (0 where not counted)
+ *   backward   after a forward call with the same inputs, state, chunk and temperature (else KDKL_ERR_STATE in the status, and
+ *              nothing is written): projects again. Upstream gradient: grad_tokens [T] where given (of the losses, weights
+ *              and divisor left out), else *grad (1 if NULL) of the loss
+ *   step       both at once, three projections for four: the sweep leaves exponentials in fp16, each 32 columns to their own
+ *              largest, and they become G in place. For *grad known beforehand
+ * G, the gradient of the chunk's logits, is rounded once to bf16, outputs once to their type; a bf16 dweight over several
+ * chunks is summed in fp32. accumulate = 1 (F32 only): dweight += . dweight and dhidden must not alias inputs.
+ * hidden [T, H] and weight [V, H] bf16, contiguous, 16-byte aligned; H a multiple of 8. state: device, 256-byte aligned,
+ * kdkl_label_loss_state_bytes(T), lives from the forward to the backward call, its first words the status block;
+ * workspace: device, 256-byte aligned, kdkl_label_loss_workspace_bytes() for the call, scratch. chunk: tokens at a time,
+ * rounded up to 256, 0 = 8192, at most 65536; the workspace's largest part is [chunk, V] of 2 bytes. Bitwise reproducible. */
+#define KDKL_LABEL_MEAN 0
+#define KDKL_LABEL_SUM 1
+#define KDKL_LABEL_FORWARD 0
+#define KDKL_LABEL_BACKWARD 1
+#define KDKL_LABEL_STEP 2
+typedef struct kdkl_label_loss_args {
+  int32_t struct_size;        /* sizeof(kdkl_label_loss_args) */
+  int32_t label_type;         /* 0: int32, 1: int64 */
+  int32_t reduction;          /* KDKL_LABEL_MEAN or _SUM */
+  int32_t dhidden_type;       /* KDKL_TYPE_BF16 or _F32 (here: 0 and 1) */
+  int32_t dweight_type;       /* the same */
+  int32_t accumulate;
+  float temperature, label_smoothing, z_loss;
+  int32_t reserved;
+  int64_t ignore_index;
+  int64_t T, H, V, chunk;
+  const void* hidden;
+  const void* weight;
+  const void* labels;         /* [T]; forward, step */
+  const float* token_weight;  /* [T] or NULL */
+  const double* denom_device; /* [1] or NULL */
+  const float* grad;          /* [1] or NULL; backward, step */
+  const float* grad_tokens;   /* [T] or NULL; backward */
+  float* loss;                /* [1]; forward, step out */
+  float* losses;              /* [T] or NULL; forward, step out */
+  float* lse;                 /* [T] or NULL; forward, step out */
+  void* dhidden;              /* [T, H]; backward, step out */
+  void* dweight;              /* [V, H]; backward, step out */
+  void* state;
+  size_t state_bytes;
+  void* workspace;
+  size_t workspace_bytes;
+} kdkl_label_loss_args;
+size_t kdkl_label_loss_state_bytes(int64_t T);
+size_t kdkl_label_loss_workspace_bytes(int64_t T, int64_t H, int64_t V, int64_t chunk, int32_t call, int32_t dweight_type);
+int kdkl_label_loss_forward(const kdkl_label_loss_args* args, void* cuda_stream);
+int kdkl_label_loss_backward(const kdkl_label_loss_args* args, void* cuda_stream);
+int kdkl_label_loss_step(const kdkl_label_loss_args* args, void* cuda_stream);
+
 /* ------------------------------------------------------------------ operators of the student's body
  * The loss above never holds the T x V logits; what then grows with T in a distillation step is what the student's
  * body keeps for its backward pass. These operators keep it in 8 bits, and compute the layers that read it: the

@@ -19,6 +19,11 @@ graph) raises instead of returning gradients of another batch. `weight_grad_fp32
 buffer over to the caller (the pool allocates a new one next time) instead of a bf16 copy; with `dweight_out`
 given, dW is accumulated into that fp32 tensor in place.
 
+    loss = label_loss(hidden, weight, labels, label_smoothing=0.1)     # hard labels; reduction "mean", "sum" or "none"
+
+is the same for one label a token (``labels``): only a few numbers a token live between its two passes, workspaces come from
+torch's allocator for the length of a call.
+
 The layers of a student's body whose backward pass reads activations kept in 8 bits (``body``):
 
     y, x, kept = block_norm(x, branch, post_weight, pre_weight, gate, act8="int8", keep_y=True)
@@ -40,6 +45,7 @@ import torch
 
 from . import binding as B
 from . import body
+from . import labels as L
 
 
 class _NoSecondDerivative(torch.autograd.Function):
@@ -594,3 +600,68 @@ def gated_linear(x, weight, act: str = "silu", act8: Optional[str] = None, recor
         raise TypeError(f"gated_linear: the record is of {(record.T, record.H, record.format)}, the input of {tuple(x.shape)}, act8 {act8}")
     h, h_record = _GatedLinear.apply(x, weight, record, act, act8, keep_h, _recorded(x, weight), bool(sync_status))
     return (h, h_record) if keep_h else h
+
+
+class _LabelLoss(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, hidden, weight, labels, token_weight, args, per_token, single_pass, train, sync_status):
+        T, H, V = hidden.shape[0], hidden.shape[1], weight.shape[0]
+        op = L.LabelLoss(T, H, V, train=train, device=hidden.device, **args)
+        if single_pass and train:
+            loss, dhidden, dweight = op.step(hidden, weight, labels, token_weight)
+            ctx.save_for_backward(dhidden, dweight)
+        else:
+            loss = op.forward(hidden, weight, labels, token_weight)
+            if train:
+                ctx.save_for_backward(hidden, weight, token_weight, op.state)
+        out = op.losses.clone() if per_token else _shaped(loss, torch.Size(()))
+        _settle(op, sync_status)
+        op.workspaces, op.dhidden, op.dweight, op.losses, op.lse, op.loss, op.state, op.token_weight = {}, None, None, None, None, None, None, None
+        ctx.op, ctx.per_token, ctx.done, ctx.sync_status = op, per_token, single_pass and train, sync_status
+        return out
+
+    @staticmethod
+    @_first_derivative_only("label_loss")
+    def backward(ctx, grad):
+        op = ctx.op
+        if ctx.done:                           # the gradients are there, for an upstream gradient of 1
+            dhidden, dweight = ctx.saved_tensors
+            return dhidden * grad.to(dhidden.dtype), dweight * grad.to(dweight.dtype), None, None, None, None, None, None, None
+        hidden, weight, op.token_weight, op.state = ctx.saved_tensors
+        op.args.state = op.state.data_ptr()
+        dhidden, dweight = op.backward(hidden, weight, grad.detach().to(torch.float32).contiguous(), per_token=ctx.per_token)
+        _settle(op, ctx.sync_status)
+        op.workspaces, op.dhidden, op.dweight, op.state, op.token_weight = {}, None, None, None, None
+        return dhidden, dweight, None, None, None, None, None, None, None
+
+
+def _settle(op, sync_status):
+    if sync_status:
+        code, detail = op.status()
+        if code not in (0, -10):               # -10: labels out of range were ignored
+            raise B.KdklError(code, f"device status of a label_loss step, detail {detail}")
+    else:
+        _watch(op.state, "label_loss")
+
+
+def label_loss(hidden, weight, labels, token_weight: Optional[torch.Tensor] = None, *, ignore_index: int = -100,
+               label_smoothing: float = 0.0, z_loss: float = 0.0, temperature: float = 1.0, reduction: str = "mean", chunk: int = 0,
+               single_pass: bool = False, sync_status: bool = False) -> torch.Tensor:
+    """Cross entropy of softmax(hidden @ weight.T / temperature) against labels [...] (int32 or int64), hidden [..., H] and weight
+    [V, H] bf16 (see labels.LabelLoss for the formula). reduction "none" gives the losses [...], 0 at ignored tokens, without
+    token weights. single_pass computes the gradients in the forward call, for an upstream gradient of 1 (three
+    projections for four), and keeps them; another one then scales them, with one more rounding."""
+    if hidden.dtype != torch.bfloat16 or weight.dtype != torch.bfloat16:
+        raise TypeError(f"label_loss: expected bf16, got {hidden.dtype} and {weight.dtype}")
+    if hidden.shape[:-1] != labels.shape or (token_weight is not None and token_weight.shape != labels.shape):
+        raise TypeError(f"label_loss: hidden {tuple(hidden.shape)} beside labels {tuple(labels.shape)}")
+    if reduction not in ("mean", "sum", "none"):
+        raise ValueError(f"label_loss: expected a reduction, got {reduction!r}")
+    if reduction == "none" and (token_weight is not None or single_pass):
+        raise ValueError("label_loss: the losses come without token weights and not in a single pass")
+    args = dict(ignore_index=ignore_index, label_smoothing=label_smoothing, z_loss=z_loss, temperature=temperature, chunk=chunk,
+                reduction="sum" if reduction == "none" else reduction)
+    flat = [None if t is None else t.reshape(-1).contiguous() for t in (labels, token_weight)]
+    out = _LabelLoss.apply(_words16(hidden.reshape(-1, hidden.shape[-1]).contiguous()), _words16(weight.contiguous()), *flat, args,
+                           reduction == "none", bool(single_pass), _recorded(hidden, weight), bool(sync_status))
+    return out.reshape(labels.shape) if reduction == "none" else out

@@ -36,7 +36,8 @@ EXPORTS = [
     "kdkl_block_norm_workspace_bytes", "kdkl_block_norm_forward", "kdkl_block_norm_backward",
     "kdkl_layer_norm_workspace_bytes", "kdkl_layer_norm_forward", "kdkl_layer_norm_backward",
     "kdkl_rotary_table", "kdkl_rotary", "kdkl_gated_linear_workspace_bytes", "kdkl_gated_linear_forward",
-    "kdkl_gated_linear_backward",
+    "kdkl_gated_linear_backward", "kdkl_label_loss_state_bytes", "kdkl_label_loss_workspace_bytes",
+    "kdkl_label_loss_forward", "kdkl_label_loss_backward", "kdkl_label_loss_step",
 ]
 
 FEATURE_MSE, FEATURE_COSINE = 0, 1
@@ -165,6 +166,13 @@ def lib() -> ctypes.CDLL:
     L.kdkl_gated_linear_forward.argtypes = [vp, vp]
     L.kdkl_gated_linear_backward.restype = ctypes.c_int
     L.kdkl_gated_linear_backward.argtypes = [vp, vp]
+    L.kdkl_label_loss_state_bytes.restype = sz
+    L.kdkl_label_loss_state_bytes.argtypes = [i64]
+    L.kdkl_label_loss_workspace_bytes.restype = sz
+    L.kdkl_label_loss_workspace_bytes.argtypes = [i64, i64, i64, i64, i32, i32]
+    for name in ("kdkl_label_loss_forward", "kdkl_label_loss_backward", "kdkl_label_loss_step"):
+        getattr(L, name).restype = ctypes.c_int
+        getattr(L, name).argtypes = [vp, vp]
     L.kdkl_wait_selftest.restype = ctypes.c_int
     L.kdkl_wait_selftest.argtypes = [vp, i64, vp]
     L.kdkl_last_error.restype = ctypes.c_char_p

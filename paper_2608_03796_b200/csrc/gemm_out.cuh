@@ -5,12 +5,12 @@
 
 namespace kdkl {
 
-// out = (part[0] + part[1] + ..., in that order) row_scale [+ out], rounded once. A row's scale of 0 gives zeros. One thread
-// per four columns.
+// out = (part[0] + part[1] + ..., in that order) scale [+ out], rounded once. One thread per four columns.
 template <bool BF16>
 __global__ void __launch_bounds__(256)
-out_join_kernel(const float* part, long long slab, int splits, long long n4, int row_n4, const float* row_scale, void* out,
-                int accumulate) {
+out_join_kernel(const float* part, long long slab, int splits, long long n4, const float* scale, void* out,
+                int accumulate, const int* go) {
+  if (go != nullptr && *go == 0) return;
   const long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x;
   if (i >= n4) return;
   float4 a = reinterpret_cast<const float4*>(part)[i];
@@ -18,10 +18,7 @@ out_join_kernel(const float* part, long long slab, int splits, long long n4, int
     const float4 b = reinterpret_cast<const float4*>(part + s * slab)[i];
     a.x += b.x; a.y += b.y; a.z += b.z; a.w += b.w;
   }
-  if (row_scale != nullptr) {
-    const float r = row_scale[i / row_n4];
-    a = r == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(a.x * r, a.y * r, a.z * r, a.w * r);
-  }
+  if (scale != nullptr) { const float r = *scale; a.x *= r; a.y *= r; a.z *= r; a.w *= r; }
   if (BF16) {
     uint2* o = reinterpret_cast<uint2*>(out) + i;
     if (accumulate) {
@@ -72,7 +69,7 @@ struct OutGemm {
   int* status;
   const int* go;
   const uint8_t* m_live; const uint8_t* k_live;
-  const float* row_scale;             // joined
+  const float* scale;                 // of the product, on the device; or null
 };
 template <bool A_MN>
 inline int launch_out(const OutGemm& o, const DeviceInfo& di, cudaStream_t st) {
@@ -82,7 +79,7 @@ inline int launch_out(const OutGemm& o, const DeviceInfo& di, cudaStream_t st) {
   else      rc = make_tmap_bf16(&ta, o.a, (uint64_t)o.K, (uint64_t)o.M, (uint64_t)o.lda * 2, BK, BM);
   if (rc) return rc;
   if ((rc = make_tmap_bf16(&tb, o.b, (uint64_t)o.N, (uint64_t)o.K, (uint64_t)o.ldb * 2, 64, BK))) return rc;
-  const bool joined = o.plan.splits > 1 || o.row_scale != nullptr || (o.bf16 && o.accumulate);
+  const bool joined = o.plan.splits > 1 || (o.bf16 && o.accumulate);
   GemmParams p;
   memset(&p, 0, sizeof(p));
   p.M = (int)o.M; p.N = (int)o.N; p.K = (int)o.K;
@@ -95,15 +92,23 @@ inline int launch_out(const OutGemm& o, const DeviceInfo& di, cudaStream_t st) {
   else if (o.bf16) rc = make_tmap_out_bf16(&tc, o.out, (uint64_t)o.N, (uint64_t)o.M, (uint64_t)o.N);
   else { rc = make_tmap_out_f32(&tc, o.out, (uint64_t)o.N, (uint64_t)o.M, (uint64_t)o.N); p.accumulate = o.accumulate; }
   if (rc) return rc;
-  if (f32) rc = o.plan.wide ? launch_gemm<EPI_STORE_F32, A_MN, true, true>(ta, tb, tc, p, di, st)
-                            : launch_gemm<EPI_STORE_F32, A_MN, true, false>(ta, tb, tc, p, di, st);
-  else     rc = o.plan.wide ? launch_gemm<EPI_STORE_BF16, A_MN, true, true>(ta, tb, tc, p, di, st)
-                            : launch_gemm<EPI_STORE_BF16, A_MN, true, false>(ta, tb, tc, p, di, st);
+  p.out_scale = joined ? nullptr : o.scale;                // (of parts, when they are joined)
+#define KDKL_OUT(EPI)                                                                 \
+  rc = o.plan.wide ? launch_gemm<EPI, A_MN, true, true>(ta, tb, tc, p, di, st)        \
+                   : launch_gemm<EPI, A_MN, true, false>(ta, tb, tc, p, di, st)
+  if (p.out_scale != nullptr) {
+    if (f32) KDKL_OUT(EPI_STORE_F32_SCALED);
+    else KDKL_OUT(EPI_STORE_BF16_SCALED);
+  } else {
+    if (f32) KDKL_OUT(EPI_STORE_F32);
+    else KDKL_OUT(EPI_STORE_BF16);
+  }
+#undef KDKL_OUT
   if (rc || !joined) return rc;
   const long long n4 = o.M * o.N / 4;
   const unsigned grid = (unsigned)((n4 + 255) / 256);
-  if (o.bf16) out_join_kernel<true><<<grid, 256, 0, st>>>(o.slab, rows * o.N, o.plan.splits, n4, (int)(o.N / 4), o.row_scale, o.out, o.accumulate);
-  else out_join_kernel<false><<<grid, 256, 0, st>>>(o.slab, rows * o.N, o.plan.splits, n4, (int)(o.N / 4), o.row_scale, o.out, o.accumulate);
+  if (o.bf16) out_join_kernel<true><<<grid, 256, 0, st>>>(o.slab, rows * o.N, o.plan.splits, n4, o.scale, o.out, o.accumulate, o.go);
+  else out_join_kernel<false><<<grid, 256, 0, st>>>(o.slab, rows * o.N, o.plan.splits, n4, o.scale, o.out, o.accumulate, o.go);
   KDKL_LAUNCHED("out_join_kernel");
   return KDKL_OK;
 }

@@ -28,9 +28,13 @@
 //                   reads them back instead of projecting again)
 //   EPI_LSE_E       EPI_LSE that also stores the unnormalised exponentials 2^(z log2e / tau - 64) in bf16, for the
 //                   single-pass forward + backward (no second projection: G is made from them once log Z is known)
-//   EPI_LSE_SUM, EPI_LSE_E_SUM
-//                   the same two that also leave each row's sum of raw logits (label smoothing)
+//   EPI_LSE_SUM     EPI_LSE that also leaves each row's sum of raw logits (label smoothing)
+//   EPI_LABEL_E     EPI_LSE_SUM that also stores the exponentials 2^(s - w) in fp16, w the largest s of the row's 32 columns
+//                   at hand, and w itself: for the label loss in one pass. Ten fraction bits where EPI_LSE_E has seven, and
+//                   no limit on the logits' range; what lies 2^-14 below its neighbours' largest loses bits, 2^-25 all
 //   EPI_LABEL_G     backward of the label loss: G = a_t exp(z/tau - logZ) - c_t, less b_t at the label, cast to bf16
+//   EPI_STORE_F32_SCALED, EPI_STORE_BF16_SCALED
+//                   the plain stores of D times one number that lies on the device
 //   EPI_GATED, EPI_GATED_ACT8
 //                   gate and up projection of a gated layer in one tile: of its 256 accumulator columns 128 are gate, from
 //                   the rows of B that the leader stages, and 128 up, from the peer's, of the same 128 features (B is a
@@ -80,7 +84,8 @@ struct GemmCfg {
 };
 
 enum { EPI_STORE_F32 = 0, EPI_STORE_BF16 = 1, EPI_LSE = 2, EPI_DLOGITS = 3, EPI_TOPK = 4, EPI_LSE_E = 5, EPI_LSE_Z = 6,
-       EPI_LSE_SUM = 7, EPI_LSE_E_SUM = 8, EPI_LABEL_G = 9, EPI_GATED = 10, EPI_GATED_ACT8 = 11, EPI_GATED_BACK = 12 };
+       EPI_LSE_SUM = 7, EPI_LABEL_E = 8, EPI_LABEL_G = 9, EPI_GATED = 10, EPI_GATED_ACT8 = 11, EPI_GATED_BACK = 12,
+       EPI_STORE_F32_SCALED = 13, EPI_STORE_BF16_SCALED = 14 };
 
 // EPI_LSE_E stores e = 2^(z log2e / tau - kExpBias) in bf16: representable for scaled logits in about
 // [-62, 190] (bf16 has fp32's exponent range), i.e. far below any weight that matters and far above any sane logit.
@@ -132,10 +137,12 @@ struct GemmParams {
   int* cand_idx;             // [rows, cand_cap]
   float* cand_val;           // [rows, cand_cap] raw logits
   int cand_cap;
-  // EPI_LSE_SUM, EPI_LSE_E_SUM: sums of raw logits, as part_m. EPI_LABEL_G: coefA any sign; coefB at the label (idx_sorted,
-  // nvalid with Ktop = 1)
+  // EPI_LSE_SUM, EPI_LABEL_E: sums of raw logits, as part_m. EPI_LABEL_E: the largest scaled logit of each row and window of
+  // 32 columns. EPI_LABEL_G: coefA any sign; coefB at the label (idx_sorted, nvalid with Ktop = 1)
   float* part_z;             // [n_tiles, part_stride]
+  float* win_max;            // [ceil(N / 32), part_stride]
   const float* coefC;        // [rows]
+  const float* out_scale;    // EPI_STORE_*_SCALED
   // EPI_GATED*: N is the number of features, n_tiles counts tiles of 128 of them
   int act, format;           // kActSilu / kActGelu; kFmtInt8 / kFmtE4M3
   ActRecord rec_gate, rec_up, rec_h;   // EPI_GATED_ACT8; rec_h optional
@@ -553,17 +560,20 @@ gemm_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
     // ------------------------------------------------------------ epilogue (warps 2..5)
     const int lg = warp & 3;                   // TMEM lane group this warp may read
     const int row_in_tile = lg * 32 + lane;
-    constexpr bool kSum = (EPI == EPI_LSE_SUM || EPI == EPI_LSE_E_SUM);
-    constexpr bool kExp = (EPI == EPI_LSE_E || EPI == EPI_LSE_E_SUM);
-    constexpr bool kBf16Out = (EPI == EPI_STORE_BF16 || EPI == EPI_DLOGITS || EPI == EPI_LABEL_G || kExp);
-    constexpr bool kLse = (EPI == EPI_LSE || EPI == EPI_LSE_Z || EPI == EPI_LSE_SUM || kExp);
-    constexpr bool kStore = (EPI == EPI_STORE_F32 || EPI == EPI_LSE_Z || kBf16Out);
+    constexpr bool kSum = (EPI == EPI_LSE_SUM || EPI == EPI_LABEL_E);
+    constexpr bool kScaled = (EPI == EPI_STORE_F32_SCALED || EPI == EPI_STORE_BF16_SCALED);
+    constexpr bool kPlainF32 = (EPI == EPI_STORE_F32 || EPI == EPI_STORE_F32_SCALED);
+    constexpr bool kBf16Out = (EPI == EPI_STORE_BF16 || EPI == EPI_STORE_BF16_SCALED || EPI == EPI_DLOGITS || EPI == EPI_LSE_E || EPI == EPI_LABEL_G ||
+                               EPI == EPI_LABEL_E /* 16 bits, too */);
+    constexpr bool kLse = (EPI == EPI_LSE || EPI == EPI_LSE_E || EPI == EPI_LSE_Z || kSum);
+    constexpr bool kStore = (kPlainF32 || EPI == EPI_LSE_Z || kBf16Out);
+    const float out_scale = kScaled ? *p.out_scale : 1.f;
     uint32_t lt = 0, nbox = 0;
     bool ok = true;
     // Dead row tiles (every token ignored) belong to no work unit. LSE / TOPK have nothing to write for
     // them; a store epilogue writes their part of the output as zeros (nothing when it would add them),
     // for every split's slab, before it turns to the computed tiles.
-    if (mskip && kStore && !(EPI == EPI_STORE_F32 && p.accumulate)) {
+    if (mskip && kStore && !(kPlainF32 && p.accumulate)) {
       const int n_dead = p.m_tiles - m_count;
       const int zero_units = n_dead * p.n_tiles * p.k_splits;
       constexpr int BOX_COLS = kBf16Out ? 64 : 32;
@@ -606,7 +616,7 @@ gemm_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
       float row_b = 0.f, row_off = -INFINITY, row_thr = INFINITY;
       float row_a = 0.f, row_c = 0.f, z_run = 0.f;
       bool row_zero = false;                   // EPI_LSE_E: a row without gradient stores zeros, not exponentials
-      if (kExp) { if (row_ok && p.coefA != nullptr) row_zero = p.coefA[row] == 0.f; }
+      if (EPI == EPI_LSE_E) { if (row_ok && p.coefA != nullptr) row_zero = p.coefA[row] == 0.f; }
       if (EPI == EPI_TOPK) { if (row_ok) row_thr = p.thr[row]; }
       const bool neg_a = EPI == EPI_DLOGITS && p.neg_a != nullptr && *p.neg_a != 0;   // uniform over the call
       if (kLse || EPI == EPI_DLOGITS || EPI == EPI_LABEL_G) {
@@ -650,6 +660,10 @@ gemm_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
         tmem_ld32(taddr + w * 32, r);
         tmem_ld_wait();
         const bool full_w = col0 + 32 <= p.N;
+        if (kScaled) {
+#pragma unroll
+          for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) * out_scale);
+        }
         float e_fac = 0.f;                     // EPI_LSE_E: 2^(running maximum - bias) of this row and window
 
         if (kLse) {
@@ -678,7 +692,7 @@ gemm_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
               for (int j = 0; j < 32; ++j) zs += full_w || col0 + j < p.N ? __uint_as_float(r[j]) : 0.f;
               z_run += zs;
             }
-            if (kExp) {
+            if (EPI == EPI_LSE_E) {
               // keep the window's exponentials (relative to the running maximum) in place of the logits:
               // e = 2^(s - bias) = 2^(s - m_new) * 2^(m_new - bias), one multiply instead of a second ex2
 #pragma unroll
@@ -693,6 +707,16 @@ gemm_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
                 atomicCAS(p.status, 0, -11);               // KDKL_ERR_NONFINITE, with the token
                 atomicCAS(p.status + 1, 0, (int)(p.row_base + row));
               }
+            } else if (EPI == EPI_LABEL_E) {
+              const float w_max = col0 < p.N ? wmax * p.scale_log2 : m_new;   // (a window past the last column has no largest)
+#pragma unroll
+              for (int j = 0; j < 32; ++j) {
+                const float tj = ex2_approx(fmaf(__uint_as_float(r[j]), p.scale_log2, -w_max));
+                acc_s += tj;
+                r[j] = __float_as_uint(tj);
+              }
+              acc_s *= ex2_approx(w_max - m_new);
+              if (col0 < p.N) p.win_max[(long long)(col0 >> 5) * p.part_stride + row] = w_max;
             } else {
 #pragma unroll
               for (int j = 0; j < 32; ++j) acc_s += ex2_approx(fmaf(__uint_as_float(r[j]), p.scale_log2, -m_new));
@@ -739,10 +763,16 @@ gemm_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
               st_shared_v4(srow + ((c ^ (lane & 7)) << 4), r[4 * c], r[4 * c + 1], r[4 * c + 2], r[4 * c + 3]);
           } else {
             uint32_t v[16];
-            if (EPI == EPI_STORE_BF16) {
+            if (EPI == EPI_STORE_BF16 || EPI == EPI_STORE_BF16_SCALED) {
 #pragma unroll
               for (int j = 0; j < 16; ++j) v[j] = pack_bf16x2(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1]));
-            } else if (kExp) {
+            } else if (EPI == EPI_LABEL_E) {
+#pragma unroll
+              for (int j = 0; j < 16; ++j) {
+                const __half2 h = __floats2half2_rn(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1]));
+                v[j] = *reinterpret_cast<const uint32_t*>(&h);
+              }
+            } else if (EPI == EPI_LSE_E) {
               // unnormalised exponentials with a fixed bias: G = A_t * e - b_t p is formed from them later
 #pragma unroll
               for (int j = 0; j < 16; ++j)
@@ -792,7 +822,7 @@ gemm_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
             if (lane == 0 && box_ok) {
               const int cx = kBf16Out ? col0 - 32 : col0;
               const int cy = box_row0 + split * p.split_rows;
-              if (EPI == EPI_STORE_F32 && p.accumulate) tma_reduce_add_2d(&tmC, sbox, cx, cy);
+              if (kPlainF32 && p.accumulate) tma_reduce_add_2d(&tmC, sbox, cx, cy);
               else tma_store_2d(&tmC, sbox, cx, cy);
             }
             if (lane == 0) bulk_commit();
