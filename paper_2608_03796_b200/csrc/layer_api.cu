@@ -13,13 +13,15 @@ using namespace kdkl;
 static bool ln_warp_rows(long long H) { return H <= kLnWarpCols; }
 static bool ln_wide(long long H) { return H > kLnBlockCols; }
 static int ln_threads(long long H) { return (int)((act_codes_pitch(H) / 8 + 31) / 32 * 32); }
+static int ln_rows_threads(long long H) { return (int)((act_codes_pitch(H) / 16 + 31) / 32 * 32); }      // in whole words
 static long long ln_blocks(long long T, long long H, int sm_count) {
   if (ln_wide(H)) return T < 2ll * sm_count ? T : 2ll * sm_count;
   if (ln_warp_rows(H)) {
     const long long need = (T + kLnWarpThreads / 32 - 1) / (kLnWarpThreads / 32), most = 3ll * sm_count;
     return need < most ? need : most;
   }
-  const long long most = (long long)sm_count * (1024 / ln_threads(H));
+  // as many blocks as an SM holds of the backward rows kernel (110 registers a thread)
+  const long long most = (long long)sm_count * (592 / ln_rows_threads(H));
   return T < most ? T : most;
 }
 static long long ln_parts(long long T, long long H, int sm_count) {
@@ -80,6 +82,30 @@ static LnParams ln_params(const kdkl_layer_norm_args* a) {
 static bool ln_vectors_are_words(const kdkl_layer_norm_args* a) {
   return words(a->weight, 0, 1, a->H, a->weight_type) && words(a->bias, 0, 1, a->H, a->weight_type);
 }
+// A rows kernel with as many blocks as fit on the device at once, at most `most`.
+template <auto KERN>
+static int launch_ln_rows(const char* name, int threads, int bytes_a_thread, long long most, const LnParams& p, const DeviceInfo& di,
+                          cudaStream_t st, int* used) {
+  struct Known { bool allowed; int fit[kLnRowsThreads / 32 + 1]; };
+  static Known known[kMaxDevices];
+  Known none = {};
+  Known& k = di.dev >= 0 && di.dev < kMaxDevices ? known[di.dev] : none;
+  const int smem = threads * bytes_a_thread;
+  if (!k.allowed) {                            // (what the widest rows need, once)
+    KDKL_CUDA(cudaFuncSetAttribute(KERN, cudaFuncAttributeMaxDynamicSharedMemorySize, kLnRowsThreads * bytes_a_thread));
+    k.allowed = true;
+  }
+  int fit = k.fit[threads / 32];
+  if (fit == 0) {
+    KDKL_CUDA(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&fit, KERN, threads, smem));
+    if (fit < 1) fit = 1;
+    k.fit[threads / 32] = fit;
+  }
+  const long long held = (long long)di.sm_count * fit;
+  const long long grid = most < held ? most : held;
+  if (used != nullptr) *used = (int)grid;
+  return launch(name, KERN, dim3((unsigned)grid), threads, (size_t)smem, st, p);
+}
 #define KDKL_LN_TYPES(a, X, Y, ...)                                                                    \
   do {                                                                                                 \
     if ((a)->x_type != KDKL_TYPE_F32) KDKL_BY_TYPE16((a)->x_type, X, { using Y = X; __VA_ARGS__; });   \
@@ -121,14 +147,19 @@ int kdkl_layer_norm_forward(const kdkl_layer_norm_args* a, void* cuda_stream) {
   const bool vec = words(a->x, a->ld_x, a->T, a->H, a->x_type) && words(a->y, a->H, a->T, a->H, a->y_type) && ln_vectors_are_words(a);
   const unsigned grid = (unsigned)ln_blocks(a->T, a->H, di.sm_count);
   KDKL_LN_TYPES(a, X, Y, KDKL_BY_BOOL(vec, VEC, {
-    if (ln_wide(a->H))
+    if (ln_wide(a->H)) {
       rc = launch("layer_norm_forward_wide_kernel", layer_norm_forward_wide_kernel<X, Y, VEC>, dim3(grid), kLnWideThreads, 0, st, p);
-    else if (!ln_warp_rows(a->H))
-      rc = launch("layer_norm_forward_kernel", layer_norm_forward_kernel<X, Y, 1, false, VEC>, dim3(grid), ln_threads(a->H), 0, st, p);
-    else if (a->H <= 256)
+    } else if (a->H <= kLnWarpCols / 2) {
       rc = launch("layer_norm_forward_kernel", layer_norm_forward_kernel<X, Y, 1, true, VEC>, dim3(grid), kLnWarpThreads, 0, st, p);
-    else
+    } else if (ln_warp_rows(a->H)) {
       rc = launch("layer_norm_forward_kernel", layer_norm_forward_kernel<X, Y, 2, true, VEC>, dim3(grid), kLnWarpThreads, 0, st, p);
+    } else if constexpr (VEC) {
+      const bool rec = p.x_record.codes != nullptr || p.y_record.codes != nullptr;
+      KDKL_BY_BOOL(rec, REC, rc = (launch_ln_rows<layer_norm_forward_rows_kernel<X, Y, REC>>("layer_norm_forward_rows_kernel",
+          ln_rows_threads(a->H), 2 * kLnAhead * 8 * (int)sizeof(X), a->T, p, di, st, nullptr)));
+    } else {
+      rc = launch("layer_norm_forward_kernel", layer_norm_forward_kernel<X, Y, 1, false, false>, dim3(grid), ln_threads(a->H), 0, st, p);
+    }
   }));
   return rc;
 }
@@ -157,12 +188,21 @@ int kdkl_layer_norm_backward(const kdkl_layer_norm_args* a, void* cuda_stream) {
         if (rc == KDKL_OK && sums)
           rc = launch("layer_norm_columns_kernel", layer_norm_columns_kernel<X, Y, REC, VEC>,
                       dim3((unsigned)((a->H + 2047) / 2048), (unsigned)blocks), 256, 0, st, p);
-      } else if (!ln_warp_rows(a->H)) {
-        rc = launch("layer_norm_backward_kernel", layer_norm_backward_kernel<X, Y, 1, false, REC, VEC>, grid, ln_threads(a->H), 0, st, p);
-      } else if (a->H <= 256) {
+      } else if (a->H <= kLnWarpCols / 2) {
         rc = launch("layer_norm_backward_kernel", layer_norm_backward_kernel<X, Y, 1, true, REC, VEC>, grid, kLnWarpThreads, 0, st, p);
-      } else {
+      } else if (ln_warp_rows(a->H)) {
         rc = launch("layer_norm_backward_kernel", layer_norm_backward_kernel<X, Y, 2, true, REC, VEC>, grid, kLnWarpThreads, 0, st, p);
+      } else if constexpr (VEC) {
+        int used = 0;
+        if constexpr (REC)
+          KDKL_BY_FORMAT(a->format, FMT, rc = (launch_ln_rows<layer_norm_backward_rows_kernel<X, Y, FMT>>("layer_norm_backward_rows_kernel",
+              ln_rows_threads(a->H), 2 * kLnAhead * 8 * (int)sizeof(Y), blocks, p, di, st, &used)));
+        else
+          rc = launch_ln_rows<layer_norm_backward_rows_kernel<X, Y, KDKL_ACT8_NONE>>("layer_norm_backward_rows_kernel", ln_rows_threads(a->H),
+              2 * kLnAhead * 8 * (int)(sizeof(X) + sizeof(Y)), blocks, p, di, st, &used);
+        blocks = used;
+      } else {
+        rc = launch("layer_norm_backward_kernel", layer_norm_backward_kernel<X, Y, 1, false, REC, false>, grid, ln_threads(a->H), 0, st, p);
       }
     })));
     if (rc) return rc;

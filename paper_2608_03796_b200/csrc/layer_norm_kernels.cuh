@@ -163,6 +163,245 @@ layer_norm_forward_kernel(const LnParams p) {
   }
 }
 
+// ------------------------------------------------------------------ rows of a block, in whole words
+// The shape most rows take: a block has a row, a thread two groups of eight columns. A thread's words of the next rows are on
+// their way into places of its own in shared memory (cp.async), kLnAhead rows ahead: no barrier but the one of the sums, and
+// enough bytes in flight to fill the memory's latency (8 KB rows, two or three blocks an SM: 50 to 100 KB). Two
+// values an instruction.
+constexpr int kLnAhead = 3, kLnRowsThreads = 512;
+template <int BYTES> __device__ __forceinline__ void cp_async(uint32_t to, const void* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+  if (BYTES == 32) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + 16), "l"(reinterpret_cast<const char*>(from) + 16) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+template <typename T> __device__ __forceinline__ void shared_pairs(uint32_t at, float2 (&f)[4]) {
+  Raw8<T> r;
+  r.v = ld_shared_v4(at);
+  if constexpr (sizeof(T) == 4) r.w = ld_shared_v4(at + 16);
+  float v[8];
+  raw_to_f32(r, v);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) f[i] = make_float2(v[2 * i], v[2 * i + 1]);
+}
+template <typename T> __device__ __forceinline__ Raw8<T> pairs_to_raw(const float2 (&f)[4]) {
+  float v[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { v[2 * i] = f[i].x; v[2 * i + 1] = f[i].y; }
+  return f32_to_raw<T>(v);
+}
+__device__ __forceinline__ void flatten(const float2 (&f)[4], float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { v[2 * i] = f[i].x; v[2 * i + 1] = f[i].y; }
+}
+__device__ __forceinline__ void affine_pairs(const void* p, int type, int c, int H, float fill, float2 (&f)[4]) {
+  float v[8];
+  if (p != nullptr) load8_typed<true>(p, type, c, H, v);
+  else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = c < H ? fill : 0.f;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) f[i] = make_float2(v[2 * i], v[2 * i + 1]);
+}
+
+template <typename X, typename Y, bool REC>
+__global__ void __launch_bounds__(kLnRowsThreads)
+layer_norm_forward_rows_kernel(const LnParams p) {
+  extern __shared__ uint4 ln_smem[];
+  __shared__ float2 slots[2][32];
+  __shared__ float counts[32];
+  constexpr int XB = 8 * sizeof(X);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  const long long cpitch = act_codes_pitch(p.H), spitch = act_scale_pitch(p.H);
+  const int c[2] = {8 * (int)threadIdx.x, 8 * (int)(threadIdx.x + blockDim.x)};
+  const float n_warp = ln_warp_sum((c[0] < p.H ? 8.f : 0.f) + (c[1] < p.H ? 8.f : 0.f));
+  if (lane == 0) counts[warp] = n_warp;
+  const uint32_t mine = smem_u32(ln_smem) + threadIdx.x * XB, group = blockDim.x * XB;
+  const X* x = reinterpret_cast<const X*>(p.x);
+  auto ask = [&](long long t, int stage) {
+    if (t < p.T) {
+#pragma unroll
+      for (int g = 0; g < 2; ++g)
+        if (c[g] < p.H) cp_async<XB>(mine + (2 * stage + g) * group, x + t * p.ld_x + c[g]);
+    }
+    cp_async_commit();
+  };
+  grid_dependents_launch();
+  grid_dependency_wait();
+#pragma unroll
+  for (int s = 0; s < kLnAhead; ++s) ask(blockIdx.x + (long long)s * gridDim.x, s);
+  float2 w[2][4], b[2][4];
+#pragma unroll
+  for (int g = 0; g < 2; ++g) {
+    affine_pairs(p.weight, p.weight_type, c[g], p.H, 1.f, w[g]);
+    affine_pairs(p.bias, p.weight_type, c[g], p.H, 0.f, b[g]);
+  }
+  const bool in[2] = {c[0] < p.H, c[1] < p.H};
+  int par = 0, stage = 0;
+  for (long long t = blockIdx.x; t < p.T; t += gridDim.x, par ^= 1) {
+    cp_async_wait<kLnAhead - 1>();
+    float2 f[2][4], s2 = both(0.f);
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      if (in[g]) shared_pairs<X>(mine + (2 * stage + g) * group, f[g]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (!in[g]) f[g][i] = both(0.f);
+        s2 = add2(s2, f[g][i]);
+      }
+    }
+    ask(t + (long long)kLnAhead * gridDim.x, stage);       // (into places that this thread alone has just read)
+    if (++stage == kLnAhead) stage = 0;
+    const float s = ln_warp_sum(s2.x + s2.y);
+    const float own = n_warp > 0.f ? s / n_warp : 0.f;
+    float2 q2 = both(0.f);
+#pragma unroll
+    for (int g = 0; g < 2; ++g)
+      if (in[g]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float2 d = add2(f[g][i], both(-own));
+          q2 = fma2(d, d, q2);
+        }
+      }
+    const LnJoin j = ln_join(slots, counts, par, warps, s, ln_warp_sum(q2.x + q2.y), (float)p.H);
+    const float rho = 1.f / sqrtf(fmaf(j.squares, 1.f / (float)p.H, p.eps));
+    if (threadIdx.x == 0 && p.mean != nullptr) { p.mean[t] = j.mean; p.rho[t] = rho; }
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      float2 y[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[i] = fma2(mul2(add2(f[g][i], both(-j.mean)), both(rho)), w[g][i], b[g][i]);
+      const Raw8<Y> out = pairs_to_raw<Y>(y);
+      store_raw8<Y, true>(reinterpret_cast<Y*>(p.y) + t * p.H, c[g], p.H, out);
+      if (REC) {
+        float v[8];
+        flatten(f[g], v);
+        if (p.x_record.codes != nullptr) record_write8<true>(p.format, p.x_record, t, cpitch, spitch, c[g], v);
+        if (p.y_record.codes != nullptr) {                 // of y as it is returned; padding codes are zeros
+          raw_to_f32(out, v);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[i] = in[g] ? v[i] : 0.f;
+          record_write8<true>(p.format, p.y_record, t, cpitch, spitch, c[g], v);
+        }
+      }
+    }
+  }
+  cp_async_wait<0>();
+}
+
+template <typename X, typename Y, int FMT /* -1: from x itself */>
+__global__ void __launch_bounds__(kLnRowsThreads)
+layer_norm_backward_rows_kernel(const LnParams p) {
+  extern __shared__ uint4 ln_smem[];
+  __shared__ float2 slots[2][32];
+  constexpr bool REC = FMT >= 0;
+  constexpr int XB = REC ? 0 : 8 * sizeof(X), YB = 8 * sizeof(Y);
+  const int warps = blockDim.x >> 5;
+  const long long cpitch = act_codes_pitch(p.H), spitch = act_scale_pitch(p.H);
+  const float inv_H = 1.f / (float)p.H;
+  const int c[2] = {8 * (int)threadIdx.x, 8 * (int)(threadIdx.x + blockDim.x)};
+  const bool in[2] = {c[0] < p.H, c[1] < p.H};
+  const uint32_t base = smem_u32(ln_smem), group = blockDim.x * (XB + YB);
+  const uint32_t my_x = base + threadIdx.x * XB, my_y = base + blockDim.x * XB + threadIdx.x * YB;
+  const X* x = reinterpret_cast<const X*>(p.x);
+  const Y* dy = reinterpret_cast<const Y*>(p.dy);
+  uint2 codes[2];
+  uint32_t bytes[2];
+  float mean = 0.f, rho = 0.f;
+  auto ask = [&](long long t, int stage) {
+    if (t < p.T) {
+#pragma unroll
+      for (int g = 0; g < 2; ++g)
+        if (in[g]) {
+          if constexpr (!REC) cp_async<XB>(my_x + (2 * stage + g) * group, x + t * p.ld_x + c[g]);
+          cp_async<YB>(my_y + (2 * stage + g) * group, dy + t * p.ld_dy + c[g]);
+        }
+    }
+    cp_async_commit();
+  };
+  auto ahead = [&](long long t) {                          // the small things, a row ahead in registers
+    if (t < p.T) {
+      mean = p.mean[t]; rho = p.rho[t];
+      if (REC) {
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+          if (in[g]) record_fetch8(p.x_record, t, cpitch, spitch, c[g], codes[g], bytes[g]);
+      }
+    }
+  };
+  grid_dependents_launch();
+  grid_dependency_wait();
+#pragma unroll
+  for (int s = 0; s < kLnAhead; ++s) ask(blockIdx.x + (long long)s * gridDim.x, s);
+  ahead(blockIdx.x);
+  float2 w[2][4], aw[2][4], ab[2][4];
+#pragma unroll
+  for (int g = 0; g < 2; ++g) {
+    affine_pairs(p.weight, p.weight_type, c[g], p.H, 1.f, w[g]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) aw[g][i] = ab[g][i] = both(0.f);
+  }
+  int par = 0, stage = 0;
+  for (long long t = blockIdx.x; t < p.T; t += gridDim.x, par ^= 1) {
+    const float m = mean, r = rho;
+    float2 xh[2][4], d[2][4], s1 = both(0.f), s2 = both(0.f);
+    if (REC) {
+#pragma unroll
+      for (int g = 0; g < 2; ++g)
+        if (in[g]) {
+          float v[8];
+          act_values<REC ? FMT : 0>(codes[g], bytes[g], v);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) xh[g][i] = make_float2(v[2 * i], v[2 * i + 1]);
+        }
+    }
+    ahead(t + gridDim.x);
+    cp_async_wait<kLnAhead - 1>();
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      if (in[g]) {
+        if constexpr (!REC) shared_pairs<X>(my_x + (2 * stage + g) * group, xh[g]);
+        shared_pairs<Y>(my_y + (2 * stage + g) * group, d[g]);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (!in[g]) xh[g][i] = d[g][i] = both(0.f);
+        xh[g][i] = mul2(add2(xh[g][i], both(-m)), both(r));
+        aw[g][i] = fma2(d[g][i], xh[g][i], aw[g][i]);
+        ab[g][i] = add2(ab[g][i], d[g][i]);
+        d[g][i] = mul2(d[g][i], w[g][i]);
+        s1 = add2(s1, d[g][i]);
+        s2 = fma2(d[g][i], xh[g][i], s2);
+      }
+    }
+    ask(t + (long long)kLnAhead * gridDim.x, stage);
+    if (++stage == kLnAhead) stage = 0;
+    const float2 sums = ln_join2(slots, par, warps, ln_warp_sum(s1.x + s1.y), ln_warp_sum(s2.x + s2.y));
+    const float a = -sums.x * inv_H, b = -sums.y * inv_H;
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      float2 o[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] = mul2(add2(d[g][i], fma2(xh[g][i], both(b), both(a))), both(r));
+      store_raw8<X, true>(reinterpret_cast<X*>(p.dx) + t * p.H, c[g], p.H, pairs_to_raw<X>(o));
+    }
+  }
+  cp_async_wait<0>();
+  if (p.part == nullptr) return;
+  float* part = p.part + (long long)blockIdx.x * 2 * p.H;
+#pragma unroll
+  for (int g = 0; g < 2; ++g)
+    if (in[g]) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        *reinterpret_cast<float2*>(part + c[g] + 2 * i) = aw[g][i];
+        *reinterpret_cast<float2*>(part + p.H + c[g] + 2 * i) = ab[g][i];
+      }
+    }
+}
+
 // Rows wider than a block's registers: three looks at the row, the second and third from the caches.
 template <typename X, typename Y, bool VEC>
 __global__ void __launch_bounds__(kLnWideThreads)
