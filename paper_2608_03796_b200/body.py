@@ -530,35 +530,51 @@ class Rotary:
 
     def _run(self, q, k, positions, out, inverse):
         a = kdkl_rotary_args.from_buffer_copy(self.args)     # a call's own: several threads may share a table
-        T = positions.shape[0] if positions.dim() == 1 else -1
-        now = _device()
+        now, dtype, D, T = _device(), q.dtype, self.D, positions.shape[0] if positions.dim() == 1 else -1
         if positions.get_device() != now or positions.dtype not in _POSITIONS or T < 0 or (T > 1 and positions.stride(0) != 1):
             raise TypeError(f"kdkl: positions: expected contiguous int32 or int64 [T] on the current CUDA device, got "
                             f"{positions.dtype} {tuple(positions.shape)} on {positions.device}")
-        outs = out if out is not None else (self._buffer(inverse, 0, q), self._buffer(inverse, 1, k))
-        a.T, a.positions, a.wide_positions, a.inverse = T, positions.data_ptr(), _POSITIONS[positions.dtype], inverse
-        a.type = _lookup(TYPES, q.dtype, "q")
-        a.q_heads, a.q, a.q_token, a.q_head = self._heads(q, T, q.dtype, "q", now)
-        n, a.q_out, a.q_out_token, a.q_out_head = self._heads(outs[0], T, q.dtype, "q's output", now)
-        same = n == a.q_heads
-        if k is not None:
-            a.k_heads, a.k, a.k_token, a.k_head = self._heads(k, T, q.dtype, "k", now)
-            n, a.k_out, a.k_out_token, a.k_out_head = self._heads(outs[1], T, q.dtype, "k's output", now)
-            same = same and n == a.k_heads
+        a.T, a.positions, a.wide_positions, a.inverse, a.type = T, positions.data_ptr(), _POSITIONS[positions.dtype], inverse, \
+            _lookup(TYPES, dtype, "q")
+        heads, a.q, a.q_token, a.q_head = self._heads(q, T, dtype, "q", now)
+        a.q_heads = heads
+        if out is None:
+            y = self._buffer(inverse, 0, q)
+            a.q_out, a.q_out_token, a.q_out_head = y.data_ptr(), heads * D, D
         else:
-            a.k_heads, outs = 0, (outs[0], None)
-        if not same:
-            raise TypeError("kdkl: an output has another number of heads than its input")
+            y = out[0]
+            n, a.q_out, a.q_out_token, a.q_out_head = self._heads(y, T, dtype, "q's output", now)
+            self._same(n, heads)
+        if k is None:
+            a.k_heads, outs, written = 0, (y, None), y
+        else:
+            heads, a.k, a.k_token, a.k_head = self._heads(k, T, dtype, "k", now)
+            a.k_heads = heads
+            if out is None:
+                z = self._buffer(inverse, 1, k)
+                a.k_out, a.k_out_token, a.k_out_head = z.data_ptr(), heads * D, D
+            else:
+                z = out[1]
+                n, a.k_out, a.k_out_token, a.k_out_head = self._heads(z, T, dtype, "k's output", now)
+                self._same(n, heads)
+            outs = written = (y, z)
         B._check(self._call(ctypes.byref(a), _stream(self.at, "rotary table")))
-        _written(outs[0] if k is None else list(outs))
+        _written(written)
         return outs
+
+    @staticmethod
+    def _same(given, heads):
+        if given != heads:
+            raise TypeError(f"kdkl: an output of {given} heads for an input of {heads}")
 
     def _heads(self, t, T, dtype, name, now):
         """(heads, address, distance of tokens, distance of heads)"""
-        if t.get_device() != now or t.dtype is not dtype or t.dim() != 3 or t.shape[0] != T or t.shape[2] != self.D or t.stride(2) != 1:
-            raise TypeError(f"kdkl: {name}: expected {dtype} [{T}, heads, {self.D}] on the current CUDA device, columns contiguous, "
-                            f"got {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}")
-        return t.shape[1], t.data_ptr(), t.stride(0), t.stride(1)
+        if t.dim() == 3:
+            (n, heads, wide), (token, head, along) = t.shape, t.stride()
+            if n == T and wide == self.D and along == 1 and t.dtype is dtype and t.get_device() == now:
+                return heads, t.data_ptr(), token, head
+        raise TypeError(f"kdkl: {name}: expected {dtype} [{T}, heads, {self.D}] on the current CUDA device, columns contiguous, "
+                        f"got {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}")
 
     def _buffer(self, inverse, which, like):
         if like is None:

@@ -18,6 +18,16 @@ gated_rows_kernel(const __nv_bfloat16* x, long long ld_x, const __nv_bfloat16* w
   const int lane = threadIdx.x & 31, f = blockIdx.x * kGatedRowsWarps + (threadIdx.x >> 5), words = H / 8;
   grid_dependents_launch();
   grid_dependency_wait();
+  const uint4* wg = reinterpret_cast<const uint4*>(weight + (long long)f * H);
+  const uint4* wu = reinterpret_cast<const uint4*>(weight + ((long long)F + f) * H);
+  constexpr int U = 4;                                     // words of each row on their way at once, the first before anything else
+  uint4 a[U], b[U];
+  auto ask = [&](int i0) {
+#pragma unroll
+    for (int k = 0; k < U; ++k)
+      if (f < F && i0 + 32 * k < words) { a[k] = wg[i0 + 32 * k]; b[k] = wu[i0 + 32 * k]; }
+  };
+  ask(lane);
   for (int i = threadIdx.x; i < TOKENS * words; i += blockDim.x) {
     const int t = i / words;
     gated_x[i] = t < T ? *reinterpret_cast<const uint4*>(x + t * ld_x + 8 * (i - t * words)) : make_uint4(0u, 0u, 0u, 0u);
@@ -25,20 +35,10 @@ gated_rows_kernel(const __nv_bfloat16* x, long long ld_x, const __nv_bfloat16* w
   if (blockIdx.x == 0 && threadIdx.x < 2) status[threadIdx.x] = 0;     // nothing here can fail
   __syncthreads();
   if (f >= F) return;
-  const uint4* wg = reinterpret_cast<const uint4*>(weight + (long long)f * H);
-  const uint4* wu = reinterpret_cast<const uint4*>(weight + ((long long)F + f) * H);
   float2 g[TOKENS], u[TOKENS];
 #pragma unroll
   for (int t = 0; t < TOKENS; ++t) g[t] = u[t] = make_float2(0.f, 0.f);
-  constexpr int U = 4;                                     // words of each row on their way at once
   for (int i0 = lane; i0 < words; i0 += 32 * U) {
-    uint4 a[U], b[U];
-#pragma unroll
-    for (int k = 0; k < U; ++k) {
-      const int i = i0 + 32 * k;
-      a[k] = i < words ? wg[i] : make_uint4(0u, 0u, 0u, 0u);
-      b[k] = i < words ? wu[i] : make_uint4(0u, 0u, 0u, 0u);
-    }
 #pragma unroll
     for (int k = 0; k < U; ++k) {
       const int i = i0 + 32 * k;
@@ -58,6 +58,7 @@ gated_rows_kernel(const __nv_bfloat16* x, long long ld_x, const __nv_bfloat16* w
         }
       }
     }
+    ask(i0 + 32 * U);
   }
 #pragma unroll
   for (int t = 0; t < TOKENS; ++t) {

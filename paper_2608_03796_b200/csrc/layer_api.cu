@@ -20,7 +20,7 @@ static long long ln_blocks(long long T, long long H, int sm_count) {
     const long long need = (T + kLnWarpThreads / 32 - 1) / (kLnWarpThreads / 32), most = 3ll * sm_count;
     return need < most ? need : most;
   }
-  // as many blocks as an SM holds of the backward rows kernel (110 registers a thread)
+  // as many blocks as an SM holds of the backward rows kernel (up to 128 registers a thread), or of smaller ones a few more
   const long long most = (long long)sm_count * (592 / ln_rows_threads(H));
   return T < most ? T : most;
 }
@@ -155,8 +155,9 @@ int kdkl_layer_norm_forward(const kdkl_layer_norm_args* a, void* cuda_stream) {
       rc = launch("layer_norm_forward_kernel", layer_norm_forward_kernel<X, Y, 2, true, VEC>, dim3(grid), kLnWarpThreads, 0, st, p);
     } else if constexpr (VEC) {
       const bool rec = p.x_record.codes != nullptr || p.y_record.codes != nullptr;
-      KDKL_BY_BOOL(rec, REC, rc = (launch_ln_rows<layer_norm_forward_rows_kernel<X, Y, REC>>("layer_norm_forward_rows_kernel",
-          ln_rows_threads(a->H), 2 * kLnAhead * 8 * (int)sizeof(X), a->T, p, di, st, nullptr)));
+      KDKL_BY_BOOL(rec, REC, KDKL_BY_BOOL(a->H % 512 == 0, FULL,
+        rc = (launch_ln_rows<layer_norm_forward_rows_kernel<X, Y, REC, FULL>>("layer_norm_forward_rows_kernel", ln_rows_threads(a->H),
+            2 * kLnAhead * 8 * (int)sizeof(X), a->T, p, di, st, nullptr))));
     } else {
       rc = launch("layer_norm_forward_kernel", layer_norm_forward_kernel<X, Y, 1, false, false>, dim3(grid), ln_threads(a->H), 0, st, p);
     }
@@ -194,12 +195,14 @@ int kdkl_layer_norm_backward(const kdkl_layer_norm_args* a, void* cuda_stream) {
         rc = launch("layer_norm_backward_kernel", layer_norm_backward_kernel<X, Y, 2, true, REC, VEC>, grid, kLnWarpThreads, 0, st, p);
       } else if constexpr (VEC) {
         int used = 0;
-        if constexpr (REC)
-          KDKL_BY_FORMAT(a->format, FMT, rc = (launch_ln_rows<layer_norm_backward_rows_kernel<X, Y, FMT>>("layer_norm_backward_rows_kernel",
-              ln_rows_threads(a->H), 2 * kLnAhead * 8 * (int)sizeof(Y), blocks, p, di, st, &used)));
-        else
-          rc = launch_ln_rows<layer_norm_backward_rows_kernel<X, Y, KDKL_ACT8_NONE>>("layer_norm_backward_rows_kernel", ln_rows_threads(a->H),
-              2 * kLnAhead * 8 * (int)(sizeof(X) + sizeof(Y)), blocks, p, di, st, &used);
+        KDKL_BY_BOOL(a->H % 512 == 0, FULL, {
+          if constexpr (REC)
+            KDKL_BY_FORMAT(a->format, FMT, rc = (launch_ln_rows<layer_norm_backward_rows_kernel<X, Y, FMT, FULL>>("layer_norm_backward_rows_kernel",
+                ln_rows_threads(a->H), 2 * kLnAhead * 8 * (int)sizeof(Y), blocks, p, di, st, &used)));
+          else
+            rc = (launch_ln_rows<layer_norm_backward_rows_kernel<X, Y, KDKL_ACT8_NONE, FULL>>("layer_norm_backward_rows_kernel", ln_rows_threads(a->H),
+                2 * kLnAhead * 8 * (int)(sizeof(X) + sizeof(Y)), blocks, p, di, st, &used));
+        });
         blocks = used;
       } else {
         rc = launch("layer_norm_backward_kernel", layer_norm_backward_kernel<X, Y, 1, false, REC, false>, grid, ln_threads(a->H), 0, st, p);

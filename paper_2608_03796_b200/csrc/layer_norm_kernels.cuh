@@ -190,10 +190,6 @@ template <typename T> __device__ __forceinline__ Raw8<T> pairs_to_raw(const floa
   for (int i = 0; i < 4; ++i) { v[2 * i] = f[i].x; v[2 * i + 1] = f[i].y; }
   return f32_to_raw<T>(v);
 }
-__device__ __forceinline__ void flatten(const float2 (&f)[4], float (&v)[8]) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) { v[2 * i] = f[i].x; v[2 * i + 1] = f[i].y; }
-}
 __device__ __forceinline__ void affine_pairs(const void* p, int type, int c, int H, float fill, float2 (&f)[4]) {
   float v[8];
   if (p != nullptr) load8_typed<true>(p, type, c, H, v);
@@ -205,85 +201,126 @@ __device__ __forceinline__ void affine_pairs(const void* p, int type, int c, int
   for (int i = 0; i < 4; ++i) f[i] = make_float2(v[2 * i], v[2 * i + 1]);
 }
 
-template <typename X, typename Y, bool REC>
+// Sums over a block, known to every thread: a warp's go to its slot, and behind the barrier every thread adds up the slots,
+// eight at a time in whole words, in their order. Slots of absent warps stay zeros (ln_slots_clear). Two joins that
+// follow one another use different slots, which spares a second barrier.
+struct __align__(16) LnSlots { float2 two[32]; float one[32]; };
+__device__ __forceinline__ void ln_slots_clear(LnSlots& s) {
+  if (threadIdx.x < 32) { s.two[threadIdx.x] = both(0.f); s.one[threadIdx.x] = 0.f; }
+}
+__device__ __forceinline__ float2 low2(const float4& v) { return make_float2(v.x, v.y); }
+__device__ __forceinline__ float2 high2(const float4& v) { return make_float2(v.z, v.w); }
+__device__ __forceinline__ float ln_block_sum(LnSlots& s, int warps, float v) {
+  v = ln_warp_sum(v);
+  if ((threadIdx.x & 31) == 0) s.one[threadIdx.x >> 5] = v;
+  __syncthreads();
+  const float4* q = reinterpret_cast<const float4*>(s.one);
+  float2 t = add2(add2(low2(q[0]), high2(q[0])), add2(low2(q[1]), high2(q[1])));
+  for (int i = 8; i < warps; i += 8, q += 2) t = add2(t, add2(add2(low2(q[2]), high2(q[2])), add2(low2(q[3]), high2(q[3]))));
+  return t.x + t.y;
+}
+__device__ __forceinline__ float2 ln_block_sum2(LnSlots& s, int warps, float a, float b) {
+  a = ln_warp_sum(a); b = ln_warp_sum(b);
+  if ((threadIdx.x & 31) == 0) s.two[threadIdx.x >> 5] = make_float2(a, b);
+  __syncthreads();
+  const float4* q = reinterpret_cast<const float4*>(s.two);
+  float2 t = both(0.f);
+  for (int i = 0; i < warps; i += 8, q += 4)
+    t = add2(t, add2(add2(add2(low2(q[0]), high2(q[0])), add2(low2(q[1]), high2(q[1]))), add2(add2(low2(q[2]), high2(q[2])), add2(low2(q[3]), high2(q[3])))));
+  return t;
+}
+// s / n with n's reciprocal at hand: the remainder of the first guess is exact, so equal values have themselves for their mean
+__device__ __forceinline__ float ln_quotient(float s, float n, float inv_n) {
+  const float m = s * inv_n;
+  return fmaf(fmaf(-m, n, s), inv_n, m);
+}
+
+// FULL: every thread's columns exist (H = 16 x threads); otherwise the places of those that do not hold zeros throughout.
+template <typename X, typename Y, bool REC, bool FULL>
 __global__ void __launch_bounds__(kLnRowsThreads)
 layer_norm_forward_rows_kernel(const LnParams p) {
   extern __shared__ uint4 ln_smem[];
-  __shared__ float2 slots[2][32];
-  __shared__ float counts[32];
+  __shared__ LnSlots first, second;
   constexpr int XB = 8 * sizeof(X);
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  const int warps = blockDim.x >> 5, far = 8 * blockDim.x, T = (int)p.T;
   const long long cpitch = act_codes_pitch(p.H), spitch = act_scale_pitch(p.H);
-  const int c[2] = {8 * (int)threadIdx.x, 8 * (int)(threadIdx.x + blockDim.x)};
-  const float n_warp = ln_warp_sum((c[0] < p.H ? 8.f : 0.f) + (c[1] < p.H ? 8.f : 0.f));
-  if (lane == 0) counts[warp] = n_warp;
+  const float H = (float)p.H, inv_H = 1.f / H;
+  const int c = 8 * (int)threadIdx.x;                      // and c + far
+  const bool in[2] = {FULL || c < p.H, FULL || c + far < p.H};
   const uint32_t mine = smem_u32(ln_smem) + threadIdx.x * XB, group = blockDim.x * XB;
-  const X* x = reinterpret_cast<const X*>(p.x);
-  auto ask = [&](long long t, int stage) {
-    if (t < p.T) {
+  ln_slots_clear(first); ln_slots_clear(second);
 #pragma unroll
-      for (int g = 0; g < 2; ++g)
-        if (c[g] < p.H) cp_async<XB>(mine + (2 * stage + g) * group, x + t * p.ld_x + c[g]);
+  for (int i = 0; i < 2 * kLnAhead; ++i)
+    if (!in[i & 1]) {
+#pragma unroll
+      for (int k = 0; k < XB; k += 16) st_shared_v4(mine + i * group + k, 0u, 0u, 0u, 0u);
+    }
+  __syncthreads();
+  const X* next = reinterpret_cast<const X*>(p.x) + blockIdx.x * p.ld_x + c;
+  const long long step = gridDim.x * p.ld_x, out_step = (long long)gridDim.x * p.H;
+  int asked = blockIdx.x;
+  auto ask = [&](int stage) {
+    if (asked < T) {
+      if (in[0]) cp_async<XB>(mine + 2 * stage * group, next);
+      if (in[1]) cp_async<XB>(mine + (2 * stage + 1) * group, next + far);
     }
     cp_async_commit();
+    next += step; asked += gridDim.x;
   };
   grid_dependents_launch();
   grid_dependency_wait();
 #pragma unroll
-  for (int s = 0; s < kLnAhead; ++s) ask(blockIdx.x + (long long)s * gridDim.x, s);
+  for (int s = 0; s < kLnAhead; ++s) ask(s);
   float2 w[2][4], b[2][4];
 #pragma unroll
   for (int g = 0; g < 2; ++g) {
-    affine_pairs(p.weight, p.weight_type, c[g], p.H, 1.f, w[g]);
-    affine_pairs(p.bias, p.weight_type, c[g], p.H, 0.f, b[g]);
+    affine_pairs(p.weight, p.weight_type, c + g * far, p.H, 1.f, w[g]);
+    affine_pairs(p.bias, p.weight_type, c + g * far, p.H, 0.f, b[g]);
   }
-  const bool in[2] = {c[0] < p.H, c[1] < p.H};
-  int par = 0, stage = 0;
-  for (long long t = blockIdx.x; t < p.T; t += gridDim.x, par ^= 1) {
+  Y* out = reinterpret_cast<Y*>(p.y) + (long long)blockIdx.x * p.H;
+  int stage = 0;
+  for (int t = blockIdx.x; t < T; t += gridDim.x, out += out_step) {
     cp_async_wait<kLnAhead - 1>();
-    float2 f[2][4], s2 = both(0.f);
+    float2 f[2][4], sum = both(0.f), squares = both(0.f);
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
-      if (in[g]) shared_pairs<X>(mine + (2 * stage + g) * group, f[g]);
+      shared_pairs<X>(mine + (2 * stage + g) * group, f[g]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum = add2(sum, f[g][i]);
+    }
+    ask(stage);                                            // (into places that this thread alone has just read)
+    if (++stage == kLnAhead) stage = 0;
+    const float mean = ln_quotient(ln_block_sum(first, warps, sum.x + sum.y), H, inv_H);
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      const float2 off = both(in[g] ? -mean : 0.f);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        if (!in[g]) f[g][i] = both(0.f);
-        s2 = add2(s2, f[g][i]);
+        f[g][i] = add2(f[g][i], off);
+        squares = fma2(f[g][i], f[g][i], squares);
       }
     }
-    ask(t + (long long)kLnAhead * gridDim.x, stage);       // (into places that this thread alone has just read)
-    if (++stage == kLnAhead) stage = 0;
-    const float s = ln_warp_sum(s2.x + s2.y);
-    const float own = n_warp > 0.f ? s / n_warp : 0.f;
-    float2 q2 = both(0.f);
-#pragma unroll
-    for (int g = 0; g < 2; ++g)
-      if (in[g]) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float2 d = add2(f[g][i], both(-own));
-          q2 = fma2(d, d, q2);
-        }
-      }
-    const LnJoin j = ln_join(slots, counts, par, warps, s, ln_warp_sum(q2.x + q2.y), (float)p.H);
-    const float rho = 1.f / sqrtf(fmaf(j.squares, 1.f / (float)p.H, p.eps));
-    if (threadIdx.x == 0 && p.mean != nullptr) { p.mean[t] = j.mean; p.rho[t] = rho; }
+    const float rho = rsqrtf(fmaf(ln_block_sum(second, warps, squares.x + squares.y), inv_H, p.eps));
+    if (threadIdx.x == 0 && p.mean != nullptr) { p.mean[t] = mean; p.rho[t] = rho; }
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
+      const int at = c + g * far;
       float2 y[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) y[i] = fma2(mul2(add2(f[g][i], both(-j.mean)), both(rho)), w[g][i], b[g][i]);
-      const Raw8<Y> out = pairs_to_raw<Y>(y);
-      store_raw8<Y, true>(reinterpret_cast<Y*>(p.y) + t * p.H, c[g], p.H, out);
+      for (int i = 0; i < 4; ++i) y[i] = fma2(mul2(f[g][i], both(rho)), w[g][i], b[g][i]);
+      const Raw8<Y> raw = pairs_to_raw<Y>(y);
+      if (in[g]) store_raw8<Y, true>(out, at, at + 1, raw);
       if (REC) {
         float v[8];
-        flatten(f[g], v);
-        if (p.x_record.codes != nullptr) record_write8<true>(p.format, p.x_record, t, cpitch, spitch, c[g], v);
+        if (p.x_record.codes != nullptr) {                 // x once more, from where it came
+          load8<X, true>(reinterpret_cast<const X*>(p.x) + t * p.ld_x, at, p.H, v);
+          record_write8<true>(p.format, p.x_record, t, cpitch, spitch, at, v);
+        }
         if (p.y_record.codes != nullptr) {                 // of y as it is returned; padding codes are zeros
-          raw_to_f32(out, v);
+          raw_to_f32(raw, v);
 #pragma unroll
           for (int i = 0; i < 8; ++i) v[i] = in[g] ? v[i] : 0.f;
-          record_write8<true>(p.format, p.y_record, t, cpitch, spitch, c[g], v);
+          record_write8<true>(p.format, p.y_record, t, cpitch, spitch, at, v);
         }
       }
     }
@@ -291,84 +328,97 @@ layer_norm_forward_rows_kernel(const LnParams p) {
   cp_async_wait<0>();
 }
 
-template <typename X, typename Y, int FMT /* -1: from x itself */>
+template <typename X, typename Y, int FMT /* -1: from x itself */, bool FULL>
 __global__ void __launch_bounds__(kLnRowsThreads)
 layer_norm_backward_rows_kernel(const LnParams p) {
   extern __shared__ uint4 ln_smem[];
-  __shared__ float2 slots[2][32];
+  __shared__ LnSlots even, odd;
   constexpr bool REC = FMT >= 0;
   constexpr int XB = REC ? 0 : 8 * sizeof(X), YB = 8 * sizeof(Y);
-  const int warps = blockDim.x >> 5;
+  const int warps = blockDim.x >> 5, far = 8 * blockDim.x, T = (int)p.T;
   const long long cpitch = act_codes_pitch(p.H), spitch = act_scale_pitch(p.H);
   const float inv_H = 1.f / (float)p.H;
-  const int c[2] = {8 * (int)threadIdx.x, 8 * (int)(threadIdx.x + blockDim.x)};
-  const bool in[2] = {c[0] < p.H, c[1] < p.H};
+  const int c = 8 * (int)threadIdx.x;
+  const bool in[2] = {FULL || c < p.H, FULL || c + far < p.H};
   const uint32_t base = smem_u32(ln_smem), group = blockDim.x * (XB + YB);
   const uint32_t my_x = base + threadIdx.x * XB, my_y = base + blockDim.x * XB + threadIdx.x * YB;
-  const X* x = reinterpret_cast<const X*>(p.x);
-  const Y* dy = reinterpret_cast<const Y*>(p.dy);
-  uint2 codes[2];
-  uint32_t bytes[2];
-  float mean = 0.f, rho = 0.f;
-  auto ask = [&](long long t, int stage) {
-    if (t < p.T) {
+  ln_slots_clear(even); ln_slots_clear(odd);
+#pragma unroll
+  for (int i = 0; i < 2 * kLnAhead; ++i)
+    if (!in[i & 1]) {
+#pragma unroll
+      for (int k = 0; k < XB; k += 16) st_shared_v4(my_x + i * group + k, 0u, 0u, 0u, 0u);
+#pragma unroll
+      for (int k = 0; k < YB; k += 16) st_shared_v4(my_y + i * group + k, 0u, 0u, 0u, 0u);
+    }
+  __syncthreads();
+  const X* next_x = reinterpret_cast<const X*>(p.x) + blockIdx.x * p.ld_x + c;
+  const Y* next_y = reinterpret_cast<const Y*>(p.dy) + blockIdx.x * p.ld_dy + c;
+  const long long step_x = gridDim.x * p.ld_x, step_y = gridDim.x * p.ld_dy, out_step = (long long)gridDim.x * p.H;
+  int asked = blockIdx.x;
+  auto ask = [&](int stage) {
+    if (asked < T) {
 #pragma unroll
       for (int g = 0; g < 2; ++g)
         if (in[g]) {
-          if constexpr (!REC) cp_async<XB>(my_x + (2 * stage + g) * group, x + t * p.ld_x + c[g]);
-          cp_async<YB>(my_y + (2 * stage + g) * group, dy + t * p.ld_dy + c[g]);
+          if constexpr (!REC) cp_async<XB>(my_x + (2 * stage + g) * group, next_x + g * far);
+          cp_async<YB>(my_y + (2 * stage + g) * group, next_y + g * far);
         }
     }
     cp_async_commit();
+    if constexpr (!REC) next_x += step_x;
+    next_y += step_y; asked += gridDim.x;
   };
-  auto ahead = [&](long long t) {                          // the small things, a row ahead in registers
-    if (t < p.T) {
+  // the small things of the next row in registers
+  uint2 codes[2] = {make_uint2(0u, 0u), make_uint2(0u, 0u)};
+  uint32_t bytes[2] = {1u, 1u};
+  float mean = 0.f, rho = 0.f;
+  auto ahead = [&](int t) {
+    if (t < T) {
       mean = p.mean[t]; rho = p.rho[t];
       if (REC) {
 #pragma unroll
         for (int g = 0; g < 2; ++g)
-          if (in[g]) record_fetch8(p.x_record, t, cpitch, spitch, c[g], codes[g], bytes[g]);
+          if (in[g]) record_fetch8(p.x_record, t, cpitch, spitch, c + g * far, codes[g], bytes[g]);
       }
     }
   };
   grid_dependents_launch();
   grid_dependency_wait();
 #pragma unroll
-  for (int s = 0; s < kLnAhead; ++s) ask(blockIdx.x + (long long)s * gridDim.x, s);
+  for (int s = 0; s < kLnAhead; ++s) ask(s);
   ahead(blockIdx.x);
   float2 w[2][4], aw[2][4], ab[2][4];
 #pragma unroll
   for (int g = 0; g < 2; ++g) {
-    affine_pairs(p.weight, p.weight_type, c[g], p.H, 1.f, w[g]);
+    affine_pairs(p.weight, p.weight_type, c + g * far, p.H, 1.f, w[g]);
 #pragma unroll
     for (int i = 0; i < 4; ++i) aw[g][i] = ab[g][i] = both(0.f);
   }
-  int par = 0, stage = 0;
-  for (long long t = blockIdx.x; t < p.T; t += gridDim.x, par ^= 1) {
-    const float m = mean, r = rho;
+  X* out = reinterpret_cast<X*>(p.dx) + (long long)blockIdx.x * p.H;
+  int stage = 0;
+  bool second = false;
+  for (int t = blockIdx.x; t < T; t += gridDim.x, out += out_step) {
+    const float2 off = both(-mean), r = both(rho);
     float2 xh[2][4], d[2][4], s1 = both(0.f), s2 = both(0.f);
-    if (REC) {
+    if constexpr (REC) {
 #pragma unroll
-      for (int g = 0; g < 2; ++g)
-        if (in[g]) {
-          float v[8];
-          act_values<REC ? FMT : 0>(codes[g], bytes[g], v);
+      for (int g = 0; g < 2; ++g) {
+        float v[8];
+        act_values<REC ? FMT : 0>(codes[g], bytes[g], v);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) xh[g][i] = make_float2(v[2 * i], v[2 * i + 1]);
-        }
+        for (int i = 0; i < 4; ++i) xh[g][i] = make_float2(v[2 * i], v[2 * i + 1]);
+      }
     }
-    ahead(t + gridDim.x);
     cp_async_wait<kLnAhead - 1>();
+    ahead(t + gridDim.x);
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
-      if (in[g]) {
-        if constexpr (!REC) shared_pairs<X>(my_x + (2 * stage + g) * group, xh[g]);
-        shared_pairs<Y>(my_y + (2 * stage + g) * group, d[g]);
-      }
+      if constexpr (!REC) shared_pairs<X>(my_x + (2 * stage + g) * group, xh[g]);
+      shared_pairs<Y>(my_y + (2 * stage + g) * group, d[g]);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        if (!in[g]) xh[g][i] = d[g][i] = both(0.f);
-        xh[g][i] = mul2(add2(xh[g][i], both(-m)), both(r));
+        xh[g][i] = mul2(add2(xh[g][i], off), r);
         aw[g][i] = fma2(d[g][i], xh[g][i], aw[g][i]);
         ab[g][i] = add2(ab[g][i], d[g][i]);
         d[g][i] = mul2(d[g][i], w[g][i]);
@@ -376,28 +426,29 @@ layer_norm_backward_rows_kernel(const LnParams p) {
         s2 = fma2(d[g][i], xh[g][i], s2);
       }
     }
-    ask(t + (long long)kLnAhead * gridDim.x, stage);
+    ask(stage);
     if (++stage == kLnAhead) stage = 0;
-    const float2 sums = ln_join2(slots, par, warps, ln_warp_sum(s1.x + s1.y), ln_warp_sum(s2.x + s2.y));
-    const float a = -sums.x * inv_H, b = -sums.y * inv_H;
+    const float2 sums = ln_block_sum2(second ? odd : even, warps, s1.x + s1.y, s2.x + s2.y);
+    second = !second;
+    const float2 a = both(-sums.x * inv_H), b = both(-sums.y * inv_H);
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
-      float2 o[4];
+      const int at = c + g * far;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) o[i] = mul2(add2(d[g][i], fma2(xh[g][i], both(b), both(a))), both(r));
-      store_raw8<X, true>(reinterpret_cast<X*>(p.dx) + t * p.H, c[g], p.H, pairs_to_raw<X>(o));
+      for (int i = 0; i < 4; ++i) d[g][i] = mul2(add2(d[g][i], fma2(xh[g][i], b, a)), r);
+      if (in[g]) store_raw8<X, true>(out, at, at + 1, pairs_to_raw<X>(d[g]));
     }
   }
   cp_async_wait<0>();
   if (p.part == nullptr) return;
-  float* part = p.part + (long long)blockIdx.x * 2 * p.H;
+  float* part = p.part + (long long)blockIdx.x * 2 * p.H + c;
 #pragma unroll
   for (int g = 0; g < 2; ++g)
     if (in[g]) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        *reinterpret_cast<float2*>(part + c[g] + 2 * i) = aw[g][i];
-        *reinterpret_cast<float2*>(part + p.H + c[g] + 2 * i) = ab[g][i];
+        *reinterpret_cast<float2*>(part + g * far + 2 * i) = aw[g][i];
+        *reinterpret_cast<float2*>(part + p.H + g * far + 2 * i) = ab[g][i];
       }
     }
 }
@@ -603,8 +654,10 @@ layer_norm_reduce_kernel(const float* part, long long parts, int H, void* dweigh
   grid_dependents_launch();
   grid_dependency_wait();
   float s = 0.f;
-  if (col < H)
+  if (col < H) {
+#pragma unroll 4
     for (long long r = warp; r < parts; r += 32) s += part[(r * 2 + which) * H + col];
+  }
   sums[warp][lane] = s;
   __syncthreads();
   if (warp != 0) return;
