@@ -630,7 +630,7 @@ int kdkl_rotary(const kdkl_rotary_args* args, void* cuda_stream);
  *                      was returned); the weight gradient then reads a record of x, which whoever made x left
  * backward: dgate = dh up act'(gate), dup = dh act(gate), rounded to bf16 into dgate_up [T, 2 F]; dx = dgate_up weight (bf16);
  * dweight (= or, with accumulate, +=) dgate_up^T x, of dweight_type. dx and dweight may be NULL. T = 0: dweight becomes
- * zeros. Bitwise reproducible. Up to 8 tokens without a format do without tensor cores (serving's single tokens).
+ * zeros. Bitwise reproducible. Up to 128 tokens go by kernels for few tokens (serving's), bound by the weights' bytes.
  * workspace: 256 bytes forward, kdkl_gated_linear_workspace_bytes() backward, 256-byte aligned; its first words are a status
  * block readable with kdkl_status (KDKL_ERR_TIMEOUT), that of the last call.
  * One struct serves both calls; a call reads the fields it needs. */

@@ -2,7 +2,7 @@
 #include <string.h>
 
 #include "body_host.cuh"
-#include "gated_linear_kernels.cuh"
+#include "gated_few_kernels.cuh"
 #include "gemm_out.cuh"
 
 using namespace kdkl;
@@ -73,12 +73,62 @@ static int gated_product(const kdkl_gated_linear_args* a, GemmParams& p, const C
   return launch_gemm<EPI, false, false>(ta, tb, tc, p, di, st);
 }
 
-template <int TOKENS>
+// Up to 128 tokens. A cluster of as many CTAs a tile (1, 2 or 4) as bring the SMs to work, while each keeps eight blocks of the
+// contraction; one CTA an SM where there are no more CTAs than SMs, else two.
+template <int N, int MODE>
+static int gated_few_launch(const kdkl_gated_linear_args* a, const CUtensorMap& tw, const CUtensorMap& tx, FewParams p, const DeviceInfo& di,
+                            cudaStream_t st) {
+  auto kern = gated_few_kernel<N, MODE>;
+  constexpr int kMost = 208 * 1024;
+  static bool attr_set[kMaxDevices];
+  if (di.dev < 0 || di.dev >= kMaxDevices || !attr_set[di.dev]) {
+    KDKL_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost));
+    if (di.dev >= 0 && di.dev < kMaxDevices) attr_set[di.dev] = true;
+  }
+  const int tiles = (int)((a->F + kFewFeatures - 1) / kFewFeatures), blocks = (int)((a->H + BK - 1) / BK);
+  p.cluster = 1;
+  while (p.cluster < 4 && tiles * p.cluster * 10 < di.sm_count * 9 && blocks >= 16 * p.cluster) p.cluster *= 2;
+  while (p.cluster > 1 && (blocks + p.cluster - 1) / p.cluster * (p.cluster - 1) >= blocks) p.cluster /= 2;   // (nobody without a block)
+  const int room = (tiles * p.cluster <= di.sm_count ? kMost : kMost / 2) - 1024;
+  p.stages = room / few_stage_bytes(N);
+  if (p.stages > kFewMaxStages) p.stages = kFewMaxStages;
+  // (the ring is also where the sums change hands: 512 bytes a token)
+  return launch_cluster(p.cluster, "gated_few_kernel", kern, dim3((unsigned)(tiles * p.cluster)), kFewThreads,
+                        (size_t)p.stages * few_stage_bytes(N) + 1024, st, tw, tx, p);
+}
+template <int MODE>
+static int gated_few(const kdkl_gated_linear_args* a, const DeviceInfo& di, cudaStream_t st) {
+  const int N = a->T <= 16 ? 16 : a->T <= 32 ? 32 : a->T <= 64 ? 64 : 128;
+  CUtensorMap tw, tx;
+  int rc;
+  if ((rc = map_halves(&tw, a->weight, (uint64_t)a->H, (uint64_t)a->F, (uint64_t)a->H * 2, (uint64_t)a->F * a->H * 2, kFewFeatures))) return rc;
+  if ((rc = make_tmap_bf16(&tx, a->x, (uint64_t)a->H, (uint64_t)a->T, (uint64_t)(a->T > 1 ? a->ld_x : a->H) * 2, BK, (uint32_t)N))) return rc;
+  FewParams p;
+  memset(&p, 0, sizeof(p));
+  p.T = (int)a->T; p.H = (int)a->H; p.F = (int)a->F; p.act = a->act; p.format = a->format;
+  p.status = at<int>(a->workspace, 0);
+  if (MODE == kFewBack) {
+    p.dh = reinterpret_cast<const __nv_bfloat16*>(a->dh); p.ld_dh = a->ld_dh;
+    p.dgate_up = reinterpret_cast<__nv_bfloat16*>(a->dgate_up);
+  } else {
+    p.h = reinterpret_cast<__nv_bfloat16*>(a->h); p.ld_h = a->ld_h;
+  }
+  if (MODE == kFewAct8) {
+    p.rec_gate = record_at(a->gate_record, a->T, a->F); p.rec_up = record_at(a->up_record, a->T, a->F);
+    p.rec_h = record_at(a->h_record, a->T, a->F);
+  }
+  if (N == 16) return gated_few_launch<16, MODE>(a, tw, tx, p, di, st);
+  if (N == 32) return gated_few_launch<32, MODE>(a, tw, tx, p, di, st);
+  if (N == 64) return gated_few_launch<64, MODE>(a, tw, tx, p, di, st);
+  return gated_few_launch<128, MODE>(a, tw, tx, p, di, st);
+}
+
+template <int TOKENS, int U>
 static int gated_rows(const kdkl_gated_linear_args* a, cudaStream_t st) {
   int rc = KDKL_OK;
   KDKL_BY_BOOL(a->act == KDKL_GATED_GELU, GELU,
-    rc = launch("gated_rows_kernel", gated_rows_kernel<TOKENS, GELU ? kActGelu : kActSilu>,
-                dim3((unsigned)((a->F + kGatedRowsWarps - 1) / kGatedRowsWarps)), 32 * kGatedRowsWarps, (size_t)TOKENS * a->H * 2, st,
+    rc = launch("gated_rows_kernel", gated_rows_kernel<TOKENS, GELU ? kActGelu : kActSilu, U>,
+                dim3((unsigned)((a->F + kGatedRowsWarps - 1) / kGatedRowsWarps)), 32 * kGatedRowsWarps, 0, st,
                 reinterpret_cast<const __nv_bfloat16*>(a->x), a->ld_x, reinterpret_cast<const __nv_bfloat16*>(a->weight), (int)a->T,
                 (int)a->H, (int)a->F, reinterpret_cast<__nv_bfloat16*>(a->h), a->ld_h, at<int>(a->workspace, 0)));
   return rc;
@@ -111,14 +161,10 @@ int kdkl_gated_linear_forward(const kdkl_gated_linear_args* a, void* cuda_stream
   DeviceInfo di;
   if ((rc = need_b200(&di))) return rc;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
-  // A few tokens, nothing kept: bound by the weights' way through memory, without tensor cores. (A block holds the tokens in
-  // shared memory: up to 48 KB of them.)
-  if (!keep && a->T <= kGatedRowsTokens && (a->T <= 1 ? 1 : a->T <= 2 ? 2 : a->T <= 4 ? 4 : 8) * a->H * 2 <= 48 * 1024) {
-    if (a->T <= 1) return gated_rows<1>(a, st);
-    if (a->T <= 2) return gated_rows<2>(a, st);
-    if (a->T <= 4) return gated_rows<4>(a, st);
-    return gated_rows<8>(a, st);
-  }
+  // One token, or two beside small weights, and nothing kept: without tensor cores (figures at the kernel).
+  if (!keep && a->T == 1) return a->F < 24ll * di.sm_count ? gated_rows<1, 8>(a, st) : gated_rows<1, 2>(a, st);
+  if (!keep && a->T == 2 && a->H * a->F <= (4ll << 20)) return gated_rows<2, 2>(a, st);
+  if (a->T <= kFewTokens) return keep ? gated_few<kFewAct8>(a, di, st) : gated_few<kFewForward>(a, di, st);
   KDKL_CUDA(cudaMemsetAsync(a->workspace, 0, 256, st));
   GemmParams p;
   memset(&p, 0, sizeof(p));
@@ -168,6 +214,8 @@ int kdkl_gated_linear_backward(const kdkl_gated_linear_args* a, void* cuda_strea
     if ((rc = kdkl_gated_act_backward(a->gate_record, a->up_record, a->record_bytes, a->format, a->dh, a->ld_dh, KDKL_TYPE_BF16, a->T, a->F,
                                       a->act, dgu, dgu + a->F, 2 * a->F, cuda_stream)))
       return rc;
+  } else if (a->T <= kFewTokens) {
+    if ((rc = gated_few<kFewBack>(a, di, st))) return rc;
   } else {
     GemmParams p;
     memset(&p, 0, sizeof(p));
