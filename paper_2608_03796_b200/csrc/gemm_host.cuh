@@ -24,11 +24,12 @@ inline int m_group_for(long long H) {
 // tenth of the tensor work (H = 4096, 1024, 1000 ...); narrow 256-column tiles otherwise.
 inline bool use_wide(long long N) { return ((N + kWideN - 1) / kWideN) * kWideN * 10 <= N * 11; }
 inline long long n_tiles_for(long long N, bool wide) { return wide ? (N + kWideN - 1) / kWideN : (N + BN - 1) / BN; }
-template <int EPI, bool A_MN, bool B_MN, bool WIDE = false>
+// NCTA = 1 takes a B map whose boxes are 256 rows (GemmCfg<1>::B_ROWS), and counts row tiles of 128.
+template <int EPI, bool A_MN, bool B_MN, bool WIDE = false, int NCTA = kNCTA>
 inline int launch_gemm(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& tc, const GemmParams& p,
                        const DeviceInfo& di, cudaStream_t st) {
-  auto kern = gemm_tcgen05_kernel<EPI, A_MN, B_MN, kNCTA, WIDE>;
-  constexpr int smem = GemmCfg<kNCTA, WIDE>::SMEM_BYTES;
+  auto kern = gemm_tcgen05_kernel<EPI, A_MN, B_MN, NCTA, WIDE>;
+  constexpr int smem = GemmCfg<NCTA, WIDE>::SMEM_BYTES;
   static_assert(smem <= 227 * 1024, "shared memory per CTA");
   // The shared-memory limit belongs to the current device's copy of this instantiation: set once per device
   // (a process may drive several), not per launch.
@@ -41,17 +42,17 @@ inline int launch_gemm(const CUtensorMap& ta, const CUtensorMap& tb, const CUten
   // persistent: one worker (a CTA, or a pair of CTAs on neighbouring SMs) per SM (pair), each walking
   // the work units with a stride of the worker count
   const int units = p.m_tiles * p.n_tiles * p.k_splits;
-  const int max_workers = sm_count / kNCTA;
+  const int max_workers = sm_count / NCTA;
   const int workers = units < max_workers ? units : max_workers;
   cudaLaunchConfig_t cfg;
   memset(&cfg, 0, sizeof(cfg));
-  cfg.gridDim = dim3((unsigned)(workers * kNCTA), 1, 1);
+  cfg.gridDim = dim3((unsigned)(workers * NCTA), 1, 1);
   cfg.blockDim = dim3(GEMM_THREADS, 1, 1);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = kNCTA;
+  attr[0].val.clusterDim.x = NCTA;
   attr[0].val.clusterDim.y = 1;
   attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;

@@ -2,6 +2,7 @@
 #include <math.h>
 #include <string.h>
 
+#include "body_host.cuh"
 #include "gemm_out.cuh"
 #include "label_kernels.cuh"
 
@@ -17,14 +18,15 @@ static long long label_chunk(long long T, long long chunk) {
 }
 
 // What lives from the forward to the backward call: a few numbers a token.
-struct LabelState { size_t col, counted, live, lz2, z_label, colread, losses, coefA, coefB, coefC, scale, total; };
+struct LabelState { size_t col, counted, live, lz2, z_label, colread, losses, coefA, coefB, coefC, scale, tile_counts, total; };
 static LabelState label_state(long long T) {
   LabelState s;
   size_t at = 256;
   auto take = [&](size_t bytes) { const size_t o = at; at = up(at + bytes, 256); return o; };
   s.col = take(4 * T); s.counted = take(4 * T); s.live = take((T + 255) / 256); s.lz2 = take(4 * T); s.z_label = take(4 * T);
   s.colread = take(4 * T); s.losses = take(4 * T); s.coefA = take(4 * T); s.coefB = take(4 * T); s.coefC = take(4 * T);
-  s.scale = take(4);
+  s.scale = take(256);                                     // and the count of arrivals
+  s.tile_counts = take(8 * ((T + 255) / 256));
   s.total = at;
   return s;
 }
@@ -122,27 +124,32 @@ static int label_run(const kdkl_label_loss_args* a, int mode, void* cuda_stream)
   p.col = at<int>(a->state, S.col); p.counted = at<int>(a->state, S.counted);
   p.lz2 = at<float>(a->state, S.lz2); p.z_label = at<float>(a->state, S.z_label); p.losses = at<float>(a->state, S.losses);
   p.coefA = at<float>(a->state, S.coefA); p.coefB = at<float>(a->state, S.coefB); p.coefC = at<float>(a->state, S.coefC);
-  p.scale = at<float>(a->state, S.scale);
+  p.scale = at<float>(a->state, S.scale); p.arrivals = at<int>(a->state, S.scale + 128); p.tile_counts = at<int>(a->state, S.tile_counts);
   uint8_t* live = at<uint8_t>(a->state, S.live);
-  if (sweep) KDKL_CUDA(cudaMemsetAsync(a->state, 0, 256, st));
   if (T == 0) {
+    if (sweep) KDKL_CUDA(cudaMemsetAsync(a->state, 0, 256, st));
     if (sweep) KDKL_CUDA(cudaMemsetAsync(a->loss, 0, 4, st));
     if (grads && !a->accumulate) KDKL_CUDA(cudaMemsetAsync(a->dweight, 0, (size_t)V * H * (a->dweight_type == KDKL_TYPE_F32 ? 4 : 2), st));
     return KDKL_OK;
   }
   const unsigned by256 = (unsigned)((T + 255) / 256);
   if (sweep) {
-    if (a->label_type == 1) label_prep_kernel<<<by256, 256, 0, st>>>(p, reinterpret_cast<const long long*>(a->labels), a->ignore_index, live);
-    else label_prep_kernel<<<by256, 256, 0, st>>>(p, reinterpret_cast<const int*>(a->labels), a->ignore_index, live);
-    KDKL_LAUNCHED("label_prep_kernel");
+    rc = a->label_type == 1 ? launch("label_prep_kernel", label_prep_kernel<long long>, dim3(by256), 256, 0, st, p,
+                                     reinterpret_cast<const long long*>(a->labels), a->ignore_index, live)
+                            : launch("label_prep_kernel", label_prep_kernel<int>, dim3(by256), 256, 0, st, p,
+                                     reinterpret_cast<const int*>(a->labels), a->ignore_index, live);
   } else {
-    label_coef_kernel<<<by256, 256, 0, st>>>(p);
-    KDKL_LAUNCHED("label_coef_kernel");
+    rc = launch("label_coef_kernel", label_coef_kernel, dim3(by256), 256, 0, st, p);
   }
+  if (rc) return rc;
   const int* go = sweep ? nullptr : &p.hdr->go;
   uint16_t* G = grads ? at<uint16_t>(a->workspace, L.G) : nullptr;
+  // The sweep's tiles: 256 rows on a pair of SMs, or 128 rows on one where that makes fewer waves (few tokens).
+  const long long pairs = di.sm_count / 2, most_rows = L.chunks > 1 ? L.C : L.last;
+  const bool single = sweep && ((most_rows + BM - 1) / BM * L.n_tiles + di.sm_count - 1) / di.sm_count <
+                               ((most_rows + kTileM - 1) / kTileM * L.n_tiles + pairs - 1) / pairs;
   CUtensorMap tmW, tmH, tmG;
-  if ((rc = make_tmap_bf16(&tmW, a->weight, (uint64_t)H, (uint64_t)V, (uint64_t)H * 2, BK, kBRows))) return rc;
+  if ((rc = make_tmap_bf16(&tmW, a->weight, (uint64_t)H, (uint64_t)V, (uint64_t)H * 2, BK, single ? GemmCfg<1>::B_ROWS : kBRows))) return rc;
   for (long long ci = 0; ci < L.chunks; ++ci) {
     const long long s0 = ci * L.C, rows = ci + 1 < L.chunks ? L.C : L.last;
     const __nv_bfloat16* hidden = reinterpret_cast<const __nv_bfloat16*>(a->hidden) + s0 * H;
@@ -165,15 +172,20 @@ static int label_run(const kdkl_label_loss_args* a, int mode, void* cuda_stream)
       g.part_m = at<float>(a->workspace, L.part_m); g.part_s = at<float>(a->workspace, L.part_s); g.part_z = at<float>(a->workspace, L.part_z);
       g.part_stride = L.C;
       if (grads) g.win_max = at<float>(a->workspace, L.win);
-      rc = grads ? launch_gemm<EPI_LABEL_E, false, false>(tmH, tmW, tmG, g, di, st) : launch_gemm<EPI_LSE_SUM, false, false>(tmH, tmW, tmG, g, di, st);
+      if (single) {
+        g.m_tiles = (int)((rows + BM - 1) / BM); g.m_group *= 2; g.m_live = nullptr;
+        rc = grads ? launch_gemm<EPI_LABEL_E, false, false, false, 1>(tmH, tmW, tmG, g, di, st) : launch_gemm<EPI_LSE_SUM, false, false, false, 1>(tmH, tmW, tmG, g, di, st);
+      } else {
+        rc = grads ? launch_gemm<EPI_LABEL_E, false, false>(tmH, tmW, tmG, g, di, st) : launch_gemm<EPI_LSE_SUM, false, false>(tmH, tmW, tmG, g, di, st);
+      }
       if (rc) return rc;
-      label_combine_kernel<<<(unsigned)((rows + 31) / 32), 1024, 0, st>>>(p, g.part_m, g.part_s, g.part_z, L.C, (int)L.n_tiles, (int)rows, s0,
-                                                                        grads ? 1 : 0, a->losses, a->lse);
-      KDKL_LAUNCHED("label_combine_kernel");
+      if ((rc = launch("label_combine_kernel", label_combine_kernel, dim3((unsigned)((rows + 31) / 32)), 1024, 0, st, p, (const float*)g.part_m,
+                       (const float*)g.part_s, (const float*)g.part_z, L.C, (int)L.n_tiles, (int)rows, s0, grads ? 1 : 0, ci + 1 == L.chunks ? 1 : 0,
+                       a->losses, a->lse, a->loss)))
+        return rc;
       if (grads) {
         const dim3 grid((unsigned)((V + kLabelGCols - 1) / kLabelGCols), (unsigned)((rows + kLabelGRows - 1) / kLabelGRows));
-        label_g_kernel<<<grid, 256, 0, st>>>(p, G, L.Vpad, g.win_max, L.C, (int)rows, s0);
-        KDKL_LAUNCHED("label_g_kernel");
+        if ((rc = launch("label_g_kernel", label_g_kernel, grid, 256, 0, st, p, G, L.Vpad, (const float*)g.win_max, L.C, (int)rows, s0))) return rc;
       }
     } else if ((rc = launch_gemm<EPI_LABEL_G, false, false>(tmH, tmW, tmG, g, di, st))) {
       return rc;
@@ -203,10 +215,6 @@ static int label_run(const kdkl_label_loss_args* a, int mode, void* cuda_stream)
     const long long n4 = V * H / 4;
     label_round_kernel<<<(unsigned)((n4 + 255) / 256), 256, 0, st>>>(at<float>(a->workspace, L.dw32), reinterpret_cast<uint2*>(a->dweight), n4, go);
     KDKL_LAUNCHED("label_round_kernel");
-  }
-  if (sweep) {
-    label_reduce_kernel<<<1, 1024, 0, st>>>(p, a->loss);
-    KDKL_LAUNCHED("label_reduce_kernel");
   }
   return KDKL_OK;
 }

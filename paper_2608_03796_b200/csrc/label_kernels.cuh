@@ -31,11 +31,13 @@ struct LabelParams {
   float* coefA; float* coefB; float* coefC;
   float* losses;                       // [T]
   float* scale;                        // [1]: upstream gradient / (divisor tau)
+  int* arrivals;                       // [1]: blocks of the last chunk's join that are done
+  int* tile_counts;                    // [2][ceil(T / 256)]: counted tokens, labels out of range
 };
 
 __device__ __forceinline__ double label_divisor(const LabelParams& p) {
   if (p.denom_device != nullptr) return *p.denom_device;
-  return p.mean ? (double)p.hdr->n_tokens : 1.0;
+  return p.mean ? (double)__ldcg(&p.hdr->n_tokens) : 1.0;
 }
 __device__ __forceinline__ void label_coefs(const LabelParams& p, long long t, float lse) {
   const float w = !p.counted[t] ? 0.f : p.grad_tokens != nullptr ? p.grad_tokens[t] : p.token_weight != nullptr ? p.token_weight[t] : 1.f;
@@ -48,10 +50,13 @@ __device__ __forceinline__ void label_scale(const LabelParams& p) {        // on
   *p.scale = d > 0.0 ? (float)(g / (d * (double)p.tau)) : 0.f;
 }
 
-// Labels to columns, the count of counted tokens, and which row tiles (256 tokens) hold one: a block has one tile.
+// Labels to columns, the counted tokens of each row tile (256 tokens) and whether it has any: a block has one tile. Clears the
+// status block.
 template <typename L>
 __global__ void __launch_bounds__(256)
 label_prep_kernel(const LabelParams p, const L* labels, long long ignore_index, uint8_t* live) {
+  grid_dependents_launch();
+  grid_dependency_wait();
   const long long t = (long long)blockIdx.x * 256 + threadIdx.x;
   bool counted = false, bad = false;
   if (t < p.T) {
@@ -64,10 +69,30 @@ label_prep_kernel(const LabelParams p, const L* labels, long long ignore_index, 
   const int n = __syncthreads_count(counted), n_bad = __syncthreads_count(bad);
   if (threadIdx.x == 0) {
     live[blockIdx.x] = n > 0 ? 1 : 0;
-    if (n > 0) atomicAdd(reinterpret_cast<unsigned long long*>(&p.hdr->n_tokens), (unsigned long long)n);   // whole numbers: any order
-    if (n_bad > 0) {
-      atomicAdd(&p.hdr->n_bad_idx, n_bad);
-      atomicCAS(&p.hdr->status, 0, -10);                   // KDKL_ERR_INDEX: taken as ignored
+    p.tile_counts[blockIdx.x] = n;
+    p.tile_counts[gridDim.x + blockIdx.x] = n_bad;
+  }
+  if (blockIdx.x == 0) {
+    if (threadIdx.x < 64) reinterpret_cast<int*>(p.hdr)[threadIdx.x] = 0;
+    if (threadIdx.x == 64) *p.arrivals = 0;
+  }
+}
+
+// The number of counted tokens, from the tiles'; a whole block of 1024 threads calls.
+__device__ __forceinline__ void label_count(const LabelParams& p, bool want_scale) {
+  __shared__ int part[2][32];
+  const int tiles = (p.T + 255) / 256;
+  int n = 0, bad = 0;
+  for (int i = threadIdx.x; i < tiles; i += 1024) { n += p.tile_counts[i]; bad += p.tile_counts[tiles + i]; }
+  n = __reduce_add_sync(0xffffffffu, n); bad = __reduce_add_sync(0xffffffffu, bad);
+  if ((threadIdx.x & 31) == 0) { part[0][threadIdx.x >> 5] = n; part[1][threadIdx.x >> 5] = bad; }
+  __syncthreads();
+  if (threadIdx.x < 32) {
+    n = __reduce_add_sync(0xffffffffu, part[0][threadIdx.x]); bad = __reduce_add_sync(0xffffffffu, part[1][threadIdx.x]);
+    if (threadIdx.x == 0) {
+      p.hdr->n_tokens = n; p.hdr->n_bad_idx = bad;
+      if (bad > 0) atomicCAS(&p.hdr->status, 0, -10);      // KDKL_ERR_INDEX: taken as ignored
+      if (want_scale) label_scale(p);
     }
   }
 }
@@ -75,8 +100,13 @@ label_prep_kernel(const LabelParams p, const L* labels, long long ignore_index, 
 // Joins the partial (max, sum, sum of logits) of a chunk's rows and vocabulary tiles; 32 rows a block, 32 lanes of partials a row.
 __global__ void __launch_bounds__(1024)
 label_combine_kernel(const LabelParams p, const float* part_m, const float* part_s, const float* part_z, long long stride, int n_tiles,
-                     int rows, long long row0, int want_coefs, float* losses_out, float* lse_out) {
+                     int rows, long long row0, int want_coefs, int last, float* losses_out, float* lse_out, float* loss_out) {
   __shared__ float sm_m[32][33], sm_s[32][33], sm_z[32][33];
+  __shared__ double sums[32];
+  __shared__ int turn;
+  grid_dependents_launch();
+  grid_dependency_wait();
+  if (row0 == 0 && blockIdx.x == 0) label_count(p, want_coefs != 0);
   const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
   const int r = blockIdx.x * 32 + tx;
   const long long t = row0 + r;
@@ -94,55 +124,58 @@ label_combine_kernel(const LabelParams p, const float* part_m, const float* part
   __syncthreads();
   // a warp a row from here on: a lane has one of its 32 partials
   const int row = blockIdx.x * 32 + ty;
-  if (row >= rows) return;
   const long long tok = row0 + row;
-  m = sm_m[tx][ty]; s = sm_s[tx][ty]; z = sm_z[tx][ty];
+  if (row < rows) {
+    m = sm_m[tx][ty]; s = sm_s[tx][ty]; z = sm_z[tx][ty];
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    const float om = __shfl_xor_sync(0xffffffffu, m, o), os = __shfl_xor_sync(0xffffffffu, s, o);
-    const float mn = fmaxf(m, om);
-    // (lanes beyond the tiles have m = -inf and s = 0; both may)
-    s = (m > -INFINITY ? s * exp2f(m - mn) : 0.f) + (om > -INFINITY ? os * exp2f(om - mn) : 0.f);
-    m = mn;
-    z += __shfl_xor_sync(0xffffffffu, z, o);
+    for (int o = 16; o > 0; o >>= 1) {
+      const float om = __shfl_xor_sync(0xffffffffu, m, o), os = __shfl_xor_sync(0xffffffffu, s, o);
+      const float mn = fmaxf(m, om);
+      // (lanes beyond the tiles have m = -inf and s = 0; both may)
+      s = (m > -INFINITY ? s * exp2f(m - mn) : 0.f) + (om > -INFINITY ? os * exp2f(om - mn) : 0.f);
+      m = mn;
+      z += __shfl_xor_sync(0xffffffffu, z, o);
+    }
+    if (tx == 0) {
+      float loss = 0.f, lse = 0.f, lz2 = 0.f;
+      if (p.counted[tok]) {
+        lz2 = m + log2f(s);
+        lse = lz2 * kLn2;
+        const float inv_tau = 1.f / p.tau;
+        // taken from the normaliser, so that a confident token's small loss keeps its digits
+        loss = (1.f - p.smoothing) * (lse - p.z_label[tok] * inv_tau) + p.smoothing * (lse - z * inv_tau / (float)p.V) + p.z_loss * lse * lse;
+        if (!isfinite(loss)) { atomicCAS(&p.hdr->status, 0, -11); atomicCAS(&p.hdr->where, 0, (int)tok); }
+      }
+      p.lz2[tok] = lz2;
+      p.losses[tok] = loss;
+      if (losses_out != nullptr) losses_out[tok] = loss;
+      if (lse_out != nullptr) lse_out[tok] = lse;
+      if (want_coefs) label_coefs(p, tok, lse);
+    }
   }
-  if (tx != 0) return;
-  float loss = 0.f, lse = 0.f, lz2 = 0.f;
-  if (p.counted[tok]) {
-    lz2 = m + log2f(s);
-    lse = lz2 * kLn2;
-    const float inv_tau = 1.f / p.tau;
-    // taken from the normaliser, so that a confident token's small loss keeps its digits
-    loss = (1.f - p.smoothing) * (lse - p.z_label[tok] * inv_tau) + p.smoothing * (lse - z * inv_tau / (float)p.V) + p.z_loss * lse * lse;
-    if (!isfinite(loss)) { atomicCAS(&p.hdr->status, 0, -11); atomicCAS(&p.hdr->where, 0, (int)tok); }
-  }
-  p.lz2[tok] = lz2;
-  p.losses[tok] = loss;
-  if (losses_out != nullptr) losses_out[tok] = loss;
-  if (lse_out != nullptr) lse_out[tok] = lse;
-  if (want_coefs) {
-    label_coefs(p, tok, lse);
-    if (tok == 0) label_scale(p);
-  }
-}
-
-// The mean or sum, in double and a fixed order; marks the state as complete.
-__global__ void __launch_bounds__(1024)
-label_reduce_kernel(const LabelParams p, float* loss_out) {
-  __shared__ double sums[1024];
-  double acc = 0.0;
-  for (int t = threadIdx.x; t < p.T; t += 1024)
-    if (p.counted[t]) acc += (double)p.losses[t] * (p.token_weight != nullptr ? (double)p.token_weight[t] : 1.0);
-  sums[threadIdx.x] = acc;
+  if (!last) return;
+  // The block that is done last adds up the losses, in double and an order of its own; it marks the state as complete.
+  __threadfence();
   __syncthreads();
-  for (int o = 512; o > 0; o >>= 1) {
-    if (threadIdx.x < o) sums[threadIdx.x] += sums[threadIdx.x + o];
-    __syncthreads();
-  }
-  if (threadIdx.x == 0) {
+  if (threadIdx.x == 0) turn = atomicAdd(p.arrivals, 1);
+  __syncthreads();
+  if (turn != (int)gridDim.x - 1) return;
+  __threadfence();
+  double acc = 0.0;
+  for (int i = threadIdx.x; i < p.T; i += 1024)
+    if (p.counted[i]) acc += (double)__ldcg(p.losses + i) * (p.token_weight != nullptr ? (double)p.token_weight[i] : 1.0);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, o);
+  if (tx == 0) sums[ty] = acc;
+  __syncthreads();
+  if (ty != 0) return;
+  acc = sums[tx];
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, o);
+  if (tx == 0) {
     const double d = label_divisor(p);
-    if (loss_out != nullptr) *loss_out = d > 0.0 ? (float)(sums[0] / d) : 0.f;
-    p.hdr->T = p.T; p.hdr->H = p.H; p.hdr->V = p.V; p.hdr->chunk = p.chunk; p.hdr->tau = p.tau; p.hdr->loss_sum = sums[0];
+    *loss_out = d > 0.0 ? (float)(acc / d) : 0.f;
+    p.hdr->T = p.T; p.hdr->H = p.H; p.hdr->V = p.V; p.hdr->chunk = p.chunk; p.hdr->tau = p.tau; p.hdr->loss_sum = acc;
     __threadfence();
     p.hdr->magic = KDKL_MAGIC;
   }
@@ -151,6 +184,8 @@ label_reduce_kernel(const LabelParams p, float* loss_out) {
 // Before a backward pass of its own: whether the state is this call's, and the tokens' three numbers.
 __global__ void __launch_bounds__(256)
 label_coef_kernel(const LabelParams p) {
+  grid_dependents_launch();
+  grid_dependency_wait();
   const WsHeader* h = p.hdr;
   const bool ok = h->magic == KDKL_MAGIC && h->T == p.T && h->H == p.H && h->V == p.V && h->chunk == p.chunk && h->tau == p.tau;
   if (blockIdx.x == 0 && threadIdx.x == 0) {
@@ -168,6 +203,8 @@ label_coef_kernel(const LabelParams p) {
 constexpr int kLabelGRows = 8, kLabelGCols = 1024;
 __global__ void __launch_bounds__(256)
 label_g_kernel(const LabelParams p, uint16_t* G, long long ldg, const float* win_max, long long stride, int rows, long long row0) {
+  grid_dependents_launch();
+  grid_dependency_wait();
   __shared__ float factor[kLabelGRows][kLabelGCols / 32];
   const int c0 = blockIdx.x * kLabelGCols, r0 = blockIdx.y * kLabelGRows;
   {
