@@ -259,7 +259,7 @@ def test_autograd(single_pass):
     def total(p, q):
         want = _Want(p, q, y, 0.1, 1e-3)
         return 0.5 * float((want.losses * weight.double() * want.counted).sum() / n)
-    assert abs(0.5 * float(loss) - total(h, w)) <= 1e-5
+    assert abs(0.5 * loss.item() - total(h, w)) <= 1e-5
     for t, grad, at in ((h, a.grad.reshape(T, H), 0), (w, b.grad, 1)):
         v = torch.randn(t.shape, dtype=F64, device="cuda", generator=torch.Generator(device="cuda").manual_seed(2))
         f = (lambda e: total(h.double() + e * v, w)) if at == 0 else (lambda e: total(h, w.double() + e * v))
