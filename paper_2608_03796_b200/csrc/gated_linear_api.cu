@@ -70,7 +70,7 @@ static int gated_product(const kdkl_gated_linear_args* a, GemmParams& p, const C
   p.m_tiles = (int)((a->T + kTileM - 1) / kTileM); p.n_tiles = (int)((a->F + kGatedN - 1) / kGatedN);
   p.m_inner = 1; p.m_group = m_group_for(a->H); p.k_splits = 1;
   p.act = a->act; p.format = a->format;
-  return launch_gemm<EPI, false, false>(ta, tb, tc, p, di, st);
+  return launch_gemm<EPI, false, false>(ta, tb, tc, p, di, st, true);
 }
 
 // Up to 128 tokens. A cluster of as many CTAs a tile (1, 2 or 4) as bring the SMs to work, while each keeps eight blocks of the
@@ -209,7 +209,7 @@ int kdkl_gated_linear_backward(const kdkl_gated_linear_args* a, void* cuda_strea
   }
   if ((rc = need_b200(&di))) return rc;
   __nv_bfloat16* dgu = reinterpret_cast<__nv_bfloat16*>(a->dgate_up);
-  KDKL_CUDA(cudaMemsetAsync(a->workspace, 0, 256, st));
+  if (records || a->T > kFewTokens) KDKL_CUDA(cudaMemsetAsync(a->workspace, 0, 256, st));   // (the kernel for few tokens does)
   if (records) {
     if ((rc = kdkl_gated_act_backward(a->gate_record, a->up_record, a->record_bytes, a->format, a->dh, a->ld_dh, KDKL_TYPE_BF16, a->T, a->F,
                                       a->act, dgu, dgu + a->F, 2 * a->F, cuda_stream)))

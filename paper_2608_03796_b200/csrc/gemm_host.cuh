@@ -24,10 +24,11 @@ inline int m_group_for(long long H) {
 // tenth of the tensor work (H = 4096, 1024, 1000 ...); narrow 256-column tiles otherwise.
 inline bool use_wide(long long N) { return ((N + kWideN - 1) / kWideN) * kWideN * 10 <= N * 11; }
 inline long long n_tiles_for(long long N, bool wide) { return wide ? (N + kWideN - 1) / kWideN : (N + BN - 1) / BN; }
-// NCTA = 1 takes a B map whose boxes are 256 rows (GemmCfg<1>::B_ROWS), and counts row tiles of 128.
+// early: the launch may be prepared while the kernel before it on the stream drains (see launch_cluster in body_host.cuh; every
+// kernel before it has then to leave what it writes complete to grid_dependency_wait, which all do). NCTA = 1 takes a B map whose boxes are 256 rows (GemmCfg<1>::B_ROWS), and counts row tiles of 128.
 template <int EPI, bool A_MN, bool B_MN, bool WIDE = false, int NCTA = kNCTA>
 inline int launch_gemm(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& tc, const GemmParams& p,
-                       const DeviceInfo& di, cudaStream_t st) {
+                       const DeviceInfo& di, cudaStream_t st, bool early = false) {
   auto kern = gemm_tcgen05_kernel<EPI, A_MN, B_MN, NCTA, WIDE>;
   constexpr int smem = GemmCfg<NCTA, WIDE>::SMEM_BYTES;
   static_assert(smem <= 227 * 1024, "shared memory per CTA");
@@ -50,13 +51,15 @@ inline int launch_gemm(const CUtensorMap& ta, const CUtensorMap& tb, const CUten
   cfg.blockDim = dim3(GEMM_THREADS, 1, 1);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = NCTA;
   attr[0].val.clusterDim.y = 1;
   attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.numAttrs = early ? 2 : 1;
   cudaError_t e = cudaLaunchKernelEx(&cfg, kern, ta, tb, tc, p);
   if (e != cudaSuccess) return cuda_fail("gemm_tcgen05_kernel launch", e);
   KDKL_LAUNCHED("gemm_tcgen05_kernel");

@@ -1,6 +1,7 @@
 // Products that write a gradient, out [M, N] = A B with B stored [K, N]: which tiles, how many parts of the contraction, and
 // the launch. A is K-major ([M, K]) or MN-major ([K, M]). The result is bf16 or fp32, written or added to.
 #pragma once
+#include "body_host.cuh"
 #include "gemm_host.cuh"
 
 namespace kdkl {
@@ -10,6 +11,8 @@ template <bool BF16>
 __global__ void __launch_bounds__(256)
 out_join_kernel(const float* part, long long slab, int splits, long long n4, const float* scale, void* out,
                 int accumulate, const int* go) {
+  grid_dependents_launch();
+  grid_dependency_wait();
   if (go != nullptr && *go == 0) return;
   const long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x;
   if (i >= n4) return;
@@ -94,8 +97,8 @@ inline int launch_out(const OutGemm& o, const DeviceInfo& di, cudaStream_t st) {
   if (rc) return rc;
   p.out_scale = joined ? nullptr : o.scale;                // (of parts, when they are joined)
 #define KDKL_OUT(EPI)                                                                 \
-  rc = o.plan.wide ? launch_gemm<EPI, A_MN, true, true>(ta, tb, tc, p, di, st)        \
-                   : launch_gemm<EPI, A_MN, true, false>(ta, tb, tc, p, di, st)
+  rc = o.plan.wide ? launch_gemm<EPI, A_MN, true, true>(ta, tb, tc, p, di, st, true)  \
+                   : launch_gemm<EPI, A_MN, true, false>(ta, tb, tc, p, di, st, true)
   if (p.out_scale != nullptr) {
     if (f32) KDKL_OUT(EPI_STORE_F32_SCALED);
     else KDKL_OUT(EPI_STORE_BF16_SCALED);
@@ -107,10 +110,10 @@ inline int launch_out(const OutGemm& o, const DeviceInfo& di, cudaStream_t st) {
   if (rc || !joined) return rc;
   const long long n4 = o.M * o.N / 4;
   const unsigned grid = (unsigned)((n4 + 255) / 256);
-  if (o.bf16) out_join_kernel<true><<<grid, 256, 0, st>>>(o.slab, rows * o.N, o.plan.splits, n4, o.scale, o.out, o.accumulate, o.go);
-  else out_join_kernel<false><<<grid, 256, 0, st>>>(o.slab, rows * o.N, o.plan.splits, n4, o.scale, o.out, o.accumulate, o.go);
-  KDKL_LAUNCHED("out_join_kernel");
-  return KDKL_OK;
+  KDKL_BY_BOOL(o.bf16, BF16,
+    rc = launch("out_join_kernel", out_join_kernel<BF16>, dim3(grid), 256, 0, st, (const float*)o.slab, rows * o.N, o.plan.splits, n4, o.scale,
+                o.out, o.accumulate, o.go));
+  return rc;
 }
 
 }  // namespace kdkl

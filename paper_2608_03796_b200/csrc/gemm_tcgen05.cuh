@@ -340,6 +340,9 @@ gemm_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
   const int warp = threadIdx.x >> 5;
   const int lane = threadIdx.x & 31;
 
+  // (of consequence only where this launch, or the next one, is a programmatic one)
+  grid_dependents_launch();
+  grid_dependency_wait();
   if (p.go != nullptr && *p.go == 0) return;   // uniform across the grid
 
   // pair bookkeeping: the leader (cluster rank 0) owns the barriers that gate the MMAs

@@ -174,9 +174,9 @@ static int label_run(const kdkl_label_loss_args* a, int mode, void* cuda_stream)
       if (grads) g.win_max = at<float>(a->workspace, L.win);
       if (single) {
         g.m_tiles = (int)((rows + BM - 1) / BM); g.m_group *= 2; g.m_live = nullptr;
-        rc = grads ? launch_gemm<EPI_LABEL_E, false, false, false, 1>(tmH, tmW, tmG, g, di, st) : launch_gemm<EPI_LSE_SUM, false, false, false, 1>(tmH, tmW, tmG, g, di, st);
+        rc = grads ? launch_gemm<EPI_LABEL_E, false, false, false, 1>(tmH, tmW, tmG, g, di, st, true) : launch_gemm<EPI_LSE_SUM, false, false, false, 1>(tmH, tmW, tmG, g, di, st, true);
       } else {
-        rc = grads ? launch_gemm<EPI_LABEL_E, false, false>(tmH, tmW, tmG, g, di, st) : launch_gemm<EPI_LSE_SUM, false, false>(tmH, tmW, tmG, g, di, st);
+        rc = grads ? launch_gemm<EPI_LABEL_E, false, false>(tmH, tmW, tmG, g, di, st, true) : launch_gemm<EPI_LSE_SUM, false, false>(tmH, tmW, tmG, g, di, st, true);
       }
       if (rc) return rc;
       if ((rc = launch("label_combine_kernel", label_combine_kernel, dim3((unsigned)((rows + 31) / 32)), 1024, 0, st, p, (const float*)g.part_m,
@@ -187,7 +187,7 @@ static int label_run(const kdkl_label_loss_args* a, int mode, void* cuda_stream)
         const dim3 grid((unsigned)((V + kLabelGCols - 1) / kLabelGCols), (unsigned)((rows + kLabelGRows - 1) / kLabelGRows));
         if ((rc = launch("label_g_kernel", label_g_kernel, grid, 256, 0, st, p, G, L.Vpad, (const float*)g.win_max, L.C, (int)rows, s0))) return rc;
       }
-    } else if ((rc = launch_gemm<EPI_LABEL_G, false, false>(tmH, tmW, tmG, g, di, st))) {
+    } else if ((rc = launch_gemm<EPI_LABEL_G, false, false>(tmH, tmW, tmG, g, di, st, true))) {
       return rc;
     }
     if (!grads) continue;
@@ -213,8 +213,9 @@ static int label_run(const kdkl_label_loss_args* a, int mode, void* cuda_stream)
   }
   if (grads && a->dweight_type == KDKL_TYPE_BF16 && L.chunks > 1) {
     const long long n4 = V * H / 4;
-    label_round_kernel<<<(unsigned)((n4 + 255) / 256), 256, 0, st>>>(at<float>(a->workspace, L.dw32), reinterpret_cast<uint2*>(a->dweight), n4, go);
-    KDKL_LAUNCHED("label_round_kernel");
+    if ((rc = launch("label_round_kernel", label_round_kernel, dim3((unsigned)((n4 + 255) / 256)), 256, 0, st,
+                     (const float*)at<float>(a->workspace, L.dw32), reinterpret_cast<uint2*>(a->dweight), n4, go)))
+      return rc;
   }
   return KDKL_OK;
 }

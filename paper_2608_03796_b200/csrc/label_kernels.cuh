@@ -248,6 +248,8 @@ label_g_kernel(const LabelParams p, uint16_t* G, long long ldg, const float* win
 
 __global__ void __launch_bounds__(256)
 label_round_kernel(const float* in, uint2* out, long long n4, const int* go) {
+  grid_dependents_launch();
+  grid_dependency_wait();
   if (go != nullptr && *go == 0) return;
   const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
   if (i >= n4) return;
