@@ -35,9 +35,9 @@ struct LabelParams {
   int* tile_counts;                    // [2][ceil(T / 256)]: counted tokens, labels out of range
 };
 
-__device__ __forceinline__ double label_divisor(const LabelParams& p) {
+__device__ __forceinline__ double label_divisor(const LabelParams& p, long long counted) {
   if (p.denom_device != nullptr) return *p.denom_device;
-  return p.mean ? (double)__ldcg(&p.hdr->n_tokens) : 1.0;
+  return p.mean ? (double)counted : 1.0;
 }
 __device__ __forceinline__ void label_coefs(const LabelParams& p, long long t, float lse) {
   const float w = !p.counted[t] ? 0.f : p.grad_tokens != nullptr ? p.grad_tokens[t] : p.token_weight != nullptr ? p.token_weight[t] : 1.f;
@@ -45,8 +45,8 @@ __device__ __forceinline__ void label_coefs(const LabelParams& p, long long t, f
   p.coefB[t] = w * (1.f - p.smoothing);
   p.coefC[t] = w * p.smoothing / (float)p.V;
 }
-__device__ __forceinline__ void label_scale(const LabelParams& p) {        // one thread
-  const double d = p.grad_tokens != nullptr ? 1.0 : label_divisor(p), g = p.grad_tokens == nullptr && p.grad != nullptr ? (double)*p.grad : 1.0;
+__device__ __forceinline__ void label_scale(const LabelParams& p, long long counted) {        // one thread
+  const double d = p.grad_tokens != nullptr ? 1.0 : label_divisor(p, counted), g = p.grad_tokens == nullptr && p.grad != nullptr ? (double)*p.grad : 1.0;
   *p.scale = d > 0.0 ? (float)(g / (d * (double)p.tau)) : 0.f;
 }
 
@@ -78,23 +78,20 @@ label_prep_kernel(const LabelParams p, const L* labels, long long ignore_index, 
   }
 }
 
-// The number of counted tokens, from the tiles'; a whole block of 1024 threads calls.
-__device__ __forceinline__ void label_count(const LabelParams& p, bool want_scale) {
+// The number of counted tokens and of labels out of range, from the tiles'; a whole block calls, thread 0 has the result.
+__device__ __forceinline__ int2 label_count(const LabelParams& p) {
   __shared__ int part[2][32];
   const int tiles = (p.T + 255) / 256;
   int n = 0, bad = 0;
-  for (int i = threadIdx.x; i < tiles; i += 1024) { n += p.tile_counts[i]; bad += p.tile_counts[tiles + i]; }
+  for (int i = threadIdx.x; i < tiles; i += blockDim.x) { n += p.tile_counts[i]; bad += p.tile_counts[tiles + i]; }
   n = __reduce_add_sync(0xffffffffu, n); bad = __reduce_add_sync(0xffffffffu, bad);
   if ((threadIdx.x & 31) == 0) { part[0][threadIdx.x >> 5] = n; part[1][threadIdx.x >> 5] = bad; }
   __syncthreads();
-  if (threadIdx.x < 32) {
-    n = __reduce_add_sync(0xffffffffu, part[0][threadIdx.x]); bad = __reduce_add_sync(0xffffffffu, part[1][threadIdx.x]);
-    if (threadIdx.x == 0) {
-      p.hdr->n_tokens = n; p.hdr->n_bad_idx = bad;
-      if (bad > 0) atomicCAS(&p.hdr->status, 0, -10);      // KDKL_ERR_INDEX: taken as ignored
-      if (want_scale) label_scale(p);
-    }
-  }
+  if (threadIdx.x >= 32) return make_int2(0, 0);
+  const bool has = threadIdx.x < blockDim.x / 32;
+  n = __reduce_add_sync(0xffffffffu, has ? part[0][threadIdx.x] : 0);
+  bad = __reduce_add_sync(0xffffffffu, has ? part[1][threadIdx.x] : 0);
+  return make_int2(n, bad);
 }
 
 // Joins the partial (max, sum, sum of logits) of a chunk's rows and vocabulary tiles; 32 rows a block, 32 lanes of partials a row.
@@ -106,7 +103,6 @@ label_combine_kernel(const LabelParams p, const float* part_m, const float* part
   __shared__ int turn;
   grid_dependents_launch();
   grid_dependency_wait();
-  if (row0 == 0 && blockIdx.x == 0) label_count(p, want_coefs != 0);
   const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
   const int r = blockIdx.x * 32 + tx;
   const long long t = row0 + r;
@@ -121,10 +117,12 @@ label_combine_kernel(const LabelParams p, const float* part_m, const float* part
     }
   }
   sm_m[ty][tx] = m; sm_s[ty][tx] = s; sm_z[ty][tx] = z;
-  __syncthreads();
   // a warp a row from here on: a lane has one of its 32 partials
   const int row = blockIdx.x * 32 + ty;
   const long long tok = row0 + row;
+  const bool counts = row < rows && p.counted[tok] != 0;
+  const float z_label = counts ? p.z_label[tok] : 0.f;
+  __syncthreads();
   if (row < rows) {
     m = sm_m[tx][ty]; s = sm_s[tx][ty]; z = sm_z[tx][ty];
 #pragma unroll
@@ -138,12 +136,12 @@ label_combine_kernel(const LabelParams p, const float* part_m, const float* part
     }
     if (tx == 0) {
       float loss = 0.f, lse = 0.f, lz2 = 0.f;
-      if (p.counted[tok]) {
+      if (counts) {
         lz2 = m + log2f(s);
         lse = lz2 * kLn2;
         const float inv_tau = 1.f / p.tau;
         // taken from the normaliser, so that a confident token's small loss keeps its digits
-        loss = (1.f - p.smoothing) * (lse - p.z_label[tok] * inv_tau) + p.smoothing * (lse - z * inv_tau / (float)p.V) + p.z_loss * lse * lse;
+        loss = (1.f - p.smoothing) * (lse - z_label * inv_tau) + p.smoothing * (lse - z * inv_tau / (float)p.V) + p.z_loss * lse * lse;
         if (!isfinite(loss)) { atomicCAS(&p.hdr->status, 0, -11); atomicCAS(&p.hdr->where, 0, (int)tok); }
       }
       p.lz2[tok] = lz2;
@@ -167,14 +165,16 @@ label_combine_kernel(const LabelParams p, const float* part_m, const float* part
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, o);
   if (tx == 0) sums[ty] = acc;
-  __syncthreads();
+  const int2 n = label_count(p);                           // (with the barrier that sums needs)
   if (ty != 0) return;
   acc = sums[tx];
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, o);
   if (tx == 0) {
-    const double d = label_divisor(p);
+    const double d = label_divisor(p, n.x);
     *loss_out = d > 0.0 ? (float)(acc / d) : 0.f;
+    p.hdr->n_tokens = n.x; p.hdr->n_bad_idx = n.y;
+    if (n.y > 0) atomicCAS(&p.hdr->status, 0, -10);        // KDKL_ERR_INDEX: taken as ignored
     p.hdr->T = p.T; p.hdr->H = p.H; p.hdr->V = p.V; p.hdr->chunk = p.chunk; p.hdr->tau = p.tau; p.hdr->loss_sum = acc;
     __threadfence();
     p.hdr->magic = KDKL_MAGIC;
@@ -190,7 +190,7 @@ label_coef_kernel(const LabelParams p) {
   const bool ok = h->magic == KDKL_MAGIC && h->T == p.T && h->H == p.H && h->V == p.V && h->chunk == p.chunk && h->tau == p.tau;
   if (blockIdx.x == 0 && threadIdx.x == 0) {
     p.hdr->go = ok ? 1 : 0;
-    label_scale(p);
+    label_scale(p, h->n_tokens);
     if (!ok) atomicCAS(&p.hdr->status, 0, -9);             // KDKL_ERR_STATE
   }
   const long long t = (long long)blockIdx.x * 256 + threadIdx.x;
@@ -199,7 +199,8 @@ label_coef_kernel(const LabelParams p) {
 
 // The chunk's exponentials (fp16, each 32 columns with their own power, see EPI_LABEL_E) become G (bf16) in place:
 // G = (a 2^(w - lz2)) e - c, less b at the label. 8 rows x 1024 columns a block: 256 factors, one a thread, then 1024 words of
-// 8 columns. One read and one write of the buffer: bound by memory.
+// 8 columns. One read and one write of the buffer: bound by memory. The first block of the first chunk also forms what all tokens
+// share, which the products behind it need.
 constexpr int kLabelGRows = 8, kLabelGCols = 1024;
 __global__ void __launch_bounds__(256)
 label_g_kernel(const LabelParams p, uint16_t* G, long long ldg, const float* win_max, long long stride, int rows, long long row0) {
@@ -217,6 +218,10 @@ label_g_kernel(const LabelParams p, uint16_t* G, long long ldg, const float* win
     factor[r][w] = f;
   }
   __syncthreads();
+  if (row0 == 0 && blockIdx.x == 0 && blockIdx.y == 0) {
+    const int2 n = label_count(p);
+    if (threadIdx.x == 0) label_scale(p, n.x);
+  }
   constexpr int kWords = kLabelGCols / 8, kEach = kLabelGRows * kWords / 256;
   uint4 word[kEach];
 #pragma unroll
