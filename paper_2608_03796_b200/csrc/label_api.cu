@@ -4,6 +4,7 @@
 
 #include "body_host.cuh"
 #include "gemm_out.cuh"
+#include "label_few_kernels.cuh"
 #include "label_kernels.cuh"
 
 using namespace kdkl;
@@ -44,7 +45,7 @@ static LabelLayout label_layout(long long T, long long H, long long V, long long
   L.chunks = (T + L.C - 1) / L.C;
   L.last = T - (L.chunks - 1) * L.C;
   L.Vpad = (long long)up((size_t)V, 64);
-  L.n_tiles = (V + BN - 1) / BN;
+  L.n_tiles = T <= kLabelFewTokens ? (V + kLabelFewRows - 1) / kLabelFewRows : (V + BN - 1) / BN;
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t o = at; at = up(at + bytes, 256); return o; };
   if (mode != kLabelBackward) {
@@ -102,6 +103,34 @@ static int check_label(const kdkl_label_loss_args* a, int mode) {
   return KDKL_OK;
 }
 
+// The sweep for up to 128 tokens: one CTA an SM, as long a ring as its shared memory holds.
+template <int N, bool STORE>
+static int label_few_launch(const CUtensorMap& tw, const CUtensorMap& tx, LabelFewParams p, const DeviceInfo& di, cudaStream_t st) {
+  auto kern = label_few_kernel<N, STORE>;
+  constexpr int kMost = 224 * 1024, kTurned = label_few_turned_bytes(N);
+  static bool attr_set[kMaxDevices];
+  if (di.dev < 0 || di.dev >= kMaxDevices || !attr_set[di.dev]) {
+    KDKL_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost));
+    if (di.dev >= 0 && di.dev < kMaxDevices) attr_set[di.dev] = true;
+  }
+  p.stages = (kMost - 1024 - kTurned) / label_few_stage_bytes(N);
+  if (p.stages > kLabelFewMaxStages) p.stages = kLabelFewMaxStages;
+  return launch("label_few_kernel", kern, dim3((unsigned)(p.tiles < di.sm_count ? p.tiles : di.sm_count)), kLabelFewThreads,
+                (size_t)1024 + kTurned + (size_t)p.stages * label_few_stage_bytes(N), st, tw, tx, p);
+}
+template <bool STORE>
+static int label_few(const kdkl_label_loss_args* a, const LabelFewParams& p, const DeviceInfo& di, cudaStream_t st) {
+  const int N = p.T <= 16 ? 16 : p.T <= 32 ? 32 : p.T <= 64 ? 64 : 128;
+  CUtensorMap tw, tx;
+  int rc;
+  if ((rc = make_tmap_bf16(&tw, a->weight, (uint64_t)p.H, (uint64_t)p.V, (uint64_t)p.H * 2, BK, kLabelFewRows))) return rc;
+  if ((rc = make_tmap_bf16(&tx, a->hidden, (uint64_t)p.H, (uint64_t)p.T, (uint64_t)p.H * 2, BK, (uint32_t)N))) return rc;
+  if (N == 16) return label_few_launch<16, STORE>(tw, tx, p, di, st);
+  if (N == 32) return label_few_launch<32, STORE>(tw, tx, p, di, st);
+  if (N == 64) return label_few_launch<64, STORE>(tw, tx, p, di, st);
+  return label_few_launch<128, STORE>(tw, tx, p, di, st);
+}
+
 static int label_run(const kdkl_label_loss_args* a, int mode, void* cuda_stream) {
   g_launches = 0;
   int rc = check_label(a, mode);
@@ -145,9 +174,9 @@ static int label_run(const kdkl_label_loss_args* a, int mode, void* cuda_stream)
   const int* go = sweep ? nullptr : &p.hdr->go;
   uint16_t* G = grads ? at<uint16_t>(a->workspace, L.G) : nullptr;
   // The sweep's tiles: 256 rows on a pair of SMs, or 128 rows on one where that makes fewer waves (few tokens).
-  const long long pairs = di.sm_count / 2, most_rows = L.chunks > 1 ? L.C : L.last;
-  const bool single = sweep && ((most_rows + BM - 1) / BM * L.n_tiles + di.sm_count - 1) / di.sm_count <
-                               ((most_rows + kTileM - 1) / kTileM * L.n_tiles + pairs - 1) / pairs;
+  const long long pairs = di.sm_count / 2, most_rows = L.chunks > 1 ? L.C : L.last, tiles = (V + BN - 1) / BN;
+  const bool single = sweep && ((most_rows + BM - 1) / BM * tiles + di.sm_count - 1) / di.sm_count <
+                               ((most_rows + kTileM - 1) / kTileM * tiles + pairs - 1) / pairs;
   CUtensorMap tmW, tmH, tmG;
   if ((rc = make_tmap_bf16(&tmW, a->weight, (uint64_t)H, (uint64_t)V, (uint64_t)H * 2, BK, single ? GemmCfg<1>::B_ROWS : kBRows))) return rc;
   for (long long ci = 0; ci < L.chunks; ++ci) {
@@ -160,7 +189,7 @@ static int label_run(const kdkl_label_loss_args* a, int mode, void* cuda_stream)
     GemmParams g;
     memset(&g, 0, sizeof(g));
     g.M = (int)rows; g.N = (int)V; g.K = (int)H;
-    g.m_tiles = (int)((rows + kTileM - 1) / kTileM); g.n_tiles = (int)L.n_tiles; g.m_inner = 1; g.m_group = m_group_for(H); g.k_splits = 1;
+    g.m_tiles = (int)((rows + kTileM - 1) / kTileM); g.n_tiles = (int)tiles; g.m_inner = 1; g.m_group = m_group_for(H); g.k_splits = 1;
     g.m_live = flags;
     g.status = &p.hdr->status; g.go = go;
     g.scale_log2 = kLog2e / p.tau; g.Ktop = 1;
@@ -172,7 +201,14 @@ static int label_run(const kdkl_label_loss_args* a, int mode, void* cuda_stream)
       g.part_m = at<float>(a->workspace, L.part_m); g.part_s = at<float>(a->workspace, L.part_s); g.part_z = at<float>(a->workspace, L.part_z);
       g.part_stride = L.C;
       if (grads) g.win_max = at<float>(a->workspace, L.win);
-      if (single) {
+      if (T <= kLabelFewTokens) {
+        LabelFewParams q;
+        memset(&q, 0, sizeof(q));
+        q.T = (int)T; q.H = (int)H; q.V = (int)V; q.tiles = (int)L.n_tiles; q.scale_log2 = g.scale_log2; q.col = p.col;
+        q.part_m = g.part_m; q.part_s = g.part_s; q.part_z = g.part_z; q.stride = L.C; q.z_label = p.z_label;
+        q.E = G; q.ld_e = L.Vpad; q.win_max = g.win_max; q.status = &p.hdr->status;
+        rc = grads ? label_few<true>(a, q, di, st) : label_few<false>(a, q, di, st);
+      } else if (single) {
         g.m_tiles = (int)((rows + BM - 1) / BM); g.m_group *= 2; g.m_live = nullptr;
         rc = grads ? launch_gemm<EPI_LABEL_E, false, false, false, 1>(tmH, tmW, tmG, g, di, st, true) : launch_gemm<EPI_LSE_SUM, false, false, false, 1>(tmH, tmW, tmG, g, di, st, true);
       } else {

@@ -93,7 +93,9 @@ def _check_loss(want, op, weight=None, divisor=None):
     return w / d
 
 
-SHAPES = [(1, 8, 1), (1, 64, 7), (2, 2048, 9001), (3, 64, 1000), (257, 128, 515), (300, 264, 2001), (700, 512, 4096)]
+# up to 128 tokens (each width of the narrow tile; ragged last tiles; more tiles than SMs), and more
+SHAPES = [(1, 8, 1), (1, 64, 7), (2, 2048, 9001), (3, 64, 1000), (16, 72, 128), (17, 512, 40001), (33, 64, 161), (64, 264, 20002),
+          (65, 1000, 33), (128, 128, 30000), (129, 128, 2000), (257, 128, 515), (300, 264, 2001), (700, 512, 4096)]
 
 
 @pytest.mark.parametrize("T,H,V", SHAPES)
