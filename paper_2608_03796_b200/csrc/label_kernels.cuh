@@ -78,12 +78,17 @@ label_prep_kernel(const LabelParams p, const L* labels, long long ignore_index, 
   }
 }
 
-// The number of counted tokens and of labels out of range, from the tiles'; a whole block calls, thread 0 has the result.
-__device__ __forceinline__ int2 label_count(const LabelParams& p) {
-  __shared__ int part[2][32];
+// The number of counted tokens and of labels out of range, from the tiles': a thread's share, and the block's sum of them, which
+// thread 0 has.
+__device__ __forceinline__ int2 label_count_share(const LabelParams& p) {
   const int tiles = (p.T + 255) / 256;
-  int n = 0, bad = 0;
-  for (int i = threadIdx.x; i < tiles; i += blockDim.x) { n += p.tile_counts[i]; bad += p.tile_counts[tiles + i]; }
+  int2 n = make_int2(0, 0);
+  for (int i = threadIdx.x; i < tiles; i += blockDim.x) { n.x += p.tile_counts[i]; n.y += p.tile_counts[tiles + i]; }
+  return n;
+}
+__device__ __forceinline__ int2 label_count(int2 share) {
+  __shared__ int part[2][32];
+  int n = share.x, bad = share.y;
   n = __reduce_add_sync(0xffffffffu, n); bad = __reduce_add_sync(0xffffffffu, bad);
   if ((threadIdx.x & 31) == 0) { part[0][threadIdx.x >> 5] = n; part[1][threadIdx.x >> 5] = bad; }
   __syncthreads();
@@ -106,6 +111,14 @@ label_combine_kernel(const LabelParams p, const float* part_m, const float* part
   const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
   const int r = blockIdx.x * 32 + tx;
   const long long t = row0 + r;
+  // what the last block will want for the sum, asked for now
+  auto factor = [&](int i) { return p.counted[i] ? (p.token_weight != nullptr ? p.token_weight[i] : 1.f) : 0.f; };
+  int2 share = make_int2(0, 0);
+  float first_factor = 0.f;
+  if (last) {
+    share = label_count_share(p);
+    if ((int)threadIdx.x < p.T) first_factor = factor(threadIdx.x);
+  }
   const bool counted = r < rows && p.counted[t] != 0;      // others' partials may not exist
   float m = -INFINITY, s = 0.f, z = 0.f;
   if (counted) {
@@ -153,19 +166,23 @@ label_combine_kernel(const LabelParams p, const float* part_m, const float* part
   }
   if (!last) return;
   // The block that is done last adds up the losses, in double and an order of its own; it marks the state as complete.
-  __threadfence();
   __syncthreads();
-  if (threadIdx.x == 0) turn = atomicAdd(p.arrivals, 1);
+  if (threadIdx.x == 0) {
+    __threadfence();                                       // the block's losses, which the barrier ordered before this
+    turn = atomicAdd(p.arrivals, 1);
+    __threadfence();
+  }
   __syncthreads();
   if (turn != (int)gridDim.x - 1) return;
-  __threadfence();
   double acc = 0.0;
-  for (int i = threadIdx.x; i < p.T; i += 1024)
-    if (p.counted[i]) acc += (double)__ldcg(p.losses + i) * (p.token_weight != nullptr ? (double)p.token_weight[i] : 1.0);
+  for (int i = threadIdx.x; i < p.T; i += 1024) {
+    const float w = i == (int)threadIdx.x ? first_factor : factor(i);
+    if (w != 0.f) acc += (double)__ldcg(p.losses + i) * (double)w;
+  }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, o);
   if (tx == 0) sums[ty] = acc;
-  const int2 n = label_count(p);                           // (with the barrier that sums needs)
+  const int2 n = label_count(share);                       // (with the barrier that sums needs)
   if (ty != 0) return;
   acc = sums[tx];
 #pragma unroll
@@ -219,7 +236,7 @@ label_g_kernel(const LabelParams p, uint16_t* G, long long ldg, const float* win
   }
   __syncthreads();
   if (row0 == 0 && blockIdx.x == 0 && blockIdx.y == 0) {
-    const int2 n = label_count(p);
+    const int2 n = label_count(label_count_share(p));
     if (threadIdx.x == 0) label_scale(p, n.x);
   }
   constexpr int kWords = kLabelGCols / 8, kEach = kLabelGRows * kWords / 256;
