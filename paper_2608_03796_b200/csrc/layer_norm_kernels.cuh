@@ -8,6 +8,9 @@
 //   sum (x - mu)^2 = sum_i [ q_i + n_i (mu_i - mu)^2 ],
 // so that a row costs one barrier. Everything is computed in fp32 and rounded once.
 //
+// Bound by memory: 4 bytes a value forward and 6 backward (bf16). 32768 x 4096, one B200: forward 88 us (6.1 TB/s), backward
+// 131 (6.1 TB/s), its column sums 6 behind it; 1021 x 2880 6.5 and 12 us.
+//
 // Three shapes, by width: rows of at most 512 columns belong to a warp (no barrier); up to 8192 columns a block has the
 // row in registers, eight columns a thread; wider rows are read again from the caches for the second look at them.
 // In the first two the backward pass keeps the columns' sums of dw and db in registers over all rows of a warp or block
@@ -167,7 +170,8 @@ layer_norm_forward_kernel(const LnParams p) {
 // The shape most rows take: a block has a row, a thread two groups of eight columns. A thread's words of the next rows are on
 // their way into places of its own in shared memory (cp.async), kLnAhead rows ahead: no barrier but the one of the sums, and
 // enough bytes in flight to fill the memory's latency (8 KB rows, two or three blocks an SM: 50 to 100 KB). Two
-// values an instruction.
+// values an instruction. What is in the loop beside the arithmetic decides: with 64-bit row counters, a test a column group
+// and true divisions the same kernels took 125 and 178 us where they take 88 and 131 now.
 constexpr int kLnAhead = 3, kLnRowsThreads = 512;
 template <int BYTES> __device__ __forceinline__ void cp_async(uint32_t to, const void* from) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
