@@ -406,8 +406,8 @@ typedef struct kdkl_label_loss_args {
   float* loss;                /* [1]; forward, step out */
   float* losses;              /* [T] or NULL; forward, step out */
   float* lse;                 /* [T] or NULL; forward, step out */
-  void* dhidden;              /* [T, H]; backward, step out */
-  void* dweight;              /* [V, H]; backward, step out */
+  void* dhidden;              /* [T, H]; backward, step out; or NULL (frozen hidden states), one product less */
+  void* dweight;              /* [V, H]; backward, step out; or NULL (a frozen head), the same */
   void* state;
   size_t state_bytes;
   void* workspace;

@@ -608,7 +608,8 @@ class _LabelLoss(torch.autograd.Function):
         T, H, V = hidden.shape[0], hidden.shape[1], weight.shape[0]
         op = L.LabelLoss(T, H, V, train=train, device=hidden.device, **args)
         if single_pass and train:
-            loss, dhidden, dweight = op.step(hidden, weight, labels, token_weight)
+            loss, dhidden, dweight = op.step(hidden, weight, labels, token_weight, want_dhidden=ctx.needs_input_grad[0],
+                                             want_dweight=ctx.needs_input_grad[1])
             ctx.save_for_backward(dhidden, dweight)
         else:
             loss = op.forward(hidden, weight, labels, token_weight)
@@ -626,10 +627,11 @@ class _LabelLoss(torch.autograd.Function):
         op = ctx.op
         if ctx.done:                           # the gradients are there, for an upstream gradient of 1
             dhidden, dweight = ctx.saved_tensors
-            return dhidden * grad.to(dhidden.dtype), dweight * grad.to(dweight.dtype), None, None, None, None, None, None, None
+            return (*(None if t is None else t * grad.to(t.dtype) for t in (dhidden, dweight)), None, None, None, None, None, None, None)
         hidden, weight, op.token_weight, op.state = ctx.saved_tensors
         op.args.state = op.state.data_ptr()
-        dhidden, dweight = op.backward(hidden, weight, grad.detach().to(torch.float32).contiguous(), per_token=ctx.per_token)
+        dhidden, dweight = op.backward(hidden, weight, grad.detach().to(torch.float32).contiguous(), per_token=ctx.per_token,
+                                       want_dhidden=ctx.needs_input_grad[0], want_dweight=ctx.needs_input_grad[1])
         _settle(op, ctx.sync_status)
         op.workspaces, op.dhidden, op.dweight, op.state, op.token_weight = {}, None, None, None, None
         return dhidden, dweight, None, None, None, None, None, None, None

@@ -90,7 +90,7 @@ static int check_label(const kdkl_label_loss_args* a, int mode) {
     if ((a->dhidden_type != KDKL_TYPE_BF16 && a->dhidden_type != KDKL_TYPE_F32) || (a->dweight_type != KDKL_TYPE_BF16 && a->dweight_type != KDKL_TYPE_F32))
       return KDKL_ERR_ARG;
     if ((a->accumulate != 0 && a->accumulate != 1) || (a->accumulate && a->dweight_type != KDKL_TYPE_F32)) return KDKL_ERR_ARG;
-    if (!a->dweight || (a->T > 0 && !a->dhidden)) return KDKL_ERR_NULL;
+    if (a->T > 0 && !a->dweight && !a->dhidden) return KDKL_ERR_NULL;
     if (((uintptr_t)a->dweight & 15) || ((uintptr_t)a->dhidden & 15)) return KDKL_ERR_ALIGN;
   }
   if (a->workspace_bytes < label_layout(a->T, a->H, a->V, a->chunk, mode, a->dweight_type).total) return KDKL_ERR_WORKSPACE;
@@ -158,7 +158,7 @@ static int label_run(const kdkl_label_loss_args* a, int mode, void* cuda_stream)
   if (T == 0) {
     if (sweep) KDKL_CUDA(cudaMemsetAsync(a->state, 0, 256, st));
     if (sweep) KDKL_CUDA(cudaMemsetAsync(a->loss, 0, 4, st));
-    if (grads && !a->accumulate) KDKL_CUDA(cudaMemsetAsync(a->dweight, 0, (size_t)V * H * (a->dweight_type == KDKL_TYPE_F32 ? 4 : 2), st));
+    if (grads && a->dweight && !a->accumulate) KDKL_CUDA(cudaMemsetAsync(a->dweight, 0, (size_t)V * H * (a->dweight_type == KDKL_TYPE_F32 ? 4 : 2), st));
     return KDKL_OK;
   }
   const unsigned by256 = (unsigned)((T + 255) / 256);
@@ -236,7 +236,8 @@ static int label_run(const kdkl_label_loss_args* a, int mode, void* cuda_stream)
     o.out = at<uint8_t>(a->dhidden, (size_t)s0 * H * (o.bf16 ? 2 : 4));
     o.plan = out_plan(rows, H, V, sm_count_or_default(), false);
     o.m_live = g.m_live;                                   // dead row tiles: zeros
-    if ((rc = launch_out<false>(o, di, st))) return rc;
+    if (a->dhidden && (rc = launch_out<false>(o, di, st))) return rc;
+    if (!a->dweight) continue;
     o.a = G; o.b = hidden;
     o.M = V; o.N = H; o.K = rows;
     o.m_live = nullptr;
@@ -247,7 +248,7 @@ static int label_run(const kdkl_label_loss_args* a, int mode, void* cuda_stream)
     o.accumulate = ci > 0 || a->accumulate ? 1 : 0;
     if ((rc = launch_out<true>(o, di, st))) return rc;
   }
-  if (grads && a->dweight_type == KDKL_TYPE_BF16 && L.chunks > 1) {
+  if (grads && a->dweight && a->dweight_type == KDKL_TYPE_BF16 && L.chunks > 1) {
     const long long n4 = V * H / 4;
     if ((rc = launch("label_round_kernel", label_round_kernel, dim3((unsigned)((n4 + 255) / 256)), 256, 0, st,
                      (const float*)at<float>(a->workspace, L.dw32), reinterpret_cast<uint2*>(a->dweight), n4, go)))

@@ -84,20 +84,25 @@ class LabelLoss:
             a.labels = _vector(labels, T, labels.dtype, "labels")
         a.token_weight = _vector(token_weight, T, torch.float32, "token_weight")
 
-    def _outputs(self, out, accumulate):
+    def _outputs(self, out, accumulate, want_dhidden=True, want_dweight=True):
         a = self.args
         if not self.train:
             raise RuntimeError("kdkl: this label loss was made for evaluation (train=False)")
-        if self.dhidden is None:
+        if not (want_dhidden or want_dweight):
+            raise ValueError("kdkl: a backward call without a gradient to compute")
+        if want_dhidden and self.dhidden is None:
             self.dhidden = torch.empty(self.T, self.H, dtype=self.dhidden_dtype, device=self.device)
-        if out is None:
+        if not want_dweight:
+            out = None
+        elif out is None:
             if self.dweight is None:
                 self.dweight = torch.zeros(self.V, self.H, dtype=self.dtype, device=self.device)
             out = self.dweight
         else:
             B._dptr(out, self.dtype, (self.V, self.H), "out")
-        a.dhidden, a.dweight, a.accumulate = self.dhidden.data_ptr(), out.data_ptr(), 1 if accumulate else 0
-        return out
+        a.dhidden, a.dweight = self.dhidden.data_ptr() if want_dhidden else None, None if out is None else out.data_ptr()
+        a.accumulate = 1 if accumulate else 0
+        return (self.dhidden if want_dhidden else None), out
 
     def _grad(self, grad):
         a = self.args
@@ -126,31 +131,31 @@ class LabelLoss:
         return self.loss
 
     def backward(self, hidden, weight, grad: Optional[torch.Tensor] = None, *, per_token: Optional[bool] = None,
-                 out: Optional[torch.Tensor] = None, accumulate: bool = False):
+                 out: Optional[torch.Tensor] = None, accumulate: bool = False, want_dhidden: bool = True, want_dweight: bool = True):
         """(dhidden, dweight) after a forward call on the same tensors. `grad`, fp32 on the device: of the loss (one element; 1 if
         None) or of the losses ([T]; `per_token` says which where T is 1). dweight goes to `out` if given; with
-        `accumulate` (fp32 only) it is added to what is there."""
+        `accumulate` (fp32 only) it is added to what is there. One that is not wanted is None and costs nothing."""
         if not self.fed:
             raise RuntimeError("kdkl: this label loss's backward call comes before any forward call")
-        out = self._outputs(out, accumulate)
+        grads = self._outputs(out, accumulate, want_dhidden, want_dweight)
         self._inputs(hidden, weight, None, self.token_weight)
         self._grad(grad)
         if per_token and self.T == 1:
             self.args.grad, self.args.grad_tokens = None, self.args.grad
-        self._run(_BACKWARD, [self.dhidden, out])
-        return self.dhidden, out
+        self._run(_BACKWARD, [t for t in grads if t is not None])
+        return grads
 
     def step(self, hidden, weight, labels, token_weight=None, grad: Optional[torch.Tensor] = None, *,
-             out: Optional[torch.Tensor] = None, accumulate: bool = False):
+             out: Optional[torch.Tensor] = None, accumulate: bool = False, want_dhidden: bool = True, want_dweight: bool = True):
         """(loss, dhidden, dweight) at once, for an upstream gradient of the loss that is known (1 if None)."""
-        out = self._outputs(out, accumulate)
+        grads = self._outputs(out, accumulate, want_dhidden, want_dweight)
         self._inputs(hidden, weight, labels, token_weight)
         if grad is not None and grad.numel() != 1:
             raise TypeError(f"kdkl: grad: expected that of the loss, one element, got {tuple(grad.shape)}")
         self.args.grad_tokens, self.args.grad = None, None if grad is None else B._dptr(grad.reshape(1), torch.float32, (1,), "grad").value
-        self._run(_STEP, [self.loss, self.losses, self.lse, self.state, self.dhidden, out])
+        self._run(_STEP, [self.loss, self.losses, self.lse, self.state, *(t for t in grads if t is not None)])
         self.token_weight, self.fed = token_weight, True
-        return self.loss, self.dhidden, out
+        return (self.loss, *grads)
 
     def status(self):
         """(code, [detail, counted tokens, labels out of range]) of the last calls on this state; waits for them."""

@@ -165,6 +165,26 @@ def test_a_gradient_that_is_added():
         LabelLoss(T, H, V).step(h, w, y, accumulate=True)
 
 
+def test_a_frozen_head_or_frozen_hidden_states():
+    T, H, V = 300, 64, 500
+    h, w, y, _ = _inputs(T, H, V)
+    op = LabelLoss(T, H, V)
+    _, dh, dw = (t.clone() for t in op.step(h, w, y))
+    assert torch.equal(op.step(h, w, y, want_dweight=False)[1], dh) and torch.equal(op.step(h, w, y, want_dhidden=False)[2], dw)
+    assert op.step(h, w, y, want_dweight=False)[2] is None
+    op.forward(h, w, y)
+    both = [t.clone() for t in op.backward(h, w)]
+    assert torch.equal(op.backward(h, w, want_dweight=False)[0], both[0]) and torch.equal(op.backward(h, w, want_dhidden=False)[1], both[1])
+    for single_pass in (False, True):
+        a, b = h.clone().requires_grad_(), w.clone().requires_grad_()
+        label_loss(a, w, y, single_pass=single_pass).backward()
+        label_loss(h, b, y, single_pass=single_pass).backward()
+        for got, want in ((a.grad, dh if single_pass else both[0]), (b.grad, dw if single_pass else both[1])):
+            assert torch.equal(got, want)
+    with pytest.raises(ValueError):
+        op.step(h, w, y, want_dhidden=False, want_dweight=False)
+
+
 def test_nothing_counted_and_labels_out_of_range():
     T, H, V = 300, 64, 100
     h, w, y, _ = _inputs(T, H, V)

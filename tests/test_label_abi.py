@@ -39,7 +39,7 @@ def test_refusals():
     for which in ("forward", "step"):
         assert _call(which, loss=None) == NULL and _call(which, labels=None) == NULL and _call(which, labels=P + 4) == ALIGN
     for which in ("backward", "step"):
-        assert _call(which, dhidden=None) == NULL and _call(which, dweight=None) == NULL and _call(which, dweight=P + 8) == ALIGN
+        assert _call(which, dhidden=None, dweight=None) == NULL and _call(which, dweight=P + 8) == ALIGN
         assert _call(which, dhidden_type=2) == ARG and _call(which, dweight_type=2) == ARG
         assert _call(which, accumulate=1) == ARG and _call(which, accumulate=2, dweight_type=1) == ARG
 
