@@ -657,6 +657,8 @@ def label_loss(hidden, weight, labels, token_weight: Optional[torch.Tensor] = No
         raise TypeError(f"label_loss: expected bf16, got {hidden.dtype} and {weight.dtype}")
     if hidden.shape[:-1] != labels.shape or (token_weight is not None and token_weight.shape != labels.shape):
         raise TypeError(f"label_loss: hidden {tuple(hidden.shape)} beside labels {tuple(labels.shape)}")
+    if token_weight is not None and token_weight.requires_grad:
+        raise TypeError("label_loss: token weights get no gradient: detach them, or weigh the losses of reduction \"none\"")
     if reduction not in ("mean", "sum", "none"):
         raise ValueError(f"label_loss: expected a reduction, got {reduction!r}")
     if reduction == "none" and (token_weight is not None or single_pass):

@@ -37,9 +37,12 @@ out_join_kernel(const float* part, long long slab, int splits, long long n4, con
   }
 }
 
-// The plan with the least estimated cycles: waves of units, a unit taking its k-blocks (512 cycles of tensor work each, 1024
-// in a WIDE tile, by the nominal rate) and about six more to start and to drain its tile; parts of a contraction cost
-// the slabs' way through memory (2600 bytes a cycle) and one more launch.
+// The plan with the least estimated cycles: waves of units, a unit taking its k-blocks (512 cycles of tensor work each by the
+// nominal rate, 952 in a WIDE tile, which brings a quarter less operand data a flop) and about six more to start and to
+// drain its tile (ten of a WIDE one's, whose stores nothing overlaps); parts of a contraction cost the slabs' way through memory (2600 bytes a cycle) and one more launch.
+// Measured (bf16 out; narrow, then WIDE, parts behind the slash): 1021 x 2816 x 14336 83 / 3 and 76 us / 3, 1021 x 2880 x 20000
+// 119 / 3 and 103 / 3, 8192 x 4096 x 131072 6823 / 1 and 6667 / 2, 131072 x 2048 x 8192 3390 / 1 and 3280 / 1; the other way
+// round 14336 x 2816 x 1021 80 / 1 and 84 / 1, 300 x 2048 x 11264 23 / 4 and 28 / 8, 4096 x 1024 x 4096 30 / 1 and 37 / 2.
 struct OutPlan { bool wide; int splits; };
 inline OutPlan out_plan(long long M, long long N, long long K, int sm_count, bool joined) {
   const long long workers = sm_count < 2 ? 1 : sm_count / 2, kb = (K + BK - 1) / BK, mt = (M + kTileM - 1) / kTileM;
@@ -51,7 +54,7 @@ inline OutPlan out_plan(long long M, long long N, long long K, int sm_count, boo
       if (sp > 1 && kb / sp < 8) break;
       if ((kb + sp - 1) / sp * (sp - 1) >= kb) continue;     // the last part would be empty
       const long long waves = (tiles * sp + workers - 1) / workers;
-      double cost = (double)waves * ((kb + sp - 1) / sp + 6) * (wide ? 1024.0 : 512.0);
+      double cost = (double)waves * ((kb + sp - 1) / sp + (wide ? 10 : 6)) * (wide ? 952.0 : 512.0);
       if (sp > 1 || joined) cost += 4000.0 + (double)M * N * (8.0 * sp + 2.0) / 2600.0;
       if (cost < least) { least = cost; best = OutPlan{wide != 0, sp}; }
     }

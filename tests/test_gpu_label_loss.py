@@ -327,6 +327,7 @@ def test_refusals():
     for bad in (lambda: op.forward(h.float(), w, y), lambda: op.forward(h, w[:50], y), lambda: op.forward(h, w, y[:8]),
                 lambda: op.forward(h, w, y, weight.double()), lambda: op.forward(h.cpu(), w, y),
                 lambda: op.step(h, w, y, grad=torch.ones(T, device="cuda")), lambda: label_loss(h, w, y[:8]),
+                lambda: label_loss(h, w, y, weight.clone().requires_grad_()),
                 lambda: label_loss(h.float(), w, y), lambda: op.forward(torch.zeros(T, 2 * H, dtype=BF16, device="cuda")[:, :H], w, y)):
         with pytest.raises(TypeError):
             bad()
