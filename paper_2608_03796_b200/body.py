@@ -38,6 +38,7 @@ def _lookup(table, key, name):
 
 
 _device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+_capturing = torch.cuda.is_current_stream_capturing
 # The library writes through addresses, which autograd does not see: a graph that has saved a tensor would use the new
 # values without a word. Every call therefore says which tensors it has written.
 _written = torch.autograd.graph.increment_version
@@ -500,8 +501,8 @@ class Rotary:
     than `original_length`, the one that was trained on; see kdkl_rotary_table for the formulas.
 
     Tokens and heads may lie any distance apart (the halves of one projection, or x.transpose(0, 1) of heads before
-    tokens); columns are neighbours. Outputs are the holder's own buffers, made for each new shape, or those given as `out`
-    (which may be the inputs themselves: then they are changed in place)."""
+    tokens); columns are neighbours. Outputs are the holder's own buffers, made for each new shape (and for each captured call,
+    to stay), or those given as `out` (which may be the inputs themselves: then they are changed in place)."""
 
     def __init__(self, D: int, rotary_dim: Optional[int] = None, *, base: float = 10000.0, layout: str = "half",
                  scaling: str = "none", factor: float = 1.0, original_length: int = 0, device="cuda"):
@@ -518,7 +519,7 @@ class Rotary:
         a.layout, a.head_dim, a.rotary_dim, a.magnitude = _lookup(LAYOUTS, layout, "layout"), D, R, magnitude.value
         self.turns = torch.tensor(list(turns), dtype=torch.float64).to(device)
         a.turns, self.at = self.turns.data_ptr(), self.turns.get_device()
-        self._call, self._own = B.lib().kdkl_rotary, {}
+        self._call, self._own, self._captured = B.lib().kdkl_rotary, {}, []
 
     def forward(self, q, k, positions, out=None):
         """(q, k) turned; k may be None."""
@@ -577,8 +578,10 @@ class Rotary:
                         f"got {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}")
 
     def _buffer(self, inverse, which, like):
-        if like is None:
-            return None
+        if _capturing():                                                        # a graph writes there as long as it is replayed
+            t = torch.empty(like.shape, dtype=like.dtype, device=like.device)
+            self._captured.append(t)
+            return t
         t = self._own.get((inverse, which))
         if t is None or t.shape != like.shape or t.dtype is not like.dtype or t.device != like.device:
             t = self._own[inverse, which] = torch.empty(like.shape, dtype=like.dtype, device=like.device)

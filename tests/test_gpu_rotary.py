@@ -191,6 +191,25 @@ def test_autograd_and_capture():
     _near(y, *_turned(x, flat, D, 32, "interleaved"), "replayed")
 
 
+def test_a_captured_call_keeps_its_outputs():
+    """Calls of other shapes between replays take other buffers, and none is freed under the graph."""
+    D, rope = 64, body.Rotary(64)
+    x, n = torch.randn(3, 4, D, device="cuda"), torch.arange(3, device="cuda")
+    rope.forward(x, None, n)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y, _ = rope.forward(x, None, n)
+    for T in (3, 500, 2):
+        other = torch.randn(T, 4, D, device="cuda")
+        z, _ = rope.forward(other, None, torch.arange(T, device="cuda"))
+        fill = [torch.full((T, 4, D), 5.0, device="cuda") for _ in range(8)]
+        want, n[0] = z.clone(), T
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(z, want) and all((f == 5).all() for f in fill)
+        _near(y, *_turned(x, n, D, D, "half"), "replayed")
+
+
 def test_refusals_on_the_device():
     rope = body.Rotary(64)
     x = torch.zeros(4, 2, 64, dtype=BF16, device="cuda")
