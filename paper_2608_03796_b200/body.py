@@ -38,7 +38,7 @@ def _lookup(table, key, name):
 
 
 _device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
-_capturing = torch.cuda.is_current_stream_capturing
+_capturing = torch._C._cuda_isCurrentStreamCapturing
 # The library writes through addresses, which autograd does not see: a graph that has saved a tensor would use the new
 # values without a word. Every call therefore says which tensors it has written.
 _written = torch.autograd.graph.increment_version
@@ -540,7 +540,8 @@ class Rotary:
         heads, a.q, a.q_token, a.q_head = self._heads(q, T, dtype, "q", now)
         a.q_heads = heads
         if out is None:
-            y = self._buffer(inverse, 0, q)
+            captured = _capturing()
+            y = self._buffer(inverse, 0, q, captured)
             a.q_out, a.q_out_token, a.q_out_head = y.data_ptr(), heads * D, D
         else:
             y = out[0]
@@ -552,7 +553,7 @@ class Rotary:
             heads, a.k, a.k_token, a.k_head = self._heads(k, T, dtype, "k", now)
             a.k_heads = heads
             if out is None:
-                z = self._buffer(inverse, 1, k)
+                z = self._buffer(inverse, 1, k, captured)
                 a.k_out, a.k_out_token, a.k_out_head = z.data_ptr(), heads * D, D
             else:
                 z = out[1]
@@ -577,8 +578,8 @@ class Rotary:
         raise TypeError(f"kdkl: {name}: expected {dtype} [{T}, heads, {self.D}] on the current CUDA device, columns contiguous, "
                         f"got {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}")
 
-    def _buffer(self, inverse, which, like):
-        if _capturing():                                                        # a graph writes there as long as it is replayed
+    def _buffer(self, inverse, which, like, captured):
+        if captured:                                                        # a graph writes there as long as it is replayed
             t = torch.empty(like.shape, dtype=like.dtype, device=like.device)
             self._captured.append(t)
             return t
