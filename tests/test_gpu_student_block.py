@@ -182,3 +182,36 @@ def test_what_holders_write_is_known_as_changed():
     norm.forward(x, one, one)
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         z.sum().backward()
+
+
+def test_calls_on_two_streams_at_once():
+    """Holders of their own on two streams, kernels for few and for many tokens beside one another (tensor memory, clusters): the
+    same bits as one after the other."""
+    def calls(T, seed):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+
+        def rand(*s):
+            return torch.randn(*s, generator=g, device="cuda").to(BF16)
+        h, f, v = 512, 1536, 5000
+        x, gu, head, dh, one = rand(T, h), rand(2 * f, h) / 20, rand(v, h) / 20, rand(T, f), rand(h)
+        y, places = torch.randint(0, v, (T,), generator=g, device="cuda"), torch.arange(T, device="cuda")
+        norm, ffn, ce, rope = body.LayerNorm(T, h), body.GatedLinear(T, h, f), LabelLoss(T, h, v), body.Rotary(64)
+
+        def run():
+            out = [norm.forward(x, one, one), *norm.backward(x)]
+            out += [ffn.forward(x, gu), *ffn.backward(dh)]
+            out += [*ce.step(x, head, y), ce.losses, rope.forward(x.view(T, 8, 64), None, places)[0]]
+            return out
+        return run
+    runs = [calls(T, T) for T in (1, 20, 100, 700)]
+    want = [[t.clone() for t in run()] for run in runs]
+    streams = [torch.cuda.Stream() for _ in runs]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        outs = []
+        for run, stream in zip(runs, streams):
+            with torch.cuda.stream(stream):
+                outs.append(run())
+    torch.cuda.synchronize()
+    for got, ref in zip(outs, want):
+        assert all(torch.equal(a, b) for a, b in zip(got, ref))
