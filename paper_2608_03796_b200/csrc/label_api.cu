@@ -48,12 +48,14 @@ static LabelLayout label_layout(long long T, long long H, long long V, long long
   L.n_tiles = T <= kLabelFewTokens ? (V + kLabelFewRows - 1) / kLabelFewRows : (V + BN - 1) / BN;
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t o = at; at = up(at + bytes, 256); return o; };
+  const bool grads = mode != kLabelForward;
+  if (grads) L.G = take((size_t)L.C * L.Vpad * 2);
+  const size_t shared = at;
   if (mode != kLabelBackward) {
     L.part_m = take((size_t)L.n_tiles * L.C * 4); L.part_s = take((size_t)L.n_tiles * L.C * 4); L.part_z = take((size_t)L.n_tiles * L.C * 4);
+    if (grads) L.win = take((size_t)((V + 31) / 32) * L.C * 4);
   }
-  if (mode != kLabelForward) {
-    L.G = take((size_t)L.C * L.Vpad * 2);
-    if (mode == kLabelStep) L.win = take((size_t)((V + 31) / 32) * L.C * 4);
+  if (grads) {
     const int sms = sm_count_or_default();
     size_t slab = 0;
     for (long long rows : {L.chunks > 1 ? L.C : L.last, L.last}) {
@@ -62,7 +64,10 @@ static LabelLayout label_layout(long long T, long long H, long long V, long long
       if (a > slab) slab = a;
       if (b > slab) slab = b;
     }
-    L.slab = take(slab);
+    // A chunk's products come after the last reader of its partials and maxima, and before the next chunk's sweep: their
+    // parts lie in the same place (8192 x 2048 x 131072: 268 MB over 185 MB, beside a G of 2.1 GB).
+    L.slab = shared;
+    if (at < shared + slab) at = up(shared + slab, 256);
     // a bf16 gradient over several chunks is summed in fp32 and rounded once
     if (L.chunks > 1 && dw_type == KDKL_TYPE_BF16) L.dw32 = take((size_t)V * H * 4);
   }
