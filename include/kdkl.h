@@ -47,7 +47,8 @@ extern "C" {
 #define KDKL_ERR_TIMEOUT (-8)   /* a bounded wait inside a kernel expired */
 #define KDKL_ERR_STATE (-9)     /* backward called on a workspace forward did not fill for this shape, chunk size and
                                    temperature (or, with stored_exponentials, whose exponentials are gone) */
-#define KDKL_ERR_INDEX (-10)    /* a teacher index >= V was seen (the entry was ignored) */
+#define KDKL_ERR_INDEX (-10)    /* a teacher index >= V or a label out of range was seen (the entry was ignored, the results
+                                   stand); any other code takes its place, and detail[2] has the count */
 #define KDKL_ERR_NONFINITE (-11)/* a counted token's loss is not finite */
 #define KDKL_ERR_RANGE (-13)    /* stored exponentials only (kdkl_forward_backward, option stored_exponentials): a
                                    counted token's scaled logits all lie below the range the bf16 exponentials

@@ -249,7 +249,7 @@ e_to_g_kernel(__nv_bfloat16* __restrict__ G, long long ldg /* elements per row *
       g_row[v] = buf[i];
     }
   }
-  if (bad) { atomicCAS(&hdr->status, 0, -11); atomicCAS(&hdr->where, 0, (int)row); }
+  if (bad) report_error(&hdr->status, -11, (int)row);
   // support entries of this row that fall into the segment (sorted ascending, duplicates merged by prep)
   const int nv = nvalid[row];
   if (nv == 0) return;
@@ -388,9 +388,7 @@ combine_kernel(const float* __restrict__ part_m, const float* __restrict__ part_
     const float l2 = row_counted ? mm + log2f(ss) : 0.f;
     // stored exponentials carry a fixed bias instead of the row maximum: a row whose scaled logits all sit
     // far below zero would flush to zero there (its softmax term would vanish from G unnoticed)
-    if (exp_stored && row_counted && l2 < kExpStoreMinLz2) {
-      atomicCAS(&hdr->status, 0, -13); atomicCAS(&hdr->where, 0, (int)(row0 + r));
-    }
+    if (exp_stored && row_counted && l2 < kExpStoreMinLz2) report_error(&hdr->status, -13, (int)(row0 + r));
     sm_lz[tx] = l2;
     lz2[row0 + r] = l2;
     logZ_nat[row0 + r] = l2 * kLn2;
@@ -428,7 +426,7 @@ combine_kernel(const float* __restrict__ part_m, const float* __restrict__ part_
       float L = 0.f;
       if (counted) {
         L = Hent[t] - c + Mv[t] * lz;
-        if (!isfinite(L)) { atomicCAS(&hdr->status, 0, -11); atomicCAS(&hdr->where, 0, (int)t); }
+        if (!isfinite(L)) report_error(&hdr->status, -11, (int)t);
       }
       loss_tok[t] = L;
       if (loss_tok_user) loss_tok_user[t] = L;
@@ -461,7 +459,7 @@ __global__ void shard_finish_kernel(const float* __restrict__ all_stats, int R, 
   float L = 0.f;
   if (counted) {
     L = Hent[t] - c + Mv[t] * l2 * kLn2;
-    if (!isfinite(L)) { atomicCAS(&hdr->status, 0, -11); atomicCAS(&hdr->where, 0, (int)t); }
+    if (!isfinite(L)) report_error(&hdr->status, -11, (int)t);
   }
   loss_tok[t] = L;
   if (loss_tok_user) loss_tok_user[t] = L;
@@ -524,7 +522,7 @@ __global__ void bwd_coef_kernel(const float* __restrict__ Mv, const uint8_t* __r
   if (blockIdx.x == 0 && threadIdx.x == 0) {
     hdr->go = state_ok ? 1 : 0;
     hdr->neg_grad = grad_loss < 0.f ? 1 : 0;
-    if (!state_ok) atomicCAS(&hdr->status, 0, -9);
+    if (!state_ok) report_error(&hdr->status, -9, 0);
   }
   if (!state_ok) return;
   const float denom = hdr->denom;
@@ -697,7 +695,7 @@ topk_select_kernel(const int* __restrict__ cand_cnt, const int* __restrict__ can
   const int row = blockIdx.x, lane = threadIdx.x;
   int n = cand_cnt[row];
   if (n > cap) {
-    if (lane == 0) { atomicCAS(status, 0, -12); atomicCAS(status + 1, 0, (int)(row0 + row)); }
+    if (lane == 0) report_error(status, -12, (int)(row0 + row));
     n = cap;
   }
   for (int i = lane; i < cpad; i += 32) {

@@ -709,10 +709,8 @@ gemm_tcgen05_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
               }
               e_fac = row_zero ? 0.f : ex2_approx(m_new - kExpBias);
               // bf16 tops out just below 2^128: a scaled logit beyond bias + 128 cannot be stored
-              if (m_new - kExpBias >= 128.f && !row_zero && p.status != nullptr) {
-                atomicCAS(p.status, 0, -11);               // KDKL_ERR_NONFINITE, with the token
-                atomicCAS(p.status + 1, 0, (int)(p.row_base + row));
-              }
+              if (m_new - kExpBias >= 128.f && !row_zero && p.status != nullptr)
+                report_error(p.status, -11, (int)(p.row_base + row));      // KDKL_ERR_NONFINITE, with the token
             } else if (EPI == EPI_LABEL_E) {
               const float w_max = col0 < p.N ? wmax * p.scale_log2 : m_new;   // (a window past the last column has no largest)
 #pragma unroll

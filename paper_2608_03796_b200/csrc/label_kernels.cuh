@@ -156,7 +156,7 @@ label_combine_kernel(const LabelParams p, const float* part_m, const float* part
         const float inv_tau = 1.f / p.tau;
         // taken from the normaliser, so that a confident token's small loss keeps its digits
         loss = (1.f - p.smoothing) * (lse - z_label * inv_tau) + p.smoothing * (lse - z * inv_tau / (float)p.V) + p.z_loss * lse * lse;
-        if (!isfinite(loss)) { atomicCAS(&p.hdr->status, 0, -11); atomicCAS(&p.hdr->where, 0, (int)tok); }
+        if (!isfinite(loss)) report_error(&p.hdr->status, -11, (int)tok);
       }
       p.lz2[tok] = lz2;
       p.losses[tok] = loss;
@@ -209,7 +209,7 @@ label_coef_kernel(const LabelParams p) {
   if (blockIdx.x == 0 && threadIdx.x == 0) {
     p.hdr->go = ok ? 1 : 0;
     label_scale(p, h->n_tokens);
-    if (!ok) atomicCAS(&p.hdr->status, 0, -9);             // KDKL_ERR_STATE
+    if (!ok) report_error(&p.hdr->status, -9, 0);          // KDKL_ERR_STATE
   }
   const long long t = (long long)blockIdx.x * 256 + threadIdx.x;
   if (ok && t < p.T) label_coefs(p, t, p.lz2[t] * kLn2);

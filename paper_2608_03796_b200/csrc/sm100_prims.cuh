@@ -79,6 +79,13 @@ __device__ __forceinline__ bool elect_one() {
 template <int N> __device__ __forceinline__ void regs_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N> __device__ __forceinline__ void regs_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
+// An error goes into a status block's first two words, code and detail, if there is none yet. -10 (KDKL_ERR_INDEX: entries were
+// ignored, the results stand) is a note and gives way to an error.
+__device__ __forceinline__ void report_error(int* status, int code, int where) {
+  const int old = atomicCAS(status, 0, code);
+  if (old == 0 || (old == -10 && atomicCAS(status, -10, code) == -10)) atomicExch(status + 1, where);
+}
+
 // Bounded wait. Returns false when the CTA has aborted (flag set by any role) or the
 // limit expired (then it sets the flag itself and records `where` in the status word).
 template <bool PAIR = false>
@@ -94,10 +101,7 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
       if (*abort_flag) return false;
       if (globaltimer_ns() - t0 > limit_ns) {
         *abort_flag = 1;
-        if (status_word != nullptr) {
-          atomicCAS(status_word, 0, -8);       // KDKL_ERR_TIMEOUT
-          atomicCAS(status_word + 1, 0, where);
-        }
+        if (status_word != nullptr) report_error(status_word, -8, where);   // KDKL_ERR_TIMEOUT
         return false;
       }
     }
