@@ -419,6 +419,10 @@ size_t kdkl_label_loss_workspace_bytes(int64_t T, int64_t H, int64_t V, int64_t 
 int kdkl_label_loss_forward(const kdkl_label_loss_args* args, void* cuda_stream);
 int kdkl_label_loss_backward(const kdkl_label_loss_args* args, void* cuda_stream);
 int kdkl_label_loss_step(const kdkl_label_loss_args* args, void* cuda_stream);
+/* out = gradient * *factor, the product in fp32 and rounded once: the gradients of a step whose upstream gradient (a device float)
+ * becomes known only afterwards. type KDKL_TYPE_BF16 or _F32, count elements (a multiple of 8), 16-byte aligned; out may be
+ * gradient. */
+int kdkl_label_loss_rescale(const void* gradient, int32_t type, int64_t count, const float* factor, void* out, void* cuda_stream);
 
 /* ------------------------------------------------------------------ operators of the student's body
  * The loss above never holds the T x V logits; what then grows with T in a distillation step is what the student's

@@ -626,8 +626,8 @@ class _LabelLoss(torch.autograd.Function):
     def backward(ctx, grad):
         op = ctx.op
         if ctx.done:                           # the gradients are there, for an upstream gradient of 1
-            dhidden, dweight = ctx.saved_tensors
-            return (*(None if t is None else t * grad.to(t.dtype) for t in (dhidden, dweight)), None, None, None, None, None, None, None)
+            factor = grad.detach().to(torch.float32)
+            return (*(None if t is None else L.rescaled(t, factor) for t in ctx.saved_tensors), None, None, None, None, None, None, None)
         hidden, weight, op.token_weight, op.state = ctx.saved_tensors
         op.args.state = op.state.data_ptr()
         dhidden, dweight = op.backward(hidden, weight, grad.detach().to(torch.float32).contiguous(), per_token=ctx.per_token,

@@ -38,6 +38,7 @@ EXPORTS = [
     "kdkl_rotary_table", "kdkl_rotary", "kdkl_gated_linear_workspace_bytes", "kdkl_gated_linear_forward",
     "kdkl_gated_linear_backward", "kdkl_label_loss_state_bytes", "kdkl_label_loss_workspace_bytes",
     "kdkl_label_loss_forward", "kdkl_label_loss_backward", "kdkl_label_loss_step",
+    "kdkl_label_loss_rescale",
 ]
 
 FEATURE_MSE, FEATURE_COSINE = 0, 1
@@ -173,6 +174,8 @@ def lib() -> ctypes.CDLL:
     for name in ("kdkl_label_loss_forward", "kdkl_label_loss_backward", "kdkl_label_loss_step"):
         getattr(L, name).restype = ctypes.c_int
         getattr(L, name).argtypes = [vp, vp]
+    L.kdkl_label_loss_rescale.restype = ctypes.c_int
+    L.kdkl_label_loss_rescale.argtypes = [vp, i32, i64, vp, vp, vp]
     L.kdkl_wait_selftest.restype = ctypes.c_int
     L.kdkl_wait_selftest.argtypes = [vp, i64, vp]
     L.kdkl_last_error.restype = ctypes.c_char_p

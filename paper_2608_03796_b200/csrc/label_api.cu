@@ -2,6 +2,8 @@
 #include <math.h>
 #include <string.h>
 
+#include <type_traits>
+
 #include "body_host.cuh"
 #include "gemm_out.cuh"
 #include "label_few_kernels.cuh"
@@ -274,5 +276,21 @@ size_t kdkl_label_loss_workspace_bytes(int64_t T, int64_t H, int64_t V, int64_t 
 int kdkl_label_loss_forward(const kdkl_label_loss_args* a, void* cuda_stream) { return label_run(a, kLabelForward, cuda_stream); }
 int kdkl_label_loss_backward(const kdkl_label_loss_args* a, void* cuda_stream) { return label_run(a, kLabelBackward, cuda_stream); }
 int kdkl_label_loss_step(const kdkl_label_loss_args* a, void* cuda_stream) { return label_run(a, kLabelStep, cuda_stream); }
+int kdkl_label_loss_rescale(const void* gradient, int32_t type, int64_t count, const float* factor, void* out, void* cuda_stream) {
+  g_launches = 0;
+  if (type != KDKL_TYPE_BF16 && type != KDKL_TYPE_F32) return KDKL_ERR_ARG;
+  const long long words = count / (type == KDKL_TYPE_F32 ? 4 : 8);
+  if (count < 0 || count % 8 || words >= (1ll << 38)) return KDKL_ERR_SHAPE;
+  if (!factor || (count > 0 && (!gradient || !out))) return KDKL_ERR_NULL;
+  if (((uintptr_t)gradient & 15) || ((uintptr_t)out & 15) || ((uintptr_t)factor & 3)) return KDKL_ERR_ALIGN;
+  if (count == 0) return KDKL_OK;
+  DeviceInfo di;
+  int rc = need_b200(&di);
+  if (rc) return rc;
+  KDKL_BY_BOOL(type == KDKL_TYPE_F32, F32,
+    rc = launch("label_rescale_kernel", label_rescale_kernel<std::conditional_t<F32, float, __nv_bfloat16>>, dim3((unsigned)((words + 255) / 256)), 256,
+                0, reinterpret_cast<cudaStream_t>(cuda_stream), reinterpret_cast<const uint4*>(gradient), factor, reinterpret_cast<uint4*>(out), words));
+  return rc;
+}
 
 }  // extern "C"

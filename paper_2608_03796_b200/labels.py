@@ -160,3 +160,13 @@ class LabelLoss:
     def status(self):
         """(code, [detail, counted tokens, labels out of range]) of the last calls on this state; waits for them."""
         return B.kdkl_status(self.state)
+
+
+def rescaled(gradient: torch.Tensor, factor: torch.Tensor) -> torch.Tensor:
+    """A gradient that a step has left, times an upstream gradient that became known later (one fp32 element on the device), in a
+    tensor of its own: rounded once, and the factor not at all (kdkl_label_loss_rescale)."""
+    out = torch.empty_like(gradient)
+    B._check(B.lib().kdkl_label_loss_rescale(
+        B._dptr(gradient, gradient.dtype, gradient.shape, "gradient"), _lookup(TYPES, gradient.dtype, "gradient"), gradient.numel(),
+        B._dptr(factor.reshape(1), torch.float32, (1,), "factor"), out.data_ptr(), _stream(out.get_device(), "gradient")))
+    return out
