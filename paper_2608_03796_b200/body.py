@@ -501,8 +501,9 @@ class Rotary:
     than `original_length`, the one that was trained on; see kdkl_rotary_table for the formulas.
 
     Tokens and heads may lie any distance apart (the halves of one projection, or x.transpose(0, 1) of heads before
-    tokens); columns are neighbours. Outputs are the holder's own buffers, made for each new shape (and for each captured call,
-    to stay), or those given as `out` (which may be the inputs themselves: then they are changed in place)."""
+    tokens); columns are neighbours. Outputs are the holder's own buffers, made for each stream and new shape (and for each captured call,
+    to stay), or those given as `out` (which may be the inputs themselves: then they are changed in place). Threads that share
+    a table give their outputs, or each has a stream of its own."""
 
     def __init__(self, D: int, rotary_dim: Optional[int] = None, *, base: float = 10000.0, layout: str = "half",
                  scaling: str = "none", factor: float = 1.0, original_length: int = 0, device="cuda"):
@@ -519,7 +520,7 @@ class Rotary:
         a.layout, a.head_dim, a.rotary_dim, a.magnitude = _lookup(LAYOUTS, layout, "layout"), D, R, magnitude.value
         self.turns = torch.tensor(list(turns), dtype=torch.float64).to(device)
         a.turns, self.at = self.turns.data_ptr(), self.turns.get_device()
-        self._call, self._own, self._captured = B.lib().kdkl_rotary, {}, []
+        self._call, self._streams, self._own, self._captured = B.lib().kdkl_rotary, {}, {}, []
 
     def forward(self, q, k, positions, out=None):
         """(q, k) turned; k may be None."""
@@ -530,7 +531,7 @@ class Rotary:
         return self._run(dq, dk, positions, out, 1)
 
     def _run(self, q, k, positions, out, inverse):
-        a = kdkl_rotary_args.from_buffer_copy(self.args)     # a call's own: several threads may share a table
+        a = kdkl_rotary_args.from_buffer_copy(self.args)     # a call's own: threads that give outputs may share a table
         now, dtype, D, T = _device(), q.dtype, self.D, positions.shape[0] if positions.dim() == 1 else -1
         if positions.get_device() != now or positions.dtype not in _POSITIONS or T < 0 or (T > 1 and positions.stride(0) != 1):
             raise TypeError(f"kdkl: positions: expected contiguous int32 or int64 [T] on the current CUDA device, got "
@@ -538,10 +539,11 @@ class Rotary:
         a.T, a.positions, a.wide_positions, a.inverse, a.type = T, positions.data_ptr(), _POSITIONS[positions.dtype], inverse, \
             _lookup(TYPES, dtype, "q")
         heads, a.q, a.q_token, a.q_head = self._heads(q, T, dtype, "q", now)
-        a.q_heads = heads
+        a.q_heads, stream = heads, _stream(self.at, "rotary table")
         if out is None:
             captured = _capturing()
-            y = self._buffer(inverse, 0, q, captured)
+            own = self._buffers(stream)
+            y = self._buffer(own, inverse, 0, q, captured)
             a.q_out, a.q_out_token, a.q_out_head = y.data_ptr(), heads * D, D
         else:
             y = out[0]
@@ -553,14 +555,14 @@ class Rotary:
             heads, a.k, a.k_token, a.k_head = self._heads(k, T, dtype, "k", now)
             a.k_heads = heads
             if out is None:
-                z = self._buffer(inverse, 1, k, captured)
+                z = self._buffer(own, inverse, 1, k, captured)
                 a.k_out, a.k_out_token, a.k_out_head = z.data_ptr(), heads * D, D
             else:
                 z = out[1]
                 n, a.k_out, a.k_out_token, a.k_out_head = self._heads(z, T, dtype, "k's output", now)
                 self._same(n, heads)
             outs = written = (y, z)
-        B._check(self._call(ctypes.byref(a), _stream(self.at, "rotary table")))
+        B._check(self._call(ctypes.byref(a), stream))
         _written(written)
         return outs
 
@@ -578,14 +580,23 @@ class Rotary:
         raise TypeError(f"kdkl: {name}: expected {dtype} [{T}, heads, {self.D}] on the current CUDA device, columns contiguous, "
                         f"got {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}")
 
-    def _buffer(self, inverse, which, like, captured):
+    def _buffers(self, stream):
+        """The outputs of calls on a stream. The allocator gives what is dropped to later work of the stream that it was made
+        on: a buffer that calls on two streams write could not be replaced while the other one's are under way."""
+        own = self._streams.get(stream)
+        if own is None:
+            own = self._streams.setdefault(stream, {})
+        self._own = own
+        return own
+
+    def _buffer(self, own, inverse, which, like, captured):
         if captured:                                                        # a graph writes there as long as it is replayed
             t = torch.empty(like.shape, dtype=like.dtype, device=like.device)
             self._captured.append(t)
             return t
-        t = self._own.get((inverse, which))
+        t = own.get((inverse, which))
         if t is None or t.shape != like.shape or t.dtype is not like.dtype or t.device != like.device:
-            t = self._own[inverse, which] = torch.empty(like.shape, dtype=like.dtype, device=like.device)
+            t = own[inverse, which] = torch.empty(like.shape, dtype=like.dtype, device=like.device)
         return t
 
 

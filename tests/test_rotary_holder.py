@@ -1,0 +1,37 @@
+"""What a rotary table owes its callers on the host. No GPU needed: the entry point is replaced where a call would reach it."""
+import pytest
+import torch
+
+from paper_2608_03796_b200 import body
+
+
+@pytest.fixture
+def rope(monkeypatch):
+    """A rotary table on the host whose calls reach nothing; (table, a function that sets the current stream, and one that says
+    whether it captures)."""
+    now = {"stream": 1, "capturing": False}
+    monkeypatch.setattr(body, "_device", lambda: -1)
+    monkeypatch.setattr(body, "_raw_stream", lambda device: now["stream"])
+    monkeypatch.setattr(body, "_capturing", lambda: now["capturing"])
+    r = body.Rotary(8, device="cpu")
+    r._call = lambda *args: 0
+    return r, lambda s: now.update(stream=s), lambda c: now.update(capturing=c)
+
+
+def _turn(r, T, heads=2):
+    return r.forward(torch.zeros(T, heads, 8), torch.zeros(T, 1, 8), torch.arange(T))
+
+
+def test_rotary_outputs_belong_to_a_stream(rope):
+    """The allocator gives freed memory to later work of the stream that it was allocated on, at once. A buffer that another
+    stream's call has written, and that the next shape then replaces, would be given away under that call's kernel."""
+    r, stream, _ = rope
+    a = _turn(r, 3)
+    stream(2)
+    b = _turn(r, 3)
+    assert a[0].data_ptr() != b[0].data_ptr() and a[1].data_ptr() != b[1].data_ptr()
+    b = _turn(r, 5)                                                         # another length on the second stream
+    stream(1)
+    again = _turn(r, 3)                                                     # the first one's are where they were
+    assert again[0] is a[0] and again[1] is a[1]
+    assert b[0].shape == (5, 2, 8)
