@@ -11,9 +11,10 @@ read them in the backward pass.
     ffn = GatedLinear(T, H, F); h = ffn.forward(x, W_gate_up); dx, dW = ffn.backward(dh)
     rope = Rotary(D); q_, k_ = rope.forward(q, k, positions); dq, dk = rope.backward(dq_, dk_, positions)
 
-The classes hold outputs, records and workspaces of one shape: calls allocate nothing, only enqueue on the current
-stream, and return the holder's own buffers, which the next call overwrites (a graph of autograd's that has saved one of
-them raises then). Marshalling only; autograd entries that allocate their outputs are in ``autograd``. Formats are "int8", "e4m3" or None (nothing is kept in 8 bits).
+The classes hold outputs, records and workspaces of one shape (Rotary: its table, and outputs of the last shape): calls only
+enqueue on the current stream and return the holder's own buffers, which the next call overwrites (a graph of autograd's that has
+saved one of them raises then). What only a backward pass needs is allocated by the first one, and a Rotary's outputs by
+a call of a new shape; calls allocate nothing else. Marshalling only; autograd entries that allocate their outputs are in ``autograd``. Formats are "int8", "e4m3" or None (nothing is kept in 8 bits).
 """
 from __future__ import annotations
 
@@ -501,9 +502,10 @@ class Rotary:
     than `original_length`, the one that was trained on; see kdkl_rotary_table for the formulas.
 
     Tokens and heads may lie any distance apart (the halves of one projection, or x.transpose(0, 1) of heads before
-    tokens); columns are neighbours. Outputs are the holder's own buffers, made for each stream and new shape (and for each captured call,
-    to stay), or those given as `out` (which may be the inputs themselves: then they are changed in place). Threads that share
-    a table give their outputs, or each has a stream of its own."""
+    tokens); columns are neighbours. Outputs are the holder's own buffers, made for each stream and new shape, or those given as
+    `out` (which may be the inputs themselves: then they are changed in place). A call that is captured into a graph makes new
+    ones, which live in the graph's memory and belong to the caller. Threads that share a table give their outputs, or each has
+    a stream of its own."""
 
     def __init__(self, D: int, rotary_dim: Optional[int] = None, *, base: float = 10000.0, layout: str = "half",
                  scaling: str = "none", factor: float = 1.0, original_length: int = 0, device="cuda"):
@@ -520,7 +522,7 @@ class Rotary:
         a.layout, a.head_dim, a.rotary_dim, a.magnitude = _lookup(LAYOUTS, layout, "layout"), D, R, magnitude.value
         self.turns = torch.tensor(list(turns), dtype=torch.float64).to(device)
         a.turns, self.at = self.turns.data_ptr(), self.turns.get_device()
-        self._call, self._streams, self._own, self._captured = B.lib().kdkl_rotary, {}, {}, []
+        self._call, self._streams, self._own = B.lib().kdkl_rotary, {}, {}
 
     def forward(self, q, k, positions, out=None):
         """(q, k) turned; k may be None."""
@@ -590,10 +592,8 @@ class Rotary:
         return own
 
     def _buffer(self, own, inverse, which, like, captured):
-        if captured:                                                        # a graph writes there as long as it is replayed
-            t = torch.empty(like.shape, dtype=like.dtype, device=like.device)
-            self._captured.append(t)
-            return t
+        if captured:                        # the graph's memory, the caller's to keep: a replay must not write into eager calls' outputs
+            return torch.empty(like.shape, dtype=like.dtype, device=like.device)
         t = own.get((inverse, which))
         if t is None or t.shape != like.shape or t.dtype is not like.dtype or t.device != like.device:
             t = own[inverse, which] = torch.empty(like.shape, dtype=like.dtype, device=like.device)

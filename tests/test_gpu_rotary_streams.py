@@ -25,3 +25,23 @@ def test_lengths_that_change_on_one_of_two_streams():
         assert all((f == 5).all() for f in fill)
     again, _ = rope.forward(x, None, n)
     assert again.data_ptr() == y.data_ptr()
+
+
+def test_captures_again_and_again():
+    """What a captured call made goes with its graph: capturing the same work anew needs no more memory each time."""
+    D, rope = 128, body.Rotary(128)
+    x, n = torch.randn(4096, 8, D, device="cuda"), torch.arange(4096, device="cuda")
+    rope.forward(x, x, n)
+    torch.cuda.synchronize()
+    sizes = []
+    for k in range(4):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            q, key = rope.forward(x, x, n)
+            total = q + key
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(total, 2 * rope.forward(x, None, n)[0])
+        del graph, q, key, total
+        sizes.append(torch.cuda.memory_allocated())
+    assert sizes[-1] == sizes[0]

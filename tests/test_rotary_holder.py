@@ -1,4 +1,7 @@
 """What a rotary table owes its callers on the host. No GPU needed: the entry point is replaced where a call would reach it."""
+import gc
+import weakref
+
 import pytest
 import torch
 
@@ -35,3 +38,19 @@ def test_rotary_outputs_belong_to_a_stream(rope):
     again = _turn(r, 3)                                                     # the first one's are where they were
     assert again[0] is a[0] and again[1] is a[1]
     assert b[0].shape == (5, 2, 8)
+
+
+def test_rotary_keeps_nothing_of_a_captured_call(rope):
+    """Outputs made while a graph is captured live in the graph's memory as long as the graph does; the caller has them, and a
+    table that is captured again and again does not pile them up."""
+    r, _, capture = rope
+    eager = _turn(r, 3)
+    capture(True)
+    first, second = _turn(r, 3), _turn(r, 3)
+    assert len({t.data_ptr() for t in (*eager, *first, *second)}) == 6
+    refs = [weakref.ref(t) for t in (*first, *second)]
+    del first, second
+    gc.collect()
+    assert all(ref() is None for ref in refs)
+    capture(False)
+    assert _turn(r, 3)[0] is eager[0]
