@@ -323,12 +323,13 @@ class BlockNorm:
         return buffers
 
     def _grad(self, name, like):
-        """The holder's gradient buffer for a weight or gate (made when first needed, or when its type changes)."""
+        """The holder's gradient buffer for a weight or gate (made when first needed, one for each type: the kernels of another
+        stream may still be at work on what would be given up)."""
         if like is None:
             return None
-        t = self.grads.get(name)
-        if t is None or t.dtype != like.dtype:
-            t = self.grads[name] = torch.empty_like(like)
+        t = self.grads.get((name, like.dtype))
+        if t is None:
+            t = self.grads[name, like.dtype] = torch.empty_like(like)
         return t
 
     def backward(self, dy, dsum=None) -> BlockNormGrads:
@@ -448,11 +449,12 @@ class LayerNorm:
         return [r.buffer for r in kept]
 
     def _grad(self, name, like):
+        """As BlockNorm's."""
         if like is None:
             return None
-        t = self.grads.get(name)
-        if t is None or t.dtype != like.dtype:
-            t = self.grads[name] = torch.empty_like(like)
+        t = self.grads.get((name, like.dtype))
+        if t is None:
+            t = self.grads[name, like.dtype] = torch.empty_like(like)
         return t
 
     def backward(self, dy) -> LayerNormGrads:
