@@ -607,6 +607,7 @@ class _LabelLoss(torch.autograd.Function):
     def forward(ctx, hidden, weight, labels, token_weight, args, per_token, single_pass, train, sync_status):
         T, H, V = hidden.shape[0], hidden.shape[1], weight.shape[0]
         op = L.LabelLoss(T, H, V, train=train, device=hidden.device, **args)
+        op.gradient_calls = (L._STEP,) if single_pass else (L._BACKWARD,)
         if single_pass and train:
             loss, dhidden, dweight = op.step(hidden, weight, labels, token_weight, want_dhidden=ctx.needs_input_grad[0],
                                              want_dweight=ctx.needs_input_grad[1])

@@ -6,9 +6,9 @@ KL loss against a teacher, and like it without the T x V logits.
     dhidden, dweight = ce.backward(hidden, weight)           # projects again
     loss, dhidden, dweight = ce.step(hidden, weight, labels) # both at once, three projections for four
 
-The class holds outputs, state and workspaces of one shape: calls only enqueue on the current stream (the first one of each kind
-also makes its workspace) and return the holder's own buffers, which the next call overwrites. Marshalling only; the
-autograd entry, which allocates its outputs, is ``autograd.label_loss``.
+The class holds outputs, state and workspaces of one shape: calls only enqueue on the current stream (the first forward call and
+the first one that computes gradients also make what they need) and return the holder's own buffers, which the next call
+overwrites. Marshalling only; the autograd entry, which allocates its outputs, is ``autograd.label_loss``.
 """
 from __future__ import annotations
 
@@ -66,6 +66,7 @@ class LabelLoss:
         a.state, a.loss, a.losses, a.lse = (t.data_ptr() for t in (self.state, self.loss, self.losses, self.lse))
         self.device, self.at = self.state.device, self.state.get_device()
         self.workspaces, self.dhidden, self.dweight, self.token_weight, self.fed = {}, None, None, None, False
+        self.gradient_calls = (_BACKWARD, _STEP)                                # those that may come
         self._ref, L = ctypes.byref(a), B.lib()
         self._calls = (L.kdkl_label_loss_forward, L.kdkl_label_loss_backward, L.kdkl_label_loss_step)
 
@@ -114,11 +115,21 @@ class LabelLoss:
         else:
             a.grad = B._dptr(grad.reshape(1) if grad.dim() == 0 else grad, torch.float32, (1,), "grad").value
 
-    def _run(self, call: int, written):
-        a = self.args
-        ws = self.workspaces.get(call)
+    def _workspace(self, call: int) -> torch.Tensor:
+        """Scratch for a call: backward and step calls share one, which forward calls use where it is there already. None is
+        ever replaced, since a captured graph may hold its address."""
+        if call == _FORWARD:
+            ws = self.workspaces.get("gradients", self.workspaces.get("forward"))
+            name, calls = "forward", (_FORWARD,)
+        else:
+            name, calls = "gradients", self.gradient_calls
+            ws = self.workspaces.get(name)
         if ws is None:
-            ws = self.workspaces[call] = torch.empty(self._need(call), dtype=torch.uint8, device=self.device)
+            ws = self.workspaces[name] = torch.empty(max(map(self._need, calls)), dtype=torch.uint8, device=self.device)
+        return ws
+
+    def _run(self, call: int, written):
+        a, ws = self.args, self._workspace(call)
         a.workspace, a.workspace_bytes = ws.data_ptr(), ws.numel()
         B._check(self._calls[call](self._ref, _stream(self.at, "label loss")))
         _written(written)
