@@ -97,7 +97,8 @@ class LabelLoss:
             out = None
         elif out is None:
             if self.dweight is None:
-                self.dweight = torch.zeros(self.V, self.H, dtype=self.dtype, device=self.device)
+                new = torch.zeros if accumulate else torch.empty                # (a call that does not add writes all of it)
+                self.dweight = new(self.V, self.H, dtype=self.dtype, device=self.device)
             out = self.dweight
         else:
             B._dptr(out, self.dtype, (self.V, self.H), "out")

@@ -32,3 +32,16 @@ def test_label_loss_has_one_workspace_for_gradients(monkeypatch, order):
     assert len(grads) == 1 and grads.pop()[1] == max(op._need(1), op._need(2)) and small == op._need(0) < op._need(2)
     op.forward(h, w, y)
     assert sum(t.numel() for t in op.workspaces.values()) <= small + max(op._need(1), op._need(2))
+
+
+def test_label_loss_fills_nothing_that_a_call_overwrites(monkeypatch):
+    """dweight is written whole, or added to: only a sum of the holder's own starts from zeros."""
+    op, _ = _label(monkeypatch, dtype=F32)
+    zeros, made = torch.zeros, []
+    monkeypatch.setattr(labels.torch, "zeros", lambda *a, **kw: made.append(a) or zeros(*a, **kw))
+    op._outputs(None, False)
+    assert not made and op.dweight.shape == (5000, 64)
+    op, _ = _label(monkeypatch, dtype=F32)
+    made.clear()
+    op._outputs(None, True)
+    assert made[-1][:2] == (5000, 64) and not op.dweight.any()
