@@ -8,6 +8,15 @@
 //   sum (x - mu)^2 = sum_i [ q_i + n_i (mu_i - mu)^2 ],
 // so that a row costs one barrier. Everything is computed in fp32 and rounded once.
 //
+// A sum of 2880 equal fp32 numbers is rounded on the way, and their mean is then not the number: off by the last bit or two,
+// of which a rho of 1 / sqrt(eps) makes hundredths. So the mean m of fp32 rows is corrected by the mean of the values less m,
+// which are exact where they lie near m:
+//   r = sum (x - m), mu = fl(m + r / H), s = mu - m (exact),  sum (x - mu)^2 = sum (x - m)^2 - s (2 r - H s)
+// Equal values of 16 bits have exact sums up to 2^13 columns (11 bits times the count; bf16 2^16): such rows do without, which
+// is 6 % of a wide bf16 row's time (8192 x 16384: 252 us).
+// It costs fp32 rows of a block nothing (32768 x 4096 196 us), of a warp 7 % (65536 x 512 50.6 us), wider ones 5 % (8192 x
+// 16384 337 us).
+//
 // Bound by memory: 4 bytes a value forward and 6 backward (bf16). 32768 x 4096, one B200: forward 88 us (6.1 TB/s), backward
 // 131 (6.1 TB/s), its column sums 6 behind it; 1021 x 2880 6.5 and 12 us.
 //
@@ -17,6 +26,8 @@
 // and leaves one partial row each, which a second kernel adds in a fixed order; of wider rows they are taken by a kernel
 // of their own that goes down the columns.
 #pragma once
+#include <type_traits>
+
 #include "act8.cuh"
 
 namespace kdkl {
@@ -68,6 +79,15 @@ template <bool VEC> __device__ __forceinline__ int columns_of(int c, int H) {   
 // (sum, squares around its own mean) of the warps of a block -> mean and squares of the row, known to every thread.
 // slots: [2][32] pairs and [32] counts in shared memory; `par` alternates from row to row, which spares a second barrier.
 struct LnJoin { float mean, squares; };
+// The corrected mean, and the squares around it, from r and q = sum (x - m)^2 (see above).
+__device__ __forceinline__ LnJoin ln_corrected(float m, float r, float q, float H) {
+  LnJoin j;
+  j.mean = m + r / H;
+  const float s = j.mean - m;
+  const float left = q - s * (2.f * r - H * s);
+  j.squares = left < 0.f ? 0.f : left;                     // (a NaN stays one)
+  return j;
+}
 __device__ __forceinline__ LnJoin ln_join(float2 (*slots)[32], const float* counts, int par, int warps, float s, float q, float H) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   if (lane == 0) slots[par][warp] = make_float2(s, q);
@@ -76,7 +96,7 @@ __device__ __forceinline__ LnJoin ln_join(float2 (*slots)[32], const float* coun
   const float2 v = has ? slots[par][lane] : make_float2(0.f, 0.f);
   const float n = has ? counts[lane] : 0.f;
   LnJoin r;
-  r.mean = ln_warp_sum(v.x) / H;         // a division: equal values have themselves for their mean
+  r.mean = ln_warp_sum(v.x) / H;         // a division: an exact sum of equal values has the value for its mean
   const float off = n > 0.f ? v.x / n - r.mean : 0.f;
   r.squares = ln_warp_sum(fmaf(n * off, off, v.y));
   return r;
@@ -129,22 +149,30 @@ layer_norm_forward_kernel(const LnParams p) {
 #pragma unroll
       for (int g = 0; g < G; ++g) raw[g] = load_raw8<X, VEC>(x + (t + step) * p.ld_x, c[g], p.H);
     }
+    constexpr bool kCorrect = sizeof(X) == 4;
     s = ln_warp_sum(s);
-    const float mine = n_warp > 0.f ? s / n_warp : 0.f;
-    float q = 0.f;
+    if (kCorrect && !WARP) s = ln_join2(slots, 0, warps, s, 0.f).x;          // (then `mine` is the row's mean)
+    const float n = kCorrect && !WARP ? (float)p.H : n_warp;
+    const float mine = n > 0.f ? s / n : 0.f;
+    float q = 0.f, r = 0.f;
 #pragma unroll
     for (int g = 0; g < G; ++g)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float d = (VEC ? c[g] : column<VEC>(c[g], i)) < p.H ? f[g][i] - mine : 0.f;
         q = fmaf(d, d, q);
+        if (kCorrect) r += d;
       }
     q = ln_warp_sum(q);
-    float mean = mine, squares = q;
-    if (!WARP) {
-      const LnJoin j = ln_join(slots, counts, par, warps, s, q, (float)p.H);
-      mean = j.mean; squares = j.squares;
+    LnJoin j = {mine, q};
+    if (kCorrect) {
+      r = ln_warp_sum(r);
+      if (!WARP) { const float2 sums = ln_join2(slots, 1, warps, r, q); r = sums.x; q = sums.y; }
+      j = ln_corrected(mine, r, q, (float)p.H);
+    } else if (!WARP) {
+      j = ln_join(slots, counts, par, warps, s, q, (float)p.H);
     }
+    const float mean = j.mean, squares = j.squares;
     const float rho = 1.f / sqrtf(fmaf(squares, inv_H, p.eps));
     if (me == 0 && p.mean != nullptr) { p.mean[t] = mean; p.rho[t] = rho; }
 #pragma unroll
@@ -233,7 +261,7 @@ __device__ __forceinline__ float2 ln_block_sum2(LnSlots& s, int warps, float a, 
     t = add2(t, add2(add2(add2(low2(q[0]), high2(q[0])), add2(low2(q[1]), high2(q[1]))), add2(add2(low2(q[2]), high2(q[2])), add2(low2(q[3]), high2(q[3])))));
   return t;
 }
-// s / n with n's reciprocal at hand: the remainder of the first guess is exact, so equal values have themselves for their mean
+// s / n with n's reciprocal at hand: the remainder of the first guess is exact, so n times a number is divided without an error
 __device__ __forceinline__ float ln_quotient(float s, float n, float inv_n) {
   const float m = s * inv_n;
   return fmaf(fmaf(-m, n, s), inv_n, m);
@@ -294,7 +322,9 @@ layer_norm_forward_rows_kernel(const LnParams p) {
     }
     ask(stage);                                            // (into places that this thread alone has just read)
     if (++stage == kLnAhead) stage = 0;
-    const float mean = ln_quotient(ln_block_sum(first, warps, sum.x + sum.y), H, inv_H);
+    constexpr bool kCorrect = sizeof(X) == 4;
+    float mean = ln_quotient(ln_block_sum(first, warps, sum.x + sum.y), H, inv_H), squared;
+    float2 rest = both(0.f);
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
       const float2 off = both(in[g] ? -mean : 0.f);
@@ -302,9 +332,26 @@ layer_norm_forward_rows_kernel(const LnParams p) {
       for (int i = 0; i < 4; ++i) {
         f[g][i] = add2(f[g][i], off);
         squares = fma2(f[g][i], f[g][i], squares);
+        if (kCorrect) rest = add2(rest, f[g][i]);
       }
     }
-    const float rho = rsqrtf(fmaf(ln_block_sum(second, warps, squares.x + squares.y), inv_H, p.eps));
+    if constexpr (kCorrect) {
+      const float2 sums = ln_block_sum2(second, warps, rest.x + rest.y, squares.x + squares.y);
+      const LnJoin j = ln_corrected(mean, sums.x, sums.y, H);
+      squared = j.squares;
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        const float2 off = both(in[g] ? mean - j.mean : 0.f);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[g][i] = add2(f[g][i], off);
+      }
+      mean = j.mean;
+    } else {
+      squared = ln_block_sum(second, warps, squares.x + squares.y);
+    }
+    // (off by two units at most, where the other shapes' root and division take one: these lie between a row's barrier and its
+    // stores, 4.7 against 4.3 us for 1021 x 2880 bf16, 92.5 against 91 for 32768 x 4096)
+    const float rho = rsqrtf(fmaf(squared, inv_H, p.eps));
     if (threadIdx.x == 0 && p.mean != nullptr) { p.mean[t] = mean; p.rho[t] = rho; }
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
@@ -466,6 +513,7 @@ layer_norm_forward_wide_kernel(const LnParams p) {
   const long long cpitch = act_codes_pitch(p.H), spitch = act_scale_pitch(p.H);
   const float inv_H = 1.f / (float)p.H;
   const int c0 = first_column<VEC>(threadIdx.x);
+  const bool correct = !std::is_same_v<X, __nv_bfloat16> || p.H > 1 << 16;
   grid_dependents_launch();
   grid_dependency_wait();
   for (long long t = blockIdx.x; t < p.T; t += gridDim.x) {
@@ -476,16 +524,29 @@ layer_norm_forward_wide_kernel(const LnParams p) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) s += f[i];
     }
-    const float mean = ln_join2(slots, 0, warps, ln_warp_sum(s), 0.f).x / (float)p.H;
-    for (int base = 0; base < p.H; base += cols) {
-      load8<X, VEC>(row, base + c0, p.H, f);
+    const float first = ln_join2(slots, 0, warps, ln_warp_sum(s), 0.f).x / (float)p.H;
+    float r = 0.f;
+    auto look = [&](auto with) {
+      for (int base = 0; base < p.H; base += cols) {
+        load8<X, VEC>(row, base + c0, p.H, f);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float d = column<VEC>(base + c0, i) < p.H ? f[i] - mean : 0.f;
-        q = fmaf(d, d, q);
+        for (int i = 0; i < 8; ++i) {
+          const float d = column<VEC>(base + c0, i) < p.H ? f[i] - first : 0.f;
+          q = fmaf(d, d, q);
+          if (decltype(with)::value) r += d;
+        }
       }
+    };
+    LnJoin j = {first, 0.f};
+    if (correct) {
+      look(std::true_type());
+      const float2 sums = ln_join2(slots, 1, warps, ln_warp_sum(r), ln_warp_sum(q));
+      j = ln_corrected(first, sums.x, sums.y, (float)p.H);
+    } else {
+      look(std::false_type());
+      j.squares = ln_join2(slots, 1, warps, ln_warp_sum(q), 0.f).x;
     }
-    const float rho = 1.f / sqrtf(fmaf(ln_join2(slots, 1, warps, ln_warp_sum(q), 0.f).x, inv_H, p.eps));
+    const float mean = j.mean, rho = 1.f / sqrtf(fmaf(j.squares, inv_H, p.eps));
     if (threadIdx.x == 0 && p.mean != nullptr) { p.mean[t] = mean; p.rho[t] = rho; }
     for (int base = 0; base < p.H; base += cols) {         // the same trips for every thread: records are a warp's work
       const int c = base + c0;
