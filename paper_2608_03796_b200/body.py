@@ -19,6 +19,7 @@ a call of a new shape; calls allocate nothing else. Marshalling only; autograd e
 from __future__ import annotations
 
 import ctypes
+import math
 from typing import NamedTuple, Optional
 
 import torch
@@ -501,7 +502,11 @@ class Rotary:
     """Rotary positions of queries [T, heads, D] and keys [T, kv heads, D] (kdkl_rotary). The first `rotary_dim` columns of a
     head (all by default) are pairs - "half": (i, i + rotary_dim / 2), "interleaved": (2 i, 2 i + 1) - turned by
     position * base ** (-2 i / rotary_dim) radians. `scaling` ("linear", "ntk", "yarn", by `factor`) is for contexts longer
-    than `original_length`, the one that was trained on; see kdkl_rotary_table for the formulas.
+    than `original_length`, the one that was trained on; see kdkl_rotary_table for the formulas. "yarn" is that of its paper: how
+    much of a frequency is kept is linear in its turns over the trained length, none at 1 and all at 32. Much model code takes
+    it linear in the pair's index between the places of those two, which turns the middle pairs by other angles: a
+    checkpoint wants the ones that it was trained with. Those, or any others, are given as `frequencies`, rotary_dim / 2 numbers
+    of radians a position in place of base and scaling; `magnitude` is the factor on turned columns, in place of scaling's.
 
     Tokens and heads may lie any distance apart (the halves of one projection, or x.transpose(0, 1) of heads before
     tokens); columns are neighbours. Outputs are the holder's own buffers, made for each stream and new shape, or those given as
@@ -510,19 +515,30 @@ class Rotary:
     a stream of its own."""
 
     def __init__(self, D: int, rotary_dim: Optional[int] = None, *, base: float = 10000.0, layout: str = "half",
-                 scaling: str = "none", factor: float = 1.0, original_length: int = 0, device="cuda"):
+                 scaling: str = "none", factor: float = 1.0, original_length: int = 0, frequencies=None,
+                 magnitude: Optional[float] = None, device="cuda"):
         R = D if rotary_dim is None else rotary_dim
         if D % 2 or R % 2 or not 2 <= R <= D <= 1024:
             raise ValueError(f"kdkl: heads of {D} columns, {R} of them turned: both are even, and at most 1024")
         a = self.args = kdkl_rotary_args()
-        turns, magnitude = (ctypes.c_double * (R // 2))(), ctypes.c_float()
         kind = _lookup(SCALINGS, scaling, "scaling")
-        if B.lib().kdkl_rotary_table(R, base, kind, factor, original_length, turns, ctypes.byref(magnitude)) != 0:
-            raise ValueError(f"kdkl: no rotary positions with base {base}, scaling {scaling!r} by {factor} of {original_length}")
+        if frequencies is None:
+            turns, m = (ctypes.c_double * (R // 2))(), ctypes.c_float()
+            if B.lib().kdkl_rotary_table(R, base, kind, factor, original_length, turns, ctypes.byref(m)) != 0:
+                raise ValueError(f"kdkl: no rotary positions with base {base}, scaling {scaling!r} by {factor} of {original_length}")
+            turns, m = torch.tensor(list(turns), dtype=torch.float64), m.value
+        else:
+            turns, m = torch.as_tensor(frequencies, dtype=torch.float64).cpu() / (2 * math.pi), 1.0
+            if kind != 0 or turns.shape != (R // 2,) or not torch.isfinite(turns).all():
+                raise ValueError(f"kdkl: frequencies: expected {R // 2} finite numbers, without a scaling, got shape "
+                                 f"{tuple(turns.shape)}, scaling {scaling!r}")
+        m = m if magnitude is None else float(magnitude)
+        if not math.isfinite(m):
+            raise ValueError(f"kdkl: magnitude: expected a finite number, got {magnitude}")
         self.D, self.R = D, R
         a.struct_size = ctypes.sizeof(a)
-        a.layout, a.head_dim, a.rotary_dim, a.magnitude = _lookup(LAYOUTS, layout, "layout"), D, R, magnitude.value
-        self.turns = torch.tensor(list(turns), dtype=torch.float64).to(device)
+        a.layout, a.head_dim, a.rotary_dim, a.magnitude = _lookup(LAYOUTS, layout, "layout"), D, R, m
+        self.turns = turns.to(device)
         a.turns, self.at = self.turns.data_ptr(), self.turns.get_device()
         self._call, self._streams, self._own = B.lib().kdkl_rotary, {}, {}
 

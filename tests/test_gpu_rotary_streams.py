@@ -45,3 +45,17 @@ def test_captures_again_and_again():
         del graph, q, key, total
         sizes.append(torch.cuda.memory_allocated())
     assert sizes[-1] == sizes[0]
+
+
+def test_frequencies_of_the_callers_own():
+    """Against the rotation in 64 bits, at the tolerance of the tables that are made here (test_gpu_rotary)."""
+    from tests.test_gpu_rotary import C, UNIT
+    T, D, R = 200, 96, 64
+    f, m = torch.rand(R // 2, dtype=torch.float64) * 3 - 1.5, 0.75
+    x, n = torch.randn(T, 3, D, device="cuda"), torch.randint(-100000, 100000, (T,), device="cuda")
+    y, _ = body.Rotary(D, rotary_dim=R, frequencies=f, magnitude=m).forward(x, None, n)
+    angle = n.double()[:, None, None] * f.cuda()
+    a, b = x[..., :R // 2].double(), x[..., R // 2:R].double()
+    want = torch.cat([a * angle.cos() - b * angle.sin(), b * angle.cos() + a * angle.sin()], -1) * m
+    size = torch.cat([a.abs() + b.abs()] * 2, -1) * m
+    assert float(((y[..., :R].double() - want).abs() - (C + 1) * UNIT * size).max()) <= 0 and torch.equal(y[..., R:], x[..., R:])

@@ -1,5 +1,6 @@
 """What a rotary table owes its callers on the host. No GPU needed: the entry point is replaced where a call would reach it."""
 import gc
+import math
 import weakref
 
 import pytest
@@ -54,3 +55,26 @@ def test_rotary_keeps_nothing_of_a_captured_call(rope):
     assert all(ref() is None for ref in refs)
     capture(False)
     assert _turn(r, 3)[0] is eager[0]
+
+
+def test_rotary_frequencies_of_the_callers_own():
+    """Model code in wide use takes the ramp between kept and stretched frequencies linear in the pair's index, not in its turns:
+    such a table, and its magnitude, go in as they are."""
+    D, base, factor, length = 128, 10000.0, 16.0, 4096
+    at = [D * math.log(length / (turns * 2 * math.pi)) / (2 * math.log(base)) for turns in (32, 1)]
+    low, high = max(0, math.floor(at[0])), min(D - 1, math.ceil(at[1]))
+    f = base ** (-torch.arange(0, D, 2, dtype=torch.float64) / D)
+    keep = 1 - ((torch.arange(D // 2, dtype=torch.float64) - low) / (high - low)).clamp(0, 1)
+    mine = keep * f + (1 - keep) * f / factor
+    theirs = body.Rotary(D, base=base, scaling="yarn", factor=factor, original_length=length, device="cpu")
+    r = body.Rotary(D, frequencies=mine, magnitude=1.25, device="cpu")
+    assert torch.equal(r.turns, mine / (2 * math.pi)) and r.args.magnitude == 1.25 and r.args.turns == r.turns.data_ptr()
+    assert abs(float(theirs.turns[33] / r.turns[33]) - 1) > 0.3             # the two readings differ in the middle pairs
+    assert body.Rotary(D, frequencies=mine.tolist(), device="cpu").args.magnitude == 1.0
+    assert body.Rotary(D, scaling="yarn", factor=factor, original_length=length, magnitude=1.0, device="cpu").args.magnitude == 1.0
+    plain = body.Rotary(8, frequencies=[1.0, 0.1, 0.01, 0.001], device="cpu").turns
+    assert torch.allclose(plain, body.Rotary(8, device="cpu").turns, rtol=1e-14, atol=0)
+    for bad in (dict(frequencies=mine[:-1]), dict(frequencies=[math.inf] * 64), dict(frequencies=mine, scaling="linear", factor=2.0),
+                dict(magnitude=math.nan), dict(magnitude=math.inf)):
+        with pytest.raises(ValueError):
+            body.Rotary(D, device="cpu", **bad)
