@@ -372,7 +372,8 @@ int kdkl_teacher_topk_stored(const void* hidden_bf16, const void* weight_bf16, i
  *   forward    one sweep; the loss, and losses and lse [T] of the tokens (0 where not counted)
  *   backward   after a forward call with the same inputs, state, chunk and temperature (else KDKL_ERR_STATE in the status, and
  *              nothing is written): projects again. Upstream gradient: grad_tokens [T] where given (of the losses, weights
- *              and divisor left out), else *grad (1 if NULL) of the loss
+ *              and divisor left out), else *grad (1 if NULL) of the loss. Smoothing, z term, reduction, weights and divisor are
+ *              taken from this call's arguments, not compared: lse is what the state holds, and does not depend on them
  *   step       both at once, three projections for four: the sweep leaves exponentials in fp16, each 32 columns to their own
  *              largest, and they become G in place. For *grad known beforehand
  * G, the gradient of the chunk's logits, is rounded once to bf16, outputs once to their type; a bf16 dweight over several
@@ -597,7 +598,9 @@ int kdkl_layer_norm_backward(const kdkl_layer_norm_args* args, void* cuda_stream
  * a position, changed for contexts longer than a model was trained on:
  *   LINEAR  f_i / factor
  *   NTK     base factor^(d / (d - 2)) in base's place, d = rotary_dim
- *   YARN    k f_i + (1 - k) f_i / factor, k = clamp((original_length f_i / (2 pi) - 1) / 31, 0, 1); magnitude 0.1 ln(factor) + 1 */
+ *   YARN    k f_i + (1 - k) f_i / factor, k = clamp((original_length f_i / (2 pi) - 1) / 31, 0, 1); magnitude 0.1 ln(factor) + 1
+ * YARN's k is linear in the turns over the trained length, as the method's paper has it; much model code takes it linear in i
+ * between the places where they are 32 and 1. Such a table, or any other, is given to kdkl_rotary as it is. */
 #define KDKL_ROTARY_HALF 0
 #define KDKL_ROTARY_INTERLEAVED 1
 #define KDKL_ROTARY_PLAIN 0

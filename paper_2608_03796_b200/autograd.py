@@ -653,7 +653,8 @@ def label_loss(hidden, weight, labels, token_weight: Optional[torch.Tensor] = No
     """Cross entropy of softmax(hidden @ weight.T / temperature) against labels [...] (int32 or int64), hidden [..., H] and weight
     [V, H] bf16 (see labels.LabelLoss for the formula). reduction "none" gives the losses [...], 0 at ignored tokens, without
     token weights. single_pass computes the gradients in the forward call, for an upstream gradient of 1 (three
-    projections for four), and keeps them; another one then scales them, with one more rounding."""
+    projections for four), and keeps them; another one then scales them, with one more rounding. Hidden states of ignored tokens
+    have to be finite: they take part in dweight's product, with zeros."""
     if hidden.dtype != torch.bfloat16 or weight.dtype != torch.bfloat16:
         raise TypeError(f"label_loss: expected bf16, got {hidden.dtype} and {weight.dtype}")
     if hidden.shape[:-1] != labels.shape or (token_weight is not None and token_weight.shape != labels.shape):

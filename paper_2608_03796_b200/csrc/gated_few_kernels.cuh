@@ -5,7 +5,8 @@
 //
 // warp 0 loads (TMA, 64 columns a block), warp 1 multiplies (tcgen05, M = 128), warps 2 to 5 finish. An SM takes in such a
 // stream at about 50 GB/s, however long the ring (5 or 11 stages: the same time), so all SMs have to take part: where
-// there are fewer tiles than SMs, a cluster of 2 or 4 CTAs shares a tile's contraction. Each hands every CTA of the cluster (itself
+// there are fewer tiles than SMs, a cluster of 2 or 4 CTAs shares a tile's contraction. Even shares come of it seldom: 5632
+// features are 88 tiles, 176 CTAs in clusters of two, and the 28 of 148 SMs that have two of them, 0.52 MB, set the time. Each hands every CTA of the cluster (itself
 // too) its sums for that CTA's share of the tokens, through shared memory, which is empty by then; a thread then
 // has one feature of half of them, adds up the parts in their order and forms the outputs, 32 features = 64 bytes a
 // token and warp; a group of a record is a warp's 32 lanes. Measured, 9 and 128 tokens, weights from memory: 2048 x

@@ -212,6 +212,8 @@ __device__ __forceinline__ uint32_t record_row32(const ActRecord& r, bool write,
 // A thread has one row: 128 gate columns at taddr and the same features' 128 up columns behind them, 32 at a time. Outputs
 // leave through the warp's two swizzled boxes as in the plain store. What lies past the last feature reads as zero (the
 // tensor map of B fills it) and is clipped by the output's map.
+// BACK rounds its two outputs to bf16, since the products that follow take 16-bit operands (as the gradients that reach
+// act8_linear are): dx and dweight are 2.3e-3 off in norm, where their own rounding alone makes 1.7e-3.
 template <int EPI>
 __device__ __forceinline__ void gated_epilogue(const GemmParams& p, const CUtensorMap& tmC, uint32_t taddr, int row, bool row_ok,
                                                int box_row0, int nt, int lane, uint32_t boxes, uint32_t& nbox) {
